@@ -135,6 +135,31 @@ _SYMS.update({
 })
 
 
+class _CAct8(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("ldc", C.c_int64), ("scales", C.c_void_p), ("lds", C.c_int64),
+                ("rows", C.c_int64), ("cols", C.c_int64)]
+
+
+class _CGroupNorm(C.Structure):
+    _fields_ = [("n", C.c_int64), ("hw", C.c_int64), ("channels", C.c_int32), ("groups", C.c_int32), ("dtype", C.c_int32),
+                ("act", C.c_int32), ("eps", C.c_float), ("reserved", C.c_int32)]
+
+
+_VP, _I64, _A8P = C.c_void_p, C.c_int64, C.POINTER(_CAct8)
+_SYMS.update({
+    "slide_act8_pack": (C.c_int, [_VP, C.c_int, _I64, C.c_int, _A8P, _VP]),
+    "slide_act8_unpack": (C.c_int, [_A8P, _VP, C.c_int, _I64, _VP]),
+    "slide_act8_linear": (C.c_int, [_VP, C.c_int, _I64, _A8P, _A8P, _VP, C.c_int, _VP, _I64, _VP, _I64, _VP]),
+    "slide_act8_wgrad_workspace_bytes": (C.c_size_t, [_I64, _I64, _I64]),
+    "slide_act8_wgrad": (C.c_int, [_VP, C.c_int, _I64, _I64, _A8P, _VP, _I64, _VP, C.c_int, _VP, C.c_size_t, _VP]),
+    "slide_group_norm_workspace_bytes": (C.c_size_t, [C.POINTER(_CGroupNorm)]),
+    "slide_group_norm_fwd": (C.c_int, [C.POINTER(_CGroupNorm), _VP, _I64, _VP, _VP, _VP, _I64, _VP, _I64, _A8P, _VP, _VP, _VP,
+                                       C.c_size_t, _VP]),
+    "slide_group_norm_bwd": (C.c_int, [C.POINTER(_CGroupNorm), _VP, _I64, _VP, _I64, _A8P, _VP, _VP, _VP, _I64, _VP, _VP, _VP,
+                                       _I64, _VP, _I64, _VP, _VP, C.c_int, _VP, C.c_size_t, _VP]),
+})
+
+
 def load_cdll():
     p = lib_path()
     if not os.path.exists(p):
@@ -401,3 +426,186 @@ class ResNetLib:
                 return out
             out.append(s.decode())
             i += 1
+
+
+ACTS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3}
+
+
+class Act8:
+    """A matrix [rows, cols] in 8 bits (include/act8.h): codes [rows, >= cols] uint8, scales [rows, >= ceil(cols / 128)] uint8."""
+
+    def __init__(self, rows, cols, codes, scales):
+        if codes.dim() != 2 or scales.dim() != 2 or codes.element_size() != 1 or scales.element_size() != 1:
+            raise ValueError("codes and scales are matrices of bytes")
+        if codes.shape[0] != rows or scales.shape[0] != rows or codes.shape[1] < cols or scales.shape[1] < -(-cols // 128):
+            raise ValueError(f"codes {tuple(codes.shape)} or scales {tuple(scales.shape)} too small for {rows} x {cols}")
+        if codes.stride(1) != 1 or scales.stride(1) != 1:
+            raise ValueError("codes and scales: rows must be contiguous")
+        if codes.device != scales.device:
+            raise ValueError("codes and scales are on different devices")
+        self.rows, self.cols, self.codes, self.scales = rows, cols, codes, scales
+        # (the stride that torch reports of a single row says nothing)
+        self._c = _CAct8(codes.data_ptr(), codes.stride(0) if rows > 1 else -(-cols // 16) * 16, scales.data_ptr(),
+                         scales.stride(0) if rows > 1 else max(scales.shape[1], 1), rows, cols)
+        self._ref = C.byref(self._c)
+
+    @staticmethod
+    def empty(rows, cols, device="cuda"):
+        import torch
+        return Act8(rows, cols, torch.empty((rows, -(-cols // 16) * 16), dtype=torch.uint8, device=device),
+                    torch.empty((rows, -(-cols // 128)), dtype=torch.uint8, device=device))
+
+    @property
+    def device(self):
+        return self.codes.device
+
+
+class Act8Lib:
+    """The calls of include/act8.h on torch tensors, whose shapes, strides and types they take; no context.  A call runs on the
+    tensors' device, on `stream` (default: that device's current stream)."""
+
+    def __init__(self):
+        import torch
+        self.lib = load_cdll()
+        self._torch = torch
+        self._types = {torch.float32: 0, torch.bfloat16: 1}
+
+    # ---- marshalling
+    def _type(self, t):
+        try:
+            return self._types[t.dtype]
+        except KeyError:
+            raise ValueError(f"float32 or bfloat16, not {t.dtype}") from None
+
+    def _matrix(self, t, rows, cols, dtype, what):
+        """(pointer, elements between rows) of a [rows, cols] matrix of dtype; a tensor of more dimensions is one of its last two's rows
+        where its strides allow it.  (None, 0) for None."""
+        if t is None:
+            return None, 0
+        if t.dtype != dtype:
+            raise ValueError(f"{what}: {t.dtype}, expected {dtype}")
+        if t.dim() == 3:
+            if t.shape[0] > 1 and t.shape[1] > 1 and t.stride(0) != t.shape[1] * t.stride(1):
+                raise ValueError(f"{what}: tiles must follow one another at one row stride")
+            have, last = t.shape[0] * t.shape[1], t.shape[2]
+            ld = t.stride(1) if t.shape[1] > 1 else t.stride(0)
+        elif t.dim() == 2:
+            (have, last), ld = t.shape, t.stride(0)
+        else:
+            raise ValueError(f"{what}: a matrix, or tiles of rows")
+        if have != rows or last != cols:
+            raise ValueError(f"{what}: {tuple(t.shape)}, expected {rows} rows of {cols}")
+        if last > 1 and t.stride(-1) != 1:
+            raise ValueError(f"{what}: rows must be contiguous")
+        return t.data_ptr(), ld if have > 1 else max(ld, cols)
+
+    def _floats(self, t, n, what):
+        if t is None:
+            return None
+        if t.dtype != self._torch.float32 or t.numel() != n or not t.is_contiguous():
+            raise ValueError(f"{what}: {n} contiguous float32 values")
+        return t.data_ptr()
+
+    def _act(self, act):
+        if isinstance(act, str):
+            try:
+                return ACTS[act]
+            except KeyError:
+                raise ValueError(f"activation {act!r}: one of {', '.join(ACTS)}") from None
+        return int(act)
+
+    def _call(self, what, first, others, args, stream):
+        """Run the entry point on the device of `first`, which all of `others` must be on."""
+        torch, dev = self._torch, first.device
+        if dev.type != "cuda":
+            raise ValueError(f"{what}: tensors must be on the GPU")
+        for t in others:
+            if t is not None and t.device != dev:
+                raise ValueError(f"{what}: tensors on {dev} and {t.device}")
+        if stream is None:
+            stream = torch.cuda.current_stream(dev).cuda_stream
+        elif not isinstance(stream, int):
+            if stream.device != dev:
+                raise ValueError(f"{what}: a stream of {stream.device} for tensors on {dev}")
+            stream = stream.cuda_stream
+        if dev.index != torch.cuda.current_device():
+            with torch.cuda.device(dev):
+                rc = getattr(self.lib, what)(*args, stream)
+        else:
+            rc = getattr(self.lib, what)(*args, stream)
+        if rc != 0:
+            raise SlideError(rc, what, self.lib.slide_last_hip_error())
+
+    def _work(self, t):
+        return (None, 0) if t is None else (t.data_ptr(), t.numel() * t.element_size())
+
+    # ---- calls
+    def slide_act8_pack(self, x, out, transpose=False, stream=None):
+        rows, cols = (out.cols, out.rows) if transpose else (out.rows, out.cols)
+        p, ld = self._matrix(x, rows, cols, x.dtype, "x")
+        self._call("slide_act8_pack", out, (x,), (p, self._type(x), ld, int(transpose), out._ref), stream)
+
+    def slide_act8_unpack(self, a, y, stream=None):
+        p, ld = self._matrix(y, a.rows, a.cols, y.dtype, "y")
+        self._call("slide_act8_unpack", a, (y,), (a._ref, p, self._type(y), ld), stream)
+
+    def slide_act8_linear(self, x, x8, w8, y, bias=None, act="none", residual=None, stream=None):
+        """y = act(x8 w8^T + bias) + residual, with x packed into x8 first (x None: x8 holds its values)."""
+        xp, ldx = (None, 0) if x is None else self._matrix(x, x8.rows, x8.cols, y.dtype, "x")
+        rp, ldr = self._matrix(residual, x8.rows, w8.rows, y.dtype, "residual")
+        yp, ldy = self._matrix(y, x8.rows, w8.rows, y.dtype, "y")
+        self._call("slide_act8_linear", y, (x, x8, w8, bias, residual),
+                   (xp, self._type(y), ldx, x8._ref, w8._ref, self._floats(bias, w8.rows, "bias"), self._act(act), rp, ldr, yp, ldy),
+                   stream)
+
+    def slide_act8_wgrad_workspace_bytes(self, rows, out, cin):
+        return int(self.lib.slide_act8_wgrad_workspace_bytes(rows, out, cin))
+
+    def slide_act8_wgrad(self, dy, x8, dW, db=None, accumulate=False, workspace=None, stream=None):
+        out = dW.shape[0]
+        p, ld = self._matrix(dy, x8.rows, out, dy.dtype, "dy")
+        wp, ldw = self._matrix(dW, out, x8.cols, self._torch.float32, "dW")
+        self._call("slide_act8_wgrad", dW, (dy, x8, db, workspace),
+                   (p, self._type(dy), ld, out, x8._ref, wp, ldw, self._floats(db, out, "db"), int(accumulate), *self._work(workspace)),
+                   stream)
+
+    def _shape(self, n, hw, channels, groups, dtype, act, eps):
+        return _CGroupNorm(n, hw, channels, groups, dtype, act, eps, 0)
+
+    def slide_group_norm_workspace_bytes(self, n, hw, channels, groups, dtype):
+        """For both directions of a group norm over [n, hw, channels]; 0 for a shape that is refused."""
+        s = self._shape(n, hw, channels, groups, self._types.get(dtype, -1), 0, 1.0)
+        return int(self.lib.slide_group_norm_workspace_bytes(C.byref(s)))
+
+    def slide_group_norm_fwd(self, x, gamma, beta, groups, y, mean, rstd, eps=1e-5, act="none", residual=None, x8=None,
+                             workspace=None, stream=None):
+        """x, y, residual: [n, hw, channels]; mean, rstd: [n, groups]."""
+        if x.dim() != 3:
+            raise ValueError("x: [n, hw, channels]")
+        n, hw, c = x.shape
+        s = self._shape(n, hw, c, groups, self._type(x), self._act(act), eps)
+        xp, ldx = self._matrix(x, n * hw, c, x.dtype, "x")
+        rp, ldr = self._matrix(residual, n * hw, c, x.dtype, "residual")
+        yp, ldy = self._matrix(y, n * hw, c, x.dtype, "y")
+        self._call("slide_group_norm_fwd", x, (gamma, beta, residual, y, x8, mean, rstd, workspace),
+                   (C.byref(s), xp, ldx, self._floats(gamma, c, "gamma"), self._floats(beta, c, "beta"), rp, ldr, yp, ldy,
+                    None if x8 is None else x8._ref, self._floats(mean, n * groups, "mean"), self._floats(rstd, n * groups, "rstd"),
+                    *self._work(workspace)), stream)
+
+    def slide_group_norm_bwd(self, dy, x, gamma, beta, mean, rstd, groups, dx, dgamma, dbeta, act="none", residual=None,
+                             dresidual=None, accumulate=False, workspace=None, stream=None):
+        """x: [n, hw, channels], or the Act8 that the forward left."""
+        if dy.dim() != 3:
+            raise ValueError("dy: [n, hw, channels]")
+        n, hw, c = dy.shape
+        t = dy.dtype
+        s = self._shape(n, hw, c, groups, self._type(dy), self._act(act), 1.0)
+        kept = isinstance(x, Act8)
+        xp, ldx = (None, 0) if kept else self._matrix(x, n * hw, c, t, "x")
+        m = self._matrix
+        self._call("slide_group_norm_bwd", dy, (x, gamma, beta, residual, mean, rstd, dx, dresidual, dgamma, dbeta, workspace),
+                   (C.byref(s), *m(dy, n * hw, c, t, "dy"), xp, ldx, x._ref if kept else None, self._floats(gamma, c, "gamma"),
+                    self._floats(beta, c, "beta"), *m(residual, n * hw, c, t, "residual"), self._floats(mean, n * groups, "mean"),
+                    self._floats(rstd, n * groups, "rstd"), *m(dx, n * hw, c, t, "dx"), *m(dresidual, n * hw, c, t, "dresidual"),
+                    self._floats(dgamma, c, "dgamma"), self._floats(dbeta, c, "dbeta"), int(accumulate), *self._work(workspace)),
+                   stream)

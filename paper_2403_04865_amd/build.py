@@ -15,7 +15,8 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libslide.so")
 SOURCES = ["slide_lib.hip", "misc.hip", "ln.hip", "gemm.hip", "gemm_f32.hip", "gemm_mfma.hip", "gemm_nt_mfma.hip", "gemm_nt_big.hip", "gemm_nt_gelu.hip", "mlp_fused.hip", "gemm_tn_big.hip", "attn.hip", "attn_f32.hip", "attn_mfma.hip", "cls_lane.hip", "pool.hip", "pool_f32.hip", "pool_mfma.hip", "pool_bwd_mfma.hip", "optim.hip",
-           "conv.hip", "bn_pool.hip", "resnet_lib.hip"]
+           "conv.hip", "bn_pool.hip", "resnet_lib.hip",
+           "act8_lib.hip", "act8_pack.hip", "act8_linear.hip", "act8_wgrad.hip", "group_norm.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-fPIC", "-std=c++17", "-Wall", "-Wno-unused-function",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 
@@ -37,7 +38,7 @@ def _newer(src_files, target):
 def build(force: bool = False, verbose: bool = True, extra_flags=()):
     os.makedirs(OBJ, exist_ok=True)
     headers = [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith(".h")]
-    headers += [os.path.join(HERE, "..", "include", h) for h in ("slide.h", "slide_prof.h", "resnet.h")]
+    headers += [os.path.join(HERE, "..", "include", h) for h in ("slide.h", "slide_prof.h", "resnet.h", "act8.h")]
     hipcc = _hipcc()
     jobs = []
     for src in SOURCES:

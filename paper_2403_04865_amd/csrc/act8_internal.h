@@ -1,0 +1,115 @@
+// Internal declarations of the layers on 8-bit activations (include/act8.h; gfx950 only).
+#pragma once
+#include "../../include/act8.h"
+#include <type_traits>
+
+#include "slide_internal.h"
+
+namespace sl {
+
+constexpr int A8_BLOCK = 128;          // columns that share a scale
+constexpr int A8_GRAIN = 16;           // a row's codes are zero up to the next multiple of this
+constexpr long long A8_MAX_ROWS = (1LL << 31) - 1, A8_MAX_COLS = (1LL << 24) - 1;
+
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+
+// The scale byte of a block from the bits of its largest finite magnitude: the magnitude is m 2^E with 1 <= m < 2, 448 is
+// 1.75 * 2^8, so the power is E - 8, one more where m > 1.75; not below 2^-127, and 1 for a block of zeros.
+__device__ __forceinline__ unsigned a8_scale_byte(unsigned amax_bits) {
+  int b = (int)(amax_bits >> 23) - 8 + ((amax_bits & 0x7fffffu) > 0x600000u);
+  b = b > 0 ? b : 0;
+  return amax_bits ? (unsigned)b : 127u;
+}
+// 2^(127 - byte): what a value is multiplied with before it is rounded to a code (byte <= 247: never subnormal)
+__device__ __forceinline__ float a8_inverse(unsigned byte) { return __uint_as_float((254u - byte) << 23); }
+// 2^(byte - 127); byte 0 is a subnormal number, byte 255 (no scale) a NaN
+__device__ __forceinline__ float a8_scale(unsigned byte) {
+  return __uint_as_float(byte == 0 ? 0x00400000u : byte == 255 ? 0x7fc00000u : byte << 23);
+}
+// magnitude bits of a value for the block's maximum: what is not finite does not count
+__device__ __forceinline__ unsigned a8_mag(float v) {
+  const unsigned a = __float_as_uint(v) & 0x7fffffffu;
+  return a < 0x7f800000u ? a : 0u;
+}
+// the largest of a value over the 16 lanes of a DPP row, in every lane of it
+__device__ __forceinline__ unsigned a8_row_max(unsigned v) {
+  auto step = [&](auto ctrl) {
+    const unsigned o = (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, decltype(ctrl)::value, 0xf, 0xf, false);
+    v = v > o ? v : o;
+  };
+  step(std::integral_constant<int, 0x128>{});   // rotate the row by 8, 4, 2, 1 lanes
+  step(std::integral_constant<int, 0x124>{});
+  step(std::integral_constant<int, 0x122>{});
+  step(std::integral_constant<int, 0x121>{});
+  return v;
+}
+// four values -> four codes: nearest, ties to even; what is not finite becomes a NaN
+__device__ __forceinline__ unsigned a8_code4(float a, float b, float c, float d) {
+  int r = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+  return (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, r, true);
+}
+// four codes -> their values times s
+__device__ __forceinline__ void a8_value4(unsigned q, float s, float (&v)[4]) {
+  const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)q, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)q, true);
+  v[0] = lo[0] * s; v[1] = lo[1] * s; v[2] = hi[0] * s; v[3] = hi[1] * s;
+}
+
+// act(u) and act'(u)
+__device__ __forceinline__ float sigmoid_f(float u) { return __builtin_amdgcn_rcpf(1.0f + __expf(-u)); }
+template <int ACT> __device__ __forceinline__ float act_f(float u) {
+  if constexpr (ACT == SLIDE_ACT_RELU) return u < 0.f ? 0.f : u;      // a NaN stays one
+  if constexpr (ACT == SLIDE_ACT_SILU) return u * sigmoid_f(u);
+  if constexpr (ACT == SLIDE_ACT_GELU) return gelu_f(u);
+  return u;
+}
+
+// A matrix [rows][cols] in 8 bits as the kernels see it.
+struct A8 { const uint8_t* codes; long long ldc; const uint8_t* scales; long long lds; };
+inline A8 a8_view(const slide_act8& a) { return A8{a.codes, a.ldc, a.scales, a.lds}; }
+
+hipError_t launch_act8_pack(const void* x, int dt, long long ldx, bool transpose, const slide_act8& out, hipStream_t s);
+hipError_t launch_act8_unpack(const slide_act8& a, void* y, int dt, long long ldy, hipStream_t s);
+
+struct A8Linear {
+  A8 x, w;
+  long long M; int N, K;
+  const float* bias;
+  int act, dt;
+  const void* resid; long long ldr;
+  void* y; long long ldy;
+};
+hipError_t launch_act8_linear(const A8Linear& g, hipStream_t s);
+
+struct A8Wgrad {
+  const void* dy; int dt; long long lddy;
+  A8 x;
+  long long M; int N, K;
+  float* dW; long long lddw;
+  float* db;
+  int accumulate;
+  float* work;
+};
+size_t act8_wgrad_bytes(long long M, int N, int K);
+hipError_t launch_act8_wgrad(const A8Wgrad& g, hipStream_t s);
+
+struct GroupNorm {
+  slide_group_norm s;
+  const void* x; long long ldx;       // bwd: null = from x8
+  const float *gamma, *beta;
+  const void* resid; long long ldr;
+  void* y; long long ldy;             // bwd: dx
+  const slide_act8* x8;               // fwd: written (may be null); bwd: read where x is null
+  float *mean, *rstd;
+  const void* dy; long long lddy;
+  void* dresid; long long lddr;
+  float *dgamma, *dbeta;
+  int accumulate;
+  float* work;
+};
+size_t group_norm_bytes(const slide_group_norm& s);
+hipError_t launch_group_norm_fwd(const GroupNorm& g, hipStream_t s);
+hipError_t launch_group_norm_bwd(const GroupNorm& g, hipStream_t s);
+
+}  // namespace sl
