@@ -146,9 +146,188 @@ hipError_t few(const A8Linear& g, hipStream_t s) {
   return hipSuccess;
 }
 
+// ---- tiles ------------------------------------------------------------------------------------------------------------
+// A workgroup takes BM rows of x by BN rows of w, a wavefront 16 FM of x by 64 of w; 128 columns per step, brought straight into LDS
+// one step ahead, in two stages.  A row of a stage is eight 16-byte pieces; piece c lies in place c ^ (3 bits of the row), chosen so
+// that eight neighbouring lanes of a fragment read find their pieces in eight different places (no bank conflicts).
+constexpr int STEP = A8_BLOCK;
+
+__device__ __forceinline__ int turn_x(int row) { return row & 7; }
+// rows of w are dealt to fragments so that neighbouring lanes have rows 0 1 2 3, 8 9 10 11
+__device__ __forceinline__ int turn_w(int row) { return (row & 3) | ((row >> 1) & 4); }
+
+template <int BM, int BN, int FM, int ACT, typename T>
+__global__ void __launch_bounds__(64 * (BM / (16 * FM)) * (BN / 64)) linear_tile_k(A8Linear g, int TM, int TN, bool vec) {
+  constexpr bool F8 = sizeof(T) == 2;
+  constexpr int WM = BM / (16 * FM), NW = WM * (BN / 64);
+  constexpr int XI = BM / 8 / NW, WI = BN / 8 / NW;   // kilobytes that a wavefront loads per step
+  static_assert(XI * 8 * NW == BM && WI * 8 * NW == BN, "loads are dealt evenly");
+  __shared__ __attribute__((aligned(16))) uint8_t ring0[(BM + BN) * STEP], ring1[(BM + BN) * STEP];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wave % WM, wn = wave / WM, r = lane & 15, kg = lane >> 4;
+  // consecutive tiles of the same rows of x run on one XCD and share them in its L2
+  const int j = blockIdx.x >> 3, tm = (int)(blockIdx.x & 7) + 8 * (j / TN), tn = j % TN;
+  if (tm >= TM) return;
+  const long long m0 = (long long)tm * BM;
+  const int n0 = tn * BN;
+  const int rows = g.M - m0 < BM ? (int)(g.M - m0) : BM, cols = g.N - n0 < BN ? g.N - n0 : BN;
+  const int k16 = (g.K + A8_GRAIN - 1) / A8_GRAIN * A8_GRAIN, steps = (g.K + STEP - 1) / STEP;
+  const int ldx = (int)g.x.ldc, ldw = (int)g.w.ldc;
+  const __amdgpu_buffer_rsrc_t xb = dma_buffer(g.x.codes + m0 * g.x.ldc, (long long)(rows - 1) * ldx + k16);
+  const __amdgpu_buffer_rsrc_t wb = dma_buffer(g.w.codes + n0 * g.w.ldc, (long long)(cols - 1) * ldw + k16);
+
+  // load i of this wavefront brings rows 8 (wave XI + i) .. + 7 of x: lane's row 8 (..) + lane / 8, place lane % 8
+  int xo[XI], wo[WI], wc[WI];
+  const int xc = 16 * ((lane & 7) ^ (lane >> 3));
+#pragma unroll
+  for (int i = 0; i < XI; ++i) xo[i] = (8 * (wave * XI + i) + (lane >> 3)) * ldx + xc;
+#pragma unroll
+  for (int i = 0; i < WI; ++i) {
+    const int row = 8 * (wave * WI + i) + (lane >> 3);
+    wc[i] = 16 * ((lane & 7) ^ turn_w(row));
+    wo[i] = row * ldw + wc[i];
+  }
+  auto fetch = [&](uint8_t* st, int k0) {
+#pragma unroll
+    for (int i = 0; i < XI; ++i)
+      dma16(xb, st + (wave * XI + i) * 1024, k0 + xc < k16 ? xo[i] : DMA_ABSENT, k0);
+#pragma unroll
+    for (int i = 0; i < WI; ++i)
+      dma16(wb, st + BM * STEP + (wave * WI + i) * 1024, k0 + wc[i] < k16 ? wo[i] : DMA_ABSENT, k0);
+  };
+
+  // scale bytes of this lane's operand rows (rows behind the last are read as the last one's; what they give is not stored)
+  const uint8_t *xs[FM], *ws[4];
+#pragma unroll
+  for (int i = 0; i < FM; ++i) {
+    const int row = (wm * FM + i) * 16 + r;
+    xs[i] = g.x.scales + (m0 + (row < rows ? row : rows - 1)) * g.x.lds;
+  }
+#pragma unroll
+  for (int f = 0; f < 4; ++f) {
+    const int row = wn * 64 + (f >> 1) * 32 + 8 * (r >> 2) + 4 * (f & 1) + (r & 3);
+    ws[f] = g.w.scales + (long long)(n0 + (row < cols ? row : cols - 1)) * g.w.lds;
+  }
+  int sx[FM], sw[4], nx[FM], nw[4];
+  auto scales = [&](int b) {
+#pragma unroll
+    for (int i = 0; i < FM; ++i) nx[i] = xs[i][b];
+#pragma unroll
+    for (int f = 0; f < 4; ++f) nw[f] = ws[f][b];
+  };
+
+  f32x4 acc[4][FM];
+#pragma unroll
+  for (int f = 0; f < 4; ++f)
+#pragma unroll
+    for (int i = 0; i < FM; ++i) acc[f][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  auto take = [&](const uint8_t* st, int row, int turn) {
+    Codes c;
+    const uint8_t* p = st + row * STEP;
+    c.lo = *reinterpret_cast<const i32x4*>(p + 16 * ((2 * kg) ^ turn));
+    c.hi = *reinterpret_cast<const i32x4*>(p + 16 * ((2 * kg + 1) ^ turn));
+    return c;
+  };
+  auto multiply = [&](const uint8_t* st) {
+    Codes cw[4];
+    Terms tw[F8 ? 1 : 4];
+#pragma unroll
+    for (int f = 0; f < 4; ++f) {
+      const int row = wn * 64 + (f >> 1) * 32 + 8 * (r >> 2) + 4 * (f & 1) + (r & 3);
+      cw[f] = take(st + BM * STEP, row, turn_w(row));
+      if constexpr (!F8) tw[f] = decode(cw[f], a8_scale(sw[f]));
+    }
+#pragma unroll
+    for (int i = 0; i < FM; ++i) {
+      const int row = (wm * FM + i) * 16 + r;
+      const Codes cx = take(st, row, turn_x(row));
+      if constexpr (F8) {
+#pragma unroll
+        for (int f = 0; f < 4; ++f) acc[f][i] = mfma_f8(cw[f], sw[f], cx, sx[i], acc[f][i]);
+      } else {
+        const Terms tx = decode(cx, a8_scale(sx[i]));
+#pragma unroll
+        for (int f = 0; f < 4; ++f) acc[f][i] = mfma_b16(tw[f], tx, acc[f][i]);
+      }
+    }
+  };
+  auto step = [&](int s, const uint8_t* st, uint8_t* other) {
+    __syncthreads();   // this stage's loads are done, the other one's readers too
+#pragma unroll
+    for (int i = 0; i < FM; ++i) sx[i] = nx[i];
+#pragma unroll
+    for (int f = 0; f < 4; ++f) sw[f] = nw[f];
+    if (s + 1 < steps) { fetch(other, (s + 1) * STEP); scales(s + 1); }
+    multiply(st);
+  };
+  fetch(ring0, 0);
+  scales(0);
+  for (int s = 0; s < steps; s += 2) {
+    step(s, ring0, ring1);
+    if (s + 1 < steps) step(s + 1, ring1, ring0);
+  }
+
+  // lane: row r of each 16, columns 32 p + 8 kg .. + 7 of the wavefront's 64
+#pragma unroll
+  for (int p = 0; p < 2; ++p) {
+    const int n = n0 + wn * 64 + p * 32 + 8 * kg;
+    float bias[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) bias[e] = g.bias && n + e < g.N ? g.bias[n + e] : 0.f;
+    const bool whole8 = vec && n + 8 <= g.N;
+#pragma unroll
+    for (int i = 0; i < FM; ++i) {
+      const int row = (wm * FM + i) * 16 + r;
+      if (row >= rows) continue;
+      T* y = (T*)g.y + (m0 + row) * g.ldy + n;
+      const T* res = g.resid ? (const T*)g.resid + (m0 + row) * g.ldr + n : nullptr;
+      float v[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = act_f<ACT>(acc[2 * p + (e >> 2)][i][e & 3] + bias[e]);
+      if (whole8) {
+        typedef T vec8 __attribute__((ext_vector_type(16 / sizeof(T))));
+        constexpr int E = 16 / sizeof(T);
+#pragma unroll
+        for (int h = 0; h < 8 / E; ++h) {
+          vec8 o;
+          if (res) {
+            const vec8 q = *reinterpret_cast<const vec8*>(res + h * E);
+#pragma unroll
+            for (int e = 0; e < E; ++e) v[h * E + e] += to_f(q[e]);
+          }
+#pragma unroll
+          for (int e = 0; e < E; ++e) o[e] = from_f<T>(v[h * E + e]);
+          *reinterpret_cast<vec8*>(y + h * E) = o;
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (n + e < g.N) y[e] = from_f<T>(v[e] + (res ? to_f(res[e]) : 0.f));
+      }
+    }
+  }
+}
+
+template <int BM, int BN, int FM, int ACT, typename T>
+hipError_t tiles(const A8Linear& g, hipStream_t s) {
+  const int TM = (int)((g.M + BM - 1) / BM), TN = (g.N + BN - 1) / BN;
+  auto ok = [&](const void* p, long long ld) { return !p || (((uintptr_t)p & 15) == 0 && ld * sizeof(T) % 16 == 0); };
+  const long long grid = (long long)(TM + 7) / 8 * 8 * TN;
+  linear_tile_k<BM, BN, FM, ACT, T><<<(unsigned)grid, 64 * (BM / (16 * FM)) * (BN / 64), 0, s>>>(
+      g, TM, TN, ok(g.y, g.ldy) && ok(g.resid, g.ldr));
+  return hipGetLastError();
+}
+
 template <int ACT, typename T>
 hipError_t run(const A8Linear& g, hipStream_t s) {
-  return few<ACT, T>(g, s);
+  const long long t128 = ((g.M + 127) / 128) * ((g.N + 127) / 128), t256 = ((g.M + 255) / 256) * ((g.N + 255) / 256);
+  // 32-bit offsets within a tile's rows; the launch's threads within 2^32
+  const bool near = g.x.ldc <= (1 << 22) && g.w.ldc <= (1 << 22) && t128 < (1 << 23);
+  if (!near || g.M <= 64 || t128 < 64) return few<ACT, T>(g, s);
+  if constexpr (sizeof(T) == 2)
+    if (t256 >= 192 && g.K >= 768) return tiles<256, 256, 8, ACT, T>(g, s);
+  return tiles<128, 128, 4, ACT, T>(g, s);
 }
 
 template <typename T>
