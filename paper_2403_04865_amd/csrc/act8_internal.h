@@ -56,12 +56,27 @@ __device__ __forceinline__ void a8_value4(unsigned q, float s, float (&v)[4]) {
   v[0] = lo[0] * s; v[1] = lo[1] * s; v[2] = hi[0] * s; v[3] = hi[1] * s;
 }
 
-// act(u) and act'(u)
-__device__ __forceinline__ float sigmoid_f(float u) { return __builtin_amdgcn_rcpf(1.0f + __expf(-u)); }
+// act(u).  GELU: with h = erfc(|u| / sqrt 2) / 2, u Phi(u) = max(u, 0) - |u| h for either sign, no difference of nearly equal numbers;
+// h by the same rational approximation as erf_exp (7.1.26 of Abramowitz & Stegun, error 7.5e-8 in h), the factors folded into its
+// constants.  Behind GELU_FAR h is below the smallest float, so the argument may stop there (an infinity stays one).
+constexpr float GELU_FAR = 16.f;
+__device__ __forceinline__ float half_erfc(float x, float* e_out) {   // 0 <= x <= GELU_FAR; e_out: exp(-x^2 / 2)
+  const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.3275911f * 0.70710678118654752f, x, 1.0f));
+  const float e = __builtin_amdgcn_exp2f(x * x * -0.72134752044448170f);
+  *e_out = e;
+  return (((((0.5f * 1.061405429f) * t - 0.5f * 1.453152027f) * t + 0.5f * 1.421413741f) * t - 0.5f * 0.284496736f) * t + 0.5f * 0.254829592f) * t * e;
+}
+__device__ __forceinline__ float sigmoid_f(float u) {
+  return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(u * -1.4426950408889634f));
+}
 template <int ACT> __device__ __forceinline__ float act_f(float u) {
   if constexpr (ACT == SLIDE_ACT_RELU) return u < 0.f ? 0.f : u;      // a NaN stays one
   if constexpr (ACT == SLIDE_ACT_SILU) return u * sigmoid_f(u);
-  if constexpr (ACT == SLIDE_ACT_GELU) return gelu_f(u);
+  if constexpr (ACT == SLIDE_ACT_GELU) {
+    float e;
+    const float x = fminf(fabsf(u), GELU_FAR), h = half_erfc(x, &e);
+    return __builtin_fmaf(-x, h, u < 0.f ? 0.f : u);   // a NaN stays one
+  }
   return u;
 }
 

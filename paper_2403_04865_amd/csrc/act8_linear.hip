@@ -21,14 +21,21 @@ namespace {
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 
-// 32 codes of a lane
-struct Codes { i32x4 lo, hi; };
-
-__device__ __forceinline__ i32x8 whole(const Codes& c) {
-  return __builtin_shufflevector(c.lo, c.hi, 0, 1, 2, 3, 4, 5, 6, 7);
+typedef i32x8 Codes;   // 32 codes of a lane
+__device__ __forceinline__ Codes codes_of(const uint8_t* lo, const uint8_t* hi) {   // two pieces of 16
+  return __builtin_shufflevector(*reinterpret_cast<const i32x4*>(lo), *reinterpret_cast<const i32x4*>(hi), 0, 1, 2, 3, 4, 5, 6, 7);
 }
 __device__ __forceinline__ f32x4 mfma_f8(const Codes& a, int sa, const Codes& b, int sb, f32x4 c) {
-  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(whole(a), whole(b), c, 0, 0, 0, sa, 0, sb);
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, 0, sa, 0, sb);
+}
+// the same with byte `at` (known when compiled, behind the unrolling) of both scale registers
+__device__ __forceinline__ f32x4 mfma_f8_at(int at, const Codes& a, int sa, const Codes& b, int sb, f32x4 c) {
+  switch (at) {
+    case 0: return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, 0, sa, 0, sb);
+    case 1: return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, 1, sa, 1, sb);
+    case 2: return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, 2, sa, 2, sb);
+    default: return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, 3, sa, 3, sb);
+  }
 }
 // eight codes -> bfloat16 values times s; exact
 __device__ __forceinline__ bf16x8 decode8(int q0, int q1, float s) {
@@ -43,7 +50,7 @@ __device__ __forceinline__ bf16x8 decode8(int q0, int q1, float s) {
 // a lane's 32 codes as the operands of four products of 32 columns
 struct Terms { bf16x8 t[4]; };
 __device__ __forceinline__ Terms decode(const Codes& c, float s) {
-  return Terms{{decode8(c.lo[0], c.lo[1], s), decode8(c.lo[2], c.lo[3], s), decode8(c.hi[0], c.hi[1], s), decode8(c.hi[2], c.hi[3], s)}};
+  return Terms{{decode8(c[0], c[1], s), decode8(c[2], c[3], s), decode8(c[4], c[5], s), decode8(c[6], c[7], s)}};
 }
 __device__ __forceinline__ f32x4 mfma_b16(const Terms& a, const Terms& b, f32x4 c) {
 #pragma unroll
@@ -51,12 +58,10 @@ __device__ __forceinline__ f32x4 mfma_b16(const Terms& a, const Terms& b, f32x4 
   return c;
 }
 
-__device__ __forceinline__ Codes load_codes(const uint8_t* p, int k, int k16) {
-  Codes c;
+__device__ __forceinline__ Codes load_codes(const uint8_t* p, int k, int k16) {   // zeros from k16 on
   const i32x4 z = {0, 0, 0, 0};
-  c.lo = k < k16 ? *reinterpret_cast<const i32x4*>(p + k) : z;
-  c.hi = k + 16 < k16 ? *reinterpret_cast<const i32x4*>(p + k + 16) : z;
-  return c;
+  const i32x4 lo = k < k16 ? *reinterpret_cast<const i32x4*>(p + k) : z, hi = k + 16 < k16 ? *reinterpret_cast<const i32x4*>(p + k + 16) : z;
+  return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
 // ---- few rows -------------------------------------------------------------------------------------------------------
@@ -151,18 +156,114 @@ hipError_t few(const A8Linear& g, hipStream_t s) {
 // one step ahead, in two stages.  A row of a stage is eight 16-byte pieces; piece c lies in place c ^ (3 bits of the row), chosen so
 // that eight neighbouring lanes of a fragment read find their pieces in eight different places (no bank conflicts).
 constexpr int STEP = A8_BLOCK;
+constexpr int CHUNK = 32, SROW = CHUNK + 4;   // blocks whose scales lie in LDS together; bytes between rows of them there
 
 __device__ __forceinline__ int turn_x(int row) { return row & 7; }
 // rows of w are dealt to fragments so that neighbouring lanes have rows 0 1 2 3, 8 9 10 11
 __device__ __forceinline__ int turn_w(int row) { return (row & 3) | ((row >> 1) & 4); }
 
+// A wavefront's 16 FM rows of 64 columns: bias, activation, residual and the way out.  A lane has row r of each 16 and columns
+// 32 p + 8 kg .. + 7.  They go through a patch of LDS, 16 rows at a time, and leave in whole rows of 64 columns: written as the
+// lanes have them, 64 bytes of a row at a time, every half cache line was fetched from memory first (403456 x 1536 -> 384: 561 us, 373
+// so).  A residual comes the same way in.  Buffer instructions: what lies behind the last row or column is left out without a branch.
+struct Store {
+  void* y; long long ldy;            // the wavefront's first value
+  const void* res; long long ldr;    // may be null
+  int have, left;                    // rows and columns that exist from there on
+  bool vec;                          // 16-byte pieces of y and the residual are aligned
+  bool stream;                       // y is larger than what the caches would keep of it
+};
+// What is written past this many bytes of y has left the 256 MB of last-level cache before anybody reads it: stores with the
+// streaming hint (403456 x 384 -> 1536: 422 -> 327 us; 200000 x 512: 111 -> 96; 134 MB of output: no difference)
+constexpr long long STREAM_BYTES = 160 << 20;
+template <typename T> constexpr int patch_row() { return 64 * (int)sizeof(T) + 16; }   // bytes between rows of a patch (no bank conflicts)
+
+template <typename T>
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t out_buffer(const void* p, long long ld, const Store& o) {
+  return dma_buffer(p, o.have > 0 && o.left > 0 ? ((o.have - 1) * ld + (o.left < 64 ? o.left : 64)) * (long long)sizeof(T) : 0);
+}
+
+template <int FM, int ACT, typename T>
+__device__ __forceinline__ void store_tile(const f32x4 (&acc)[4][FM], const f32x4 (&bias)[2][2], uint8_t* patch, int lane, const Store& o) {
+  constexpr int E = 16 / sizeof(T), PROW = patch_row<T>(), LR = 64 / E, RP = 64 / LR, NH = 16 / RP;   // lanes of a row, rows at a time
+  typedef T vec16 __attribute__((ext_vector_type(E)));
+  const int r = lane & 15, kg = lane >> 4, orow = lane / LR, oc = lane % LR * E;
+  const bool fast = o.vec && (o.left >= 64 || o.left % E == 0);   // uniform
+  const __amdgpu_buffer_rsrc_t yb = out_buffer<T>(o.y, o.ldy, o), rb = out_buffer<T>(o.res, o.res ? o.ldr : 0, o);
+  const int yo = oc < o.left ? (orow * (int)o.ldy + oc) * (int)sizeof(T) : DMA_ABSENT, ro = oc < o.left ? (orow * (int)o.ldr + oc) * (int)sizeof(T) : DMA_ABSENT;
+  uint8_t* const out = patch + orow * PROW + oc * sizeof(T);
+  u32x4 q[NH];
+  auto fetch = [&](int i) {
+#pragma unroll
+    for (int h = 0; h < NH; ++h) q[h] = __builtin_amdgcn_raw_buffer_load_b128(rb, ro, (i * 16 + h * RP) * (int)o.ldr * (int)sizeof(T), 0);
+  };
+  if (o.res && fast) fetch(0);
+#pragma unroll
+  for (int i = 0; i < FM; ++i) {
+    if (o.res) {   // uniform
+      if (fast) {
+#pragma unroll
+        for (int h = 0; h < NH; ++h) *reinterpret_cast<u32x4*>(out + h * RP * PROW) = q[h];
+        if (i + 1 < FM) fetch(i + 1);
+      } else {
+#pragma unroll 1
+        for (int k = lane; k < 16 * 64; k += 64) {
+          const int row = k >> 6, c = k & 63;
+          if (i * 16 + row < o.have && c < o.left)
+            *reinterpret_cast<T*>(patch + row * PROW + c * sizeof(T)) = ((const T*)o.res)[(i * 16 + row) * o.ldr + c];
+        }
+      }
+      __builtin_amdgcn_wave_barrier();   // the patch is this wavefront's own; its LDS accesses are in order
+    }
+#pragma unroll
+    for (int p = 0; p < 2; ++p)
+#pragma unroll
+      for (int h = 0; h < 8 / E; ++h) {
+        vec16* at = reinterpret_cast<vec16*>(patch + r * PROW + (32 * p + 8 * kg + h * E) * sizeof(T));
+        float v[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          const int k = h * E + e;
+          v[e] = act_f<ACT>(acc[2 * p + (k >> 2)][i][k & 3] + bias[p][k >> 2][k & 3]);
+        }
+        if (o.res) {
+          const vec16 z = *at;
+#pragma unroll
+          for (int e = 0; e < E; ++e) v[e] += to_f(z[e]);
+        }
+        vec16 w;
+#pragma unroll
+        for (int e = 0; e < E; ++e) w[e] = from_f<T>(v[e]);
+        *at = w;
+      }
+    __builtin_amdgcn_wave_barrier();
+    if (fast) {
+#pragma unroll
+      for (int h = 0; h < NH; ++h) {
+        const u32x4 w = *reinterpret_cast<const u32x4*>(out + h * RP * PROW);
+        const int at = (i * 16 + h * RP) * (int)o.ldy * (int)sizeof(T);
+        if (o.stream) __builtin_amdgcn_raw_buffer_store_b128(w, yb, yo, at, 2);
+        else __builtin_amdgcn_raw_buffer_store_b128(w, yb, yo, at, 0);
+      }
+    } else {
+#pragma unroll 1
+      for (int k = lane; k < 16 * 64; k += 64) {
+        const int row = k >> 6, c = k & 63;
+        if (i * 16 + row < o.have && c < o.left)
+          ((T*)o.y)[(i * 16 + row) * o.ldy + c] = *reinterpret_cast<const T*>(patch + row * PROW + c * sizeof(T));
+      }
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
 template <int BM, int BN, int FM, int ACT, typename T>
-__global__ void __launch_bounds__(64 * (BM / (16 * FM)) * (BN / 64)) linear_tile_k(A8Linear g, int TM, int TN, bool vec) {
+__global__ void __launch_bounds__(64 * (BM / (16 * FM)) * (BN / 64)) linear_tile_k(A8Linear g, int TM, int TN, bool vec, bool stream) {
   constexpr bool F8 = sizeof(T) == 2;
   constexpr int WM = BM / (16 * FM), NW = WM * (BN / 64);
   constexpr int XI = BM / 8 / NW, WI = BN / 8 / NW;   // kilobytes that a wavefront loads per step
   static_assert(XI * 8 * NW == BM && WI * 8 * NW == BN, "loads are dealt evenly");
-  __shared__ __attribute__((aligned(16))) uint8_t ring0[(BM + BN) * STEP], ring1[(BM + BN) * STEP];
+  __shared__ __attribute__((aligned(16))) uint8_t ring0[(BM + BN) * STEP], ring1[(BM + BN) * STEP], sc[(BM + BN) * SROW];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave % WM, wn = wave / WM, r = lane & 15, kg = lane >> 4;
   // consecutive tiles of the same rows of x run on one XCD and share them in its L2
@@ -196,24 +297,45 @@ __global__ void __launch_bounds__(64 * (BM / (16 * FM)) * (BN / 64)) linear_tile
       dma16(wb, st + BM * STEP + (wave * WI + i) * 1024, k0 + wc[i] < k16 ? wo[i] : DMA_ABSENT, k0);
   };
 
-  // scale bytes of this lane's operand rows (rows behind the last are read as the last one's; what they give is not stored)
-  const uint8_t *xs[FM], *ws[4];
+  // Scale bytes of up to CHUNK blocks of every row of the tile go to LDS together (rows behind the last one: any byte, what they give is
+  // not stored), and from there four blocks of a row per register.  As single bytes out of memory, a dozen loads of 16 rows per
+  // wavefront and step, they cost as much as the products (8192 x 4096 x 4096: 253 us, 125 without them).
+  auto stage_scales = [&](int b0) {
+    const int nb = steps - b0 < CHUNK ? steps - b0 : CHUNK;
+    auto rows_of = [&](const uint8_t* p, long long ld, int have, uint8_t* to) {
+      if (((uintptr_t)p & 3) == 0 && (ld & 3) == 0) {   // uniform
+        const int nd = (nb + 3) / 4;
+        for (int i = tid; i < have * nd; i += 64 * NW) {
+          const int row = i / nd, d = 4 * (i - row * nd);
+          const uint8_t* from = p + row * ld + d;
+          if (d + 4 <= nb) *reinterpret_cast<unsigned*>(to + row * SROW + d) = *reinterpret_cast<const unsigned*>(from);
+          else
+            for (int e = 0; d + e < nb; ++e) to[row * SROW + d + e] = from[e];
+        }
+      } else {
+        for (int i = tid; i < have * nb; i += 64 * NW) {
+          const int row = i / nb, d = i - row * nb;
+          to[row * SROW + d] = p[row * ld + d];
+        }
+      }
+    };
+    rows_of(g.x.scales + m0 * g.x.lds + b0, g.x.lds, rows, sc);
+    rows_of(g.w.scales + (long long)n0 * g.w.lds + b0, g.w.lds, cols, sc + BM * SROW);
+  };
+  int sx[FM], sw[4];
+  auto scales = [&](int b) {   // b: block within the chunk
+    if ((b & 3) == 0) {
 #pragma unroll
-  for (int i = 0; i < FM; ++i) {
-    const int row = (wm * FM + i) * 16 + r;
-    xs[i] = g.x.scales + (m0 + (row < rows ? row : rows - 1)) * g.x.lds;
-  }
+      for (int i = 0; i < FM; ++i) sx[i] = *reinterpret_cast<const int*>(sc + ((wm * FM + i) * 16 + r) * SROW + b);
 #pragma unroll
-  for (int f = 0; f < 4; ++f) {
-    const int row = wn * 64 + (f >> 1) * 32 + 8 * (r >> 2) + 4 * (f & 1) + (r & 3);
-    ws[f] = g.w.scales + (long long)(n0 + (row < cols ? row : cols - 1)) * g.w.lds;
-  }
-  int sx[FM], sw[4], nx[FM], nw[4];
-  auto scales = [&](int b) {
+      for (int f = 0; f < 4; ++f)
+        sw[f] = *reinterpret_cast<const int*>(sc + (BM + wn * 64 + (f >> 1) * 32 + 8 * (r >> 2) + 4 * (f & 1) + (r & 3)) * SROW + b);
+    } else {
 #pragma unroll
-    for (int i = 0; i < FM; ++i) nx[i] = xs[i][b];
+      for (int i = 0; i < FM; ++i) sx[i] = (int)((unsigned)sx[i] >> 8);
 #pragma unroll
-    for (int f = 0; f < 4; ++f) nw[f] = ws[f][b];
+      for (int f = 0; f < 4; ++f) sw[f] = (int)((unsigned)sw[f] >> 8);
+    }
   };
 
   f32x4 acc[4][FM];
@@ -223,11 +345,8 @@ __global__ void __launch_bounds__(64 * (BM / (16 * FM)) * (BN / 64)) linear_tile
     for (int i = 0; i < FM; ++i) acc[f][i] = f32x4{0.f, 0.f, 0.f, 0.f};
 
   auto take = [&](const uint8_t* st, int row, int turn) {
-    Codes c;
     const uint8_t* p = st + row * STEP;
-    c.lo = *reinterpret_cast<const i32x4*>(p + 16 * ((2 * kg) ^ turn));
-    c.hi = *reinterpret_cast<const i32x4*>(p + 16 * ((2 * kg + 1) ^ turn));
-    return c;
+    return codes_of(p + 16 * ((2 * kg) ^ turn), p + 16 * ((2 * kg + 1) ^ turn));
   };
   auto multiply = [&](const uint8_t* st) {
     Codes cw[4];
@@ -236,7 +355,7 @@ __global__ void __launch_bounds__(64 * (BM / (16 * FM)) * (BN / 64)) linear_tile
     for (int f = 0; f < 4; ++f) {
       const int row = wn * 64 + (f >> 1) * 32 + 8 * (r >> 2) + 4 * (f & 1) + (r & 3);
       cw[f] = take(st + BM * STEP, row, turn_w(row));
-      if constexpr (!F8) tw[f] = decode(cw[f], a8_scale(sw[f]));
+      if constexpr (!F8) tw[f] = decode(cw[f], a8_scale(sw[f] & 0xff));
     }
 #pragma unroll
     for (int i = 0; i < FM; ++i) {
@@ -246,7 +365,7 @@ __global__ void __launch_bounds__(64 * (BM / (16 * FM)) * (BN / 64)) linear_tile
 #pragma unroll
         for (int f = 0; f < 4; ++f) acc[f][i] = mfma_f8(cw[f], sw[f], cx, sx[i], acc[f][i]);
       } else {
-        const Terms tx = decode(cx, a8_scale(sx[i]));
+        const Terms tx = decode(cx, a8_scale(sx[i] & 0xff));
 #pragma unroll
         for (int f = 0; f < 4; ++f) acc[f][i] = mfma_b16(tw[f], tx, acc[f][i]);
       }
@@ -254,59 +373,31 @@ __global__ void __launch_bounds__(64 * (BM / (16 * FM)) * (BN / 64)) linear_tile
   };
   auto step = [&](int s, const uint8_t* st, uint8_t* other) {
     __syncthreads();   // this stage's loads are done, the other one's readers too
-#pragma unroll
-    for (int i = 0; i < FM; ++i) sx[i] = nx[i];
-#pragma unroll
-    for (int f = 0; f < 4; ++f) sw[f] = nw[f];
-    if (s + 1 < steps) { fetch(other, (s + 1) * STEP); scales(s + 1); }
+    if (s > 0 && (s & (CHUNK - 1)) == 0) { stage_scales(s); __syncthreads(); }
+    if (s + 1 < steps) fetch(other, (s + 1) * STEP);
+    scales(s & (CHUNK - 1));
     multiply(st);
   };
   fetch(ring0, 0);
-  scales(0);
+  stage_scales(0);
   for (int s = 0; s < steps; s += 2) {
     step(s, ring0, ring1);
     if (s + 1 < steps) step(s + 1, ring1, ring0);
   }
 
-  // lane: row r of each 16, columns 32 p + 8 kg .. + 7 of the wavefront's 64
+  __syncthreads();   // every wavefront has left the stages
+  const int nw = n0 + wn * 64, nl = nw + 8 * kg, row0 = wm * FM * 16;
+  f32x4 bias[2][2];
 #pragma unroll
-  for (int p = 0; p < 2; ++p) {
-    const int n = n0 + wn * 64 + p * 32 + 8 * kg;
-    float bias[8];
+  for (int p = 0; p < 2; ++p)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) bias[e] = g.bias && n + e < g.N ? g.bias[n + e] : 0.f;
-    const bool whole8 = vec && n + 8 <= g.N;
-#pragma unroll
-    for (int i = 0; i < FM; ++i) {
-      const int row = (wm * FM + i) * 16 + r;
-      if (row >= rows) continue;
-      T* y = (T*)g.y + (m0 + row) * g.ldy + n;
-      const T* res = g.resid ? (const T*)g.resid + (m0 + row) * g.ldr + n : nullptr;
-      float v[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = act_f<ACT>(acc[2 * p + (e >> 2)][i][e & 3] + bias[e]);
-      if (whole8) {
-        typedef T vec8 __attribute__((ext_vector_type(16 / sizeof(T))));
-        constexpr int E = 16 / sizeof(T);
-#pragma unroll
-        for (int h = 0; h < 8 / E; ++h) {
-          vec8 o;
-          if (res) {
-            const vec8 q = *reinterpret_cast<const vec8*>(res + h * E);
-#pragma unroll
-            for (int e = 0; e < E; ++e) v[h * E + e] += to_f(q[e]);
-          }
-#pragma unroll
-          for (int e = 0; e < E; ++e) o[e] = from_f<T>(v[h * E + e]);
-          *reinterpret_cast<vec8*>(y + h * E) = o;
-        }
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (n + e < g.N) y[e] = from_f<T>(v[e] + (res ? to_f(res[e]) : 0.f));
-      }
+    for (int e = 0; e < 8; ++e) {
+      const int n = nl + 32 * p + e;
+      bias[p][e >> 2][e & 3] = g.bias ? g.bias[n < g.N ? n : g.N - 1] : 0.f;
     }
-  }
+  const Store o{(T*)g.y + (m0 + row0) * g.ldy + nw, g.ldy, g.resid ? (const T*)g.resid + (m0 + row0) * g.ldr + nw : nullptr, g.ldr,
+                rows - row0, g.N - nw, vec, stream};
+  store_tile<FM, ACT, T>(acc, bias, ring0 + wave * 16 * patch_row<T>(), lane, o);
 }
 
 template <int BM, int BN, int FM, int ACT, typename T>
@@ -315,18 +406,157 @@ hipError_t tiles(const A8Linear& g, hipStream_t s) {
   auto ok = [&](const void* p, long long ld) { return !p || (((uintptr_t)p & 15) == 0 && ld * sizeof(T) % 16 == 0); };
   const long long grid = (long long)(TM + 7) / 8 * 8 * TN;
   linear_tile_k<BM, BN, FM, ACT, T><<<(unsigned)grid, 64 * (BM / (16 * FM)) * (BN / 64), 0, s>>>(
-      g, TM, TN, ok(g.y, g.ldy) && ok(g.resid, g.ldr));
+      g, TM, TN, ok(g.y, g.ldy) && ok(g.resid, g.ldr), g.M * g.N * (long long)sizeof(T) >= STREAM_BYTES);
   return hipGetLastError();
+}
+
+// ---- many rows, short contraction ------------------------------------------------------------------------------------
+// With K <= 384 a wavefront holds all of its rows of x, 16 FM of them, in registers (KB blocks of 128), and w streams past in stages of
+// 64 rows, one stage ahead, shared by the workgroup's wavefronts.  Next to a tile of the kernel above, which starts, loads three steps
+// and stores: x is read once, nothing drains between tiles, and the epilogue of one wavefront runs under the products of the others
+// (403456 x 384 -> 1536: 422 us, 487 by tiles of 256, 637 by tiles of 128; from K = 512 on the tiles of 256 were the faster ones).
+constexpr int RN = 64, RCOLS = 1024;   // rows of w per stage; most columns of y of a workgroup
+
+constexpr int RWAVES = 4;              // two such workgroups per compute unit
+template <int KB> constexpr int rows_fm() { return KB <= 2 ? 4 : 3; }   // what fits 256 registers
+
+template <int KB, int ACT>
+__global__ void __launch_bounds__(64 * RWAVES, 2) linear_rows_k(A8Linear g, int TM, int TN, int ncols, bool vec, bool stream) {
+  constexpr int FM = rows_fm<KB>(), NW = RWAVES, STAGE = RN * KB * STEP, LOADS = RN / 8 * KB / NW;
+  static_assert(LOADS * NW * 8 == RN * KB, "loads are dealt evenly");
+  __shared__ __attribute__((aligned(16))) uint8_t ring0[STAGE], ring1[STAGE], wsc[RCOLS * 4], patch[NW][16 * patch_row<bf16>()];
+  __shared__ __attribute__((aligned(16))) float bia[RCOLS];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, kg = lane >> 4;
+  const int j = blockIdx.x >> 3, tm = (int)(blockIdx.x & 7) + 8 * (j / TN), tn = j % TN;   // column pieces of the same rows on one XCD
+  if (tm >= TM) return;
+  const long long m0 = (long long)tm * (16 * FM * NW) + wave * (16 * FM);
+  const int n0 = tn * ncols, cols = g.N - n0 < ncols ? g.N - n0 : ncols, stages = (cols + RN - 1) / RN;
+  const int k16 = (g.K + A8_GRAIN - 1) / A8_GRAIN * A8_GRAIN;
+  const int ldw = (int)g.w.ldc;
+
+  int wo[LOADS], wk[LOADS];   // load i: eight rows of one block; offset in memory, column
+#pragma unroll
+  for (int i = 0; i < LOADS; ++i) {
+    const int q = wave * LOADS + i, b = q >> 3, row = 8 * (q & 7) + (lane >> 3);
+    wk[i] = b * STEP + 16 * ((lane & 7) ^ turn_w(row));
+    wo[i] = row * ldw + wk[i];
+  }
+  auto fetch = [&](uint8_t* st, int s) {
+    const int n = n0 + s * RN, left = cols - s * RN < RN ? cols - s * RN : RN;
+    const __amdgpu_buffer_rsrc_t wb = dma_buffer(g.w.codes + (long long)n * g.w.ldc, (long long)(left - 1) * ldw + k16);
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) dma16(wb, st + (wave * LOADS + i) * 1024, wk[i] < k16 ? wo[i] : DMA_ABSENT, 0);
+  };
+  fetch(ring0, 0);
+  for (int c = tid; c < cols; c += 64 * NW) {
+    const uint8_t* p = g.w.scales + (long long)(n0 + c) * g.w.lds;
+#pragma unroll
+    for (int b = 0; b < KB; ++b) wsc[c * 4 + b] = p[b];
+    bia[c] = g.bias ? g.bias[n0 + c] : 0.f;
+  }
+
+  // this wavefront's rows (behind the last: the last one again, nothing of it is stored)
+  Codes x[FM][KB];
+  unsigned sx[FM];   // a byte per block
+#pragma unroll
+  for (int i = 0; i < FM; ++i) {
+    const long long m = m0 + 16 * i + r < g.M ? m0 + 16 * i + r : g.M - 1;
+    const uint8_t *p = g.x.codes + m * g.x.ldc, *q = g.x.scales + m * g.x.lds;
+#pragma unroll
+    for (int b = 0; b < KB; ++b) x[i][b] = load_codes(p, b * A8_BLOCK + 32 * kg, k16);
+    sx[i] = 0;
+#pragma unroll
+    for (int b = 0; b < KB; ++b) sx[i] |= (unsigned)q[b] << (8 * b);
+  }
+
+  const int have = (int)(g.M - m0 < 16 * FM ? g.M - m0 : 16 * FM);   // may be negative
+  // where a lane's two pieces of fragment 0 lie: row 8 (r / 4) + r % 4 (fragment f: 32 (f / 2) + 4 (f % 2) rows on, the same turn)
+  const int wrow = 8 * (r >> 2) + (r & 3), wlo = wrow * STEP + 16 * ((2 * kg) ^ turn_w(wrow)), whi = wrow * STEP + 16 * ((2 * kg + 1) ^ turn_w(wrow));
+  auto step = [&](int s, const uint8_t* st, uint8_t* other) {
+    __syncthreads();   // this stage's loads are done, the other one's readers too
+    if (s + 1 < stages) fetch(other, s + 1);
+    f32x4 acc[4][FM];
+    unsigned sw[4];
+#pragma unroll
+    for (int f = 0; f < 4; ++f) {
+      const int row = (f >> 1) * 32 + 8 * (r >> 2) + 4 * (f & 1) + (r & 3);
+      sw[f] = *reinterpret_cast<const unsigned*>(wsc + (s * RN + row) * 4);
+#pragma unroll
+      for (int i = 0; i < FM; ++i) acc[f][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    // Fragments of w two ahead of their products; the fences keep the compiler from fetching all of them first (it spilled).
+    auto frag = [&](int q) {   // q: fragment q % 4 of block q / 4
+      const uint8_t* p = st + (q >> 2) * RN * STEP + ((q >> 1) & 1) * 32 * STEP + (q & 1) * 4 * STEP;
+      return codes_of(p + wlo, p + whi);
+    };
+    Codes cw[3];
+    cw[0] = frag(0);
+    cw[1] = frag(1);
+#pragma unroll
+    for (int q = 0; q < 4 * KB; ++q) {
+      const int f = q & 3, b = q >> 2;
+      if (q + 2 < 4 * KB) cw[(q + 2) % 3] = frag(q + 2);
+#pragma unroll
+      for (int i = 0; i < FM; ++i) acc[f][i] = mfma_f8_at(b, cw[q % 3], (int)sw[f], x[i][b], (int)sx[i], acc[f][i]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    // (keeps the products here: sunk into the branches of the epilogue, they left all their operands waiting in registers)
+#pragma unroll
+    for (int f = 0; f < 4; ++f)
+#pragma unroll
+      for (int i = 0; i < FM; ++i) asm volatile("" : "+v"(acc[f][i]));
+    const int c0 = s * RN;
+    f32x4 bi[2][2];
+#pragma unroll
+    for (int p = 0; p < 2; ++p)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) bi[p][h] = *reinterpret_cast<const f32x4*>(bia + c0 + 32 * p + 8 * kg + 4 * h);
+    const Store o{(bf16*)g.y + m0 * g.ldy + n0 + c0, g.ldy, g.resid ? (const bf16*)g.resid + m0 * g.ldr + n0 + c0 : nullptr, g.ldr,
+                  have, cols - c0, vec, stream};
+    store_tile<FM, ACT, bf16>(acc, bi, patch[wave], lane, o);
+  };
+  for (int s = 0; s < stages; s += 2) {
+    step(s, ring0, ring1);
+    if (s + 1 < stages) step(s + 1, ring1, ring0);
+  }
+}
+
+template <int KB, int ACT>
+hipError_t rows_kb(const A8Linear& g, hipStream_t s) {
+  constexpr int BM = 16 * rows_fm<KB>() * RWAVES, SLOTS = 512;
+  const long long TM = (g.M + BM - 1) / BM;
+  // columns of a workgroup: eight rounds of the chip's workgroups where there is work for them, whole stages, at most RCOLS
+  const int st = (g.N + RN - 1) / RN;
+  long long tn = (8LL * SLOTS + TM - 1) / TM;
+  if (tn > st) tn = st;
+  const int least = (st + RCOLS / RN - 1) / (RCOLS / RN);
+  if (tn < least) tn = least;
+  const int per = (int)((st + tn - 1) / tn), TN = (st + per - 1) / per;
+  auto ok = [&](const void* p, long long ld) { return !p || (((uintptr_t)p & 15) == 0 && ld % 8 == 0); };
+  linear_rows_k<KB, ACT><<<(unsigned)((TM + 7) / 8 * 8 * TN), 64 * RWAVES, 0, s>>>(
+      g, (int)TM, TN, per * RN, ok(g.y, g.ldy) && ok(g.resid, g.ldr), g.M * g.N * 2 >= STREAM_BYTES);
+  return hipGetLastError();
+}
+
+template <int ACT>
+hipError_t rows(const A8Linear& g, hipStream_t s) {
+  if (g.K <= A8_BLOCK) return rows_kb<1, ACT>(g, s);
+  if (g.K <= 2 * A8_BLOCK) return rows_kb<2, ACT>(g, s);
+  return rows_kb<3, ACT>(g, s);
 }
 
 template <int ACT, typename T>
 hipError_t run(const A8Linear& g, hipStream_t s) {
   const long long t128 = ((g.M + 127) / 128) * ((g.N + 127) / 128), t256 = ((g.M + 255) / 256) * ((g.N + 255) / 256);
   // 32-bit offsets within a tile's rows; the launch's threads within 2^32
-  const bool near = g.x.ldc <= (1 << 22) && g.w.ldc <= (1 << 22) && t128 < (1 << 23);
+  const bool near = g.x.ldc <= (1 << 22) && g.w.ldc <= (1 << 22) && g.ldy <= (1 << 21) && g.ldr <= (1 << 21) && t128 < (1 << 22);
   if (!near || g.M <= 64 || t128 < 64) return few<ACT, T>(g, s);
-  if constexpr (sizeof(T) == 2)
-    if (t256 >= 192 && g.K >= 768) return tiles<256, 256, 8, ACT, T>(g, s);
+  if constexpr (sizeof(T) == 2) {
+    // the rows kernel wants several stages of w per workgroup (16384 x 384 -> 384: 13.7 us, 10.2 by tiles of 128; 7289 x 384 -> 1152: 13.1,
+    // 14.6 and by tiles of 256 12.6)
+    if (g.K <= 3 * A8_BLOCK && g.M * g.N >= (1LL << 25)) return rows<ACT>(g, s);
+    if (t256 >= 144) return tiles<256, 256, 8, ACT, T>(g, s);
+  }
   return tiles<128, 128, 4, ACT, T>(g, s);
 }
 

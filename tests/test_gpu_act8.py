@@ -235,7 +235,7 @@ def test_linear_strides_in_place_and_packed_before(rows, cin, cout, extra, dtype
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
-@pytest.mark.parametrize("rows,cin,cout", [(9001, 520, 1160), (8200, 1040, 1500), (70000, 384, 264)])
+@pytest.mark.parametrize("rows,cin,cout", [(9001, 520, 1160), (8200, 1040, 1500), (70000, 384, 520), (140000, 104, 264), (131100, 256, 256), (60000, 384, 1000)])
 def test_linear_many_tiles(rows, cin, cout, dtype):
     """As many output tiles as compute units and more, against float64 products on the device."""
     import torch
