@@ -33,16 +33,16 @@ __device__ __forceinline__ unsigned a8_mag(float v) {
   const unsigned a = __float_as_uint(v) & 0x7fffffffu;
   return a < 0x7f800000u ? a : 0u;
 }
-// the largest of a value over the 16 lanes of a DPP row, in every lane of it
-__device__ __forceinline__ unsigned a8_row_max(unsigned v) {
+// the largest of a value over neighbouring groups of `lanes` lanes (1, 2, 4, 8 or 16; uniform), in every lane of them
+__device__ __forceinline__ unsigned a8_group_max(unsigned v, int lanes) {
   auto step = [&](auto ctrl) {
     const unsigned o = (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, decltype(ctrl)::value, 0xf, 0xf, false);
     v = v > o ? v : o;
   };
-  step(std::integral_constant<int, 0x128>{});   // rotate the row by 8, 4, 2, 1 lanes
-  step(std::integral_constant<int, 0x124>{});
-  step(std::integral_constant<int, 0x122>{});
-  step(std::integral_constant<int, 0x121>{});
+  if (lanes > 1) step(std::integral_constant<int, 0xb1>{});    // lane ^ 1
+  if (lanes > 2) step(std::integral_constant<int, 0x4e>{});    // lane ^ 2
+  if (lanes > 4) step(std::integral_constant<int, 0x141>{});   // 7 - lane within eight: the other four, which are all alike
+  if (lanes > 8) step(std::integral_constant<int, 0x140>{});   // 15 - lane within sixteen
   return v;
 }
 // four values -> four codes: nearest, ties to even; what is not finite becomes a NaN

@@ -1,6 +1,6 @@
 // Activations to 8 bits and back (gfx950).
 //
-// Pack: 16 lanes take a block of 128 columns of one row, 8 columns each: largest finite magnitude over the 16 (rotations within
+// Pack: 16 lanes take a block of 128 columns of one row, 8 columns each: largest finite magnitude over the 16 (within
 // a DPP row), the block's power of two, one exact multiplication and one rounding per value.  One pass, 16-byte loads, 8-byte
 // stores; bound by memory: es + 1 + 1/128 bytes a value (es: 2 or 4).
 #include "act8_internal.h"
@@ -29,7 +29,7 @@ __device__ __forceinline__ void put8(const float (&v)[8], uint8_t* codes, uint8_
   unsigned m = 0;
 #pragma unroll
   for (int e = 0; e < 8; ++e) { const unsigned a = a8_mag(v[e]); m = m > a ? m : a; }
-  const unsigned b = a8_scale_byte(a8_row_max(m));
+  const unsigned b = a8_scale_byte(a8_group_max(m, 16));
   const float s = a8_inverse(b);
   u32x2 q;
   q[0] = a8_code4(v[0] * s, v[1] * s, v[2] * s, v[3] * s);

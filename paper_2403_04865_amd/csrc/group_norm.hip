@@ -2,24 +2,26 @@
 //
 // A unit is one tile's slice of whole groups.  Bound by memory traffic: forward x in, y out (and one byte of checkpoint), backward
 // dy and x in, dx out; everything else is to keep a value from being read twice.
-//   * Where a unit fits the registers of one workgroup it is loaded once and stays there: sums of every channel over the rows,
-//     the groups' means out of these, squares of the distances from the mean the same way, then the result (forward);
-//     the two sums per channel that the gradients need, then dx (backward).
-//   * Larger units are split over rows: partial statistics per channel (count, mean, sum of squared distances: merged, never a
+//   * One workgroup per unit.  Statistics of every thread's rows (count, mean, sum of squared distances, four rows at a time, merged), of the
+//     groups out of these, then the result: the unit is read twice, the second time out of the caches, and rows that fit the
+//     registers once.  The backward likewise: the two sums that dx needs of each group, then dx.
+//   * Few large units are split over rows: partial statistics per channel (count, mean, sum of squared distances: merged, never a
 //     difference of large sums), one small kernel for the groups, one pass for the result.
 // A thread owns V neighbouring channels (16 bytes of bfloat16) and strides over rows.  All statistics and sums are float32; the
 // gradients of gain and shift add the workgroups' sums in double, in a fixed order.
 #include "act8_internal.h"
+#include "lds_dma.h"
 
 namespace sl {
 
 namespace {
 
-// V values of a row as they are in memory
+// V values of a row as they are in memory.
 template <typename T, int V> struct Vec;
 template <> struct Vec<bf16, 8> {
   u32x4 r;
   __device__ __forceinline__ void load(const bf16* p) { r = *reinterpret_cast<const u32x4*>(p); }
+  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t b, int v, int s) { r = __builtin_amdgcn_raw_buffer_load_b128(b, v, s, 0); }
   __device__ __forceinline__ void zero() { r = u32x4{0, 0, 0, 0}; }
   __device__ __forceinline__ void get(float (&v)[8]) const {
 #pragma unroll
@@ -30,33 +32,60 @@ template <> struct Vec<bf16, 8> {
   }
 };
 template <> struct Vec<float, 8> {
-  f32x4 lo, hi;
+  u32x4 lo, hi;
   __device__ __forceinline__ void load(const float* p) {
-    lo = *reinterpret_cast<const f32x4*>(p); hi = *reinterpret_cast<const f32x4*>(p + 4);
+    lo = *reinterpret_cast<const u32x4*>(p); hi = *reinterpret_cast<const u32x4*>(p + 4);
   }
-  __device__ __forceinline__ void zero() { lo = hi = f32x4{0.f, 0.f, 0.f, 0.f}; }
+  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t b, int v, int s) {
+    lo = __builtin_amdgcn_raw_buffer_load_b128(b, v, s, 0);
+    hi = __builtin_amdgcn_raw_buffer_load_b128(b, v + 16, s, 0);
+  }
+  __device__ __forceinline__ void zero() { lo = hi = u32x4{0, 0, 0, 0}; }
   __device__ __forceinline__ void get(float (&v)[8]) const {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) { v[e] = lo[e]; v[4 + e] = hi[e]; }
+    for (int e = 0; e < 4; ++e) { v[e] = __uint_as_float(lo[e]); v[4 + e] = __uint_as_float(hi[e]); }
   }
 };
-template <typename T> struct Vec<T, 1> {
-  T r;
-  __device__ __forceinline__ void load(const T* p) { r = *p; }
-  __device__ __forceinline__ void zero() { r = (T)0.f; }
-  __device__ __forceinline__ void get(float (&v)[1]) const { v[0] = to_f(r); }
+template <> struct Vec<bf16, 1> {
+  unsigned short r;
+  __device__ __forceinline__ void load(const bf16* p) { r = *reinterpret_cast<const unsigned short*>(p); }
+  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t b, int v, int s) { r = __builtin_amdgcn_raw_buffer_load_b16(b, v, s, 0); }
+  __device__ __forceinline__ void zero() { r = 0; }
+  __device__ __forceinline__ void get(float (&v)[1]) const { v[0] = __uint_as_float((unsigned)r << 16); }
 };
-__device__ __forceinline__ void store_vec(bf16* p, const float (&v)[8]) {
+template <> struct Vec<float, 1> {
+  unsigned r;
+  __device__ __forceinline__ void load(const float* p) { r = *reinterpret_cast<const unsigned*>(p); }
+  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t b, int v, int s) { r = __builtin_amdgcn_raw_buffer_load_b32(b, v, s, 0); }
+  __device__ __forceinline__ void zero() { r = 0; }
+  __device__ __forceinline__ void get(float (&v)[1]) const { v[0] = __uint_as_float(r); }
+};
+__device__ __forceinline__ u32x4 rounded(const float (&v)[8]) {
   bf16x8 t;
 #pragma unroll
   for (int e = 0; e < 8; ++e) t[e] = (bf16)v[e];
-  *reinterpret_cast<bf16x8*>(p) = t;
+  return __builtin_bit_cast(u32x4, t);
 }
+__device__ __forceinline__ void store_vec(bf16* p, const float (&v)[8]) { *reinterpret_cast<u32x4*>(p) = rounded(v); }
 __device__ __forceinline__ void store_vec(float* p, const float (&v)[8]) {
   *reinterpret_cast<f32x4*>(p) = f32x4{v[0], v[1], v[2], v[3]};
   *reinterpret_cast<f32x4*>(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
 }
 template <typename T> __device__ __forceinline__ void store_vec(T* p, const float (&v)[1]) { *p = from_f<T>(v[0]); }
+template <typename T> __device__ __forceinline__ void store_buf(__amdgpu_buffer_rsrc_t b, int o, int s, const float (&v)[8]) {
+  if constexpr (sizeof(T) == 2) __builtin_amdgcn_raw_buffer_store_b128(rounded(v), b, o, s, 0);
+  else {
+    u32x4 lo, hi;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) { lo[e] = __float_as_uint(v[e]); hi[e] = __float_as_uint(v[4 + e]); }
+    __builtin_amdgcn_raw_buffer_store_b128(lo, b, o, s, 0);
+    __builtin_amdgcn_raw_buffer_store_b128(hi, b, o + 16, s, 0);
+  }
+}
+template <typename T> __device__ __forceinline__ void store_buf(__amdgpu_buffer_rsrc_t b, int o, int s, const float (&v)[1]) {
+  if constexpr (sizeof(T) == 2) __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(unsigned short, (bf16)v[0]), b, o, s, 0);
+  else __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v[0]), b, o, s, 0);
+}
 
 // eight codes of a checkpoint and their scale byte, or (V = 1) one
 template <int V> struct Vec8;
@@ -66,7 +95,10 @@ template <> struct Vec8<8> {
     q = *reinterpret_cast<const u32x2*>(a.codes + row * a.ldc + c);
     b = a.scales[row * a.lds + (c >> 7)];
   }
-  __device__ __forceinline__ void zero() { q = u32x2{0, 0}; b = 127; }
+  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t c, int v, int s, __amdgpu_buffer_rsrc_t sc, int vs, int ss) {
+    q = __builtin_amdgcn_raw_buffer_load_b64(c, v, s, 0);
+    b = __builtin_amdgcn_raw_buffer_load_b8(sc, vs, ss, 0);
+  }
   __device__ __forceinline__ void get(float (&v)[8]) const {
     const float s = a8_scale(b);
     float t[4];
@@ -84,16 +116,29 @@ template <> struct Vec8<1> {
     q = a.codes[row * a.ldc + c];
     b = a.scales[row * a.lds + (c >> 7)];
   }
-  __device__ __forceinline__ void zero() { q = 0; b = 127; }
+  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t c, int v, int s, __amdgpu_buffer_rsrc_t sc, int vs, int ss) {
+    q = __builtin_amdgcn_raw_buffer_load_b8(c, v, s, 0);
+    b = __builtin_amdgcn_raw_buffer_load_b8(sc, vs, ss, 0);
+  }
   __device__ __forceinline__ void get(float (&v)[1]) const { v[0] = __builtin_amdgcn_cvt_f32_fp8((int)q, 0) * a8_scale(b); }
 };
 
-__device__ __forceinline__ float act_any(float u, int act) {   // act: uniform
+// act: uniform, one branch for all V values
+template <int V> __device__ __forceinline__ void act_vec(float (&u)[V], int act) {
   switch (act) {
-    case SLIDE_ACT_RELU: return act_f<SLIDE_ACT_RELU>(u);
-    case SLIDE_ACT_SILU: return act_f<SLIDE_ACT_SILU>(u);
-    case SLIDE_ACT_GELU: return act_f<SLIDE_ACT_GELU>(u);
-    default: return u;
+    case SLIDE_ACT_RELU:
+#pragma unroll
+      for (int v = 0; v < V; ++v) u[v] = act_f<SLIDE_ACT_RELU>(u[v]);
+      break;
+    case SLIDE_ACT_SILU:
+#pragma unroll
+      for (int v = 0; v < V; ++v) u[v] = act_f<SLIDE_ACT_SILU>(u[v]);
+      break;
+    case SLIDE_ACT_GELU:
+#pragma unroll
+      for (int v = 0; v < V; ++v) u[v] = act_f<SLIDE_ACT_GELU>(u[v]);
+      break;
+    default: break;
   }
 }
 
@@ -102,7 +147,9 @@ struct P {
   A8 x8;
   int S, slices, G, per, C, hw;   // channels of a slice, slices, groups, channels of a group
   long long n;
-  int units_p;                    // workgroups per slice that share out the tiles (resident kernels)
+  int rows;                       // rows of a thread (unit kernels)
+  int pack;                       // lanes of a block of the checkpoint that the forward writes; 0: it writes none
+  int units_p;                    // workgroups per slice that share out the tiles (unit kernels)
   int chunks, rows_chunk;         // split kernels: pieces of a tile's rows
   float* part;                    // [..][2][C]
   float* sums;                    // [n][G][2]
@@ -119,8 +166,18 @@ template <int V> struct Own {
   }
 };
 
-// Sums over the rows of the workgroup: s[V] per thread -> ch[S] per channel of the slice.  red: TH V floats, red2: TH (or S, where
-// larger) floats.  Ends with a barrier.
+// (count, mean, squared distances) of two disjoint sets, merged into the first
+__device__ __forceinline__ void merge(float& n, float& m, float& q, float nb, float mb, float qb) {
+  const float t = n + nb;
+  if (t == 0.f) return;
+  const float d = mb - m, f = nb / t;
+  m = fmaf(d, f, m);
+  q += qb + d * d * n * f;
+  n = t;
+}
+
+// Sums over the rows of the workgroup: s[V] per thread -> ch[S] per channel of the slice.  red: TH V floats, red2: TH floats.  Ends with
+// a barrier.
 template <int TH, int V>
 __device__ __forceinline__ void channel_sums(const float (&s)[V], const Own<V>& o, int S, float* red, float* red2, float* ch) {
   if (o.on) {
@@ -152,141 +209,262 @@ __device__ __forceinline__ void channel_sums(const float (&s)[V], const Own<V>& 
   __syncthreads();
 }
 
-// per-channel values ch[S] (times w[S] where w is not null) -> their sum over each group of the slice, gs[groups].  Ends with a barrier.
-template <int TH>
-__device__ __forceinline__ void group_sums(const float* ch, const float* w, int S, int per, float* gs) {
+// Sums over each group of the slice of NS values s[i][V] per thread -> gs[i][groups].  A thread adds its channels of one group first: W
+// neighbouring channels always are of one group (8, 4 or 2, dividing the group's channels or divided by them; else 1).  red: NS TH V
+// floats.  Ends with a barrier.
+constexpr int SMAX = 512;   // most channels of a unit's slice
+
+template <int TH, int V, int NS>
+__device__ __forceinline__ void group_sums(const float (&s)[NS][V], const Own<V>& o, int S, int per, float* red, float (*gs)[SMAX]) {
   const int gl = S / per;
+  int slots = S;   // per row of threads
+  auto put = [&](auto width) {
+    constexpr int W = decltype(width)::value;
+    slots = S / W;
+    if (!o.on) return;
+#pragma unroll
+    for (int i = 0; i < NS; ++i)
+#pragma unroll
+      for (int h = 0; h < V / W; ++h) {
+        float a = 0.f;
+#pragma unroll
+        for (int v = 0; v < W; ++v) a += s[i][h * W + v];
+        red[i * TH * V + o.tr * slots + o.tc * (V / W) + h] = a;
+      }
+  };
+  if (V == 8 && per % 8 == 0) put(std::integral_constant<int, V>{});
+  else if (V == 8 && per % 4 == 0) put(std::integral_constant<int, V == 8 ? 4 : 1>{});
+  else if (V == 8 && per % 2 == 0) put(std::integral_constant<int, V == 8 ? 2 : 1>{});
+  else put(std::integral_constant<int, 1>{});
+  __syncthreads();
   int L = 64;
   while (L > 1 && L * gl > TH) L >>= 1;
-  const int sub = (int)threadIdx.x / L, lane = (int)threadIdx.x & (L - 1);
+  const int sub = (int)threadIdx.x / L, lane = (int)threadIdx.x & (L - 1), sg = slots / gl, all = o.rpp * sg;
   for (int g = sub; g < gl; g += TH / L) {
-    float a = 0.f;
-    for (int c = lane; c < per; c += L) a += w ? ch[g * per + c] * w[g * per + c] : ch[g * per + c];
-    for (int k = L >> 1; k > 0; k >>= 1) a += __shfl_xor(a, k, 64);
-    if (lane == 0) gs[g] = a;
+    float a[NS];
+#pragma unroll
+    for (int i = 0; i < NS; ++i) a[i] = 0.f;
+    for (int k = lane; k < all; k += L) {
+      const int r = k / sg, at = r * slots + g * sg + (k - r * sg);
+#pragma unroll
+      for (int i = 0; i < NS; ++i) a[i] += red[i * TH * V + at];
+    }
+    for (int k = L >> 1; k > 0; k >>= 1)
+#pragma unroll
+      for (int i = 0; i < NS; ++i) a[i] += __shfl_xor(a[i], k, 64);
+    if (lane == 0)
+#pragma unroll
+      for (int i = 0; i < NS; ++i) gs[i][g] = a[i];
   }
   __syncthreads();
 }
 
-// ---- resident units -------------------------------------------------------------------------------------------------
+// ---- a workgroup per unit ----------------------------------------------------------------------------------------------
 
-constexpr int SMAX = 2048;   // most channels of a slice
+constexpr int RG = 4;   // rows whose loads are in flight together, and whose statistics are formed together
+// Rows are taken one after the other: interleaved by the compiler they took twice the registers (and spilled).
+__device__ __forceinline__ void row_end() { __builtin_amdgcn_sched_barrier(0); }
 
-template <typename T, int V, int TH, int E>
-__global__ void __launch_bounds__(TH) gn_fwd_k(P p) {
-  __shared__ __attribute__((aligned(16))) float red[TH * V];
-  __shared__ float red2[TH], ch[TH * V], gs[TH * V];
+// a tile's rows of S channels from p on; rows behind the last are outside, whatever is loaded from there is zero and nothing is stored
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t tile_buffer(const void* p, long long ld, int es, int hw, int S) {
+  return dma_buffer(p, p ? ((hw - 1) * ld + S) * es : 0);
+}
+
+// V per-channel values of this thread
+template <int V> __device__ __forceinline__ void mine(const float* ch, int c, float (&v)[V]) {
+#pragma unroll
+  for (int k = 0; k < V; ++k) v[k] = ch[c + k];
+}
+
+// KG: groups of RG rows of a thread that stay in registers
+template <typename T, int V, int TH, int KG>
+__global__ void __launch_bounds__(TH, 2) gn_fwd_k(P p) {
+  __shared__ float red[TH * V], gs[1][SMAX], cm[SMAX], ca[SMAX], cb[SMAX];
   const GroupNorm& g = p.g;
   const Own<V> o(p.S, TH);
   const int j = blockIdx.x >> 3, slice = j % p.slices, first = (int)(blockIdx.x & 7) + 8 * (j / p.slices);
   if (first >= p.units_p) return;
-  const int c0 = slice * p.S + o.tc * V, per = p.per;
+  const int s0 = slice * p.S, tc = o.tc * V, at = o.on ? tc : 0, per = p.per, gl = p.S / per;
   const float count = (float)p.hw * (float)per;
-  float gam[V], bet[V];
-  int gi[V];
-#pragma unroll
-  for (int v = 0; v < V; ++v) {
-    gam[v] = o.on ? g.gamma[c0 + v] : 0.f;
-    bet[v] = o.on ? g.beta[c0 + v] : 0.f;
-    gi[v] = (o.tc * V + v) / per;
-  }
+  constexpr int es = sizeof(T);
+  const int ldx = (int)g.ldx * es, ldy = (int)g.ldy * es, ldr = (int)g.ldr * es;
+  const int vx = o.on ? o.tr * ldx + tc * es : DMA_ABSENT, vy = o.on ? o.tr * ldy + tc * es : DMA_ABSENT, vr = o.on ? o.tr * ldr + tc * es : DMA_ABSENT;
+  for (int c = threadIdx.x; c < p.S; c += TH) cb[c] = g.beta[s0 + c];
   for (long long tile = first; tile < p.n; tile += p.units_p) {
     const long long r0 = tile * p.hw;
-    const T* x = (const T*)g.x + r0 * g.ldx + c0;
-    Vec<T, V> buf[E];
+    const __amdgpu_buffer_rsrc_t xb = tile_buffer((const T*)g.x + r0 * g.ldx + s0, g.ldx, es, p.hw, p.S);
+    const __amdgpu_buffer_rsrc_t cbuf = tile_buffer(p.pack ? p.x8.codes + r0 * p.x8.ldc + s0 : nullptr, p.x8.ldc, 1, p.hw, p.S);
+    const __amdgpu_buffer_rsrc_t sbuf = tile_buffer(p.pack ? p.x8.scales + r0 * p.x8.lds + (s0 >> 7) : nullptr, p.x8.lds, 1, p.hw, (p.S + 127) >> 7);
+    const int ldc = (int)p.x8.ldc, lds = (int)p.x8.lds;
+    const int vc = o.on ? o.tr * ldc + tc : DMA_ABSENT, vs = o.on && (o.tc & (p.pack - 1)) == 0 ? o.tr * lds + (tc >> 7) : DMA_ABSENT;
+    Vec<T, V> buf[KG][RG];
+    auto load = [&](Vec<T, V> (&b)[RG], int e) __attribute__((always_inline)) {
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const int r = o.tr + e * o.rpp;
-      if (o.on && r < p.hw) buf[e].load(x + (long long)r * g.ldx);
-      else buf[e].zero();
+      for (int k = 0; k < RG; ++k) b[k].load(xb, vx, (e + k) * o.rpp * ldx);
+    };
+    // ---- statistics of this thread's rows
+    float n = 0.f, m[V], q[1][V], s[1][V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) m[v] = q[0][v] = 0.f;
+    auto stat = [&](const Vec<T, V> (&b)[RG], int e) __attribute__((always_inline)) {
+      float l[V], d2[V];
+#pragma unroll
+      for (int v = 0; v < V; ++v) l[v] = d2[v] = 0.f;
+#pragma unroll
+      for (int k = 0; k < RG; ++k) {
+        float t[V];
+        b[k].get(t);
+#pragma unroll
+        for (int v = 0; v < V; ++v) l[v] += t[v];
+        if (V == 8 && p.pack) {   // uniform
+          unsigned mag = 0;
+#pragma unroll
+          for (int v = 0; v < V; ++v) { const unsigned a = a8_mag(t[v]); mag = mag > a ? mag : a; }
+          const unsigned sc = a8_scale_byte(a8_group_max(mag, p.pack));
+          const float inv = a8_inverse(sc);
+          if constexpr (V == 8) {
+            u32x2 w;
+            w[0] = a8_code4(t[0] * inv, t[1] * inv, t[2] * inv, t[3] * inv);
+            w[1] = a8_code4(t[4] * inv, t[5] * inv, t[6] * inv, t[7] * inv);
+            __builtin_amdgcn_raw_buffer_store_b64(w, cbuf, vc, (e + k) * o.rpp * ldc, 0);
+          }
+          __builtin_amdgcn_raw_buffer_store_b8((unsigned char)sc, sbuf, vs, (e + k) * o.rpp * lds, 0);
+        }
+      }
+      // rows of these that exist; where all do (uniform) nothing is left out
+      int have = 0;
+#pragma unroll
+      for (int k = 0; k < RG; ++k) have += o.on && o.tr + (e + k) * o.rpp < p.hw;
+      const float nb = (float)have, inv = have ? 1.0f / nb : 0.f;
+#pragma unroll
+      for (int v = 0; v < V; ++v) l[v] *= inv;
+      const bool whole = (e + RG) * o.rpp <= p.hw;
+#pragma unroll
+      for (int k = 0; k < RG; ++k) {
+        float t[V];
+        b[k].get(t);
+        if (!whole && k >= have) continue;   // (a thread's rows exist up to some row)
+#pragma unroll
+        for (int v = 0; v < V; ++v) { const float d = t[v] - l[v]; d2[v] = fmaf(d, d, d2[v]); }
+      }
+      const float all = n + nb, f = all > 0.f ? nb / all : 0.f, nf = n * f;
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        const float d = l[v] - m[v];
+        m[v] = fmaf(d, f, m[v]);
+        q[0][v] += fmaf(d * d, nf, d2[v]);
+      }
+      n = all;
+      row_end();
+    };
+#pragma unroll
+    for (int h = 0; h < KG; ++h)
+      if (h * RG < p.rows) load(buf[h], h * RG);
+#pragma unroll
+    for (int h = 0; h < KG; ++h)
+      if (h * RG < p.rows) stat(buf[h], h * RG);
+    for (int e = KG * RG; e < p.rows; e += RG) {
+      Vec<T, V> b[RG];
+      load(b, e);
+      stat(b, e);
     }
-    float s[V];
+    // ---- of the groups
 #pragma unroll
-    for (int v = 0; v < V; ++v) s[v] = 0.f;
+    for (int v = 0; v < V; ++v) s[0][v] = n * m[v];
+    group_sums<TH, V, 1>(s, o, p.S, per, red, gs);
+    for (int c = threadIdx.x; c < p.S; c += TH) cm[c] = gs[0][c / per] / count;
+    if ((int)threadIdx.x < gl) g.mean[tile * p.G + slice * gl + threadIdx.x] = gs[0][threadIdx.x] / count;
+    __syncthreads();
+    float mean[V];
+    mine<V>(cm, at, mean);
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      float t[V];
-      buf[e].get(t);
-#pragma unroll
-      for (int v = 0; v < V; ++v) s[v] += t[v];
-    }
-    channel_sums<TH, V>(s, o, p.S, red, red2, ch);
-    group_sums<TH>(ch, nullptr, p.S, per, gs);
-    float m[V];
-#pragma unroll
-    for (int v = 0; v < V; ++v) { m[v] = o.on ? gs[gi[v]] / count : 0.f; s[v] = 0.f; }
-    const float my_mean = (int)threadIdx.x < p.S / per ? gs[threadIdx.x] / count : 0.f;
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-      if (!(o.on && o.tr + e * o.rpp < p.hw)) continue;
-      float t[V];
-      buf[e].get(t);
-#pragma unroll
-      for (int v = 0; v < V; ++v) { const float d = t[v] - m[v]; s[v] = fmaf(d, d, s[v]); }
-    }
-    channel_sums<TH, V>(s, o, p.S, red, red2, ch);
-    group_sums<TH>(ch, nullptr, p.S, per, gs);
-    for (int k = threadIdx.x; k < p.S / per; k += TH) {
-      const long long at = tile * p.G + slice * (p.S / per) + k;
-      g.mean[at] = my_mean;    // S / per <= TH: one group per thread
-      g.rstd[at] = 1.0f / sqrtf(gs[k] / count + g.s.eps);
-    }
-    float a[V];
-#pragma unroll
-    for (int v = 0; v < V; ++v) a[v] = o.on ? gam[v] * (1.0f / sqrtf(gs[gi[v]] / count + g.s.eps)) : 0.f;
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const int r = o.tr + e * o.rpp;
-      if (!(o.on && r < p.hw)) continue;
-      float t[V], u[V];
-      buf[e].get(t);
-#pragma unroll
-      for (int v = 0; v < V; ++v) u[v] = fmaf(t[v] - m[v], a[v], bet[v]);
+    for (int v = 0; v < V; ++v) { const float d = m[v] - mean[v]; s[0][v] = fmaf(d * d, n, q[0][v]); }
+    group_sums<TH, V, 1>(s, o, p.S, per, red, gs);
+    for (int c = threadIdx.x; c < p.S; c += TH) ca[c] = g.gamma[s0 + c] * (1.0f / sqrtf(gs[0][c / per] / count + g.s.eps));
+    if ((int)threadIdx.x < gl) g.rstd[tile * p.G + slice * gl + threadIdx.x] = 1.0f / sqrtf(gs[0][threadIdx.x] / count + g.s.eps);
+    __syncthreads();
+    // ---- the result
+    const __amdgpu_buffer_rsrc_t yb = tile_buffer((T*)g.y + r0 * g.ldy + s0, g.ldy, es, p.hw, p.S);
+    const __amdgpu_buffer_rsrc_t rb = tile_buffer(g.resid ? (const T*)g.resid + r0 * g.ldr + s0 : nullptr, g.ldr, es, p.hw, p.S);
+    float a[V], b[V];
+    mine<V>(ca, at, a);
+    mine<V>(cb, at, b);
+    auto apply = [&](const Vec<T, V> (&x)[RG], int e) __attribute__((always_inline)) {
+      Vec<T, V> w[RG];
       if (g.resid) {
-        Vec<T, V> q;
-        q.load((const T*)g.resid + (r0 + r) * g.ldr + c0);
-        q.get(t);
 #pragma unroll
-        for (int v = 0; v < V; ++v) u[v] += t[v];
+        for (int k = 0; k < RG; ++k) w[k].load(rb, vr, (e + k) * o.rpp * ldr);
       }
 #pragma unroll
-      for (int v = 0; v < V; ++v) u[v] = act_any(u[v], g.s.act);
-      store_vec((T*)g.y + (r0 + r) * g.ldy + c0, u);
-    }
-    __syncthreads();
-  }
-}
-
-// du = dy act'(u) of one value.  A rectifier asks which side of zero u is on: where float32 cannot tell, it is formed again in
-// double (mean and rstd are what the forward stored; products of two floats are exact there).
-__device__ __forceinline__ float slope(float u, float mag, int act, float x, float mean, float rstd, float gam, float bet, float res) {
-  switch (act) {
-    case SLIDE_ACT_RELU: {
-      bool pos = u > 0.f;
-      if (fabsf(u) <= 1e-6f * mag)
-        pos = (((double)x - (double)mean) * (double)rstd) * (double)gam + (double)bet + (double)res > 0.0;
-      return pos ? 1.f : 0.f;
-    }
-    case SLIDE_ACT_SILU: {
-      const float s = sigmoid_f(u);
-      return s * fmaf(u, 1.0f - s, 1.0f);
-    }
-    case SLIDE_ACT_GELU: return gelu_grad_f(u);
-    default: return 1.f;
-  }
-}
-
-// du and xhat of a thread's V values of one row
-template <int V>
-__device__ __forceinline__ void du_xhat(const float (&x)[V], const float (&dy)[V], const float (&res)[V], const float (&mean)[V],
-                                        const float (&rstd)[V], const float (&gam)[V], const float (&bet)[V], int act,
-                                        float (&du)[V], float (&xh)[V]) {
+      for (int k = 0; k < RG; ++k) {
+        float t[V], u[V];
+        x[k].get(t);
 #pragma unroll
-  for (int v = 0; v < V; ++v) {
-    xh[v] = (x[v] - mean[v]) * rstd[v];
-    const float z = xh[v] * gam[v], u = z + bet[v] + res[v];
-    const float mag = fabsf(z) + fabsf(bet[v]) + fabsf(res[v]);
-    du[v] = act == SLIDE_ACT_NONE ? dy[v] : dy[v] * slope(u, mag, act, x[v], mean[v], rstd[v], gam[v], bet[v], res[v]);
+        for (int v = 0; v < V; ++v) u[v] = fmaf(t[v] - mean[v], a[v], b[v]);
+        if (g.resid) {
+          w[k].get(t);
+#pragma unroll
+          for (int v = 0; v < V; ++v) u[v] += t[v];
+        }
+        act_vec<V>(u, g.s.act);
+        store_buf<T>(yb, vy, (e + k) * o.rpp * ldy, u);
+        row_end();
+      }
+    };
+#pragma unroll
+    for (int h = 0; h < KG; ++h)
+      if (h * RG < p.rows) apply(buf[h], h * RG);
+    for (int e = KG * RG; e < p.rows; e += RG) {
+      Vec<T, V> x[RG];
+      load(x, e);
+      apply(x, e);
+    }
+    __syncthreads();   // (cm, ca, gs are written again by the next tile)
+  }
+}
+
+// du = dy act'(u) of V values, u = (x - mean) (rstd gamma) + beta + residual.  A rectifier asks which side of zero u is on: where float32
+// cannot tell, it is formed again in double (mean and rstd are what the forward stored).
+template <int V, typename F>
+__device__ __forceinline__ void du_vec(const float (&d)[V], const float (&dy)[V], const float (&res)[V], const float (&rg)[V],
+                                       const float (&bet)[V], int act, float (&du)[V], F exactly) {
+  if (act == SLIDE_ACT_NONE) {
+#pragma unroll
+    for (int v = 0; v < V; ++v) du[v] = dy[v];
+    return;
+  }
+  float u[V];
+  if (act == SLIDE_ACT_RELU) {
+    bool near = false;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const float z = d[v] * rg[v];
+      u[v] = z + bet[v] + res[v];
+      near |= fabsf(u[v]) <= 1e-6f * (fabsf(z) + fabsf(bet[v]) + fabsf(res[v]));
+    }
+    if (near) {
+#pragma unroll
+      for (int v = 0; v < V; ++v) { u[v] = exactly(v); row_end(); }
+    }
+#pragma unroll
+    for (int v = 0; v < V; ++v) du[v] = u[v] > 0.f ? dy[v] : 0.f * dy[v];
+    return;
+  }
+#pragma unroll
+  for (int v = 0; v < V; ++v) u[v] = fmaf(d[v], rg[v], bet[v]) + res[v];
+  if (act == SLIDE_ACT_SILU) {
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const float s = sigmoid_f(u[v]);
+      du[v] = dy[v] * (s * fmaf(u[v], 1.0f - s, 1.0f));
+    }
+  } else {
+#pragma unroll
+    for (int v = 0; v < V; ++v) {   // Phi(u) + u phi(u)
+      float e;
+      const float h = half_erfc(fminf(fabsf(u[v]), GELU_FAR), &e);
+      du[v] = dy[v] * fmaf(u[v] * 0.39894228040143268f, e, u[v] < 0.f ? h : 1.0f - h);
+    }
   }
 }
 
@@ -298,104 +476,133 @@ __device__ __forceinline__ void load_in(Vec<T, V>& b, const P& p, long long row,
 template <int V>
 __device__ __forceinline__ void load_in(Vec8<V>& b, const P& p, long long row, int c) { b.load(p.x8, row, c); }
 
-template <typename T, int V, int TH, int E, bool X8>
-__global__ void __launch_bounds__(TH) gn_bwd_k(P p) {
-  __shared__ __attribute__((aligned(16))) float red[TH * V];
-  __shared__ float red2[TH], ca[TH * V], cb[TH * V], ga[TH * V], gb[TH * V], wg[TH * V];
+// sign of x's place before the activation, in double
+__device__ __forceinline__ float side(double x, double mean, double rstd, double gam, double bet, double res) {
+  const double u = (x - mean) * rstd * gam + bet + res;
+  return u > 0.0 ? 1.f : u < 0.0 ? -1.f : (float)u;
+}
+
+template <typename T, int V, int TH, int KG, bool X8>
+__global__ void __launch_bounds__(TH, 2) gn_bwd_k(P p) {
+  __shared__ float red[2 * TH * V], gs[2][SMAX], cm[SMAX], cr[SMAX], crg[SMAX], cbet[SMAX], red2[TH];
   const GroupNorm& g = p.g;
   const Own<V> o(p.S, TH);
   const int j = blockIdx.x >> 3, slice = j % p.slices, first = (int)(blockIdx.x & 7) + 8 * (j / p.slices);
   if (first >= p.units_p) return;
-  const int c0 = slice * p.S + o.tc * V, per = p.per, act = g.s.act;
+  const int s0 = slice * p.S, tc = o.tc * V, at = o.on ? tc : 0, per = p.per, act = g.s.act, gl = p.S / per;
   const float inv = 1.0f / ((float)p.hw * (float)per);
-  float gam[V], bet[V];
-  int gi[V];
-#pragma unroll
-  for (int v = 0; v < V; ++v) {
-    gam[v] = o.on ? g.gamma[c0 + v] : 0.f;
-    bet[v] = o.on ? g.beta[c0 + v] : 0.f;
-    gi[v] = (o.tc * V + v) / per;
-  }
-  for (int c = threadIdx.x; c < p.S; c += TH) wg[c] = g.gamma[slice * p.S + c];
-  // sums of this workgroup's tiles for the gain and the shift: thread t keeps those of channels t, t + TH, ...
-  float tg[V], tb[V];
+  constexpr int es = sizeof(T), esx = X8 ? 1 : es;
+  const int ldx = X8 ? (int)p.x8.ldc : (int)g.ldx * es, lds = (int)p.x8.lds;
+  const int ldd = (int)g.lddy * es, ldy = (int)g.ldy * es, ldr = (int)g.ldr * es, ldq = (int)g.lddr * es;
+  auto lane_at = [&](int ld, int c) { return o.on ? o.tr * ld + c : DMA_ABSENT; };
+  const int vx = lane_at(ldx, tc * esx), vs = lane_at(lds, (s0 + tc) / A8_BLOCK), vd = lane_at(ldd, tc * es), vy = lane_at(ldy, tc * es),
+            vr = lane_at(ldr, tc * es), vq = lane_at(ldq, tc * es);
+  float tg[V], tb[V];   // this thread's sums for the gain and the shift, over all of its tiles
 #pragma unroll
   for (int v = 0; v < V; ++v) tg[v] = tb[v] = 0.f;
+  for (int c = threadIdx.x; c < p.S; c += TH) cbet[c] = g.beta[s0 + c];
   for (long long tile = first; tile < p.n; tile += p.units_p) {
     const long long r0 = tile * p.hw;
-    typename Input<T, V, X8>::type bx[E];
-    Vec<T, V> bd[E];
+    const __amdgpu_buffer_rsrc_t xb = X8 ? tile_buffer(p.x8.codes + r0 * p.x8.ldc + s0, p.x8.ldc, 1, p.hw, p.S)
+                                         : tile_buffer((const T*)g.x + r0 * g.ldx + s0, g.ldx, es, p.hw, p.S);
+    const __amdgpu_buffer_rsrc_t sb = tile_buffer(X8 ? p.x8.scales + r0 * p.x8.lds : nullptr, p.x8.lds, 1, p.hw, (p.C + 127) >> 7);
+    const __amdgpu_buffer_rsrc_t db = tile_buffer((const T*)g.dy + r0 * g.lddy + s0, g.lddy, es, p.hw, p.S);
+    const __amdgpu_buffer_rsrc_t rb = tile_buffer(g.resid ? (const T*)g.resid + r0 * g.ldr + s0 : nullptr, g.ldr, es, p.hw, p.S);
+    typedef typename Input<T, V, X8>::type In;
+    struct Rows { In x[RG]; Vec<T, V> d[RG]; } kept[KG > 0 ? KG : 1];
+    auto load = [&](Rows& b, int e) __attribute__((always_inline)) {
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const int r = o.tr + e * o.rpp;
-      if (o.on && r < p.hw) {
-        load_in(bx[e], p, r0 + r, c0);
-        bd[e].load((const T*)g.dy + (r0 + r) * g.lddy + c0);
-      } else { bx[e].zero(); bd[e].zero(); }
-    }
-    float mean[V], rstd[V];
+      for (int k = 0; k < RG; ++k) {
+        const int row = (e + k) * o.rpp;
+        if constexpr (X8) b.x[k].load(xb, vx, row * ldx, sb, vs, row * lds);
+        else b.x[k].load(xb, vx, row * ldx);
+        b.d[k].load(db, vd, row * ldd);
+      }
+    };
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-      const long long at = tile * p.G + slice * (p.S / per) + gi[v];
-      mean[v] = o.on ? g.mean[at] : 0.f;
-      rstd[v] = o.on ? g.rstd[at] : 0.f;
+    for (int h = 0; h < KG; ++h)
+      if (h * RG < p.rows) load(kept[h], h * RG);
+    for (int c = threadIdx.x; c < p.S; c += TH) {
+      const long long k = tile * p.G + slice * gl + c / per;
+      const float r = g.rstd[k];
+      cm[c] = g.mean[k]; cr[c] = r; crg[c] = r * g.gamma[s0 + c];
     }
+    __syncthreads();
+    float m[V], rg[V], bet[V];
+    mine<V>(cm, at, m);
+    mine<V>(crg, at, rg);
+    mine<V>(cbet, at, bet);
+    // f(x - mean, du, row index) of RG rows
+    auto take = [&](const Rows& b, int e, auto f) __attribute__((always_inline)) {
+      Vec<T, V> w[RG];
+      if (g.resid) {
+#pragma unroll
+        for (int k = 0; k < RG; ++k) w[k].load(rb, vr, (e + k) * o.rpp * ldr);
+      }
+#pragma unroll
+      for (int k = 0; k < RG; ++k) {
+        float x[V], dy[V], res[V], d[V], du[V];
+        b.x[k].get(x);
+        b.d[k].get(dy);
+#pragma unroll
+        for (int v = 0; v < V; ++v) { res[v] = 0.f; d[v] = x[v] - m[v]; }
+        if (g.resid) w[k].get(res);
+        du_vec<V>(d, dy, res, rg, bet, act, du, [&](int v) { return side(x[v], m[v], cr[at + v], g.gamma[s0 + at + v], bet[v], res[v]); });
+        f(d, du, e + k);
+        row_end();
+      }
+    };
+    auto each = [&](auto f) __attribute__((always_inline)) {
+#pragma unroll
+      for (int h = 0; h < KG; ++h)
+        if (h * RG < p.rows) take(kept[h], h * RG, f);
+      for (int e = KG * RG; e < p.rows; e += RG) {
+        Rows b;
+        load(b, e);
+        take(b, e, f);
+      }
+    };
     float s[V], q[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) s[v] = q[v] = 0.f;
-    auto one = [&](int e, float (&du)[V], float (&xh)[V]) __attribute__((always_inline)) {
-      float x[V], dy[V], res[V];
-      bx[e].get(x);
-      bd[e].get(dy);
+    each([&](const float (&d)[V], const float (&du)[V], int) __attribute__((always_inline)) {   // (dy of a row that does not exist is zero)
 #pragma unroll
-      for (int v = 0; v < V; ++v) res[v] = 0.f;
-      if (g.resid) {
-        Vec<T, V> b;
-        b.load((const T*)g.resid + (r0 + o.tr + e * o.rpp) * g.ldr + c0);
-        b.get(res);
-      }
-      du_xhat<V>(x, dy, res, mean, rstd, gam, bet, act, du, xh);
-    };
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-      if (!(o.on && o.tr + e * o.rpp < p.hw)) continue;
-      float du[V], xh[V];
-      one(e, du, xh);
-#pragma unroll
-      for (int v = 0; v < V; ++v) { s[v] += du[v]; q[v] = fmaf(du[v], xh[v], q[v]); }
-    }
-    channel_sums<TH, V>(s, o, p.S, red, red2, cb);
-    channel_sums<TH, V>(q, o, p.S, red, red2, ca);
-    group_sums<TH>(cb, wg, p.S, per, gb);
-    group_sums<TH>(ca, wg, p.S, per, ga);
+      for (int v = 0; v < V; ++v) { s[v] += du[v]; q[v] = fmaf(du[v], d[v], q[v]); }
+    });
+    float r[V], w[2][V];
+    mine<V>(cr, at, r);
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      const int c = threadIdx.x + v * TH;
-      if (c < p.S) { tg[v] += ca[c]; tb[v] += cb[c]; }
+      tb[v] += s[v];
+      tg[v] = fmaf(q[v], r[v], tg[v]);
+      w[0][v] = s[v] * rg[v];           // of du gamma, times rstd
+      w[1][v] = q[v] * rg[v] * r[v];    // of du gamma xhat, times rstd
     }
-    float m1[V], m2[V];
+    group_sums<TH, V, 2>(w, o, p.S, per, red, gs);
+    // dx = rstd (du gamma - mean of it - xhat mean of (du gamma xhat)) = du (rstd gamma) - k1 - (x - mean) k2
+    float k1[V], k2[V];
 #pragma unroll
-    for (int v = 0; v < V; ++v) { m1[v] = o.on ? gb[gi[v]] * inv : 0.f; m2[v] = o.on ? ga[gi[v]] * inv : 0.f; }
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const int r = o.tr + e * o.rpp;
-      if (!(o.on && r < p.hw)) continue;
-      float du[V], xh[V];
-      one(e, du, xh);
-      if (g.dresid) store_vec((T*)g.dresid + (r0 + r) * g.lddr + c0, du);
-#pragma unroll
-      for (int v = 0; v < V; ++v) du[v] = rstd[v] * ((du[v] * gam[v] - m1[v]) - xh[v] * m2[v]);
-      store_vec((T*)g.y + (r0 + r) * g.ldy + c0, du);
+    for (int v = 0; v < V; ++v) {
+      const int gr = (at + v) / per;
+      k1[v] = gs[0][gr] * inv;
+      k2[v] = gs[1][gr] * inv * r[v];
     }
-    __syncthreads();
+    const __amdgpu_buffer_rsrc_t yb = tile_buffer((T*)g.y + r0 * g.ldy + s0, g.ldy, es, p.hw, p.S);
+    const __amdgpu_buffer_rsrc_t qb = tile_buffer(g.dresid ? (T*)g.dresid + r0 * g.lddr + s0 : nullptr, g.lddr, es, p.hw, p.S);
+    each([&](const float (&d)[V], const float (&du)[V], int e) __attribute__((always_inline)) {
+      if (g.dresid) store_buf<T>(qb, vq, e * o.rpp * ldq, du);
+      float z[V];
+#pragma unroll
+      for (int v = 0; v < V; ++v) z[v] = fmaf(-d[v], k2[v], fmaf(du[v], rg[v], -k1[v]));
+      store_buf<T>(yb, vy, e * o.rpp * ldy, z);
+    });
+    __syncthreads();   // (the arrays per channel are written again by the next tile)
   }
-#pragma unroll
-  for (int v = 0; v < V; ++v) {
-    const int c = threadIdx.x + v * TH;
-    if (c < p.S) {
-      p.part[((long long)first * 2 + 0) * p.C + slice * p.S + c] = tg[v];
-      p.part[((long long)first * 2 + 1) * p.C + slice * p.S + c] = tb[v];
-    }
+  channel_sums<TH, V>(tg, o, p.S, red, red2, cm);
+  channel_sums<TH, V>(tb, o, p.S, red, red2, cr);
+  for (int c = threadIdx.x; c < p.S; c += TH) {
+    p.part[((long long)first * 2 + 0) * p.C + s0 + c] = cm[c];
+    p.part[((long long)first * 2 + 1) * p.C + s0 + c] = cr[c];
   }
 }
 
@@ -420,16 +627,6 @@ __global__ void __launch_bounds__(1024) gn_sum_k(const float* __restrict__ part,
 // ---- units split over rows --------------------------------------------------------------------------------------------
 
 constexpr int ST = 256, SE = 8;   // threads; rows of a thread whose loads are in flight together
-
-// (count, mean, squared distances) of two disjoint sets, merged into the first
-__device__ __forceinline__ void merge(float& n, float& m, float& q, float nb, float mb, float qb) {
-  const float t = n + nb;
-  if (t == 0.f) return;
-  const float d = mb - m, f = nb / t;
-  m = fmaf(d, f, m);
-  q += qb + d * d * n * f;
-  n = t;
-}
 
 struct Where { long long tile; int slice, chunk, lo, hi; };
 __device__ __forceinline__ Where where(const P& p, long long unit) {
@@ -587,8 +784,7 @@ __global__ void __launch_bounds__(ST) gn_apply_k(P p) {
 #pragma unroll
         for (int v = 0; v < V; ++v) u[v] += t[v];
       }
-#pragma unroll
-      for (int v = 0; v < V; ++v) u[v] = act_any(u[v], g.s.act);
+      act_vec<V>(u, g.s.act);
       store_vec((T*)g.y + row * g.ldy + c0, u);
     }
   }
@@ -607,47 +803,59 @@ __global__ void __launch_bounds__(ST) gn_bwd_split_k(P p) {
     const int S = p.C - w.slice * p.S < p.S ? p.C - w.slice * p.S : p.S;
     const Own<V> o(S, ST);
     const int c0 = w.slice * p.S + o.tc * V;
-    float mean[V], rstd[V], gam[V], bet[V], s[V], q[V];
+    float mean[V], rstd[V], rg[V], bet[V], s[V], q[V];
 #pragma unroll
-    for (int v = 0; v < V; ++v) { mean[v] = rstd[v] = gam[v] = bet[v] = s[v] = q[v] = 0.f; }
+    for (int v = 0; v < V; ++v) { mean[v] = rstd[v] = rg[v] = bet[v] = s[v] = q[v] = 0.f; }
     if (o.on) {
       group_stats<V>(p, w.tile, c0, mean, rstd);
 #pragma unroll
       for (int v = 0; v < V; ++v) {
-        gam[v] = g.gamma[c0 + v]; bet[v] = g.beta[c0 + v];
-        if constexpr (DX) {
+        rg[v] = rstd[v] * g.gamma[c0 + v]; bet[v] = g.beta[c0 + v];
+        if constexpr (DX) {   // dx = du (rstd gamma) - s - (x - mean) q
           const float* gsum = p.sums + (w.tile * p.G + (c0 + v) / p.per) * 2;
-          q[v] = gsum[0] * inv;   // of du gamma xhat
-          s[v] = gsum[1] * inv;   // of du gamma
+          q[v] = gsum[0] * inv * rstd[v] * rstd[v];   // of du gamma xhat
+          s[v] = gsum[1] * inv * rstd[v];             // of du gamma
         }
       }
-#pragma unroll 2
-      for (int r = w.lo + o.tr; r < w.hi; r += o.rpp) {
-        const long long row = w.tile * p.hw + r;
-        typename Input<T, V, X8>::type bx;
-        Vec<T, V> b;
-        float x[V], dy[V], res[V], du[V], xh[V];
-        load_in(bx, p, row, c0);
-        b.load((const T*)g.dy + row * g.lddy + c0);
-        bx.get(x);
-        b.get(dy);
+      for (int r = w.lo + o.tr; r < w.hi; r += RG * o.rpp) {
+        typename Input<T, V, X8>::type bx[RG];
+        Vec<T, V> bd[RG], br[RG];
 #pragma unroll
-        for (int v = 0; v < V; ++v) res[v] = 0.f;
-        if (g.resid) { b.load((const T*)g.resid + row * g.ldr + c0); b.get(res); }
-        du_xhat<V>(x, dy, res, mean, rstd, gam, bet, act, du, xh);
-        if constexpr (DX) {
-          if (g.dresid) store_vec((T*)g.dresid + row * g.lddr + c0, du);
+        for (int k = 0; k < RG; ++k) {   // (rows behind the last: the last one's values, left out below)
+          const int at = r + k * o.rpp;
+          const long long row = w.tile * p.hw + (at < w.hi ? at : w.hi - 1);
+          load_in(bx[k], p, row, c0);
+          bd[k].load((const T*)g.dy + row * g.lddy + c0);
+          if (g.resid) br[k].load((const T*)g.resid + row * g.ldr + c0);
+        }
 #pragma unroll
-          for (int v = 0; v < V; ++v) du[v] = rstd[v] * ((du[v] * gam[v] - s[v]) - xh[v] * q[v]);
-          store_vec((T*)g.y + row * g.ldy + c0, du);
-        } else {
+        for (int k = 0; k < RG; ++k) {
+          if (r + k * o.rpp >= w.hi) break;
+          const long long row = w.tile * p.hw + r + k * o.rpp;
+          float x[V], dy[V], res[V], d[V], du[V];
+          bx[k].get(x);
+          bd[k].get(dy);
 #pragma unroll
-          for (int v = 0; v < V; ++v) { s[v] += du[v]; q[v] = fmaf(du[v], xh[v], q[v]); }
+          for (int v = 0; v < V; ++v) { res[v] = 0.f; d[v] = x[v] - mean[v]; }
+          if (g.resid) br[k].get(res);
+          du_vec<V>(d, dy, res, rg, bet, act, du, [&](int v) { return side(x[v], mean[v], rstd[v], g.gamma[c0 + v], bet[v], res[v]); });
+          if constexpr (DX) {
+            if (g.dresid) store_vec((T*)g.dresid + row * g.lddr + c0, du);
+#pragma unroll
+            for (int v = 0; v < V; ++v) du[v] = fmaf(-d[v], q[v], fmaf(du[v], rg[v], -s[v]));
+            store_vec((T*)g.y + row * g.ldy + c0, du);
+          } else {
+#pragma unroll
+            for (int v = 0; v < V; ++v) { s[v] += du[v]; q[v] = fmaf(du[v], d[v], q[v]); }
+          }
+          row_end();
         }
       }
     }
     if constexpr (!DX) {
       float* out = p.part + (w.tile * p.chunks + w.chunk) * 2 * p.C + w.slice * p.S;
+#pragma unroll
+      for (int v = 0; v < V; ++v) q[v] *= rstd[v];
       channel_sums<ST, V>(q, o, S, red, red2, ch);
       for (int c = threadIdx.x; c < S; c += ST) out[c] = ch[c];
       __syncthreads();
@@ -681,28 +889,11 @@ __global__ void __launch_bounds__(256) gn_bwd_group_k(P p) {
 
 // ---- host -------------------------------------------------------------------------------------------------------------
 
-constexpr int FWD_E = 49, BWD_E = 20;   // most rows of a thread that stay in registers (bfloat16; float32: half)
 constexpr int WANT = 1024;              // workgroups of a split launch
+constexpr int SPLIT_SMAX = 2048;
+constexpr long long MOST_P = 4096;      // rows of partial sums that the unit kernels leave
 
 int gcd(int a, int b) { while (b) { const int t = a % b; a = b; b = t; } return a; }
-
-// The channels of a resident slice: whole groups and whole pieces of V, the fewest that are 128 bytes of a row and 256 pieces in all, as
-// long as they divide the channels.  0: a unit does not fit.
-int resident_slice(const slide_group_norm& s, int V, int es, int most_e, int th) {
-  const int per = s.channels / s.groups, base = per / gcd(per, V) * V;   // lcm
-  if (base > s.channels || s.channels % base) return 0;
-  int pick = 0;
-  for (int k = 1; k <= s.channels / base; ++k) {
-    if ((s.channels / base) % k) continue;
-    const int S = base * k, vpr = S / V;
-    if (vpr > th || S / per > th) break;
-    const long long rpp = th / vpr, e = (s.hw + rpp - 1) / rpp;
-    if (e > most_e) break;
-    pick = S;
-    if ((long long)S * es >= 128 && s.hw * vpr >= 256) break;
-  }
-  return pick;
-}
 
 int pieces(const GroupNorm& g, bool bwd) {   // 8: every row can be read and written in pieces of eight channels
   const size_t es = elem_size(g.s.dtype);
@@ -713,7 +904,7 @@ int pieces(const GroupNorm& g, bool bwd) {   // 8: every row can be read and wri
 }
 
 void split_plan(const slide_group_norm& s, int V, P* p) {
-  const int most = ST * V < SMAX ? ST * V : SMAX;
+  const int most = ST * V < SPLIT_SMAX ? ST * V : SPLIT_SMAX;
   p->S = s.channels < most ? s.channels : most;
   p->slices = (s.channels + p->S - 1) / p->S;
   const long long have = s.n * p->slices;
@@ -735,32 +926,47 @@ P base(const GroupNorm& g) {
   return p;
 }
 
-constexpr long long MOST_P = 4096;   // rows of partial sums that the resident backward leaves
-
 size_t part_floats(const slide_group_norm& s) {
   P a{}, b{};
   split_plan(s, 8, &a);
   split_plan(s, 1, &b);
-  long long rows = s.n * (a.chunks > b.chunks ? a.chunks : b.chunks);
+  const long long rows = s.n * (a.chunks > b.chunks ? a.chunks : b.chunks);
   return (size_t)rows * 2 * s.channels;
 }
 
-template <typename T, int V, int E>
-hipError_t fwd_e(const P& p, unsigned grid, bool small, hipStream_t s) {
-  if (small) gn_fwd_k<T, V, 256, E><<<grid, 256, 0, s>>>(p);
-  else gn_fwd_k<T, V, 512, E><<<grid, 512, 0, s>>>(p);
-  return hipGetLastError();
-}
-template <typename T, int V, int E>
-hipError_t bwd_e(const P& p, unsigned grid, bool small, hipStream_t s) {
-  if (p.g.x) {
-    if (small) gn_bwd_k<T, V, 256, E, false><<<grid, 256, 0, s>>>(p);
-    else gn_bwd_k<T, V, 512, E, false><<<grid, 512, 0, s>>>(p);
-  } else {
-    if (small) gn_bwd_k<T, V, 256, E, true><<<grid, 256, 0, s>>>(p);
-    else gn_bwd_k<T, V, 512, E, true><<<grid, 512, 0, s>>>(p);
+// A workgroup per unit: its slice, threads and rows.  False: the rows are split.
+//   * The slice: whole groups, whole pieces of V, dividing the channels; the fewest channels that are 128 bytes of a row (narrower slices
+//     fetch cache lines that other units want too) and PIECES pieces in all (a unit costs some microseconds of barriers), or all of them.
+//   * 256 threads up to eight rows of a thread, else 512.
+//   * With fewer units than half the compute units a longer unit is split instead.
+constexpr int PIECES = 2048;
+bool by_units(P* p, int V, int es, unsigned* grid, bool* small) {
+  const slide_group_norm& s = p->g.s;
+  const int base = p->per / gcd(p->per, V) * V;   // lcm
+  if (base > SMAX || p->C % base) return false;
+  long long ld = s.channels;
+  for (long long q : {p->g.ldx, p->g.ldy, p->g.x8 ? p->x8.ldc : 0, p->g.x8 ? p->x8.lds : 0, p->g.resid ? p->g.ldr : 0,
+                      p->g.dy ? p->g.lddy : 0, p->g.dresid ? p->g.lddr : 0})
+    if (q > ld) ld = q;
+  if ((s.hw + 4096) * ld * es > DMA_MAX) return false;   // 32-bit offsets, with rows behind the last
+  p->S = 0;
+  for (int k = 1; base * k <= SMAX && base * k <= p->C; ++k) {
+    if ((p->C / base) % k) continue;
+    const int S = base * k;
+    if (S / V > 512) break;
+    p->S = S;
+    if ((long long)S * es >= 128 && s.hw * (S / V) >= PIECES) break;
   }
-  return hipGetLastError();
+  if (!p->S) return false;
+  const int vpr = p->S / V;
+  *small = vpr <= 256 && (s.hw + 256 / vpr - 1) / (256 / vpr) <= 8;
+  const int rpp = (*small ? 256 : 512) / vpr;
+  p->slices = p->C / p->S;
+  p->rows = (int)((s.hw + rpp - 1) / rpp);
+  if (s.n * p->slices < 128 && p->rows > 8) return false;
+  p->units_p = (int)(s.n < MOST_P ? s.n : MOST_P);
+  *grid = (unsigned)((p->units_p + 7) / 8 * 8 * p->slices);
+  return true;
 }
 
 unsigned split_grid(const P& p) {
@@ -772,40 +978,35 @@ unsigned group_grid(const P& p) {
   return (unsigned)(u < (1 << 20) ? u : (1 << 20));
 }
 
-// slice, threads and rows per thread of the resident kernels; false: the unit is split
-template <typename T>
-bool resident(P* p, int V, int most_e, int* rows, bool* small, unsigned* grid) {
-  const slide_group_norm& s = p->g.s;
-  p->S = 0;
-  // 256 threads with up to eight rows of a thread, else 512
-  for (int t = 0; t < 2 && !p->S; ++t) {
-    *small = t == 0;
-    p->S = resident_slice(s, V, sizeof(T), t == 0 ? (most_e < 8 ? most_e : 8) : most_e, t == 0 ? 256 : 512);
-  }
-  if (!p->S) return false;
-  p->slices = p->C / p->S;
-  const int rpp = (*small ? 256 : 512) / (p->S / V);
-  *rows = (p->hw + rpp - 1) / rpp;
-  p->units_p = (int)(s.n < MOST_P ? s.n : MOST_P);
-  *grid = (unsigned)((p->units_p + 7) / 8 * 8 * p->slices);
-  return true;
+// groups of rows in registers: what 256 registers hold without spilling (a row of V = 8: 4 registers in bfloat16, 8 in float32, twice
+// that in the backward)
+template <typename T, int V> constexpr int fwd_kept() { return V == 8 && sizeof(T) == 4 ? 1 : 2; }
+template <typename T, int V> constexpr int bwd_kept() { return V == 8 && sizeof(T) == 4 ? 0 : 1; }
+
+template <typename T, int V>
+hipError_t fwd_units(const P& p, unsigned grid, bool small, hipStream_t s) {
+  if (small) gn_fwd_k<T, V, 256, fwd_kept<T, V>()><<<grid, 256, 0, s>>>(p);
+  else gn_fwd_k<T, V, 512, fwd_kept<T, V>()><<<grid, 512, 0, s>>>(p);
+  return hipGetLastError();
 }
 
 template <typename T, int V>
 hipError_t fwd(const GroupNorm& g, hipStream_t s) {
   P p = base(g);
-  int e;
-  bool small;
   unsigned grid;
-  constexpr int MOST = V == 1 ? FWD_E : FWD_E / ((int)sizeof(T) / 2);
-  if (resident<T>(&p, V, MOST, &e, &small, &grid)) {
-    if (e <= 2) return fwd_e<T, V, 2>(p, grid, small, s);
-    if (e <= 4) return fwd_e<T, V, 4>(p, grid, small, s);
-    if (e <= 8) return fwd_e<T, V, 8>(p, grid, small, s);
-    if (e <= 13) return fwd_e<T, V, 13>(p, grid, small, s);
-    if (e <= 24) return fwd_e<T, V, 24>(p, grid, small, s);
-    if constexpr (MOST > 24) return e <= 36 ? fwd_e<T, V, 36>(p, grid, small, s) : fwd_e<T, V, 49>(p, grid, small, s);
+  bool small;
+  const bool units = by_units(&p, V, sizeof(T), &grid, &small);
+  // the checkpoint comes out of the same pass where 16 lanes (or the fewer of a narrow row) hold a block of its columns
+  if (g.x8) {
+    const int vpr = p.S / 8;
+    if (units && V == 8 && p.S % A8_BLOCK == 0) p.pack = 16;
+    else if (units && V == 8 && p.S == p.C && p.C < A8_BLOCK && p.C % A8_GRAIN == 0 && (vpr & (vpr - 1)) == 0) p.pack = vpr;
+    else {
+      const hipError_t e = launch_act8_pack(g.x, g.s.dtype, g.ldx, false, *g.x8, s);   // before y, which may be x, is written
+      if (e != hipSuccess) return e;
+    }
   }
+  if (units) return fwd_units<T, V>(p, grid, small, s);
   split_plan(g.s, V, &p);
   p.part = g.work;
   gn_stat_k<T, V><<<split_grid(p), ST, 0, s>>>(p);
@@ -818,23 +1019,24 @@ hipError_t fwd(const GroupNorm& g, hipStream_t s) {
   return hipGetLastError();
 }
 
+template <typename T, int V, bool X8>
+hipError_t bwd_units(const P& p, unsigned grid, bool small, hipStream_t s) {
+  if (small) gn_bwd_k<T, V, 256, bwd_kept<T, V>(), X8><<<grid, 256, 0, s>>>(p);
+  else gn_bwd_k<T, V, 512, bwd_kept<T, V>(), X8><<<grid, 512, 0, s>>>(p);
+  return hipGetLastError();
+}
+
 template <typename T, int V>
 hipError_t bwd(const GroupNorm& g, hipStream_t s) {
   P p = base(g);
-  int e;
-  bool small;
   unsigned grid;
+  bool small;
   long long rows;
-  constexpr int MOST = V == 1 ? BWD_E : BWD_E / ((int)sizeof(T) / 2);
   hipError_t err;
   p.part = g.work;
-  if (resident<T>(&p, V, MOST, &e, &small, &grid)) {
+  if (by_units(&p, V, sizeof(T), &grid, &small)) {
     rows = p.units_p;
-    if (e <= 2) err = bwd_e<T, V, 2>(p, grid, small, s);
-    else if (e <= 4) err = bwd_e<T, V, 4>(p, grid, small, s);
-    else if (e <= 8) err = bwd_e<T, V, 8>(p, grid, small, s);
-    else if constexpr (MOST > 10) err = e <= 13 ? bwd_e<T, V, 13>(p, grid, small, s) : bwd_e<T, V, 20>(p, grid, small, s);
-    else err = bwd_e<T, V, 10>(p, grid, small, s);
+    err = g.x ? bwd_units<T, V, false>(p, grid, small, s) : bwd_units<T, V, true>(p, grid, small, s);
   } else {
     split_plan(g.s, V, &p);
     rows = p.n * p.chunks;
@@ -864,10 +1066,6 @@ size_t group_norm_bytes(const slide_group_norm& s) {
 
 hipError_t launch_group_norm_fwd(const GroupNorm& g, hipStream_t s) {
   const int V = pieces(g, false);
-  if (g.x8) {   // before y, which may be x, is written
-    const hipError_t e = launch_act8_pack(g.x, g.s.dtype, g.ldx, false, *g.x8, s);
-    if (e != hipSuccess) return e;
-  }
   if (g.s.dtype == DT_F32) return V == 8 ? fwd<float, 8>(g, s) : fwd<float, 1>(g, s);
   return V == 8 ? fwd<bf16, 8>(g, s) : fwd<bf16, 1>(g, s);
 }
