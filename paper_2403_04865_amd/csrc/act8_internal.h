@@ -33,17 +33,31 @@ __device__ __forceinline__ unsigned a8_mag(float v) {
   const unsigned a = __float_as_uint(v) & 0x7fffffffu;
   return a < 0x7f800000u ? a : 0u;
 }
-// the largest of a value over neighbouring groups of `lanes` lanes (1, 2, 4, 8 or 16; uniform), in every lane of them
-__device__ __forceinline__ unsigned a8_group_max(unsigned v, int lanes) {
+// the largest of a magnitude over neighbouring groups of `lanes` lanes (1, 2, 4, 8 or 16; uniform), in every lane of them
+__device__ __forceinline__ float a8_group_max(float v, int lanes) {
   auto step = [&](auto ctrl) {
-    const unsigned o = (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, decltype(ctrl)::value, 0xf, 0xf, false);
-    v = v > o ? v : o;
+    v = fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), decltype(ctrl)::value, 0xf, 0xf, false)));
   };
   if (lanes > 1) step(std::integral_constant<int, 0xb1>{});    // lane ^ 1
   if (lanes > 2) step(std::integral_constant<int, 0x4e>{});    // lane ^ 2
   if (lanes > 4) step(std::integral_constant<int, 0x141>{});   // 7 - lane within eight: the other four, which are all alike
   if (lanes > 8) step(std::integral_constant<int, 0x140>{});   // 15 - lane within sixteen
   return v;
+}
+// scale byte of the block that `lanes` neighbouring lanes hold, eight values each.  The maximum drops NaN by itself; where an infinity is
+// among the values it is taken again over the finite ones.
+__device__ __forceinline__ unsigned a8_block_byte(const float (&v)[8], int lanes) {
+  float m = 0.f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) m = fmaxf(m, fabsf(v[e]));
+  m = a8_group_max(m, lanes);
+  if (m == __builtin_huge_valf()) {   // alike in all lanes of a block
+    m = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) m = fmaxf(m, __uint_as_float(a8_mag(v[e])));
+    m = a8_group_max(m, lanes);
+  }
+  return a8_scale_byte(__float_as_uint(m));
 }
 // four values -> four codes: nearest, ties to even; what is not finite becomes a NaN
 __device__ __forceinline__ unsigned a8_code4(float a, float b, float c, float d) {

@@ -26,10 +26,7 @@ template <> __device__ __forceinline__ void load8<float>(const float* p, float (
 
 // 8 values of a lane (zeros behind the last column) -> codes and, by lane 0 of the 16, the scale
 __device__ __forceinline__ void put8(const float (&v)[8], uint8_t* codes, uint8_t* scale, bool store, bool first) {
-  unsigned m = 0;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) { const unsigned a = a8_mag(v[e]); m = m > a ? m : a; }
-  const unsigned b = a8_scale_byte(a8_group_max(m, 16));
+  const unsigned b = a8_block_byte(v, 16);
   const float s = a8_inverse(b);
   u32x2 q;
   q[0] = a8_code4(v[0] * s, v[1] * s, v[2] * s, v[3] * s);

@@ -2,7 +2,7 @@
 //
 // A unit is one tile's slice of whole groups.  Bound by memory traffic: forward x in, y out (and one byte of checkpoint), backward
 // dy and x in, dx out; everything else is to keep a value from being read twice.
-//   * One workgroup per unit.  Statistics of every thread's rows (count, mean, sum of squared distances, four rows at a time, merged), of the
+//   * One workgroup per unit.  Statistics of every thread's rows (count, mean, sum of squared distances, two rows at a time, merged), of the
 //     groups out of these, then the result: the unit is read twice, the second time out of the caches, and rows that fit the
 //     registers once.  The backward likewise: the two sums that dx needs of each group, then dx.
 //   * Few large units are split over rows: partial statistics per channel (count, mean, sum of squared distances: merged, never a
@@ -60,6 +60,11 @@ template <> struct Vec<float, 1> {
   __device__ __forceinline__ void zero() { r = 0; }
   __device__ __forceinline__ void get(float (&v)[1]) const { v[0] = __uint_as_float(r); }
 };
+template <typename T, int V> __device__ __forceinline__ void less_of(const Vec<T, V>& b, const float (&m)[V], float (&v)[V]) {
+  b.get(v);
+#pragma unroll
+  for (int e = 0; e < V; ++e) v[e] -= m[e];
+}
 __device__ __forceinline__ u32x4 rounded(const float (&v)[8]) {
   bf16x8 t;
 #pragma unroll
@@ -99,6 +104,17 @@ template <> struct Vec8<8> {
     q = __builtin_amdgcn_raw_buffer_load_b64(c, v, s, 0);
     b = __builtin_amdgcn_raw_buffer_load_b8(sc, vs, ss, 0);
   }
+  // the values less m: a code times its power is exact, so this rounds once, as a difference of the values does
+  __device__ __forceinline__ void less(const float (&m)[8], float (&v)[8]) const {
+    const float s = a8_scale(b);
+    float t[4];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      a8_value4(q[h], 1.f, t);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[4 * h + e] = fmaf(t[e], s, -m[4 * h + e]);
+    }
+  }
   __device__ __forceinline__ void get(float (&v)[8]) const {
     const float s = a8_scale(b);
     float t[4];
@@ -121,7 +137,10 @@ template <> struct Vec8<1> {
     b = __builtin_amdgcn_raw_buffer_load_b8(sc, vs, ss, 0);
   }
   __device__ __forceinline__ void get(float (&v)[1]) const { v[0] = __builtin_amdgcn_cvt_f32_fp8((int)q, 0) * a8_scale(b); }
+  __device__ __forceinline__ void less(const float (&m)[1], float (&v)[1]) const { get(v); v[0] -= m[0]; }
 };
+
+template <int V> __device__ __forceinline__ void less_of(const Vec8<V>& b, const float (&m)[V], float (&v)[V]) { b.less(m, v); }
 
 // act: uniform, one branch for all V values
 template <int V> __device__ __forceinline__ void act_vec(float (&u)[V], int act) {
@@ -261,7 +280,7 @@ __device__ __forceinline__ void group_sums(const float (&s)[NS][V], const Own<V>
 
 // ---- a workgroup per unit ----------------------------------------------------------------------------------------------
 
-constexpr int RG = 4;   // rows whose loads are in flight together, and whose statistics are formed together
+constexpr int RG = 2;   // rows whose loads are in flight together, and whose statistics are formed together
 // Rows are taken one after the other: interleaved by the compiler they took twice the registers (and spilled).
 __device__ __forceinline__ void row_end() { __builtin_amdgcn_sched_barrier(0); }
 
@@ -278,7 +297,7 @@ template <int V> __device__ __forceinline__ void mine(const float* ch, int c, fl
 
 // KG: groups of RG rows of a thread that stay in registers
 template <typename T, int V, int TH, int KG>
-__global__ void __launch_bounds__(TH, 2) gn_fwd_k(P p) {
+__global__ void __launch_bounds__(TH, 4) gn_fwd_k(P p) {
   __shared__ float red[TH * V], gs[1][SMAX], cm[SMAX], ca[SMAX], cb[SMAX];
   const GroupNorm& g = p.g;
   const Own<V> o(p.S, TH);
@@ -302,6 +321,20 @@ __global__ void __launch_bounds__(TH, 2) gn_fwd_k(P p) {
 #pragma unroll
       for (int k = 0; k < RG; ++k) b[k].load(xb, vx, (e + k) * o.rpp * ldx);
     };
+    // the rows that are not kept, the next ones on their way while these are worked on (behind the last row: zeros)
+    auto again = [&](auto f) __attribute__((always_inline)) {
+      if (KG * RG >= p.rows) return;
+      Vec<T, V> b[2][RG];
+      load(b[0], KG * RG);
+      for (int e = KG * RG; e < p.rows; e += 2 * RG) {
+        load(b[1], e + RG);
+        row_end();
+        f(b[0], e);
+        load(b[0], e + 2 * RG);
+        row_end();
+        if (e + RG < p.rows) f(b[1], e + RG);
+      }
+    };
     // ---- statistics of this thread's rows
     float n = 0.f, m[V], q[1][V], s[1][V];
 #pragma unroll
@@ -317,18 +350,15 @@ __global__ void __launch_bounds__(TH, 2) gn_fwd_k(P p) {
 #pragma unroll
         for (int v = 0; v < V; ++v) l[v] += t[v];
         if (V == 8 && p.pack) {   // uniform
-          unsigned mag = 0;
-#pragma unroll
-          for (int v = 0; v < V; ++v) { const unsigned a = a8_mag(t[v]); mag = mag > a ? mag : a; }
-          const unsigned sc = a8_scale_byte(a8_group_max(mag, p.pack));
-          const float inv = a8_inverse(sc);
           if constexpr (V == 8) {
+            const unsigned sc = a8_block_byte(t, p.pack);
+            const float inv = a8_inverse(sc);
             u32x2 w;
             w[0] = a8_code4(t[0] * inv, t[1] * inv, t[2] * inv, t[3] * inv);
             w[1] = a8_code4(t[4] * inv, t[5] * inv, t[6] * inv, t[7] * inv);
             __builtin_amdgcn_raw_buffer_store_b64(w, cbuf, vc, (e + k) * o.rpp * ldc, 0);
+            __builtin_amdgcn_raw_buffer_store_b8((unsigned char)sc, sbuf, vs, (e + k) * o.rpp * lds, 0);
           }
-          __builtin_amdgcn_raw_buffer_store_b8((unsigned char)sc, sbuf, vs, (e + k) * o.rpp * lds, 0);
         }
       }
       // rows of these that exist; where all do (uniform) nothing is left out
@@ -363,11 +393,7 @@ __global__ void __launch_bounds__(TH, 2) gn_fwd_k(P p) {
 #pragma unroll
     for (int h = 0; h < KG; ++h)
       if (h * RG < p.rows) stat(buf[h], h * RG);
-    for (int e = KG * RG; e < p.rows; e += RG) {
-      Vec<T, V> b[RG];
-      load(b, e);
-      stat(b, e);
-    }
+    again([&](const Vec<T, V> (&b)[RG], int e) __attribute__((always_inline)) { stat(b, e); });
     // ---- of the groups
 #pragma unroll
     for (int v = 0; v < V; ++v) s[0][v] = n * m[v];
@@ -414,49 +440,43 @@ __global__ void __launch_bounds__(TH, 2) gn_fwd_k(P p) {
 #pragma unroll
     for (int h = 0; h < KG; ++h)
       if (h * RG < p.rows) apply(buf[h], h * RG);
-    for (int e = KG * RG; e < p.rows; e += RG) {
-      Vec<T, V> x[RG];
-      load(x, e);
-      apply(x, e);
-    }
+    again([&](const Vec<T, V> (&b)[RG], int e) __attribute__((always_inline)) { apply(b, e); });
     __syncthreads();   // (cm, ca, gs are written again by the next tile)
   }
 }
 
 // du = dy act'(u) of V values, u = (x - mean) (rstd gamma) + beta + residual.  A rectifier asks which side of zero u is on: where float32
 // cannot tell, it is formed again in double (mean and rstd are what the forward stored).
-template <int V, typename F>
-__device__ __forceinline__ void du_vec(const float (&d)[V], const float (&dy)[V], const float (&res)[V], const float (&rg)[V],
-                                       const float (&bet)[V], int act, float (&du)[V], F exactly) {
+template <bool RES, int V, typename F>
+__device__ __forceinline__ void du_vec(const float (&d)[V], const float (&dy)[V], const float (&rg)[V], const float (&bet)[V], const float (&res)[V],
+                                       int act, float (&du)[V], F exactly) {
   if (act == SLIDE_ACT_NONE) {
 #pragma unroll
     for (int v = 0; v < V; ++v) du[v] = dy[v];
     return;
   }
   float u[V];
+#pragma unroll
+  for (int v = 0; v < V; ++v) u[v] = fmaf(d[v], rg[v], bet[v]);
+  if constexpr (RES) {
+#pragma unroll
+    for (int v = 0; v < V; ++v) u[v] += res[v];
+  }
   if (act == SLIDE_ACT_RELU) {
     bool near = false;
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-      const float z = d[v] * rg[v];
-      u[v] = z + bet[v] + res[v];
-      near |= fabsf(u[v]) <= 1e-6f * (fabsf(z) + fabsf(bet[v]) + fabsf(res[v]));
-    }
+    for (int v = 0; v < V; ++v) near |= fabsf(u[v]) <= 1e-6f * (fabsf(d[v] * rg[v]) + fabsf(bet[v]) + (RES ? fabsf(res[v]) : 0.f));
     if (near) {
 #pragma unroll
-      for (int v = 0; v < V; ++v) { u[v] = exactly(v); row_end(); }
+      for (int v = 0; v < V; ++v) { u[v] = exactly(v); __builtin_amdgcn_sched_barrier(0); }
     }
 #pragma unroll
     for (int v = 0; v < V; ++v) du[v] = u[v] > 0.f ? dy[v] : 0.f * dy[v];
-    return;
-  }
+  } else if (act == SLIDE_ACT_SILU) {
 #pragma unroll
-  for (int v = 0; v < V; ++v) u[v] = fmaf(d[v], rg[v], bet[v]) + res[v];
-  if (act == SLIDE_ACT_SILU) {
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
+    for (int v = 0; v < V; ++v) {   // s (1 + u (1 - s))
       const float s = sigmoid_f(u[v]);
-      du[v] = dy[v] * (s * fmaf(u[v], 1.0f - s, 1.0f));
+      du[v] = dy[v] * fmaf(u[v] * s, 1.0f - s, s);
     }
   } else {
 #pragma unroll
@@ -482,7 +502,7 @@ __device__ __forceinline__ float side(double x, double mean, double rstd, double
   return u > 0.0 ? 1.f : u < 0.0 ? -1.f : (float)u;
 }
 
-template <typename T, int V, int TH, int KG, bool X8>
+template <typename T, int V, int TH, int KG, bool X8, bool RES>
 __global__ void __launch_bounds__(TH, 2) gn_bwd_k(P p) {
   __shared__ float red[2 * TH * V], gs[2][SMAX], cm[SMAX], cr[SMAX], crg[SMAX], cbet[SMAX], red2[TH];
   const GroupNorm& g = p.g;
@@ -507,9 +527,9 @@ __global__ void __launch_bounds__(TH, 2) gn_bwd_k(P p) {
                                          : tile_buffer((const T*)g.x + r0 * g.ldx + s0, g.ldx, es, p.hw, p.S);
     const __amdgpu_buffer_rsrc_t sb = tile_buffer(X8 ? p.x8.scales + r0 * p.x8.lds : nullptr, p.x8.lds, 1, p.hw, (p.C + 127) >> 7);
     const __amdgpu_buffer_rsrc_t db = tile_buffer((const T*)g.dy + r0 * g.lddy + s0, g.lddy, es, p.hw, p.S);
-    const __amdgpu_buffer_rsrc_t rb = tile_buffer(g.resid ? (const T*)g.resid + r0 * g.ldr + s0 : nullptr, g.ldr, es, p.hw, p.S);
+    const __amdgpu_buffer_rsrc_t rb = tile_buffer(RES ? (const T*)g.resid + r0 * g.ldr + s0 : nullptr, g.ldr, es, p.hw, p.S);
     typedef typename Input<T, V, X8>::type In;
-    struct Rows { In x[RG]; Vec<T, V> d[RG]; } kept[KG > 0 ? KG : 1];
+    struct Rows { In x[RG]; Vec<T, V> d[RG], w[RES ? RG : 1]; } kept[KG];
     auto load = [&](Rows& b, int e) __attribute__((always_inline)) {
 #pragma unroll
       for (int k = 0; k < RG; ++k) {
@@ -517,6 +537,7 @@ __global__ void __launch_bounds__(TH, 2) gn_bwd_k(P p) {
         if constexpr (X8) b.x[k].load(xb, vx, row * ldx, sb, vs, row * lds);
         else b.x[k].load(xb, vx, row * ldx);
         b.d[k].load(db, vd, row * ldd);
+        if constexpr (RES) b.w[k].load(rb, vr, row * ldr);
       }
     };
 #pragma unroll
@@ -534,20 +555,17 @@ __global__ void __launch_bounds__(TH, 2) gn_bwd_k(P p) {
     mine<V>(cbet, at, bet);
     // f(x - mean, du, row index) of RG rows
     auto take = [&](const Rows& b, int e, auto f) __attribute__((always_inline)) {
-      Vec<T, V> w[RG];
-      if (g.resid) {
-#pragma unroll
-        for (int k = 0; k < RG; ++k) w[k].load(rb, vr, (e + k) * o.rpp * ldr);
-      }
 #pragma unroll
       for (int k = 0; k < RG; ++k) {
-        float x[V], dy[V], res[V], d[V], du[V];
-        b.x[k].get(x);
+        float dy[V], res[V], d[V], du[V];
+        less_of<>(b.x[k], m, d);
         b.d[k].get(dy);
-#pragma unroll
-        for (int v = 0; v < V; ++v) { res[v] = 0.f; d[v] = x[v] - m[v]; }
-        if (g.resid) w[k].get(res);
-        du_vec<V>(d, dy, res, rg, bet, act, du, [&](int v) { return side(x[v], m[v], cr[at + v], g.gamma[s0 + at + v], bet[v], res[v]); });
+        if constexpr (RES) b.w[k].get(res);
+        du_vec<RES, V>(d, dy, rg, bet, res, act, du, [&](int v) __attribute__((always_inline)) {
+          float x[V];
+          b.x[k].get(x);
+          return side(x[v], m[v], cr[at + v], g.gamma[s0 + at + v], bet[v], RES ? res[v] : 0.f);
+        });
         f(d, du, e + k);
         row_end();
       }
@@ -556,10 +574,16 @@ __global__ void __launch_bounds__(TH, 2) gn_bwd_k(P p) {
 #pragma unroll
       for (int h = 0; h < KG; ++h)
         if (h * RG < p.rows) take(kept[h], h * RG, f);
-      for (int e = KG * RG; e < p.rows; e += RG) {
-        Rows b;
-        load(b, e);
-        take(b, e, f);
+      if (KG * RG >= p.rows) return;
+      Rows b[2];   // the next rows are on their way while these are worked on (behind the last row: zeros)
+      load(b[0], KG * RG);
+      for (int e = KG * RG; e < p.rows; e += 2 * RG) {
+        load(b[1], e + RG);
+        row_end();
+        take(b[0], e, f);
+        load(b[0], e + 2 * RG);
+        row_end();
+        if (e + RG < p.rows) take(b[1], e + RG, f);
       }
     };
     float s[V], q[V];
@@ -791,7 +815,7 @@ __global__ void __launch_bounds__(ST) gn_apply_k(P p) {
 }
 
 // DX false: the chunk's sums of du xhat and du per channel -> part; true: dx (and dresidual) out of the groups' sums
-template <typename T, int V, bool X8, bool DX>
+template <typename T, int V, bool X8, bool DX, bool RES>
 __global__ void __launch_bounds__(ST) gn_bwd_split_k(P p) {
   __shared__ __attribute__((aligned(16))) float red[DX ? 1 : ST * V];
   __shared__ float red2[DX ? 1 : ST], ch[DX ? 1 : ST * V];
@@ -826,19 +850,21 @@ __global__ void __launch_bounds__(ST) gn_bwd_split_k(P p) {
           const long long row = w.tile * p.hw + (at < w.hi ? at : w.hi - 1);
           load_in(bx[k], p, row, c0);
           bd[k].load((const T*)g.dy + row * g.lddy + c0);
-          if (g.resid) br[k].load((const T*)g.resid + row * g.ldr + c0);
+          if constexpr (RES) br[k].load((const T*)g.resid + row * g.ldr + c0);
         }
 #pragma unroll
         for (int k = 0; k < RG; ++k) {
           if (r + k * o.rpp >= w.hi) break;
           const long long row = w.tile * p.hw + r + k * o.rpp;
-          float x[V], dy[V], res[V], d[V], du[V];
-          bx[k].get(x);
+          float dy[V], res[V], d[V], du[V];
+          less_of<>(bx[k], mean, d);
           bd[k].get(dy);
-#pragma unroll
-          for (int v = 0; v < V; ++v) { res[v] = 0.f; d[v] = x[v] - mean[v]; }
-          if (g.resid) br[k].get(res);
-          du_vec<V>(d, dy, res, rg, bet, act, du, [&](int v) { return side(x[v], mean[v], rstd[v], g.gamma[c0 + v], bet[v], res[v]); });
+          if constexpr (RES) br[k].get(res);
+          du_vec<RES, V>(d, dy, rg, bet, res, act, du, [&](int v) __attribute__((always_inline)) {
+            float x[V];
+            bx[k].get(x);
+            return side(x[v], mean[v], rstd[v], g.gamma[c0 + v], bet[v], RES ? res[v] : 0.f);
+          });
           if constexpr (DX) {
             if (g.dresid) store_vec((T*)g.dresid + row * g.lddr + c0, du);
 #pragma unroll
@@ -937,7 +963,7 @@ size_t part_floats(const slide_group_norm& s) {
 // A workgroup per unit: its slice, threads and rows.  False: the rows are split.
 //   * The slice: whole groups, whole pieces of V, dividing the channels; the fewest channels that are 128 bytes of a row (narrower slices
 //     fetch cache lines that other units want too) and PIECES pieces in all (a unit costs some microseconds of barriers), or all of them.
-//   * 256 threads up to eight rows of a thread, else 512.
+//   * 256 threads up to sixteen rows of a thread, else 512.
 //   * With fewer units than half the compute units a longer unit is split instead.
 constexpr int PIECES = 2048;
 bool by_units(P* p, int V, int es, unsigned* grid, bool* small) {
@@ -959,11 +985,11 @@ bool by_units(P* p, int V, int es, unsigned* grid, bool* small) {
   }
   if (!p->S) return false;
   const int vpr = p->S / V;
-  *small = vpr <= 256 && (s.hw + 256 / vpr - 1) / (256 / vpr) <= 8;
+  *small = vpr <= 256 && (s.hw + 256 / vpr - 1) / (256 / vpr) <= 16;
   const int rpp = (*small ? 256 : 512) / vpr;
   p->slices = p->C / p->S;
   p->rows = (int)((s.hw + rpp - 1) / rpp);
-  if (s.n * p->slices < 128 && p->rows > 8) return false;
+  if (s.n * p->slices < 128 && p->rows > 16) return false;
   p->units_p = (int)(s.n < MOST_P ? s.n : MOST_P);
   *grid = (unsigned)((p->units_p + 7) / 8 * 8 * p->slices);
   return true;
@@ -978,15 +1004,14 @@ unsigned group_grid(const P& p) {
   return (unsigned)(u < (1 << 20) ? u : (1 << 20));
 }
 
-// groups of rows in registers: what 256 registers hold without spilling (a row of V = 8: 4 registers in bfloat16, 8 in float32, twice
-// that in the backward)
-template <typename T, int V> constexpr int fwd_kept() { return V == 8 && sizeof(T) == 4 ? 1 : 2; }
-template <typename T, int V> constexpr int bwd_kept() { return V == 8 && sizeof(T) == 4 ? 0 : 1; }
+// Groups of rows that stay in registers.  More of them (seven: a unit of 28 x 28 x 64 whole) cost more than they saved: one workgroup per
+// compute unit then, whose loads, sums and stores wait for each other (1024 such tiles, backward: 299 us, 424 with seven groups).
+constexpr int KEPT = 1;
 
 template <typename T, int V>
 hipError_t fwd_units(const P& p, unsigned grid, bool small, hipStream_t s) {
-  if (small) gn_fwd_k<T, V, 256, fwd_kept<T, V>()><<<grid, 256, 0, s>>>(p);
-  else gn_fwd_k<T, V, 512, fwd_kept<T, V>()><<<grid, 512, 0, s>>>(p);
+  if (small) gn_fwd_k<T, V, 256, KEPT><<<grid, 256, 0, s>>>(p);
+  else gn_fwd_k<T, V, 512, KEPT><<<grid, 512, 0, s>>>(p);
   return hipGetLastError();
 }
 
@@ -1019,10 +1044,23 @@ hipError_t fwd(const GroupNorm& g, hipStream_t s) {
   return hipGetLastError();
 }
 
-template <typename T, int V, bool X8>
+template <typename T, int V, bool X8, bool RES>
 hipError_t bwd_units(const P& p, unsigned grid, bool small, hipStream_t s) {
-  if (small) gn_bwd_k<T, V, 256, bwd_kept<T, V>(), X8><<<grid, 256, 0, s>>>(p);
-  else gn_bwd_k<T, V, 512, bwd_kept<T, V>(), X8><<<grid, 512, 0, s>>>(p);
+  if (small) gn_bwd_k<T, V, 256, KEPT, X8, RES><<<grid, 256, 0, s>>>(p);
+  else gn_bwd_k<T, V, 512, KEPT, X8, RES><<<grid, 512, 0, s>>>(p);
+  return hipGetLastError();
+}
+
+// the sums of the chunks, of the groups, then dx
+template <typename T, int V, bool X8, bool RES>
+hipError_t bwd_split(const P& p, hipStream_t s) {
+  gn_bwd_split_k<T, V, X8, false, RES><<<split_grid(p), ST, 0, s>>>(p);
+  hipError_t err = hipGetLastError();
+  if (err != hipSuccess) return err;
+  gn_bwd_group_k<<<group_grid(p), 256, 0, s>>>(p);
+  err = hipGetLastError();
+  if (err != hipSuccess) return err;
+  gn_bwd_split_k<T, V, X8, true, RES><<<split_grid(p), ST, 0, s>>>(p);
   return hipGetLastError();
 }
 
@@ -1036,22 +1074,14 @@ hipError_t bwd(const GroupNorm& g, hipStream_t s) {
   p.part = g.work;
   if (by_units(&p, V, sizeof(T), &grid, &small)) {
     rows = p.units_p;
-    err = g.x ? bwd_units<T, V, false>(p, grid, small, s) : bwd_units<T, V, true>(p, grid, small, s);
+    if (g.resid) err = g.x ? bwd_units<T, V, false, true>(p, grid, small, s) : bwd_units<T, V, true, true>(p, grid, small, s);
+    else err = g.x ? bwd_units<T, V, false, false>(p, grid, small, s) : bwd_units<T, V, true, false>(p, grid, small, s);
   } else {
     split_plan(g.s, V, &p);
     rows = p.n * p.chunks;
     p.sums = g.work + part_floats(g.s);
-    const unsigned sg = split_grid(p);
-    if (g.x) gn_bwd_split_k<T, V, false, false><<<sg, ST, 0, s>>>(p);
-    else gn_bwd_split_k<T, V, true, false><<<sg, ST, 0, s>>>(p);
-    err = hipGetLastError();
-    if (err != hipSuccess) return err;
-    gn_bwd_group_k<<<group_grid(p), 256, 0, s>>>(p);
-    err = hipGetLastError();
-    if (err != hipSuccess) return err;
-    if (g.x) gn_bwd_split_k<T, V, false, true><<<sg, ST, 0, s>>>(p);
-    else gn_bwd_split_k<T, V, true, true><<<sg, ST, 0, s>>>(p);
-    err = hipGetLastError();
+    if (g.resid) err = g.x ? bwd_split<T, V, false, true>(p, s) : bwd_split<T, V, true, true>(p, s);
+    else err = g.x ? bwd_split<T, V, false, false>(p, s) : bwd_split<T, V, true, false>(p, s);
   }
   if (err != hipSuccess) return err;
   gn_sum_k<<<(p.C + 15) / 16, 1024, 0, s>>>(p.part, rows, p.C, g.dgamma, g.dbeta, g.accumulate);
