@@ -87,7 +87,7 @@ int slide_act8_wgrad(const void* dy, int dtype, int64_t lddy, int64_t out, const
       !matrix_ok(dW, DT_F32, lddw, x8->cols) || (db && !floats_ok(db)))
     return SLIDE_EINVAL;
   const size_t need = slide_act8_wgrad_workspace_bytes(x8->rows, out, x8->cols);
-  if (!need) return SLIDE_EUNSUPPORTED;
+  if (!need || x8->ldc > (1 << 24) || x8->lds > (1 << 24)) return SLIDE_EUNSUPPORTED;   // 32-bit offsets within 64 rows
   const int rc = work_ok(work, work_bytes, need);
   if (rc) return rc;
   (void)hipGetLastError();

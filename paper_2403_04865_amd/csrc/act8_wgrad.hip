@@ -7,6 +7,8 @@
 // The rows are split into slabs: a work item is (slab, output tile), writes its partial tile once, and a second kernel adds the slabs
 // in a fixed order.
 #include "act8_internal.h"
+#include "lds_dma.h"
+#include "split_f32.h"
 
 namespace sl {
 
@@ -38,20 +40,16 @@ __device__ __forceinline__ bf16x8 frag_tr(const bf16* S, int c0, int k0, int lan
   return __builtin_bit_cast(bf16x8, r);
 }
 
-// 16 codes times their power of two, as two pieces of eight bfloat16: exact
+// 16 codes times their power of two, as two pieces of eight bfloat16 (the instruction is exact for every code under every scale)
 __device__ __forceinline__ void decode16(const u32x4& q, float s, bf16x8 (&o)[2]) {
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    float v[4], w[4];
-    a8_value4(q[2 * h], s, v);
-    a8_value4(q[2 * h + 1], s, w);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) { o[h][e] = (bf16)v[e]; o[h][4 + e] = (bf16)w[e]; }
+  for (int w = 0; w < 4; ++w) {
+    const bf16x2 lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(q[w], s, false), hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(q[w], s, true);
+    o[w >> 1][4 * (w & 1) + 0] = lo[0]; o[w >> 1][4 * (w & 1) + 1] = lo[1];
+    o[w >> 1][4 * (w & 1) + 2] = hi[0]; o[w >> 1][4 * (w & 1) + 3] = hi[1];
   }
 }
-
-// eight values of dy in float32
-struct Eight { float v[8]; };
 
 // YG: the tile is 128 rows of dW by 128 YG columns.  V: dy's rows can be read in 16-byte pieces.
 template <typename T, int YG, bool V>
@@ -60,7 +58,7 @@ __global__ void __launch_bounds__(NTH) wgrad_k(Item it) {
   constexpr int BY = 128 * YG, LDW = TERMS * BX + BY + 32, STAGE = BK * LDW;
   constexpr int YCHUNKS = BY / 16 * BK / NTH;
   constexpr int WBN = BY / (32 * WVN);   // 32-column products of a wavefront; two of 32 rows
-  __shared__ __attribute__((aligned(16))) bf16 ring[2][STAGE];
+  __shared__ __attribute__((aligned(16))) bf16 ring0[STAGE], ring1[STAGE];
   const A8Wgrad& g = it.g;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave / WVN, wn = wave % WVN;
@@ -77,66 +75,92 @@ __global__ void __launch_bounds__(NTH) wgrad_k(Item it) {
   const int k16 = (g.K + A8_GRAIN - 1) / A8_GRAIN * A8_GRAIN;
 
   const int xr = tid >> 4, xc = (tid & 15) * 8;            // dy: rows xr + 32 i
-  const T* const xb = (const T*)g.dy + lo * g.lddy + x0 + xc;
+  const int yr = tid / (BY / 16), yc = tid % (BY / 16) * 16;   // codes: rows yr + (NTH / (BY / 16)) j, one column of pieces
+  constexpr int XR = NTH / 16, YR = NTH / (BY / 16);
+  static_assert(YR * (BY / 16) == NTH || YG == 3, "loader split");
+  const bool bias = g.db && y0 == 0;   // uniform
   T rx[XCHUNKS][8];
   u32x4 ry[YCHUNKS];
-  float rs[YCHUNKS];
-  auto fetch = [&](int step) {
+  unsigned rs[YCHUNKS];
+  // Buffers of one step's 64 rows, so that offsets stay small; rows that do not exist are outside of them: zeros.
+  const int ldx = (int)(V ? g.lddy * (long long)sizeof(T) : 0), ldc = (int)g.x.ldc, lds = (int)g.x.lds;
+  const int vx = V && x0 + xc < g.N ? xr * ldx + xc * (int)sizeof(T) : DMA_ABSENT;
+  auto rows_left = [&](int step) { const int r = span - step * BK; return r < BK ? r : BK; };
+  auto fetch_x = [&](int step) __attribute__((always_inline)) {
+    const T* p = (const T*)g.dy + (lo + (long long)step * BK) * g.lddy + x0;
+    const int left = rows_left(step);
+    if constexpr (V) {
+      const __amdgpu_buffer_rsrc_t b = dma_buffer(p, left > 0 ? (left - 1) * (long long)ldx + (g.N - x0) * (long long)sizeof(T) : 0);
 #pragma unroll
-    for (int i = 0; i < XCHUNKS; ++i) {
-      const int r = step * BK + xr + (NTH / 16) * i;
-      const T* p = xb + (long long)r * g.lddy;
-      if (V && r < span && x0 + xc + 8 <= g.N) {
-        typedef T vec __attribute__((ext_vector_type(16 / sizeof(T))));
+      for (int i = 0; i < XCHUNKS; ++i)
 #pragma unroll
         for (int h = 0; h < (int)sizeof(T) / 2; ++h)
-          *reinterpret_cast<vec*>(&rx[i][h * (16 / sizeof(T))]) = *reinterpret_cast<const vec*>(p + h * (16 / sizeof(T)));
-      } else {
+          *reinterpret_cast<u32x4*>(&rx[i][h * (16 / sizeof(T))]) = __builtin_amdgcn_raw_buffer_load_b128(b, vx + 16 * h, XR * i * ldx, 0);
+    } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) rx[i][e] = r < span && x0 + xc + e < g.N ? p[e] : (T)0.f;
-      }
+      for (int i = 0; i < XCHUNKS; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int r = xr + XR * i;
+          rx[i][e] = r < left && x0 + xc + e < g.N ? p[r * g.lddy + xc + e] : (T)0.f;
+        }
     }
+  };
+  auto piece = [&](int j, int* row, int* col) {   // with 24 pieces a row the threads do not stay in their column
+    const int c = tid + NTH * j;
+    *row = YG == 3 ? c / (BY / 16) : yr + YR * j;
+    *col = YG == 3 ? c % (BY / 16) * 16 : yc;
+  };
+  auto fetch_y = [&](int step) __attribute__((always_inline)) {
+    const long long r0 = lo + (long long)step * BK;
+    const int left = rows_left(step);
+    const __amdgpu_buffer_rsrc_t b = dma_buffer(g.x.codes + r0 * g.x.ldc + y0, left > 0 ? (left - 1) * (long long)ldc + k16 - y0 : 0);
+    const __amdgpu_buffer_rsrc_t sb = dma_buffer(g.x.scales + r0 * g.x.lds + (y0 >> 7), left > 0 ? (left - 1) * (long long)lds + ((k16 - y0 + 127) >> 7) : 0);
 #pragma unroll
     for (int j = 0; j < YCHUNKS; ++j) {
-      const int c = tid + NTH * j, r = step * BK + c / (BY / 16), col = y0 + c % (BY / 16) * 16;
-      const bool have = r < span && col < k16;
-      const u32x4 z = {0, 0, 0, 0};
-      ry[j] = have ? *reinterpret_cast<const u32x4*>(g.x.codes + (lo + r) * g.x.ldc + col) : z;
-      rs[j] = have ? a8_scale(g.x.scales[(lo + r) * g.x.lds + (col >> 7)]) : 0.f;
+      int row, col;
+      piece(j, &row, &col);
+      const bool have = y0 + col < k16;
+      ry[j] = __builtin_amdgcn_raw_buffer_load_b128(b, have ? row * ldc + col : DMA_ABSENT, 0, 0);
+      rs[j] = __builtin_amdgcn_raw_buffer_load_b8(sb, have ? row * lds + (col >> 7) : DMA_ABSENT, 0, 0);
     }
   };
   float cs[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) cs[e] = 0.f;
-  auto stash = [&](int st) {
-    bf16* S = ring[st];
+  auto stash_x = [&](bf16* S, int i) __attribute__((always_inline)) {
+    bf16* p = S + (xr + XR * i) * LDW + xc;
+    float f[8];
+    if (bias || TERMS > 1) {
 #pragma unroll
-    for (int i = 0; i < XCHUNKS; ++i) {
-      bf16* p = S + (xr + (NTH / 16) * i) * LDW + xc;
-      float f[8];
+      for (int e = 0; e < 8; ++e) f[e] = to_f(rx[i][e]);
+    }
+    if (bias) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) { f[e] = to_f(rx[i][e]); cs[e] += f[e]; }
+      for (int e = 0; e < 8; ++e) cs[e] += f[e];
+    }
 #pragma unroll
-      for (int t = 0; t < TERMS; ++t) {
-        bf16x8 o;
+    for (int t = 0; t < TERMS; ++t) {
+      bf16x8 o;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
+      for (int e = 0; e < 8; ++e) {
+        if constexpr (TERMS == 1) o[e] = rx[i][e];
+        else {
           o[e] = (bf16)f[e];
-          // (what rounds to an infinity, or is none, has no further terms)
-          if constexpr (TERMS > 1) f[e] = a8_mag((float)o[e]) ? f[e] - (float)o[e] : 0.f;
+          f[e] = a8_mag((float)o[e]) ? f[e] - (float)o[e] : 0.f;   // (what rounds to an infinity, or is none, has no further terms)
         }
-        *reinterpret_cast<bf16x8*>(p + t * BX) = o;
       }
+      *reinterpret_cast<bf16x8*>(p + t * BX) = o;
     }
-#pragma unroll
-    for (int j = 0; j < YCHUNKS; ++j) {
-      const int c = tid + NTH * j;
-      bf16x8 o[2];
-      decode16(ry[j], rs[j], o);
-      bf16* p = S + c / (BY / 16) * LDW + TERMS * BX + c % (BY / 16) * 16;
-      *reinterpret_cast<bf16x8*>(p) = o[0];
-      *reinterpret_cast<bf16x8*>(p + 8) = o[1];
-    }
+  };
+  auto stash_y = [&](bf16* S, int j) __attribute__((always_inline)) {
+    int row, col;
+    piece(j, &row, &col);
+    bf16x8 o[2];
+    decode16(ry[j], a8_scale(rs[j]), o);
+    bf16* p = S + row * LDW + TERMS * BX + col;
+    *reinterpret_cast<bf16x8*>(p) = o[0];
+    *reinterpret_cast<bf16x8*>(p + 8) = o[1];
   };
 
   f32x16 acc[2][WBN];
@@ -147,31 +171,66 @@ __global__ void __launch_bounds__(NTH) wgrad_k(Item it) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
 
+  struct Frags { bf16x8 x[TERMS][2], y[WBN]; };
+  auto read = [&](Frags& f, const bf16* S, int k) __attribute__((always_inline)) {   // 16 rows of the stage
+#pragma unroll
+    for (int j = 0; j < WBN; ++j) f.y[j] = frag_tr<LDW>(S, TERMS * BX + (wn * WBN + j) * 32, k, lane);
+#pragma unroll
+    for (int t = 0; t < TERMS; ++t)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) f.x[t][i] = frag_tr<LDW>(S, t * BX + (wm * 2 + i) * 32, k, lane);
+  };
+  auto multiply = [&](const Frags& f) __attribute__((always_inline)) {
+#pragma unroll
+    for (int t = 0; t < TERMS; ++t)
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < WBN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.x[t][i], f.y[j], acc[i][j], 0, 0, 0);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  // A step multiplies out of one stage, writes what was fetched a step ago to the other and fetches the rows after those: memory has a
+  // whole step, and the decoding and the LDS writes lie between the products of the slices.  The fragments are read a slice
+  // ahead; the barrier (it waits for LDS, not for the loads) stands before the last slice's products, so that the next step's first
+  // fragments come under these.
+  Frags fa, fb;
+  auto step = [&](int s, const bf16* S, bf16* N) __attribute__((always_inline)) {
+    const bool more = s + 1 < steps;   // uniform
+    read(fb, S, 16);
+    if (more) {
+#pragma unroll
+      for (int i = 0; i < XCHUNKS; ++i) stash_x(N, i);
+    }
+    fetch_x(s + 2);
+    multiply(fa);
+    read(fa, S, 32);
+    if (more) {
+#pragma unroll
+      for (int j = 0; j < YCHUNKS; ++j) stash_y(N, j);
+    }
+    fetch_y(s + 2);
+    multiply(fb);
+    read(fb, S, 48);
+    multiply(fa);
+    step_barrier();
+    if (more) read(fa, N, 0);
+    multiply(fb);
+  };
   if (steps > 0) {
-    fetch(0);
-    stash(0);
+    fetch_x(0);
+    fetch_y(0);
+#pragma unroll
+    for (int i = 0; i < XCHUNKS; ++i) stash_x(ring0, i);
+#pragma unroll
+    for (int j = 0; j < YCHUNKS; ++j) stash_y(ring0, j);
+    fetch_x(1);
+    fetch_y(1);
   }
   __syncthreads();
-  for (int s = 0; s < steps; ++s) {
-    const bool more = s + 1 < steps;   // uniform
-    if (more) fetch(s + 1);
-    const bf16* S = ring[s & 1];
-#pragma unroll
-    for (int k = 0; k < BK; k += 16) {
-      bf16x8 fy[WBN];
-#pragma unroll
-      for (int j = 0; j < WBN; ++j) fy[j] = frag_tr<LDW>(S, TERMS * BX + (wn * WBN + j) * 32, k, lane);
-#pragma unroll
-      for (int t = 0; t < TERMS; ++t)
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const bf16x8 fx = frag_tr<LDW>(S, t * BX + (wm * 2 + i) * 32, k, lane);
-#pragma unroll
-          for (int j = 0; j < WBN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fx, fy[j], acc[i][j], 0, 0, 0);
-        }
-    }
-    if (more) stash((s + 1) & 1);
-    __syncthreads();
+  if (steps > 0) read(fa, ring0, 0);
+  for (int s = 0; s < steps; s += 2) {
+    step(s, ring0, ring1);
+    if (s + 1 < steps) step(s + 1, ring1, ring0);
   }
 
   // lane: column l % 32, rows 8 (r / 4) + 4 (l / 32) + r % 4
@@ -193,9 +252,9 @@ __global__ void __launch_bounds__(NTH) wgrad_k(Item it) {
       }
     }
   // bias gradient: the tiles of the first columns add the rows their threads loaded
-  if (g.db && y0 == 0) {
+  if (bias) {
     __syncthreads();
-    float* red = reinterpret_cast<float*>(ring[0]);   // [32 threads][128 columns]
+    float* red = reinterpret_cast<float*>(ring0);   // [32 threads][128 columns]
 #pragma unroll
     for (int e = 0; e < 8; ++e) red[xr * BX + xc + e] = cs[e];
     __syncthreads();
@@ -280,7 +339,8 @@ hipError_t launch_act8_wgrad(const A8Wgrad& g, hipStream_t s) {
   it.part = g.work;
   it.cpart = g.work + (((size_t)it.slabs * g.N * g.K * 4 + 255) & ~(size_t)255) / 4;
   const size_t es = elem_size(g.dt);
-  const bool v = ((uintptr_t)g.dy & 15) == 0 && (g.lddy * es) % 16 == 0;
+  // whole 16-byte pieces of eight columns, 32-bit offsets within 64 rows
+  const bool v = ((uintptr_t)g.dy & 15) == 0 && (g.lddy * es) % 16 == 0 && g.N % 8 == 0 && g.lddy <= (1 << 22);
   hipError_t e;
   if (g.dt == DT_F32) e = v ? run<float, true>(it, yg, s) : run<float, false>(it, yg, s);
   else e = v ? run<bf16, true>(it, yg, s) : run<bf16, false>(it, yg, s);

@@ -91,6 +91,8 @@ def test_wgrad(lib):
         assert call(**bad) == EINVAL, bad
     assert call(work=None) == EARENA and call(bytes=need - 1) == EARENA
     assert call(out=1 << 24, ld=1 << 24) == EUNSUPPORTED
+    x8 = a8(1000, 200, ldc=(1 << 24) + 16)
+    assert call() == EUNSUPPORTED
 
 
 def _shape(**kw):
