@@ -59,6 +59,7 @@ __global__ void __launch_bounds__(NTH) wgrad_k(Item it) {
   constexpr int YCHUNKS = BY / 16 * BK / NTH;
   constexpr int WBN = BY / (32 * WVN);   // 32-column products of a wavefront; two of 32 rows
   __shared__ __attribute__((aligned(16))) bf16 ring0[STAGE], ring1[STAGE];
+  __shared__ float scale[4][BK * YG];
   const A8Wgrad& g = it.g;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave / WVN, wn = wave % WVN;
@@ -79,14 +80,12 @@ __global__ void __launch_bounds__(NTH) wgrad_k(Item it) {
   constexpr int XR = NTH / 16, YR = NTH / (BY / 16);
   static_assert(YR * (BY / 16) == NTH || YG == 3, "loader split");
   const bool bias = g.db && y0 == 0;   // uniform
-  T rx[XCHUNKS][8];
-  u32x4 ry[YCHUNKS];
-  unsigned rs[YCHUNKS];
+  struct Rows { T x[XCHUNKS][8]; u32x4 y[YCHUNKS]; } r0, r1;   // this thread's pieces of the rows of odd and of even steps
   // Buffers of one step's 64 rows, so that offsets stay small; rows that do not exist are outside of them: zeros.
   const int ldx = (int)(V ? g.lddy * (long long)sizeof(T) : 0), ldc = (int)g.x.ldc, lds = (int)g.x.lds;
   const int vx = V && x0 + xc < g.N ? xr * ldx + xc * (int)sizeof(T) : DMA_ABSENT;
   auto rows_left = [&](int step) { const int r = span - step * BK; return r < BK ? r : BK; };
-  auto fetch_x = [&](int step) __attribute__((always_inline)) {
+  auto fetch_x = [&](Rows& R, int step) __attribute__((always_inline)) {
     const T* p = (const T*)g.dy + (lo + (long long)step * BK) * g.lddy + x0;
     const int left = rows_left(step);
     if constexpr (V) {
@@ -95,14 +94,14 @@ __global__ void __launch_bounds__(NTH) wgrad_k(Item it) {
       for (int i = 0; i < XCHUNKS; ++i)
 #pragma unroll
         for (int h = 0; h < (int)sizeof(T) / 2; ++h)
-          *reinterpret_cast<u32x4*>(&rx[i][h * (16 / sizeof(T))]) = __builtin_amdgcn_raw_buffer_load_b128(b, vx + 16 * h, XR * i * ldx, 0);
+          *reinterpret_cast<u32x4*>(&R.x[i][h * (16 / sizeof(T))]) = __builtin_amdgcn_raw_buffer_load_b128(b, vx + 16 * h, XR * i * ldx, 0);
     } else {
 #pragma unroll
       for (int i = 0; i < XCHUNKS; ++i)
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const int r = xr + XR * i;
-          rx[i][e] = r < left && x0 + xc + e < g.N ? p[r * g.lddy + xc + e] : (T)0.f;
+          R.x[i][e] = r < left && x0 + xc + e < g.N ? p[r * g.lddy + xc + e] : (T)0.f;
         }
     }
   };
@@ -111,40 +110,42 @@ __global__ void __launch_bounds__(NTH) wgrad_k(Item it) {
     *row = YG == 3 ? c / (BY / 16) : yr + YR * j;
     *col = YG == 3 ? c % (BY / 16) * 16 : yc;
   };
-  auto fetch_y = [&](int step) __attribute__((always_inline)) {
-    const long long r0 = lo + (long long)step * BK;
+  auto fetch_y = [&](Rows& R, int step) __attribute__((always_inline)) {
+    const long long row0 = lo + (long long)step * BK;
     const int left = rows_left(step);
-    const __amdgpu_buffer_rsrc_t b = dma_buffer(g.x.codes + r0 * g.x.ldc + y0, left > 0 ? (left - 1) * (long long)ldc + k16 - y0 : 0);
-    const __amdgpu_buffer_rsrc_t sb = dma_buffer(g.x.scales + r0 * g.x.lds + (y0 >> 7), left > 0 ? (left - 1) * (long long)lds + ((k16 - y0 + 127) >> 7) : 0);
+    const __amdgpu_buffer_rsrc_t b = dma_buffer(g.x.codes + row0 * g.x.ldc + y0, left > 0 ? (left - 1) * (long long)ldc + k16 - y0 : 0);
 #pragma unroll
     for (int j = 0; j < YCHUNKS; ++j) {
       int row, col;
       piece(j, &row, &col);
-      const bool have = y0 + col < k16;
-      ry[j] = __builtin_amdgcn_raw_buffer_load_b128(b, have ? row * ldc + col : DMA_ABSENT, 0, 0);
-      rs[j] = __builtin_amdgcn_raw_buffer_load_b8(sb, have ? row * lds + (col >> 7) : DMA_ABSENT, 0, 0);
+      R.y[j] = __builtin_amdgcn_raw_buffer_load_b128(b, y0 + col < k16 ? row * ldc + col : DMA_ABSENT, 0, 0);
     }
   };
-  float cs[8];
-#pragma unroll
-  for (int e = 0; e < 8; ++e) cs[e] = 0.f;
-  auto stash_x = [&](bf16* S, int i) __attribute__((always_inline)) {
+  // The powers of a step's rows and blocks: one byte of memory by each of the first 64 YG threads, through LDS to the threads that decode
+  // (as a byte load beside every piece of codes: 641 us for 403456 x 1536 -> 384, 518 without).
+  const bool scaler = tid < BK * YG;
+  auto fetch_s = [&](int step) __attribute__((always_inline)) {
+    const int left = rows_left(step), row = tid / YG, blk = tid - row * YG;
+    const __amdgpu_buffer_rsrc_t sb = dma_buffer(g.x.scales + (lo + (long long)step * BK) * g.x.lds + (y0 >> 7),
+                                                 left > 0 ? (left - 1) * (long long)lds + ((k16 - y0 + 127) >> 7) : 0);
+    return (unsigned)__builtin_amdgcn_raw_buffer_load_b8(sb, scaler && y0 + 128 * blk < k16 ? row * lds + blk : DMA_ABSENT, 0, 0);
+  };
+  auto put_s = [&](int step, unsigned b) __attribute__((always_inline)) {
+    if (scaler) scale[step & 3][tid] = a8_scale(b);
+  };
+  auto stash_x = [&](const Rows& R, bf16* S, int i) __attribute__((always_inline)) {
     bf16* p = S + (xr + XR * i) * LDW + xc;
     float f[8];
-    if (bias || TERMS > 1) {
+    if constexpr (TERMS > 1) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) f[e] = to_f(rx[i][e]);
-    }
-    if (bias) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) cs[e] += f[e];
+      for (int e = 0; e < 8; ++e) f[e] = to_f(R.x[i][e]);
     }
 #pragma unroll
     for (int t = 0; t < TERMS; ++t) {
       bf16x8 o;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        if constexpr (TERMS == 1) o[e] = rx[i][e];
+        if constexpr (TERMS == 1) o[e] = R.x[i][e];
         else {
           o[e] = (bf16)f[e];
           f[e] = a8_mag((float)o[e]) ? f[e] - (float)o[e] : 0.f;   // (what rounds to an infinity, or is none, has no further terms)
@@ -153,11 +154,11 @@ __global__ void __launch_bounds__(NTH) wgrad_k(Item it) {
       *reinterpret_cast<bf16x8*>(p + t * BX) = o;
     }
   };
-  auto stash_y = [&](bf16* S, int j) __attribute__((always_inline)) {
+  auto stash_y = [&](const Rows& R, bf16* S, int step, int j) __attribute__((always_inline)) {
     int row, col;
     piece(j, &row, &col);
     bf16x8 o[2];
-    decode16(ry[j], a8_scale(rs[j]), o);
+    decode16(R.y[j], scale[step & 3][row * YG + (col >> 7)], o);
     bf16* p = S + row * LDW + TERMS * BX + col;
     *reinterpret_cast<bf16x8*>(p) = o[0];
     *reinterpret_cast<bf16x8*>(p + 8) = o[1];
@@ -180,7 +181,21 @@ __global__ void __launch_bounds__(NTH) wgrad_k(Item it) {
 #pragma unroll
       for (int i = 0; i < 2; ++i) f.x[t][i] = frag_tr<LDW>(S, t * BX + (wm * 2 + i) * 32, k, lane);
   };
-  auto multiply = [&](const Frags& f) __attribute__((always_inline)) {
+  // Bias gradient out of the fragments, whose lanes hold eight rows of a column: four two-term sums a fragment, and the four wavefronts that
+  // read the same ones take a slice each (as additions of what a thread loads, or as products with ones: 100 to 150 us of the 690 of
+  // 403456 x 384 -> 1536).
+  float cs[2] = {0.f, 0.f};
+  auto multiply = [&](const Frags& f, int q) __attribute__((always_inline)) {   // q: slice
+    if (bias && wn == q) {   // uniform
+      typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+      const bf16x2 one = {(bf16)1.f, (bf16)1.f};
+#pragma unroll
+      for (int t = 0; t < TERMS; ++t)
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int e = 0; e < 8; e += 2) cs[i] = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{f.x[t][i][e], f.x[t][i][e + 1]}, one, cs[i], false);
+    }
 #pragma unroll
     for (int t = 0; t < TERMS; ++t)
 #pragma unroll
@@ -189,48 +204,59 @@ __global__ void __launch_bounds__(NTH) wgrad_k(Item it) {
         for (int j = 0; j < WBN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.x[t][i], f.y[j], acc[i][j], 0, 0, 0);
     __builtin_amdgcn_sched_barrier(0);
   };
-  // A step multiplies out of one stage, writes what was fetched a step ago to the other and fetches the rows after those: memory has a
-  // whole step, and the decoding and the LDS writes lie between the products of the slices.  The fragments are read a slice
+  // A step multiplies out of one stage, writes what was fetched two steps ago to the other and fetches the rows two steps after those
+  // (one step ahead: 549 us for 403456 x 384 -> 1536, ONEAHEAD), and the decoding and the LDS writes lie between the products of the slices.  The fragments are read a slice
   // ahead; the barrier (it waits for LDS, not for the loads) stands before the last slice's products, so that the next step's first
   // fragments come under these.
   Frags fa, fb;
-  auto step = [&](int s, const bf16* S, bf16* N) __attribute__((always_inline)) {
+  unsigned s0 = 0, s1 = 0;   // scales of the next even and odd step but one
+  auto step = [&](int s, const bf16* S, bf16* N, Rows& R, unsigned& sr) __attribute__((always_inline)) {
     const bool more = s + 1 < steps;   // uniform
     read(fb, S, 16);
     if (more) {
 #pragma unroll
-      for (int i = 0; i < XCHUNKS; ++i) stash_x(N, i);
+      for (int i = 0; i < XCHUNKS; ++i) stash_x(R, N, i);
     }
-    fetch_x(s + 2);
-    multiply(fa);
+    fetch_x(R, s + 3);
+    put_s(s + 2, sr);
+    sr = fetch_s(s + 4);
+    multiply(fa, 0);
     read(fa, S, 32);
     if (more) {
 #pragma unroll
-      for (int j = 0; j < YCHUNKS; ++j) stash_y(N, j);
+      for (int j = 0; j < YCHUNKS; ++j) stash_y(R, N, s + 1, j);
     }
-    fetch_y(s + 2);
-    multiply(fb);
+    fetch_y(R, s + 3);
+    multiply(fb, 1);
     read(fb, S, 48);
-    multiply(fa);
+    multiply(fa, 2);
     step_barrier();
     if (more) read(fa, N, 0);
-    multiply(fb);
+    multiply(fb, 3);
   };
   if (steps > 0) {
-    fetch_x(0);
-    fetch_y(0);
+    fetch_x(r1, 0);
+    fetch_y(r1, 0);
+    const unsigned first = fetch_s(0), second = fetch_s(1);
+    s0 = fetch_s(2);
+    s1 = fetch_s(3);
+    fetch_x(r0, 1);
+    fetch_y(r0, 1);
+    put_s(0, first);
+    put_s(1, second);
+    __syncthreads();
 #pragma unroll
-    for (int i = 0; i < XCHUNKS; ++i) stash_x(ring0, i);
+    for (int i = 0; i < XCHUNKS; ++i) stash_x(r1, ring0, i);
 #pragma unroll
-    for (int j = 0; j < YCHUNKS; ++j) stash_y(ring0, j);
-    fetch_x(1);
-    fetch_y(1);
+    for (int j = 0; j < YCHUNKS; ++j) stash_y(r1, ring0, 0, j);
+    fetch_x(r1, 2);
+    fetch_y(r1, 2);
   }
   __syncthreads();
   if (steps > 0) read(fa, ring0, 0);
   for (int s = 0; s < steps; s += 2) {
-    step(s, ring0, ring1);
-    if (s + 1 < steps) step(s + 1, ring1, ring0);
+    step(s, ring0, ring1, r0, s0);
+    if (s + 1 < steps) step(s + 1, ring1, ring0, r1, s1);
   }
 
   // lane: column l % 32, rows 8 (r / 4) + 4 (l / 32) + r % 4
@@ -251,16 +277,18 @@ __global__ void __launch_bounds__(NTH) wgrad_k(Item it) {
         }
       }
     }
-  // bias gradient: the tiles of the first columns add the rows their threads loaded
+  // bias gradient: the four wavefronts' slices, in order
   if (bias) {
     __syncthreads();
-    float* red = reinterpret_cast<float*>(ring0);   // [32 threads][128 columns]
+    float* red = reinterpret_cast<float*>(ring0);   // [4][128]
 #pragma unroll
-    for (int e = 0; e < 8; ++e) red[xr * BX + xc + e] = cs[e];
+    for (int i = 0; i < 2; ++i) {
+      const float v = cs[i] + __shfl_xor(cs[i], 32, 64);
+      if (lane < 32) red[wn * BX + (wm * 2 + i) * 32 + lane] = v;
+    }
     __syncthreads();
     if (tid < BX && x0 + tid < g.N) {
-      float v = 0.f;
-      for (int r = 0; r < NTH / 16; ++r) v += red[r * BX + tid];
+      const float v = (red[tid] + red[BX + tid]) + (red[2 * BX + tid] + red[3 * BX + tid]);
       if (direct) g.db[x0 + tid] = g.accumulate ? g.db[x0 + tid] + v : v;
       else it.cpart[(long long)slab * g.N + x0 + tid] = v;
     }
