@@ -455,9 +455,8 @@ class Act8:
         return Act8(rows, cols, torch.empty((rows, -(-cols // 16) * 16), dtype=torch.uint8, device=device),
                     torch.empty((rows, -(-cols // 128)), dtype=torch.uint8, device=device))
 
-    @property
-    def device(self):
-        return self.codes.device
+    def get_device(self):
+        return self.codes.get_device()
 
 
 class Act8Lib:
@@ -469,6 +468,8 @@ class Act8Lib:
         self.lib = load_cdll()
         self._torch = torch
         self._types = {torch.float32: 0, torch.bfloat16: 1}
+        self._entry = {n: getattr(self.lib, n) for n in ("slide_act8_pack", "slide_act8_unpack", "slide_act8_linear", "slide_act8_wgrad",
+                                                         "slide_group_norm_fwd", "slide_group_norm_bwd")}
 
     # ---- marshalling
     def _type(self, t):
@@ -478,24 +479,27 @@ class Act8Lib:
             raise ValueError(f"float32 or bfloat16, not {t.dtype}") from None
 
     def _matrix(self, t, rows, cols, dtype, what):
-        """(pointer, elements between rows) of a [rows, cols] matrix of dtype; a tensor of more dimensions is one of its last two's rows
-        where its strides allow it.  (None, 0) for None."""
+        """(pointer, elements between rows) of a [rows, cols] matrix of dtype, or of tiles [n, hw, cols] whose rows lie at one stride.
+        (None, 0) for None."""
         if t is None:
             return None, 0
         if t.dtype != dtype:
             raise ValueError(f"{what}: {t.dtype}, expected {dtype}")
-        if t.dim() == 3:
-            if t.shape[0] > 1 and t.shape[1] > 1 and t.stride(0) != t.shape[1] * t.stride(1):
+        shape, stride = t.shape, t.stride()
+        if len(shape) == 2:
+            have, last = shape
+            ld = stride[0]
+        elif len(shape) == 3:
+            n, hw, last = shape
+            if n > 1 and hw > 1 and stride[0] != hw * stride[1]:
                 raise ValueError(f"{what}: tiles must follow one another at one row stride")
-            have, last = t.shape[0] * t.shape[1], t.shape[2]
-            ld = t.stride(1) if t.shape[1] > 1 else t.stride(0)
-        elif t.dim() == 2:
-            (have, last), ld = t.shape, t.stride(0)
+            have = n * hw
+            ld = stride[1] if hw > 1 else stride[0]
         else:
             raise ValueError(f"{what}: a matrix, or tiles of rows")
         if have != rows or last != cols:
-            raise ValueError(f"{what}: {tuple(t.shape)}, expected {rows} rows of {cols}")
-        if last > 1 and t.stride(-1) != 1:
+            raise ValueError(f"{what}: {tuple(shape)}, expected {rows} rows of {cols}")
+        if last > 1 and stride[-1] != 1:
             raise ValueError(f"{what}: rows must be contiguous")
         return t.data_ptr(), ld if have > 1 else max(ld, cols)
 
@@ -516,23 +520,24 @@ class Act8Lib:
 
     def _call(self, what, first, others, args, stream):
         """Run the entry point on the device of `first`, which all of `others` must be on."""
-        torch, dev = self._torch, first.device
-        if dev.type != "cuda":
+        dev = first.get_device()
+        if dev < 0:
             raise ValueError(f"{what}: tensors must be on the GPU")
         for t in others:
-            if t is not None and t.device != dev:
-                raise ValueError(f"{what}: tensors on {dev} and {t.device}")
+            if t is not None and t.get_device() != dev:
+                raise ValueError(f"{what}: tensors on different devices")
+        cuda = self._torch.cuda
         if stream is None:
-            stream = torch.cuda.current_stream(dev).cuda_stream
+            stream = cuda.current_stream(dev).cuda_stream
         elif not isinstance(stream, int):
-            if stream.device != dev:
-                raise ValueError(f"{what}: a stream of {stream.device} for tensors on {dev}")
+            if stream.device.index != dev:
+                raise ValueError(f"{what}: a stream of {stream.device} for tensors on device {dev}")
             stream = stream.cuda_stream
-        if dev.index != torch.cuda.current_device():
-            with torch.cuda.device(dev):
-                rc = getattr(self.lib, what)(*args, stream)
+        if dev != cuda.current_device():
+            with cuda.device(dev):
+                rc = self._entry[what](*args, stream)
         else:
-            rc = getattr(self.lib, what)(*args, stream)
+            rc = self._entry[what](*args, stream)
         if rc != 0:
             raise SlideError(rc, what, self.lib.slide_last_hip_error())
 

@@ -204,8 +204,8 @@ __global__ void __launch_bounds__(NTH) wgrad_k(Item it) {
         for (int j = 0; j < WBN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.x[t][i], f.y[j], acc[i][j], 0, 0, 0);
     __builtin_amdgcn_sched_barrier(0);
   };
-  // A step multiplies out of one stage, writes what was fetched two steps ago to the other and fetches the rows two steps after those
-  // (one step ahead: 549 us for 403456 x 384 -> 1536, ONEAHEAD), and the decoding and the LDS writes lie between the products of the slices.  The fragments are read a slice
+  // A step multiplies out of one stage, writes what was fetched two steps ago to the other and fetches the rows two steps after
+  // those, and the decoding and the LDS writes lie between the products of the slices.  The fragments are read a slice
   // ahead; the barrier (it waits for LDS, not for the loads) stands before the last slice's products, so that the next step's first
   // fragments come under these.
   Frags fa, fb;
@@ -310,27 +310,22 @@ __global__ void __launch_bounds__(256) wgrad_sum_k(Item it) {
   }
 }
 
-int tile_groups(int K) {   // 128-column groups of a tile: the fewest columns beyond K, then the widest
-  int best = 1;
-  long long waste = 1LL << 60;
-  for (int yg = 1; yg <= 3; ++yg) {
-    const long long cols = (long long)(K + 128 * yg - 1) / (128 * yg) * 128 * yg;
-    if (cols <= waste) { waste = cols; best = yg; }
-  }
-  return best;
-}
-
-void plan(long long M, int N, int K, int yg, Item* it) {
-  it->TX = (N + BX - 1) / BX;
-  it->TY = (K + 128 * yg - 1) / (128 * yg);
-  const long long tiles = (long long)it->TX * it->TY, steps = (M + BK - 1) / BK;
-  // slabs: the fewest rounds of 256 workgroups; a slab has eight steps at least, and costs its partial's way out and back
+// Tile width (128 yg columns) and slabs that a model of the time says are the fastest.  Its parts were measured (microseconds): a step of a
+// workgroup 0.85, 1.3, 1.65 (yg 1, 2, 3; float32 1.6), 1.45 where two workgroups of yg 1 share a compute unit; launches and prologue 4;
+// a second kernel 5, and a slab's partial out and back at 6 MB a microsecond.  It finds 7289 x 384 -> 1152: yg 1, 8 slabs, 28 us (yg 3:
+// 30 at best); 403456 x 384 -> 1536: yg 3, 21 slabs, 545 us (yg 1: 661); 65536 x 1024 -> 1024: yg 2, 8 slabs, 181 us.
+void plan(long long M, int N, int K, bool f32, Item* it, int* width) {
+  const long long steps = (M + BK - 1) / BK;
   double best = 1e300;
-  it->slabs = 1;
-  for (int s = 1; s <= MAX_SLABS && (s == 1 || steps / s >= 8); ++s) {
-    const double rounds = (double)((tiles * s + 255) / 256);
-    const double cost = rounds * (double)((steps + s - 1) / s + 4) + (s > 1 ? s * (double)N * K * 8e-6 / 2.0 : 0.0);
-    if (cost < best) { best = cost; it->slabs = s; }
+  for (int yg = 1; yg <= (f32 ? 1 : 3); ++yg) {
+    const int TX = (N + BX - 1) / BX, TY = (int)((K + 128LL * yg - 1) / (128 * yg));
+    const long long tiles = (long long)TX * TY, slots = yg == 1 && !f32 ? 512 : 256;
+    for (int s = 1; s <= MAX_SLABS && (s == 1 || steps / s >= 2); ++s) {
+      const long long wgs = tiles * s, rounds = (wgs + slots - 1) / slots;
+      const double t = f32 ? 1.6 : yg == 1 ? (wgs > 256 ? 1.45 : 0.85) : yg == 2 ? 1.3 : 1.65;
+      const double cost = (double)rounds * (double)((steps + s - 1) / s) * t + 4 + (s > 1 ? 5 + (double)s * N * K * 8e-6 / 6.0 : 0.0);
+      if (cost < best) { best = cost; it->slabs = s; it->TX = TX; it->TY = TY; *width = yg; }
+    }
   }
   it->per = (steps + it->slabs - 1) / it->slabs * BK;
 }
@@ -353,17 +348,18 @@ size_t part_bytes(const Item& it, int N, int K) {
 
 size_t act8_wgrad_bytes(long long M, int N, int K) {
   Item a{}, b{};
-  plan(M, N, K, tile_groups(K), &a);
-  plan(M, N, K, 1, &b);   // float32 gradients
+  int yg;
+  plan(M, N, K, false, &a, &yg);
+  plan(M, N, K, true, &b, &yg);
   const size_t x = part_bytes(a, N, K), y = part_bytes(b, N, K);
   return ((x > y ? x : y) + 256 + 255) & ~(size_t)255;
 }
 
 hipError_t launch_act8_wgrad(const A8Wgrad& g, hipStream_t s) {
-  const int yg = g.dt == DT_F32 ? 1 : tile_groups(g.K);
+  int yg;
   Item it{};
   it.g = g;
-  plan(g.M, g.N, g.K, yg, &it);
+  plan(g.M, g.N, g.K, g.dt == DT_F32, &it, &yg);
   it.part = g.work;
   it.cpart = g.work + (((size_t)it.slabs * g.N * g.K * 4 + 255) & ~(size_t)255) / 4;
   const size_t es = elem_size(g.dt);
