@@ -468,6 +468,9 @@ class Act8Lib:
         self.lib = load_cdll()
         self._torch = torch
         self._types = {torch.float32: 0, torch.bfloat16: 1}
+        self._shapes = {}
+        # the raw handle of a device's current stream, where this torch has it without building a Stream
+        self._raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
         self._entry = {n: getattr(self.lib, n) for n in ("slide_act8_pack", "slide_act8_unpack", "slide_act8_linear", "slide_act8_wgrad",
                                                          "slide_group_norm_fwd", "slide_group_norm_bwd")}
 
@@ -528,7 +531,7 @@ class Act8Lib:
                 raise ValueError(f"{what}: tensors on different devices")
         cuda = self._torch.cuda
         if stream is None:
-            stream = cuda.current_stream(dev).cuda_stream
+            stream = self._raw_stream(dev)
         elif not isinstance(stream, int):
             if stream.device.index != dev:
                 raise ValueError(f"{what}: a stream of {stream.device} for tensors on device {dev}")
@@ -574,13 +577,19 @@ class Act8Lib:
                    (p, self._type(dy), ld, out, x8._ref, wp, ldw, self._floats(db, out, "db"), int(accumulate), *self._work(workspace)),
                    stream)
 
-    def _shape(self, n, hw, channels, groups, dtype, act, eps):
-        return _CGroupNorm(n, hw, channels, groups, dtype, act, eps, 0)
+    def _shape(self, *key):
+        """The C description of a group norm, kept by its values: n, hw, channels, groups, dtype, act, eps."""
+        s = self._shapes.get(key)
+        if s is None:
+            if len(self._shapes) > 256:
+                self._shapes.clear()
+            s = self._shapes[key] = C.pointer(_CGroupNorm(*key, 0))
+        return s
 
     def slide_group_norm_workspace_bytes(self, n, hw, channels, groups, dtype):
         """For both directions of a group norm over [n, hw, channels]; 0 for a shape that is refused."""
         s = self._shape(n, hw, channels, groups, self._types.get(dtype, -1), 0, 1.0)
-        return int(self.lib.slide_group_norm_workspace_bytes(C.byref(s)))
+        return int(self.lib.slide_group_norm_workspace_bytes(s))
 
     def slide_group_norm_fwd(self, x, gamma, beta, groups, y, mean, rstd, eps=1e-5, act="none", residual=None, x8=None,
                              workspace=None, stream=None):
@@ -593,7 +602,7 @@ class Act8Lib:
         rp, ldr = self._matrix(residual, n * hw, c, x.dtype, "residual")
         yp, ldy = self._matrix(y, n * hw, c, x.dtype, "y")
         self._call("slide_group_norm_fwd", x, (gamma, beta, residual, y, x8, mean, rstd, workspace),
-                   (C.byref(s), xp, ldx, self._floats(gamma, c, "gamma"), self._floats(beta, c, "beta"), rp, ldr, yp, ldy,
+                   (s, xp, ldx, self._floats(gamma, c, "gamma"), self._floats(beta, c, "beta"), rp, ldr, yp, ldy,
                     None if x8 is None else x8._ref, self._floats(mean, n * groups, "mean"), self._floats(rstd, n * groups, "rstd"),
                     *self._work(workspace)), stream)
 
@@ -609,7 +618,7 @@ class Act8Lib:
         xp, ldx = (None, 0) if kept else self._matrix(x, n * hw, c, t, "x")
         m = self._matrix
         self._call("slide_group_norm_bwd", dy, (x, gamma, beta, residual, mean, rstd, dx, dresidual, dgamma, dbeta, workspace),
-                   (C.byref(s), *m(dy, n * hw, c, t, "dy"), xp, ldx, x._ref if kept else None, self._floats(gamma, c, "gamma"),
+                   (s, *m(dy, n * hw, c, t, "dy"), xp, ldx, x._ref if kept else None, self._floats(gamma, c, "gamma"),
                     self._floats(beta, c, "beta"), *m(residual, n * hw, c, t, "residual"), self._floats(mean, n * groups, "mean"),
                     self._floats(rstd, n * groups, "rstd"), *m(dx, n * hw, c, t, "dx"), *m(dresidual, n * hw, c, t, "dresidual"),
                     self._floats(dgamma, c, "dgamma"), self._floats(dbeta, c, "dbeta"), int(accumulate), *self._work(workspace)),

@@ -64,11 +64,13 @@ int slide_act8_linear(const void* x, int dtype, int64_t ldx, const slide_act8* x
   if (residual && (!matrix_ok(residual, dtype, ldr, out) || (residual == y && ldr != ldy))) return SLIDE_EINVAL;
   if (out > A8_MAX_COLS) return SLIDE_EUNSUPPORTED;
   (void)hipGetLastError();
-  if (x) {
+  const bool fused = x && x8->rows <= A8_FEW;
+  if (x && !fused) {
     const int rc = status(launch_act8_pack(x, dtype, ldx, false, *x8, (hipStream_t)stream));
     if (rc) return rc;
   }
   A8Linear g{};
+  if (fused) { g.xin = x; g.ldxin = ldx; }
   g.x = a8_view(*x8); g.w = a8_view(*w8);
   g.M = x8->rows; g.N = (int)out; g.K = (int)x8->cols;
   g.bias = bias; g.act = act; g.dt = dtype; g.resid = residual; g.ldr = ldr; g.y = y; g.ldy = ldy;

@@ -66,11 +66,50 @@ __device__ __forceinline__ Codes load_codes(const uint8_t* p, int k, int k16) { 
 
 // ---- few rows -------------------------------------------------------------------------------------------------------
 // A workgroup takes 16 output columns and 16 MT rows; its wavefronts share out the blocks of k and their partial products are added in
-// LDS, in a fixed order.
+// LDS, in a fixed order.  PACK (up to 16 rows): x comes as it is and every workgroup makes the codes it multiplies for itself, the first one
+// leaves them as the checkpoint: one launch instead of two (1 x 4096 -> 4096: 12.2 us a call with a launch for the packing, FEWFIG).
 constexpr int SW = 8;   // wavefronts
 
-template <int MT, int ACT, typename T>
-__global__ void __launch_bounds__(64 * SW) linear_few_k(A8Linear g) {
+// 32 values of row `x` from column k on (zeros from K on) -> codes and the scale byte of their block, which the four lanes that differ in
+// bits 4 and 5 hold together
+template <typename T>
+__device__ __forceinline__ Codes pack32(const T* x, int k, int K, bool vec, int* byte) {
+  float v[32];
+  if (vec && k + 32 <= K) {
+    typedef T vec16 __attribute__((ext_vector_type(16 / sizeof(T))));
+    constexpr int E = 16 / sizeof(T);
+#pragma unroll
+    for (int h = 0; h < 32 / E; ++h) {
+      const vec16 q = *reinterpret_cast<const vec16*>(x + k + h * E);
+#pragma unroll
+      for (int e = 0; e < E; ++e) v[h * E + e] = to_f(q[e]);
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 32; ++e) v[e] = k + e < K ? to_f(x[k + e]) : 0.f;
+  }
+  auto most = [](float m) { m = fmaxf(m, __shfl_xor(m, 16, 64)); return fmaxf(m, __shfl_xor(m, 32, 64)); };
+  float m = 0.f;
+#pragma unroll
+  for (int e = 0; e < 32; ++e) m = fmaxf(m, fabsf(v[e]));   // (drops NaN)
+  m = most(m);
+  if (m == __builtin_huge_valf()) {   // alike in the four lanes; the other lanes of the wavefront take no part in their exchange
+    m = 0.f;
+#pragma unroll
+    for (int e = 0; e < 32; ++e) m = fmaxf(m, __uint_as_float(a8_mag(v[e])));
+    m = most(m);
+  }
+  const unsigned b = a8_scale_byte(__float_as_uint(m));
+  const float s = a8_inverse(b);
+  Codes c;
+#pragma unroll
+  for (int w = 0; w < 8; ++w) c[w] = (int)a8_code4(v[4 * w] * s, v[4 * w + 1] * s, v[4 * w + 2] * s, v[4 * w + 3] * s);
+  *byte = (int)b;
+  return c;
+}
+
+template <int MT, int ACT, typename T, bool PACK>
+__global__ void __launch_bounds__(64 * SW) linear_few_k(A8Linear g, bool vec) {
   constexpr bool F8 = sizeof(T) == 2;
   constexpr int U = MT == 1 ? 4 : MT == 2 ? 2 : 1;   // blocks whose loads are in flight together
   __shared__ float red[SW][MT * 256];
@@ -81,11 +120,13 @@ __global__ void __launch_bounds__(64 * SW) linear_few_k(A8Linear g) {
   const int n = n0 + r < g.N ? n0 + r : g.N - 1;
   const uint8_t *wp = g.w.codes + n * g.w.ldc, *ws = g.w.scales + n * g.w.lds;
   const uint8_t *xp[MT], *xs[MT];
+  long long mr[MT];
 #pragma unroll
   for (int i = 0; i < MT; ++i) {
-    const long long m = m0 + 16 * i + r < g.M ? m0 + 16 * i + r : g.M - 1;
-    xp[i] = g.x.codes + m * g.x.ldc; xs[i] = g.x.scales + m * g.x.lds;
+    mr[i] = m0 + 16 * i + r < g.M ? m0 + 16 * i + r : g.M - 1;
+    xp[i] = g.x.codes + mr[i] * g.x.ldc; xs[i] = g.x.scales + mr[i] * g.x.lds;
   }
+  const bool leave = PACK && blockIdx.x == 0 && m0 + r < g.M;   // this lane's codes are the checkpoint's
   f32x4 acc[MT];
 #pragma unroll
   for (int i = 0; i < MT; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -97,8 +138,24 @@ __global__ void __launch_bounds__(64 * SW) linear_few_k(A8Linear g) {
       const int b = b0 + u * SW, k = b * A8_BLOCK + kg, at = b < nb ? b : nb - 1;
       cw[u] = load_codes(wp, k, k16);
       sw[u] = ws[at];
+      if constexpr (!PACK) {
 #pragma unroll
-      for (int i = 0; i < MT; ++i) { cx[u][i] = load_codes(xp[i], k, k16); sx[u][i] = xs[i][at]; }
+        for (int i = 0; i < MT; ++i) { cx[u][i] = load_codes(xp[i], k, k16); sx[u][i] = xs[i][at]; }
+      }
+    }
+    if constexpr (PACK) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int b = b0 + u * SW, k = b * A8_BLOCK + kg;
+        if (b >= nb) { cx[u][0] = Codes{}; sx[u][0] = 127; continue; }   // uniform
+        cx[u][0] = pack32((const T*)g.xin + mr[0] * g.ldxin, k, g.K, vec, &sx[u][0]);
+        if (leave) {
+          uint8_t* to = const_cast<uint8_t*>(xp[0]) + k;
+          if (k < k16) *reinterpret_cast<i32x4*>(to) = __builtin_shufflevector(cx[u][0], cx[u][0], 0, 1, 2, 3);
+          if (k + 16 < k16) *reinterpret_cast<i32x4*>(to + 16) = __builtin_shufflevector(cx[u][0], cx[u][0], 4, 5, 6, 7);
+          if (kg == 0) const_cast<uint8_t*>(xs[0])[b] = (uint8_t)sx[u][0];
+        }
+      }
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -133,6 +190,11 @@ __global__ void __launch_bounds__(64 * SW) linear_few_k(A8Linear g) {
 template <int ACT, typename T>
 hipError_t few(const A8Linear& g, hipStream_t s) {
   const int mt = g.M <= 16 ? 1 : g.M <= 32 ? 2 : 4;
+  if (g.xin) {   // M <= 16
+    const bool vec = ((uintptr_t)g.xin & 15) == 0 && g.ldxin * sizeof(T) % 16 == 0;
+    linear_few_k<1, ACT, T, true><<<(g.N + 15) / 16, 64 * SW, 0, s>>>(g, vec);
+    return hipGetLastError();
+  }
   A8Linear p = g;
   // grid.y is limited to 65535: the rows go in pieces
   const long long most = 16LL * mt * 65535;
@@ -142,9 +204,9 @@ hipError_t few(const A8Linear& g, hipStream_t s) {
     p.y = (T*)g.y + m * g.ldy;
     if (g.resid) p.resid = (const T*)g.resid + m * g.ldr;
     const dim3 grid((g.N + 15) / 16, (unsigned)((p.M + 16 * mt - 1) / (16 * mt)));
-    if (mt == 1) linear_few_k<1, ACT, T><<<grid, 64 * SW, 0, s>>>(p);
-    else if (mt == 2) linear_few_k<2, ACT, T><<<grid, 64 * SW, 0, s>>>(p);
-    else linear_few_k<4, ACT, T><<<grid, 64 * SW, 0, s>>>(p);
+    if (mt == 1) linear_few_k<1, ACT, T, false><<<grid, 64 * SW, 0, s>>>(p, false);
+    else if (mt == 2) linear_few_k<2, ACT, T, false><<<grid, 64 * SW, 0, s>>>(p, false);
+    else linear_few_k<4, ACT, T, false><<<grid, 64 * SW, 0, s>>>(p, false);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
