@@ -67,7 +67,7 @@ __device__ __forceinline__ Codes load_codes(const uint8_t* p, int k, int k16) { 
 // ---- few rows -------------------------------------------------------------------------------------------------------
 // A workgroup takes 16 output columns and 16 MT rows; its wavefronts share out the blocks of k and their partial products are added in
 // LDS, in a fixed order.  PACK (up to 16 rows): x comes as it is and every workgroup makes the codes it multiplies for itself, the first one
-// leaves them as the checkpoint: one launch instead of two (1 x 4096 -> 4096: 12.2 us a call with a launch for the packing, FEWFIG).
+// leaves them as the checkpoint: one launch instead of two (1 x 4096 -> 4096: 12.2 us a call with a launch for the packing, 8.5 so).
 constexpr int SW = 8;   // wavefronts
 
 // 32 values of row `x` from column k on (zeros from K on) -> codes and the scale byte of their block, which the four lanes that differ in
@@ -304,8 +304,8 @@ __device__ __forceinline__ void store_tile(const f32x4 (&acc)[4][FM], const f32x
       for (int h = 0; h < NH; ++h) {
         const u32x4 w = *reinterpret_cast<const u32x4*>(out + h * RP * PROW);
         const int at = (i * 16 + h * RP) * (int)o.ldy * (int)sizeof(T);
-        if (o.stream) __builtin_amdgcn_raw_buffer_store_b128(w, yb, yo, at, 2);
-        else __builtin_amdgcn_raw_buffer_store_b128(w, yb, yo, at, 0);
+        if (o.stream) store16<2>(w, yb, yo + at);
+        else store16(w, yb, yo + at);
       }
     } else {
 #pragma unroll 1

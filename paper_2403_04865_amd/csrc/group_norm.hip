@@ -78,13 +78,13 @@ __device__ __forceinline__ void store_vec(float* p, const float (&v)[8]) {
 }
 template <typename T> __device__ __forceinline__ void store_vec(T* p, const float (&v)[1]) { *p = from_f<T>(v[0]); }
 template <typename T> __device__ __forceinline__ void store_buf(__amdgpu_buffer_rsrc_t b, int o, int s, const float (&v)[8]) {
-  if constexpr (sizeof(T) == 2) __builtin_amdgcn_raw_buffer_store_b128(rounded(v), b, o, s, 0);
+  if constexpr (sizeof(T) == 2) store16(rounded(v), b, o + s);
   else {
     u32x4 lo, hi;
 #pragma unroll
     for (int e = 0; e < 4; ++e) { lo[e] = __float_as_uint(v[e]); hi[e] = __float_as_uint(v[4 + e]); }
-    __builtin_amdgcn_raw_buffer_store_b128(lo, b, o, s, 0);
-    __builtin_amdgcn_raw_buffer_store_b128(hi, b, o + 16, s, 0);
+    store16(lo, b, o + s);
+    store16(hi, b, o + s + 16);
   }
 }
 template <typename T> __device__ __forceinline__ void store_buf(__amdgpu_buffer_rsrc_t b, int o, int s, const float (&v)[1]) {
@@ -636,8 +636,18 @@ __global__ void __launch_bounds__(1024) gn_sum_k(const float* __restrict__ part,
   __shared__ double ra[64][17], rb[64][17];
   const int c = threadIdx.x & 15, q = threadIdx.x >> 4, ch = blockIdx.x * 16 + c;
   double a = 0.0, b = 0.0;
-  if (ch < C)
-    for (long long r = q; r < rows; r += 64) { a += (double)part[r * 2 * C + ch]; b += (double)part[(r * 2 + 1) * C + ch]; }
+  if (ch < C) {
+    const float* p = part + ch;
+    long long r = q;
+    for (; r + 192 < rows; r += 256) {   // eight loads in flight
+      float u[4], v[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) { u[k] = p[(r + 64 * k) * 2 * C]; v[k] = p[((r + 64 * k) * 2 + 1) * C]; }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) { a += (double)u[k]; b += (double)v[k]; }
+    }
+    for (; r < rows; r += 64) { a += (double)p[r * 2 * C]; b += (double)p[(r * 2 + 1) * C]; }
+  }
   ra[q][c] = a; rb[q][c] = b;
   __syncthreads();
   if (threadIdx.x < 16 && ch < C) {
@@ -672,7 +682,9 @@ __global__ void __launch_bounds__(ST) gn_stat_k(P p) {
   for (long long unit = blockIdx.x; unit < p.n * p.chunks * p.slices; unit += gridDim.x) {
     const Where w = where(p, unit);
     const int S = p.C - w.slice * p.S < p.S ? p.C - w.slice * p.S : p.S;   // the last slice may be short
-    const Own<V> o(S, ST);
+    // (with a checkpoint the pieces of a row are padded to whole DPP rows of 16 lanes, which hold a block of its columns)
+    Own<V> o(p.pack ? (S / V + 15) / 16 * 16 * V : S, ST);
+    o.on = o.on && o.tc * V < S;
     const int c0 = w.slice * p.S + o.tc * V;
     const T* x = (const T*)g.x + w.tile * p.hw * g.ldx + c0;
     float n = 0.f, m[V], q[V];
@@ -697,6 +709,18 @@ __global__ void __launch_bounds__(ST) gn_stat_k(P p) {
           buf[e].get(t);
 #pragma unroll
           for (int v = 0; v < V; ++v) s[v] += t[v];
+          if constexpr (V == 8) {
+            if (p.pack && r + e * o.rpp < w.hi) {   // (lanes behind the last column take no part: nothing)
+              const unsigned sc = a8_block_byte(t, 16);
+              const float inv = a8_inverse(sc);
+              const long long row = w.tile * p.hw + r + e * o.rpp;
+              u32x2 z;
+              z[0] = a8_code4(t[0] * inv, t[1] * inv, t[2] * inv, t[3] * inv);
+              z[1] = a8_code4(t[4] * inv, t[5] * inv, t[6] * inv, t[7] * inv);
+              *reinterpret_cast<u32x2*>(const_cast<uint8_t*>(p.x8.codes) + row * p.x8.ldc + c0) = z;
+              if ((o.tc & 15) == 0) const_cast<uint8_t*>(p.x8.scales)[row * p.x8.lds + (c0 >> 7)] = (uint8_t)sc;
+            }
+          }
         }
 #pragma unroll
         for (int v = 0; v < V; ++v) s[v] /= (float)have;
@@ -730,32 +754,36 @@ __global__ void __launch_bounds__(ST) gn_stat_k(P p) {
   }
 }
 
+constexpr int GT = 1024;   // threads that add up a group
 __device__ __forceinline__ double block_sum(double v, double* red) {
 #pragma unroll
   for (int k = 32; k > 0; k >>= 1) v += __shfl_xor(v, k, 64);
   __syncthreads();
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
   __syncthreads();
-  return red[0] + red[1] + red[2] + red[3];
+  double s = 0.0;
+#pragma unroll
+  for (int k = 0; k < GT / 64; ++k) s += red[k];
+  return s;
 }
 
 // mean and rstd of a group from the partials of its channels and chunks
-__global__ void __launch_bounds__(256) gn_stat_group_k(P p) {
-  __shared__ double red[4];
+__global__ void __launch_bounds__(GT) gn_stat_group_k(P p) {
+  __shared__ double red[GT / 64];
   for (long long u = blockIdx.x; u < p.n * p.G; u += gridDim.x) {
     const long long tile = u / p.G;
     const int gr = (int)(u - tile * p.G);
     const float* part = p.part + tile * p.chunks * 2 * p.C + gr * p.per;
     const int all = p.chunks * p.per;
     double s = 0.0;
-    for (int i = threadIdx.x; i < all; i += 256) {
+    for (int i = threadIdx.x; i < all; i += GT) {
       const int k = i / p.per, c = i - k * p.per;
       const int rows = p.hw - k * p.rows_chunk < p.rows_chunk ? p.hw - k * p.rows_chunk : p.rows_chunk;
       s += (double)rows * (double)part[(long long)k * 2 * p.C + c];
     }
     const double count = (double)p.hw * p.per, mean = block_sum(s, red) / count;
     double q = 0.0;
-    for (int i = threadIdx.x; i < all; i += 256) {
+    for (int i = threadIdx.x; i < all; i += GT) {
       const int k = i / p.per, c = i - k * p.per;
       const int rows = p.hw - k * p.rows_chunk < p.rows_chunk ? p.hw - k * p.rows_chunk : p.rows_chunk;
       const double d = (double)part[(long long)k * 2 * p.C + c] - mean;
@@ -893,14 +921,14 @@ __global__ void __launch_bounds__(ST) gn_bwd_split_k(P p) {
 }
 
 // sums[tile][group] = sums over chunks and channels of the partials times the gain
-__global__ void __launch_bounds__(256) gn_bwd_group_k(P p) {
-  __shared__ double red[4];
+__global__ void __launch_bounds__(GT) gn_bwd_group_k(P p) {
+  __shared__ double red[GT / 64];
   for (long long u = blockIdx.x; u < p.n * p.G; u += gridDim.x) {
     const long long tile = u / p.G;
     const int gr = (int)(u - tile * p.G);
     const float* part = p.part + tile * p.chunks * 2 * p.C + gr * p.per;
     double a = 0.0, b = 0.0;
-    for (int i = threadIdx.x; i < p.chunks * p.per; i += 256) {
+    for (int i = threadIdx.x; i < p.chunks * p.per; i += GT) {
       const int k = i / p.per, c = i - k * p.per;
       const double w = p.g.gamma[gr * p.per + c];
       a += w * (double)part[(long long)k * 2 * p.C + c];
@@ -962,7 +990,8 @@ size_t part_floats(const slide_group_norm& s) {
 
 // A workgroup per unit: its slice, threads and rows.  False: the rows are split.
 //   * The slice: whole groups, whole pieces of V, dividing the channels; the fewest channels that are 128 bytes of a row (narrower slices
-//     fetch cache lines that other units want too) and PIECES pieces in all (a unit costs some microseconds of barriers), or all of them.
+//     fetch cache lines that other units want too) and, where there are units enough, PIECES pieces in all (a unit costs some
+//     microseconds of barriers), or all of them.
 //   * 256 threads up to sixteen rows of a thread, else 512.
 //   * With fewer units than half the compute units a longer unit is split instead.
 constexpr int PIECES = 2048;
@@ -981,7 +1010,7 @@ bool by_units(P* p, int V, int es, unsigned* grid, bool* small) {
     const int S = base * k;
     if (S / V > 512) break;
     p->S = S;
-    if ((long long)S * es >= 128 && s.hw * (S / V) >= PIECES) break;
+    if ((long long)S * es >= 128 && (s.hw * (S / V) >= PIECES || s.n * (p->C / S) < 512)) break;
   }
   if (!p->S) return false;
   const int vpr = p->S / V;
@@ -1021,23 +1050,24 @@ hipError_t fwd(const GroupNorm& g, hipStream_t s) {
   unsigned grid;
   bool small;
   const bool units = by_units(&p, V, sizeof(T), &grid, &small);
-  // the checkpoint comes out of the same pass where 16 lanes (or the fewer of a narrow row) hold a block of its columns
+  if (!units) split_plan(g.s, V, &p);
+  // The checkpoint comes out of the same pass where 16 lanes (or the fewer of a narrow row) hold a block of its columns, and no byte behind
+  // the last column is to be cleared.
   if (g.x8) {
     const int vpr = p.S / 8;
-    if (units && V == 8 && p.S % A8_BLOCK == 0) p.pack = 16;
-    else if (units && V == 8 && p.S == p.C && p.C < A8_BLOCK && p.C % A8_GRAIN == 0 && (vpr & (vpr - 1)) == 0) p.pack = vpr;
+    if (V == 8 && p.C % A8_GRAIN == 0 && (!units || p.S % A8_BLOCK == 0)) p.pack = 16;
+    else if (V == 8 && p.C % A8_GRAIN == 0 && p.S == p.C && p.C < A8_BLOCK && (vpr & (vpr - 1)) == 0) p.pack = vpr;
     else {
       const hipError_t e = launch_act8_pack(g.x, g.s.dtype, g.ldx, false, *g.x8, s);   // before y, which may be x, is written
       if (e != hipSuccess) return e;
     }
   }
   if (units) return fwd_units<T, V>(p, grid, small, s);
-  split_plan(g.s, V, &p);
   p.part = g.work;
   gn_stat_k<T, V><<<split_grid(p), ST, 0, s>>>(p);
   hipError_t err = hipGetLastError();
   if (err != hipSuccess) return err;
-  gn_stat_group_k<<<group_grid(p), 256, 0, s>>>(p);
+  gn_stat_group_k<<<group_grid(p), GT, 0, s>>>(p);
   err = hipGetLastError();
   if (err != hipSuccess) return err;
   gn_apply_k<T, V><<<split_grid(p), ST, 0, s>>>(p);
@@ -1057,7 +1087,7 @@ hipError_t bwd_split(const P& p, hipStream_t s) {
   gn_bwd_split_k<T, V, X8, false, RES><<<split_grid(p), ST, 0, s>>>(p);
   hipError_t err = hipGetLastError();
   if (err != hipSuccess) return err;
-  gn_bwd_group_k<<<group_grid(p), 256, 0, s>>>(p);
+  gn_bwd_group_k<<<group_grid(p), GT, 0, s>>>(p);
   err = hipGetLastError();
   if (err != hipSuccess) return err;
   gn_bwd_split_k<T, V, X8, true, RES><<<split_grid(p), ST, 0, s>>>(p);

@@ -267,3 +267,38 @@ def test_a_rectifier_at_zero():
                            residual=_dev(res), dresidual=dres, workspace=work)
     sure = np.abs(sign) > 1e-14
     assert sure.mean() > 0.9 and np.array_equal(dres.cpu().numpy()[sure], (sign > 0).astype(np.float32)[sure])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_every_value_of_many_tiles(dtype):
+    """All values of a hundred megabytes of output, five times over, against the formula on the device: a store whose data the next
+    instruction overwrote was wrong in one value of some thousands."""
+    import torch
+    L = _lib()
+    t = _types()[dtype]
+    for n, hw, c, groups in ((600, 784, 64, 32), (200, 196, 320, 32)):
+        g = torch.Generator(device="cuda").manual_seed(n)
+        x = torch.randn(n, hw, c, device="cuda", generator=g).to(t)
+        dy = torch.randn(n, hw, c, device="cuda", generator=g).to(t)
+        gamma, beta = 1 + 0.1 * torch.randn(c, device="cuda", generator=g), 0.1 * torch.randn(c, device="cuda", generator=g)
+        work = torch.empty(L.slide_group_norm_workspace_bytes(n, hw, c, groups, t), dtype=torch.uint8, device="cuda")
+        v = x.double().view(n, hw, groups, -1)
+        m = v.mean((1, 3), keepdim=True)
+        r = 1 / torch.sqrt(v.var((1, 3), unbiased=False, keepdim=True) + 1e-5)
+        xhat = ((v - m) * r).view(n, hw, c)
+        want = xhat * gamma + beta
+        du = dy.double()
+        q = (du * gamma).view(n, hw, groups, -1)
+        h = xhat.view(n, hw, groups, -1)
+        want_dx = (r * (q - q.mean((1, 3), keepdim=True) - h * (q * h).mean((1, 3), keepdim=True))).view(n, hw, c)
+        for _ in range(5):
+            y, dx, dres = (torch.full_like(x, float("nan")) for _ in range(3))
+            mean, rstd = torch.empty(n, groups, device="cuda"), torch.empty(n, groups, device="cuda")
+            dg, db = torch.empty(c, device="cuda"), torch.empty(c, device="cuda")
+            L.slide_group_norm_fwd(x, gamma, beta, groups, y, mean, rstd, workspace=work)
+            L.slide_group_norm_bwd(dy, x, gamma, beta, mean, rstd, groups, dx, dg, db, dresidual=dres, workspace=work)
+            # statistics to D (above) of values of size one, gains up to 1.5, |xhat| up to 6
+            tol = 20 * D + _half_step(dtype) * 1.01 * want.abs()
+            assert ((y.double() - want).abs() <= tol).all()
+            assert ((dx.double() - want_dx).abs() <= 20 * D + _half_step(dtype) * 1.01 * want_dx.abs()).all()
+            assert torch.equal(dres, dy)
