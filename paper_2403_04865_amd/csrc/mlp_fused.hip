@@ -31,6 +31,7 @@
 // loads), so that case stays two launches.  Tried besides: stores spread over the step (slower: each is waited for with
 // the weight loads behind it, and vmcnt is in order), weight loads split between wavefronts by stage (no change), fragments
 // read two to four at a time (no change).
+#include "lds_dma.h"
 #include "slide_internal.h"
 
 #include <type_traits>
@@ -222,7 +223,7 @@ __global__ void __launch_bounds__(NTH, 1) mlp_k(MlpArgs g, int tiles) {
       ht[1] = pk[i + 1];
       swap16(ht[0], ht[1]);
     }
-    __builtin_amdgcn_raw_buffer_store_b128(ht[i & 1], rh, hoff, s * (FS * 2) + (i >> 1) * 64 + (i & 1) * 32 * g.F, 0);
+    store16(ht[i & 1], rh, hoff + s * (FS * 2) + (i >> 1) * 64 + (i & 1) * 32 * g.F);
   };
   auto load_c = [&](int s, int i) __attribute__((always_inline)) {
     cd[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rc, coff, s * FS + i * 16 * g.F, 0));
@@ -464,7 +465,7 @@ __global__ void __launch_bounds__(NTH, 1) mlp_k(MlpArgs g, int tiles) {
             o[w] = pack2(__uint_as_float(o[w] << 16) + __uint_as_float(rs[h][p][w] << 16),
                          __uint_as_float(o[w] & 0xffff0000u) + __uint_as_float(rs[h][p][w] & 0xffff0000u));
         }
-        __builtin_amdgcn_raw_buffer_store_b128(o, ro, qoff[p % 3], (p / 3) * 8 * 2 * D + h * 384, 0);
+        store16(o, ro, qoff[p % 3] + (p / 3) * 8 * 2 * D + h * 384);
       }
     }
     if (next >= tiles) break;
