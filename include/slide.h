@@ -56,7 +56,9 @@ typedef struct slide_config {
   int32_t dtype;       /* 0 = float32 path, 1 = bfloat16 storage / float32 accumulate */
   int32_t recompute;   /* 0 = keep every block's activations; 1 = keep block inputs, re-run blocks in backward */
   float   ln_eps;      /* LayerNorm epsilon (1e-6) */
-  int32_t reserved;    /* must be 0 (pixel gradients are requested per call by a non-null pointer) */
+  int32_t checkpoint8; /* 1 = the block inputs that `recompute` keeps are kept in 8 bits (act8.h): half their bytes; the forward is as
+                        * without, the blocks run again on the rounded inputs, one backward per forward.  bfloat16 and recompute == 1 only;
+                        * else 0 */
 } slide_config;
 
 typedef struct slide_ctx slide_ctx;

@@ -27,7 +27,7 @@ class SlideError(RuntimeError):
 class _CConfig(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("tile", "patch", "dim", "layers", "heads", "mlp_ratio", "mil_hidden",
                                          "n_classes", "dtype", "recompute")] + \
-               [("ln_eps", C.c_float), ("reserved", C.c_int32)]
+               [("ln_eps", C.c_float), ("checkpoint8", C.c_int32)]
 
 
 @dataclass
@@ -43,6 +43,7 @@ class SlideConfig:
     dtype: int = 0          # 0 float32, 1 bfloat16
     recompute: int = 0
     ln_eps: float = 1e-6
+    checkpoint8: int = 0    # with recompute: block inputs in 8 bits
 
 
 def config_from(shape, dtype: int, recompute: int = 0) -> SlideConfig:
@@ -200,7 +201,7 @@ class SlideLib:
         self.lib = load_cdll()
         self.cfg = cfg
         cc = _CConfig(cfg.tile, cfg.patch, cfg.dim, cfg.layers, cfg.heads, cfg.mlp_ratio, cfg.mil_hidden,
-                      cfg.n_classes, cfg.dtype, cfg.recompute, cfg.ln_eps, 0)
+                      cfg.n_classes, cfg.dtype, cfg.recompute, cfg.ln_eps, cfg.checkpoint8)
         h = C.c_void_p()
         self._check(self.lib.slide_ctx_create(C.byref(cc), C.byref(h)), "slide_ctx_create")
         self.ctx = h

@@ -1,6 +1,7 @@
 // libslide: C ABI, parameter layout, arena carving and the launch sequence of one slide step.
 #include "../../include/slide.h"
 #include "../../include/slide_prof.h"
+#include "act8_internal.h"
 #include "slide_internal.h"
 #include "run_internal.h"
 
@@ -65,6 +66,9 @@ struct Layout {
   // encoder
   size_t enc_begin;
   size_t e_patches, e_x, e_qkv, e_O, e_lse, e_xmid, e_m;              // first instance
+  // checkpoint8: the inputs of all blocks but the last in 8 bits, codes and scales (stride s_c8), and x slots that take turns
+  size_t e_c8 = 0, s_c8 = 0, c8_scales = 0;
+  bool c8 = false;
   size_t e_postab;                                                    // [T, D] rows the patch embedding adds (bf16 path)
   size_t e_dl;                                                        // [n][H][T] fp32 work space of the attention backward
   size_t s_x, s_qkv, s_O, s_lse, s_xmid, s_m, s_a;                    // per-layer strides (0 when not saved)
@@ -128,6 +132,9 @@ void add_shadow(slide_ctx* c, size_t poff, int R, int Cc) {
   if (n > c->max_w) c->max_w = n;
 }
 
+// block l's input in the arena (with checkpoint8 the blocks' inputs take turns in two slots)
+char* x_of(const slide_ctx* c, const Layout& y, int l);
+
 // Carve the arena for an encoder call on n tiles (with or without saved activations) and a
 // pool over pool_N rows.  Pure arithmetic; the same inputs always give the same layout.
 // keep: 0 = nothing is saved (feature extraction), 1 = every block's activations, 2 = block inputs only
@@ -169,9 +176,17 @@ Layout make_layout(const slide_ctx* c, long long n, long long pool_N, int keep) 
   int inst = save ? c->L : (c->L > 0 ? 1 : 0);
   y.e_postab = take((size_t)c->T * D * rs);
   y.e_patches = take((size_t)nn * c->T * c->Kp * e);   // one row per token: the CLS slot is a row of zeros
+  y.c8 = keep == KEEP_INPUTS && c->cfg.checkpoint8;
   y.s_x = bwd ? align256(M * D * rs) : 0;
   y.e_x = take(0);
-  cur += (bwd ? (size_t)(c->L + 1) : 1) * align256(M * D * rs);
+  cur += (bwd ? (size_t)(y.c8 && c->L > 1 ? 2 : c->L + 1) : 1) * align256(M * D * rs);
+  if (y.c8) {
+    const size_t ldc = ((size_t)D + A8_GRAIN - 1) / A8_GRAIN * A8_GRAIN, lds = ((size_t)D + A8_BLOCK - 1) / A8_BLOCK;
+    y.c8_scales = align256(M * ldc);
+    y.s_c8 = y.c8_scales + align256(M * lds);
+    y.e_c8 = take(0);
+    cur += (size_t)(c->L > 1 ? c->L - 1 : 0) * y.s_c8;
+  }
   y.s_qkv = save ? align256(M * 3 * D * e) : 0;
   y.e_qkv = take(0); cur += (size_t)inst * align256(M * 3 * D * e);
   y.s_O = save ? align256(M * D * e) : 0;
@@ -483,6 +498,20 @@ void ln_fwd_lane(Run& r, const Layout& y, const void* x, const float* gam, const
 }
 
 // dg: the derivative of the activation is kept for the backward
+char* x_of(const slide_ctx* c, const Layout& y, int l) { return c->arena + y.e_x + (size_t)(y.c8 && c->L > 1 ? l & 1 : l) * y.s_x; }
+
+// checkpoint8: block l's input to 8 bits before its slot is written over, and back before the block runs again
+void checkpoint(Run& r, const Layout& y, int l, long long n, bool back) {
+  slide_ctx* c = r.c;
+  const long long M = n * c->T;
+  uint8_t* const codes = (uint8_t*)c->arena + y.e_c8 + (size_t)l * y.s_c8;
+  const slide_act8 a{codes, (c->D + A8_GRAIN - 1) / A8_GRAIN * A8_GRAIN, codes + y.c8_scales, (c->D + A8_BLOCK - 1) / A8_BLOCK, M, c->D};
+  char* x = x_of(c, y, l);
+  launch(r, K_ELEMWISE, 0, (double)M * c->D * 3, [&] {
+    return back ? launch_act8_unpack(a, x, DT_BF16, c->D, r.s) : launch_act8_pack(x, DT_BF16, c->D, false, a, r.s);
+  });
+}
+
 void block_fwd(Run& r, const Layout& y, int l, long long n, bool replay, bool dg) {
   slide_ctx* c = r.c;
   hipStream_t s = r.s;
@@ -490,8 +519,8 @@ void block_fwd(Run& r, const Layout& y, int l, long long n, bool replay, bool dg
   int D = c->D, T = c->T, F = c->F, dt = c->dt;
   long long M = n * T;
   const LayerOff& o = c->lo[l];
-  char* xin = ar + y.e_x + (size_t)l * y.s_x;
-  char* xout = ar + y.e_x + (size_t)(l + 1) * y.s_x;
+  char* xin = x_of(c, y, l);
+  char* xout = x_of(c, y, l + 1);
   char* xmid = ar + y.e_xmid + (size_t)l * y.s_xmid;
   char* qkv = ar + y.e_qkv + (size_t)l * y.s_qkv;
   char* O = ar + y.e_O + (size_t)l * y.s_O;
@@ -628,8 +657,11 @@ int enc_fwd(slide_ctx* c, const void* pixels, long long n, void* feats_out, bool
     launch(r, K_CLS_LANE, 0, (double)n * D * 4,
            [&] { return launch_lane_init(c->params + c->o_cls, c->params + c->o_pos, lane_xc(c, y, 0), n, D, s); });
   // the derivative of the activation: for the backward only, and of blocks that run again there not yet
-  for (int l = 0; l < c->L; ++l) block_fwd(r, y, l, n, false, save && (!c->cfg.recompute || l == c->L - 1));
-  char* xL = ar + y.e_x + (size_t)c->L * y.s_x;
+  for (int l = 0; l < c->L; ++l) {
+    if (y.c8 && l != c->L - 1) checkpoint(r, y, l, n, false);
+    block_fwd(r, y, l, n, false, save && (!c->cfg.recompute || l == c->L - 1));
+  }
+  char* xL = x_of(c, y, c->L);
   if (c->use_lane)   // the features are the final LayerNorm of the lane's stream (its rounded copy is the CLS row of xL)
     launch(r, K_CLS_LANE, 0, (double)n * D * 8, [&] {
       return launch_lane_ln(lane_xc(c, y, c->L), D, c->params + c->o_lnfg, c->params + c->o_lnfb, (float*)feats_out, D, n, D,
@@ -667,12 +699,12 @@ int enc_bwd(slide_ctx* c, const void* dfeats, long long n, int accumulate, void*
     launch(r, K_ELEMWISE, 0, (double)M * D * rs, [&] { return launch_fill_zero(dxA, (size_t)M * D * rs, s); });
     if (dual) launch(r, K_ELEMWISE, 0, (double)M * D * e, [&] { return launch_fill_zero(dxAt, (size_t)M * D * e, s); });
   }
-  char* xL = ar + y.e_x + (size_t)c->L * y.s_x;
+  char* xL = x_of(c, y, c->L);
   ln_bwd(q, xL, (long long)T * D, dfeats, D, c->o_lnfg, c->o_lnfb, nullptr, dxA, dxAt, (long long)T * D, n,
          accumulate, true);
   for (int l = c->L - 1; l >= 0; --l) {
     const LayerOff& o = c->lo[l];
-    char* xin = ar + y.e_x + (size_t)l * y.s_x;
+    char* xin = x_of(c, y, l);
     char* xmid = ar + y.e_xmid + (size_t)l * y.s_xmid;
     char* qkv = ar + y.e_qkv + (size_t)l * y.s_qkv;
     char* O = ar + y.e_O + (size_t)l * y.s_O;
@@ -683,7 +715,10 @@ int enc_bwd(slide_ctx* c, const void* dfeats, long long n, int accumulate, void*
     int wi = 1 + 4 * l;
     // block inputs only were kept: re-create this block's activations in the shared slots (the
     // last block's are still there from the forward)
-    if (c->cfg.recompute && l != c->L - 1) block_fwd(r, y, l, n, true, true);
+    if (c->cfg.recompute && l != c->L - 1) {
+      if (y.c8) checkpoint(r, y, l, n, true);
+      block_fwd(r, y, l, n, true, true);
+    }
     char* a = ar + y.e_a + (size_t)l * y.s_a;
     if (l == c->L - 1 && prune_last_block(c)) {
       // the gradient of the last block's output is zero away from the CLS rows: its MLP, LN2 and projection
@@ -799,6 +834,7 @@ int enc_bwd(slide_ctx* c, const void* dfeats, long long n, int accumulate, void*
            [&] { return launch_unpatchify(dt, dm, pixel_grad, n, c->cfg.tile, c->cfg.patch, s, T - c->g2); });
   }
   q.flush();
+  if (y.c8) c->enc_saved = false;   // the slots of the blocks' inputs have been written over
   return finish(r);
 }
 
@@ -930,7 +966,7 @@ int slide_ctx_create(const slide_config* cfg, slide_ctx** out) {
   if (cfg->dim > 1024 || cfg->n_classes > 64 || cfg->mil_hidden > 1024) return SLIDE_EUNSUPPORTED;
   if (attn_lds_bytes(T, dh) > 160 * 1024) return SLIDE_EUNSUPPORTED;
   if (cfg->recompute != 0 && cfg->recompute != 1) return SLIDE_EINVAL;
-  if (cfg->reserved != 0) return SLIDE_EINVAL;
+  if (cfg->checkpoint8 != 0 && (cfg->checkpoint8 != 1 || cfg->recompute != 1 || cfg->dtype != DT_BF16)) return SLIDE_EINVAL;
   slide_ctx* c = new (std::nothrow) slide_ctx();
   if (!c) return SLIDE_EINVAL;
   c->cfg = *cfg;
