@@ -201,6 +201,8 @@ def resnet_bench(a):
         N = a.tiles
     ds, ws, ls = gen.RESNET_SEEDS[a.workload]
     dev = torch.device("cuda:0")
+    from dataclasses import replace
+    cfg = replace(cfg, norm_groups=a.norm_groups, checkpoint8=a.checkpoint8)
     lib = ResNetLib(resnet_config_from(cfg))
     prm = gen.make_resnet_params(cfg, ws)
     flat = np.zeros(lib.resnet_param_count(), dtype=np.float32)
@@ -281,12 +283,13 @@ def resnet_bench(a):
         "ms_per_step": round(dt / a.steps * 1e3, 3), "higher_is_better": True, "scaling": "weak", "vs_baseline": None,
         "dtype": "bf16", "data": "synthetic",
         "config": {"workload": f"{a.workload}: {N} tiles {cfg.tile}x{cfg.tile}x3, ResNet {cfg.block} blocks {list(cfg.depths)} "
-                               f"width {cfg.width}, batch statistics over all tiles, gated-attention MIL hidden "
+                               f"width {cfg.width}, " + (f"group normalisation, {cfg.norm_groups} groups" if cfg.norm_groups else
+                                                         "batch statistics over all tiles") + ", gated-attention MIL hidden "
                                f"{cfg.mil_hidden}, {cfg.n_classes} classes",
                    "tiles": N, "slide_steps_per_s": round(a.steps / dt, 4),
                    "model_gflop_per_tile": round(mflops / 1e9, 3),
                    "mfu_bf16_peak": round(tiles_per_s * mflops / PEAK["mfma_bf16"], 4),
-                   "activation_policy": "all activations kept",
+                   "activation_policy": "all activations kept" + (", convolution outputs in 8 bits" if cfg.checkpoint8 else ""),
                    "arena_gb": round(nbytes / 1e9, 2), "peak_alloc_gb_of_288": round(peak_alloc, 2),
                    "loss": float(loss.item()), "input_gen_s": round(gen_s, 1)},
         "roofline": roof, "roofline_all": roof_all,
@@ -344,6 +347,9 @@ def main():
     ap.add_argument("--prof-kernel", default="gemm_nt")
     ap.add_argument("--recompute", type=int, default=-1,
                     help="1 = keep block inputs only and re-run blocks in the backward (default: only for 'full')")
+    ap.add_argument("--checkpoint8", type=int, default=0,
+                    help="keep for the backward in 8 bits: the blocks' inputs (with --recompute 1), the convolutions' outputs (with --norm-groups)")
+    ap.add_argument("--norm-groups", type=int, default=0, help="ResNet: group normalisation with this many groups")
     ap.add_argument("--calib-copy", type=int, default=0, help="run the plain copy kernel over this many bytes and exit")
     ap.add_argument("--adamw", action="store_true", help="time the AdamW update of the workload's parameters instead")
     ap.add_argument("--pool-sweep", action="store_true", help="bandwidth sweep of the pool kernels instead of the step")
@@ -381,7 +387,9 @@ def main():
     dev = torch.device("cuda:0")
     dtype = 1  # bf16 storage / fp32 accumulate
     recompute = a.recompute if a.recompute >= 0 else int(a.workload == "full")
-    lib = SlideLib(lib_config(cfg, dtype, recompute))
+    lc = lib_config(cfg, dtype, recompute)
+    lc.checkpoint8 = a.checkpoint8
+    lib = SlideLib(lc)
     layout = lib.param_layout()
     prm = gen.make_params(cfg, ws)
     flat = np.zeros(lib.slide_param_count(), dtype=np.float32)
@@ -480,7 +488,7 @@ def main():
                    "tiles": N, "slide_steps_per_s": round(a.steps / dt, 4),
                    "model_gflop_per_tile": round(mflops / 1e9, 3), "mfu_bf16_peak": round(mfu, 4),
                    "last_block": "CLS row only after attention (exact; its FLOPs are not counted)",
-                   "activation_policy": ("block inputs + re-run blocks in backward" if recompute else "all block activations kept") +
+                   "activation_policy": ("block inputs" + (" in 8 bits" if a.checkpoint8 else "") + " + re-run blocks in backward" if recompute else "all block activations kept") +
                                         (f"; encoder in chunks of {a.chunk_tiles} tiles (one extra forward)" if a.chunk_tiles else ""),
                    "arena_gb": round(nbytes / 1e9, 2), "peak_alloc_gb_of_288": round(peak_alloc, 2),
                    "loss": float(loss.item()), "input_gen_s": round(gen_s, 1)},

@@ -21,6 +21,8 @@ class ResNetConfig:
     mil_hidden: int      # M_h of the gated-attention aggregator
     n_classes: int       # C: 1 -> one logit + BCE, >1 -> softmax cross-entropy
     bn_eps: float = 1e-5
+    norm_groups: int = 0  # 0 batch normalisation, else the groups of a group normalisation
+    checkpoint8: int = 0  # with group normalisation: its backward reads the convolutions' outputs in 8 bits
 
     @property
     def expansion(self) -> int:

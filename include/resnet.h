@@ -11,7 +11,8 @@
  * the tile's feature row.  Convolutions carry no bias.  Batch normalisation uses the statistics of the batch it sees:
  * over every tile and position of the call (Results, gradient equivalence: the normalisation layers were
  * synchronised, i.e. the statistics are those of all tiles of the slide).  Because of that the tiles of a call are
- * coupled: there is no chunked variant of this step, and one call must hold the whole slide.
+ * coupled: there is no chunked variant of this step, and one call must hold the whole slide.  With group normalisation
+ * (resnet_config.norm_groups) they are not.
  *
  * Conventions as in slide.h: device pointers unless a comment says "host"; `hip_stream` is a hipStream_t passed as
  * void*; every call only enqueues work and returns; the library never allocates device memory (the caller owns the
@@ -38,7 +39,16 @@ typedef struct resnet_config {
   int32_t mil_hidden;   /* M_h of the gated-attention aggregator */
   int32_t n_classes;    /* C: 1 = one logit with binary cross-entropy; >1 = softmax cross-entropy */
   float   bn_eps;       /* batch-normalisation epsilon (1e-5) */
-  int32_t reserved;     /* must be 0 */
+  /* The normalisation (both 0: batch normalisation; the two stand where one 32-bit field that had to be 0 stood).
+   * norm_groups > 0: group normalisation with that many groups (a divisor of width) after every convolution, with the same
+   * parameters and bn_eps: the statistics are those of a tile's group (slide_group_norm of act8.h), so the tiles of a call do not
+   * depend on each other and resnet_encoder_fwd_tiles / _bwd_tiles (accumulate) may take a slide in parts.
+   * checkpoint8 != 0 (with norm_groups > 0): the convolutions' outputs are kept in 8 bits (act8.h) for the backward, which
+   * normalises them again: half their bytes in the arena.  The forward's results stay the same.  In the backward the values are off
+   * by 2^-4 of themselves at most, and where that turns a ReLU's decision a gradient passes or not: gradients of networks with
+   * random weights came out 0.15 to 0.3 (relative L2, the worst tensor) off those without checkpoints. */
+  int16_t norm_groups;
+  int16_t checkpoint8;
 } resnet_config;
 
 typedef struct resnet_ctx resnet_ctx;
@@ -96,8 +106,10 @@ const void* resnet_feature_grads(const resnet_ctx* ctx);
 /* The activations the last encoder forward left in the arena, for inspection (the tests replay the backward on them).
  * They are bfloat16, channels-last: tensor `index` is [n_tiles][side][side][channels].  Order: stem convolution
  * output, stem ReLU output, max-pooling output, then per residual block: per convolution its output and (except the
- * last) the ReLU output behind its normalisation, the projection's output where the block has one, the block output.
- * resnet_saved_activations: how many there are.  SLIDE_ESTATE without a saved forward. */
+ * last) the ReLU output behind its normalisation, the projection's output where the block has one (with group
+ * normalisation also what its normalisation makes of it), the block output.
+ * resnet_saved_activations: how many there are.  SLIDE_ESTATE without a saved forward, SLIDE_EUNSUPPORTED for the
+ * convolutions' outputs with checkpoint8, which does not keep them. */
 int  resnet_saved_activations(const resnet_ctx* ctx);
 int  resnet_saved_activation(const resnet_ctx* ctx, int index, const void** ptr, int32_t* side, int32_t* channels);
 

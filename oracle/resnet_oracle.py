@@ -25,6 +25,11 @@ the call and all positions (Results, gradient equivalence: the normalisation lay
 synchronised across devices so that the statistics are those of the whole slide; on one device
 that is the plain batch statistic over every tile of the slide).
 
+Group normalisation (cfg.norm_groups > 0) stands in the same places, with the statistics of a tile's group of channels
+instead of the batch's.  With cfg.checkpoint8 its backward sees the convolution's output as its 8-bit
+checkpoint holds it (act8_oracle.pack), under the forward's statistics; ReLU decisions in front of
+which such a normalisation stands are taken there too.
+
 Storage precision.  The paper trains these encoders with 16-bit mixed precision (Method, the
 tiles-per-device figures with automatic mixed precision), and a ReLU or a max pooling turns a
 floating-point value into a decision (which inputs pass a gradient).  For a comparison with a path
@@ -45,6 +50,7 @@ from __future__ import annotations
 
 import numpy as np
 
+from . import act8_oracle as a8
 from .slide_oracle import pool_fwd, pool_bwd
 
 
@@ -103,6 +109,38 @@ def bn_bwd(dy, g, cache):
     return dx, (dy * xh).sum(axis=(0, 2, 3)), dy.sum(axis=(0, 2, 3))
 
 
+def _group_mean(x, groups):
+    n, C, H, W = x.shape
+    m = x.reshape(n, groups, -1).mean(axis=2)
+    return np.repeat(m, C // groups, axis=1)[:, :, None, None]
+
+
+def gn_fwd(x, g, b, eps, groups, kept=None):
+    """Group normalisation (biased variance over a tile's group of channels and all positions).  kept: what the backward
+    sees in x's place.  Also returned: the output that the kept values give."""
+    mu = _group_mean(x, groups)
+    rstd = 1.0 / np.sqrt(_group_mean((x - mu) ** 2, groups) + eps)
+    gg, bb = g[None, :, None, None], b[None, :, None, None]
+    y = (x - mu) * rstd * gg + bb
+    xh = (x if kept is None else kept) - mu
+    xh = xh * rstd
+    return y, (xh, rstd, groups), y if kept is None else xh * gg + bb
+
+
+def gn_bwd(dy, g, cache):
+    xh, rstd, groups = cache
+    dxh = dy * g[None, :, None, None]
+    dx = rstd * (dxh - _group_mean(dxh, groups) - xh * _group_mean(dxh * xh, groups))
+    return dx, (dy * xh).sum(axis=(0, 2, 3)), dy.sum(axis=(0, 2, 3))
+
+
+def checkpoint_values(x):
+    """What the 8-bit checkpoint of an activation holds: channels-last rows in blocks of 128 channels."""
+    n, C, H, W = x.shape
+    codes, scales = a8.pack(x.transpose(0, 2, 3, 1).reshape(-1, C))
+    return a8.unpack(codes, scales, C).reshape(n, H, W, C).transpose(0, 3, 1, 2)
+
+
 def maxpool_fwd(x):
     """3x3 window, stride 2, padding 1 (padding never wins).  Of equal maxima the first in
     (kh, kw) scan order takes the gradient."""
@@ -148,51 +186,64 @@ def _identity(a):
     return a
 
 
-def _conv_bn(P, x, conv, bn, stride, pad, eps, store):
+def _conv_bn(P, x, conv, bn, stride, pad, cfg, store):
+    """Output behind the normalisation, the cache, and the output on which the backward takes a ReLU's decisions
+    (None: the stored activation)."""
     c = store(conv2d_fwd(x, P[conv + ".W"], stride, pad))
-    y, bc = bn_fwd(c, P[bn + ".g"], P[bn + ".b"], eps)
-    return y, (x, conv, bn, stride, pad, bc)
+    groups = getattr(cfg, "norm_groups", 0)
+    if not groups:
+        y, bc = bn_fwd(c, P[bn + ".g"], P[bn + ".b"], cfg.bn_eps)
+        return y, (x, conv, bn, stride, pad, bc), None
+    kept = checkpoint_values(c) if cfg.checkpoint8 else None
+    y, bc, u = gn_fwd(c, P[bn + ".g"], P[bn + ".b"], cfg.bn_eps, groups, kept)
+    return y, (x, conv, bn, stride, pad, bc), u if cfg.checkpoint8 else None
 
 
 def _conv_bn_bwd(P, g, dy, cache):
     x, conv, bn, stride, pad, bc = cache
-    dc, g[bn + ".g"], g[bn + ".b"] = bn_bwd(dy, P[bn + ".g"], bc)
+    dc, g[bn + ".g"], g[bn + ".b"] = (bn_bwd if len(bc) == 2 else gn_bwd)(dy, P[bn + ".g"], bc)
     dx, g[conv + ".W"] = conv2d_bwd(dc, x, P[conv + ".W"], stride, pad)
     return dx
+
+
+def _relu(y, u, store):
+    """The stored activation and where its backward lets a gradient pass."""
+    r = store(np.maximum(y, 0.0))
+    return r, (r if u is None else u) > 0.0
 
 
 def encoder_fwd(prm, X, cfg, dtype=np.float64, store=_identity):
     """Tile features H [n, dim] and the cache for encoder_bwd.  X: [n,3,S,S] normalised pixels."""
     P = {k: np.asarray(v, dtype=dtype) for k, v in prm.items() if not k.startswith(("mil.", "head."))}
-    eps = cfg.bn_eps
     x = np.asarray(X, dtype=dtype)
-    y, c0 = _conv_bn(P, x, "stem.conv", "stem.bn", 2, 3, eps, store)
-    r0 = store(np.maximum(y, 0.0))
+    y, c0, u = _conv_bn(P, x, "stem.conv", "stem.bn", 2, 3, cfg, store)
+    r0, on0 = _relu(y, u, store)
     x, mp = maxpool_fwd(r0)
     caches = []
     for name, stride, down in _blocks(cfg):
         p = name + "."
         x0 = x
         if cfg.block == "basic":
-            y1, k1 = _conv_bn(P, x0, p + "conv1", p + "bn1", stride, 1, eps, store)
-            r1 = store(np.maximum(y1, 0.0))
-            y2, k2 = _conv_bn(P, r1, p + "conv2", p + "bn2", 1, 1, eps, store)
-            body, ks, rs = y2, [k1, k2], [r1]
+            convs = [("conv1", "bn1", stride, 1), ("conv2", "bn2", 1, 1)]
         else:
-            y1, k1 = _conv_bn(P, x0, p + "conv1", p + "bn1", 1, 0, eps, store)
-            r1 = store(np.maximum(y1, 0.0))
-            y2, k2 = _conv_bn(P, r1, p + "conv2", p + "bn2", stride, 1, eps, store)
-            r2 = store(np.maximum(y2, 0.0))
-            y3, k3 = _conv_bn(P, r2, p + "conv3", p + "bn3", 1, 0, eps, store)
-            body, ks, rs = y3, [k1, k2, k3], [r1, r2]
+            convs = [("conv1", "bn1", 1, 0), ("conv2", "bn2", stride, 1), ("conv3", "bn3", 1, 0)]
+        ks, on, r = [], [], x0
+        for i, (cv, bn, st, pad) in enumerate(convs):
+            body, k, u = _conv_bn(P, r, p + cv, p + bn, st, pad, cfg, store)
+            ks.append(k)
+            if i + 1 < len(convs):
+                r, m = _relu(body, u, store)
+                on.append(m)
         if down:
-            sc, kd = _conv_bn(P, x0, p + "down.conv", p + "down.bn", stride, 0, eps, store)
+            sc, kd, _ = _conv_bn(P, x0, p + "down.conv", p + "down.bn", stride, 0, cfg, store)
+            if getattr(cfg, "norm_groups", 0):
+                sc = store(sc)     # written on its own there
         else:
             sc, kd = x0, None
-        x = store(np.maximum(body + sc, 0.0))
-        caches.append((ks, rs, kd, x))
+        x, m = _relu(body + sc, None if u is None else u + sc, store)
+        caches.append((ks, on, kd, m))
     H = x.mean(axis=(2, 3))
-    return H, {"P": P, "stem": (c0, r0, mp), "blocks": caches, "last_shape": x.shape}
+    return H, {"P": P, "stem": (c0, on0, mp), "blocks": caches, "last_shape": x.shape}
 
 
 def encoder_bwd(cache, G):
@@ -202,15 +253,15 @@ def encoder_bwd(cache, G):
     g = {}
     n, C, Hh, Ww = cache["last_shape"]
     dx = np.broadcast_to(np.asarray(G, dtype=np.float64)[:, :, None, None] / (Hh * Ww), (n, C, Hh, Ww)).copy()
-    for ks, rs, kd, out in reversed(cache["blocks"]):
-        dz = np.where(out > 0.0, dx, 0.0)                 # ReLU behind the sum
+    for ks, on, kd, out in reversed(cache["blocks"]):
+        dz = np.where(out, dx, 0.0)                       # ReLU behind the sum
         d = _conv_bn_bwd(P, g, dz, ks[-1])
-        for k, r in zip(reversed(ks[:-1]), reversed(rs)):
-            d = _conv_bn_bwd(P, g, np.where(r > 0.0, d, 0.0), k)
+        for k, m in zip(reversed(ks[:-1]), reversed(on)):
+            d = _conv_bn_bwd(P, g, np.where(m, d, 0.0), k)
         dx = d + (_conv_bn_bwd(P, g, dz, kd) if kd is not None else dz)
-    c0, r0, mp = cache["stem"]
+    c0, on0, mp = cache["stem"]
     d = maxpool_bwd(dx, mp)
-    _conv_bn_bwd(P, g, np.where(r0 > 0.0, d, 0.0), c0)
+    _conv_bn_bwd(P, g, np.where(on0, d, 0.0), c0)
     return g
 
 

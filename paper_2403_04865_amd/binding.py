@@ -90,7 +90,8 @@ _SYMS = {
 
 class _CResNetConfig(C.Structure):
     _fields_ = [("tile", C.c_int32), ("block", C.c_int32), ("depths", C.c_int32 * 4), ("width", C.c_int32),
-                ("mil_hidden", C.c_int32), ("n_classes", C.c_int32), ("bn_eps", C.c_float), ("reserved", C.c_int32)]
+                ("mil_hidden", C.c_int32), ("n_classes", C.c_int32), ("bn_eps", C.c_float), ("norm_groups", C.c_int16),
+                ("checkpoint8", C.c_int16)]
 
 
 @dataclass
@@ -102,13 +103,15 @@ class ResNetConfig:
     mil_hidden: int
     n_classes: int
     bn_eps: float = 1e-5
+    norm_groups: int = 0    # 0 batch normalisation, else groups of a group normalisation
+    checkpoint8: int = 0    # with group normalisation: convolution outputs kept in 8 bits for the backward
 
 
 def resnet_config_from(shape) -> ResNetConfig:
     """ResNetConfig from any object with the fields tile, block ("basic" / "bottleneck"), depths, width, mil_hidden,
-    n_classes and bn_eps (such as a workload description of the input generators)."""
+    n_classes and bn_eps (such as a workload description of the input generators), and norm_groups and checkpoint8 where it has them."""
     return ResNetConfig(shape.tile, 0 if shape.block == "basic" else 1, tuple(shape.depths), shape.width,
-                        shape.mil_hidden, shape.n_classes, shape.bn_eps)
+                        shape.mil_hidden, shape.n_classes, shape.bn_eps, getattr(shape, "norm_groups", 0), getattr(shape, "checkpoint8", 0))
 
 
 _P4 = [C.POINTER(C.c_double), C.POINTER(C.c_int), C.POINTER(C.c_double), C.POINTER(C.c_double)]
@@ -332,7 +335,7 @@ class ResNetLib:
         self.lib = load_cdll()
         self.cfg = cfg
         cc = _CResNetConfig(cfg.tile, cfg.block, (C.c_int32 * 4)(*cfg.depths), cfg.width, cfg.mil_hidden, cfg.n_classes,
-                            cfg.bn_eps, 0)
+                            cfg.bn_eps, cfg.norm_groups, cfg.checkpoint8)
         h = C.c_void_p()
         self._check(self.lib.resnet_ctx_create(C.byref(cc), C.byref(h)), "resnet_ctx_create")
         self.ctx = h

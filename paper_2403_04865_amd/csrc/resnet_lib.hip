@@ -1,6 +1,7 @@
 // libslide, convolutional tile encoders: C ABI of resnet.h, parameter layout, arena carving and the launch sequence of
 // one slide step with a ResNet encoder.  The aggregator is the one of slide.h, run through an aggregator-only context.
 #include "../../include/resnet.h"
+#include "act8_internal.h"
 #include "run_internal.h"
 #include "resnet_internal.h"
 
@@ -22,7 +23,8 @@ struct Tensor { std::string name; size_t off, len; };
 
 // an activation tensor [n * H * H][C] (bf16): per-tile element count and, once laid out, its arena offset
 // bits: one bit per element, set where the stored value is positive (kept for ReLU outputs: the mask of the backward)
-struct Act { int H, C; bool relu; size_t off = 0, bits = 0; };
+// conv: a convolution's output; with 8-bit checkpoints all of them share one buffer and are kept as codes and scales
+struct Act { int H, C; bool relu, conv = false; size_t off = 0, bits = 0, codes = 0, scales = 0; };
 
 // one convolution with its batch normalisation
 struct ConvL {
@@ -30,6 +32,7 @@ struct ConvL {
   int inH, outH;
   size_t oW, og, ob;               // parameter offsets
   int t_src, t_conv;               // activation ids: source rows, convolution output
+  int t_norm;                      // projection of a shortcut with group normalisation: its normalised output; else -1
   // what the kernels see: the stem is a 1x1 convolution with 256 columns read from the padded pixel image
   int kCs, kK, kstride, kpad, kinH;
   int ldk() const { return kK * kK * kCs; }
@@ -49,7 +52,7 @@ struct BlockL {
 
 struct RLayout {
   size_t total = 0;
-  size_t pool, pool_bytes, H, G, bnpart, tpart, coef, wpart, wpart_bytes, img, parg, gA, gB, gC;
+  size_t pool, pool_bytes, H, G, bnpart, tpart, coef, norm_work, norm_work_bytes, wpart, wpart_bytes, img, parg, gA, gB, gC;
 };
 
 }  // namespace
@@ -107,6 +110,8 @@ int add_conv(resnet_ctx* c, const std::string& conv, const std::string& bn, int 
   L.ob = add_tensor(c, bn + ".b", Cout);
   L.t_src = t_src;
   L.t_conv = add_act(c, L.outH, Cout, false);
+  c->acts[L.t_conv].conv = true;
+  L.t_norm = -1;
   L.kCs = Cin; L.kK = K; L.kstride = stride; L.kpad = pad; L.kinH = inH;
   L.need_wt = need_wt;
   if (Cout > c->Cmax) c->Cmax = Cout;
@@ -114,8 +119,13 @@ int add_conv(resnet_ctx* c, const std::string& conv, const std::string& bn, int 
   return (int)c->convs.size() - 1;
 }
 
+slide_group_norm norm_shape(const resnet_ctx* c, const ConvL& L, long long n, int act) {
+  return slide_group_norm{n, (int64_t)L.outH * L.outH, L.Cout, c->cfg.norm_groups, DT_BF16, act, c->cfg.bn_eps, 0};
+}
+
 // Arena for n tiles: aggregator work space, H, G, weight copies and statistics, reduction work space, every activation,
-// three gradient buffers of the largest activation.  Pure arithmetic; also fills the offsets kept in the context.
+// three gradient buffers of the largest activation.  Group normalisation keeps mean and rstd per tile and group in the place of
+// the batch's statistics and needs no ReLU bits (its backward takes them from the sum it forms).  Pure arithmetic; also fills the offsets kept in the context.
 RLayout make_layout(resnet_ctx* c, long long n, bool commit) {
   RLayout y;
   size_t cur = 0;
@@ -128,7 +138,7 @@ RLayout make_layout(resnet_ctx* c, long long n, bool commit) {
   size_t wmax = 0;
   for (ConvL& L : c->convs) {
     size_t wb = (size_t)L.Cout * L.ldk() * 2;
-    size_t w = take(wb), wt = L.need_wt ? take(wb) : 0, st = take((size_t)4 * L.Cout * 4);
+    size_t w = take(wb), wt = L.need_wt ? take(wb) : 0, st = take(c->cfg.norm_groups ? nn * c->cfg.norm_groups * 8 : (size_t)4 * L.Cout * 4);
     const bool frag = L.kK == 3 && L.kstride == 1 && L.need_wt;
     size_t wf = frag ? take(wb) : 0, wtf = frag ? take(wb) : 0;
     if (commit) { L.w = w; L.wt = wt; L.stats = st; L.wf = wf; L.wtf = wtf; }
@@ -136,11 +146,18 @@ RLayout make_layout(resnet_ctx* c, long long n, bool commit) {
     if (wb * 2 > wmax) wmax = wb * 2;   // one slab in fp32
   }
   y.bnpart = take((size_t)4096 * 2 * c->Cmax * 4);
+  y.norm_work_bytes = 0;
+  for (const ConvL& L : c->convs)
+    if (c->cfg.norm_groups && nn) {
+      const size_t b = group_norm_bytes(norm_shape(c, L, (long long)nn, SLIDE_ACT_NONE));
+      if (b > y.norm_work_bytes) y.norm_work_bytes = b;
+    }
+  y.norm_work = take(y.norm_work_bytes);
   // per-tile channel sums of a convolution's output: 8 bytes per channel and row tile of at least 128 rows
   size_t tp = 0;
   for (const ConvL& L : c->convs) {
     const size_t rows = nn * L.outH * L.outH, tiles = (rows + 127) / 128;
-    if (tiles * L.Cout * 8 > tp) tp = tiles * L.Cout * 8;
+    if (!c->cfg.norm_groups && tiles * L.Cout * 8 > tp) tp = tiles * L.Cout * 8;
   }
   y.tpart = take(tp);
   y.coef = take((size_t)2 * c->Cmax * 4);
@@ -148,13 +165,17 @@ RLayout make_layout(resnet_ctx* c, long long n, bool commit) {
   y.wpart_bytes = (size_t)512 << 20;
   if (y.wpart_bytes < 16 * wmax) y.wpart_bytes = 16 * wmax;
   y.wpart = take(y.wpart_bytes);
+  y.gA = take(nn * c->max_act * 2);
+  const size_t conv_out = y.gA;   // with 8-bit checkpoints: the forward's outputs in turn, where the backward's gradients go later
   for (Act& a : c->acts) {
-    size_t o = take(nn * a.H * a.H * a.C * 2), b = a.relu ? take(nn * a.H * a.H * a.C / 8) : 0;
-    if (commit) { a.off = o; a.bits = b; }
+    const size_t rows = nn * a.H * a.H;
+    const bool c8 = a.conv && c->cfg.checkpoint8;
+    size_t o = c8 ? conv_out : take(rows * a.C * 2), b = a.relu && !c->cfg.norm_groups ? take(rows * a.C / 8) : 0;
+    size_t q = c8 ? take(rows * a.C) : 0, qs = c8 ? take(rows * ((a.C + 127) / 128)) : 0;
+    if (commit) { a.off = o; a.bits = b; a.codes = q; a.scales = qs; }
   }
   y.img = take(nn * (c->S + 6) * (c->S + 8) * 4 * 2);   // padded pixel image of the stem
   y.parg = take(nn * (c->S / 4) * (c->S / 4) * c->cfg.width);   // winning taps of the max pooling, one byte each
-  y.gA = take(nn * c->max_act * 2);
   y.gB = take(nn * c->max_act * 2);
   y.gC = take(nn * c->max_act * 2);
   y.total = cur;
@@ -204,7 +225,7 @@ void cast_weights(Run& r) {
   flush();
 }
 
-// convolution forward + batch statistics of its output
+// convolution forward + batch statistics of its output (group normalisation takes its own)
 void conv_fwd(Run& r, int id, long long n) {
   resnet_ctx* c = r.c;
   const ConvL& L = c->convs[id];
@@ -212,10 +233,11 @@ void conv_fwd(Run& r, int id, long long n) {
   p.src = conv_src(c, L); p.Cs = L.kCs; p.W = (const bf16*)(c->arena + L.w);
   p.Wf = L.wf ? (const bf16*)(c->arena + L.wf) : nullptr;
   p.out = act(c, L.t_conv); p.N = L.Cout; p.M = rows_of(c, L.t_conv, n); p.g = geom_fwd(L); p.add = 0;
-  p.stat_part = (float*)(c->arena + c->lay.tpart);
+  p.stat_part = c->cfg.norm_groups ? nullptr : (float*)(c->arena + c->lay.tpart);
   const double K = (double)L.Cin * L.K * L.K;
   launch(r, RK_CONV_FWD, 2.0 * p.M * L.Cout * K, conv_bytes(c, L, p.M, n),
          [&] { return launch_conv_nt(p, r.s); });
+  if (c->cfg.norm_groups) return;
   // the statistics come from the per-tile sums the convolution's epilogue left
   const int tiles = conv_nt_row_tiles(p);
   launch(r, RK_BN_STATS, 0, (double)tiles * L.Cout * 8, [&] {
@@ -244,6 +266,49 @@ void bn_bwd(Run& r, int id, long long n, const bf16* dy, const unsigned char* ma
     return launch_bn_bwd(dy, mask, act(c, L.t_conv), M, L.Cout, stats_of(c, id), (float*)(c->arena + c->lay.bnpart),
                          (float*)(c->arena + c->lay.coef), c->grads + L.og, c->grads + L.ob, accumulate, dx, r.s);
   });
+}
+
+slide_act8 act8_of(const resnet_ctx* c, int id, long long n) {
+  const Act& a = c->acts[id];
+  return slide_act8{(uint8_t*)(c->arena + a.codes), a.C, (uint8_t*)(c->arena + a.scales), (a.C + 127) / 128, rows_of(c, id, n), a.C};
+}
+
+GroupNorm norm_call(const resnet_ctx* c, const ConvL& L, long long n, int resid, int act_) {
+  GroupNorm g{};
+  g.s = norm_shape(c, L, n, act_);
+  g.gamma = c->params + L.og; g.beta = c->params + L.ob;
+  g.resid = resid >= 0 ? act(c, resid) : nullptr; g.ldr = L.Cout;
+  g.mean = (float*)(c->arena + L.stats); g.rstd = g.mean + n * c->cfg.norm_groups;
+  g.work = (float*)(c->arena + c->lay.norm_work);
+  return g;
+}
+
+// group normalisation of a convolution's output, + activation `resid` (-1: none), ReLU unless it is a shortcut's; the output goes
+// to its 8-bit checkpoint in the same pass where there is one
+void gn_fwd(Run& r, int id, long long n, int resid, int act_, int t_out) {
+  resnet_ctx* c = r.c;
+  const ConvL& L = c->convs[id];
+  GroupNorm g = norm_call(c, L, n, resid, act_);
+  const slide_act8 x8 = act8_of(c, L.t_conv, n);
+  g.x = act(c, L.t_conv); g.ldx = L.Cout; g.y = act(c, t_out); g.ldy = L.Cout;
+  g.x8 = c->cfg.checkpoint8 ? &x8 : nullptr;
+  launch(r, RK_BN_APPLY, 0, (double)rows_of(c, L.t_conv, n) * L.Cout * (2 * (resid >= 0 ? 3 : 2) + (g.x8 ? 1 : 0)),
+         [&] { return launch_group_norm_fwd(g, r.s); });
+}
+
+// dx (rows of the convolution's output) from dy through ReLU and group normalisation; dresid (may be null): the gradient behind the
+// ReLU, which is the residual's
+void gn_bwd(Run& r, int id, long long n, const bf16* dy, int resid, int act_, bf16* dx, bf16* dresid, int accumulate) {
+  resnet_ctx* c = r.c;
+  const ConvL& L = c->convs[id];
+  GroupNorm g = norm_call(c, L, n, resid, act_);
+  const slide_act8 x8 = act8_of(c, L.t_conv, n);
+  if (c->cfg.checkpoint8) g.x8 = &x8;
+  else { g.x = act(c, L.t_conv); g.ldx = L.Cout; }
+  g.dy = dy; g.lddy = L.Cout; g.y = dx; g.ldy = L.Cout; g.dresid = dresid; g.lddr = L.Cout;
+  g.dgamma = c->grads + L.og; g.dbeta = c->grads + L.ob; g.accumulate = accumulate != 0;
+  launch(r, RK_BN_BWD, 0, (double)rows_of(c, L.t_conv, n) * L.Cout * ((g.x ? 6 : 5) + (resid >= 0 ? 2 : 0) + (dresid ? 2 : 0)),
+         [&] { return launch_group_norm_bwd(g, r.s); });
 }
 
 // Weight gradients whose slab partials wait for their sum: they lie one behind the other in the room for them, and the sums of up to 32 MB
@@ -328,6 +393,9 @@ int check_bound(const resnet_ctx* c) {
   return SLIDE_OK;
 }
 
+// group normalisation: the activation that a block adds
+int shortcut(const resnet_ctx* c, const BlockL& b) { return b.down >= 0 ? c->convs[b.down].t_norm : b.t_in; }
+
 int enc_fwd(resnet_ctx* c, const void* pixels, long long n, void* feats_out, hipStream_t s) {
   c->enc_saved = false; c->step_saved = false;
   if (n >= (1LL << 31) / ((long long)(c->S / 2) * (c->S / 2))) return SLIDE_EUNSUPPORTED;   // 32-bit row indices
@@ -339,7 +407,9 @@ int enc_fwd(resnet_ctx* c, const void* pixels, long long n, void* feats_out, hip
   launch(r, RK_ELEMWISE, 0, (double)n * (3 * c->S * c->S + 4.0 * (c->S + 6) * (c->S + 8)) * 2,
          [&] { return launch_stem_pad_pixels((const bf16*)pixels, (bf16*)(c->arena + c->lay.img), n, c->S, s); });
   conv_fwd(r, 0, n);
-  bn_apply(r, 0, n, nullptr, nullptr, c->t_r0);
+  const bool gn = c->cfg.norm_groups != 0;
+  if (gn) gn_fwd(r, 0, n, -1, SLIDE_ACT_RELU, c->t_r0);
+  else bn_apply(r, 0, n, nullptr, nullptr, c->t_r0);
   {
     const Act& a = c->acts[c->t_r0];
     launch(r, RK_POOLING, 0, (double)rows_of(c, c->t_r0, n) * a.C * 2 * 1.375,
@@ -349,6 +419,18 @@ int enc_fwd(resnet_ctx* c, const void* pixels, long long n, void* feats_out, hip
            });
   }
   for (const BlockL& b : c->blocks) {
+    if (gn) {   // the shortcut's projection first: its output may share the buffer of the other convolutions'
+      if (b.down >= 0) {
+        conv_fwd(r, b.down, n);
+        gn_fwd(r, b.down, n, -1, SLIDE_ACT_NONE, c->convs[b.down].t_norm);
+      }
+      for (int k = 0; k < b.nconv; ++k) {
+        const bool last = k + 1 == b.nconv;
+        conv_fwd(r, b.conv[k], n);
+        gn_fwd(r, b.conv[k], n, last ? shortcut(c, b) : -1, SLIDE_ACT_RELU, last ? b.t_out : b.t_r[k]);
+      }
+      continue;
+    }
     for (int k = 0; k < b.nconv; ++k) {
       conv_fwd(r, b.conv[k], n);
       if (k + 1 < b.nconv) bn_apply(r, b.conv[k], n, nullptr, nullptr, b.t_r[k]);
@@ -368,6 +450,7 @@ int enc_fwd(resnet_ctx* c, const void* pixels, long long n, void* feats_out, hip
 
 int enc_bwd(resnet_ctx* c, const void* dfeats, long long n, int accumulate, hipStream_t s) {
   if (!c->enc_saved || c->enc_n != n) return SLIDE_ESTATE;
+  const bool gn = c->cfg.norm_groups != 0;
   Run r{c, s};
   WgradSums sums{r};
   bf16* gA = (bf16*)(c->arena + c->lay.gA);
@@ -381,6 +464,24 @@ int enc_bwd(resnet_ctx* c, const void* dfeats, long long n, int accumulate, hipS
   }
   for (int bi = (int)c->blocks.size() - 1; bi >= 0; --bi) {
     const BlockL& b = c->blocks[bi];
+    if (gn) {
+      // gA: gradient at the block's output, in its place then the gradient of the sum (behind the ReLU); an identity shortcut ends
+      // there: the residual branch is added to it
+      gn_bwd(r, b.conv[b.nconv - 1], n, gA, shortcut(c, b), SLIDE_ACT_RELU, gB, gA, accumulate);
+      for (int k = b.nconv - 1; k >= 0; --k) {
+        conv_wgrad(sums, b.conv[k], n, gB, accumulate);
+        if (k == 0 && b.down < 0) conv_dgrad(r, b.conv[k], n, gB, gA, 1);
+        else conv_dgrad(r, b.conv[k], n, gB, gC, 0);
+        if (k > 0) gn_bwd(r, b.conv[k - 1], n, gC, -1, SLIDE_ACT_RELU, gB, nullptr, accumulate);
+      }
+      if (b.down >= 0) {
+        gn_bwd(r, b.down, n, gA, -1, SLIDE_ACT_NONE, gB, nullptr, accumulate);
+        conv_wgrad(sums, b.down, n, gB, accumulate);
+        conv_dgrad(r, b.down, n, gB, gC, 1);
+        bf16* t = gA; gA = gC; gC = t;
+      }
+      continue;
+    }
     const unsigned char* out = act_bits(c, b.t_out);   // where the block's output is positive
     // gA: gradient at the block's output (behind the ReLU)
     bn_bwd(r, b.conv[b.nconv - 1], n, gA, out, gB, accumulate);
@@ -406,7 +507,8 @@ int enc_bwd(resnet_ctx* c, const void* dfeats, long long n, int accumulate, hipS
     launch(r, RK_POOLING, 0, (double)rows_of(c, c->t_r0, n) * a.C * 2 * 1.375, [&] {
       return launch_maxpool_bwd((const unsigned char*)(c->arena + c->lay.parg), gA, gB, n, a.H, a.H, a.C, s);
     });
-    bn_bwd(r, 0, n, gB, act_bits(c, c->t_r0), gC, accumulate);
+    if (gn) gn_bwd(r, 0, n, gB, -1, SLIDE_ACT_RELU, gC, nullptr, accumulate);
+    else bn_bwd(r, 0, n, gB, act_bits(c, c->t_r0), gC, accumulate);
     conv_wgrad(sums, 0, n, gC, accumulate);
   }
   return finish(r);
@@ -426,7 +528,10 @@ int resnet_ctx_create(const resnet_config* cfg, resnet_ctx** out) {
   if (cfg->tile <= 0 || cfg->tile % 32 || (cfg->block != 0 && cfg->block != 1)) return SLIDE_EINVAL;
   for (int s = 0; s < 4; ++s)
     if (cfg->depths[s] < 1 || cfg->depths[s] > 64) return SLIDE_EINVAL;
-  if (cfg->width <= 0 || cfg->mil_hidden <= 0 || cfg->n_classes <= 0 || !(cfg->bn_eps > 0.f) || cfg->reserved != 0)
+  if (cfg->width <= 0 || cfg->mil_hidden <= 0 || cfg->n_classes <= 0 || !(cfg->bn_eps > 0.f))
+    return SLIDE_EINVAL;
+  if (cfg->norm_groups < 0 || (cfg->norm_groups > 0 && cfg->width % cfg->norm_groups) || cfg->checkpoint8 < 0 || cfg->checkpoint8 > 1 ||
+      (cfg->checkpoint8 && !cfg->norm_groups))
     return SLIDE_EINVAL;
   const int exp = cfg->block ? 4 : 1;
   if (cfg->width < 64 || (cfg->width & (cfg->width - 1)) || cfg->width * 8 * exp > 2048) return SLIDE_EUNSUPPORTED;
@@ -466,6 +571,10 @@ int resnet_ctx_create(const resnet_config* cfg, resnet_ctx** out) {
         b.conv[2] = add_conv(c, p + "conv3", p + "bn3", mid, cout, 1, 1, 0, c->convs[b.conv[1]].outH, b.t_r[1], true);
       }
       if (down) b.down = add_conv(c, p + "down.conv", p + "down.bn", cin, cout, 1, stride, 0, H, t_in, true);
+      if (down && cfg->norm_groups) {
+        const int t = add_act(c, c->convs[b.down].outH, cout, false);
+        c->convs[b.down].t_norm = t;
+      }
       H = c->convs[b.conv[b.nconv - 1]].outH;
       b.t_out = add_act(c, H, cout, true);
       c->blocks.push_back(b);
@@ -609,6 +718,7 @@ int resnet_saved_activation(const resnet_ctx* c, int index, const void** ptr, in
   if (!c || !ptr || !side || !channels || index < 0 || index >= (int)c->acts.size()) return SLIDE_EINVAL;
   if (!c->arena || !c->enc_saved) return SLIDE_ESTATE;
   const Act& a = c->acts[index];
+  if (a.conv && c->cfg.checkpoint8) return SLIDE_EUNSUPPORTED;
   *ptr = c->arena + a.off; *side = a.H; *channels = a.C;
   return SLIDE_OK;
 }
