@@ -446,11 +446,12 @@ __global__ void __launch_bounds__(TH, 4) gn_fwd_k(P p) {
 }
 
 // du = dy act'(u) of V values, u = (x - mean) (rstd gamma) + beta + residual.  A rectifier asks which side of zero u is on: where float32
-// cannot tell, it is formed again in double (mean and rstd are what the forward stored).
-template <bool RES, int V, typename F>
+// cannot tell, it is formed again in double (mean and rstd are what the forward stored).  The kernels of that branch are their own
+// (RELU): in the others it would cost up to 50 registers (1024 tiles of 56 x 56 x 64, SiLU out of a checkpoint: 340 us with it, 310 without).
+template <bool RES, bool RELU, int V, typename F>
 __device__ __forceinline__ void du_vec(const float (&d)[V], const float (&dy)[V], const float (&rg)[V], const float (&bet)[V], const float (&res)[V],
                                        int act, float (&du)[V], F exactly) {
-  if (act == SLIDE_ACT_NONE) {
+  if (!RELU && act == SLIDE_ACT_NONE) {
 #pragma unroll
     for (int v = 0; v < V; ++v) du[v] = dy[v];
     return;
@@ -462,10 +463,11 @@ __device__ __forceinline__ void du_vec(const float (&d)[V], const float (&dy)[V]
 #pragma unroll
     for (int v = 0; v < V; ++v) u[v] += res[v];
   }
-  if (act == SLIDE_ACT_RELU) {
+  if constexpr (RELU) {
+    // u is off by less than 1e-6 of its parts' magnitudes; where it is as small as that, the first part is as large as the others
     bool near = false;
 #pragma unroll
-    for (int v = 0; v < V; ++v) near |= fabsf(u[v]) <= 1e-6f * (fabsf(d[v] * rg[v]) + fabsf(bet[v]) + (RES ? fabsf(res[v]) : 0.f));
+    for (int v = 0; v < V; ++v) near |= fabsf(u[v]) <= 2.1e-6f * (RES ? fabsf(bet[v]) + fabsf(res[v]) : fabsf(bet[v]));
     if (near) {
 #pragma unroll
       for (int v = 0; v < V; ++v) { u[v] = exactly(v); __builtin_amdgcn_sched_barrier(0); }
@@ -502,7 +504,7 @@ __device__ __forceinline__ float side(double x, double mean, double rstd, double
   return u > 0.0 ? 1.f : u < 0.0 ? -1.f : (float)u;
 }
 
-template <typename T, int V, int TH, int KG, bool X8, bool RES>
+template <typename T, int V, int TH, int KG, bool X8, bool RES, bool RELU>
 __global__ void __launch_bounds__(TH, 2) gn_bwd_k(P p) {
   __shared__ float red[2 * TH * V], gs[2][SMAX], cm[SMAX], cr[SMAX], crg[SMAX], cbet[SMAX], red2[TH];
   const GroupNorm& g = p.g;
@@ -561,7 +563,7 @@ __global__ void __launch_bounds__(TH, 2) gn_bwd_k(P p) {
         less_of<>(b.x[k], m, d);
         b.d[k].get(dy);
         if constexpr (RES) b.w[k].get(res);
-        du_vec<RES, V>(d, dy, rg, bet, res, act, du, [&](int v) __attribute__((always_inline)) {
+        du_vec<RES, RELU, V>(d, dy, rg, bet, res, act, du, [&](int v) __attribute__((always_inline)) {
           float x[V];
           b.x[k].get(x);
           return side(x[v], m[v], cr[at + v], g.gamma[s0 + at + v], bet[v], RES ? res[v] : 0.f);
@@ -571,12 +573,14 @@ __global__ void __launch_bounds__(TH, 2) gn_bwd_k(P p) {
       }
     };
     auto each = [&](auto f) __attribute__((always_inline)) {
+      Rows b[2];   // the next rows are on their way while these are worked on (behind the last row: zeros)
+      const bool more = KG * RG < p.rows;
+      if (more) load(b[0], KG * RG);
+      row_end();
 #pragma unroll
       for (int h = 0; h < KG; ++h)
         if (h * RG < p.rows) take(kept[h], h * RG, f);
-      if (KG * RG >= p.rows) return;
-      Rows b[2];   // the next rows are on their way while these are worked on (behind the last row: zeros)
-      load(b[0], KG * RG);
+      if (!more) return;
       for (int e = KG * RG; e < p.rows; e += 2 * RG) {
         load(b[1], e + RG);
         row_end();
@@ -843,7 +847,7 @@ __global__ void __launch_bounds__(ST) gn_apply_k(P p) {
 }
 
 // DX false: the chunk's sums of du xhat and du per channel -> part; true: dx (and dresidual) out of the groups' sums
-template <typename T, int V, bool X8, bool DX, bool RES>
+template <typename T, int V, bool X8, bool DX, bool RES, bool RELU>
 __global__ void __launch_bounds__(ST) gn_bwd_split_k(P p) {
   __shared__ __attribute__((aligned(16))) float red[DX ? 1 : ST * V];
   __shared__ float red2[DX ? 1 : ST], ch[DX ? 1 : ST * V];
@@ -888,7 +892,7 @@ __global__ void __launch_bounds__(ST) gn_bwd_split_k(P p) {
           less_of<>(bx[k], mean, d);
           bd[k].get(dy);
           if constexpr (RES) br[k].get(res);
-          du_vec<RES, V>(d, dy, rg, bet, res, act, du, [&](int v) __attribute__((always_inline)) {
+          du_vec<RES, RELU, V>(d, dy, rg, bet, res, act, du, [&](int v) __attribute__((always_inline)) {
             float x[V];
             bx[k].get(x);
             return side(x[v], mean[v], rstd[v], g.gamma[c0 + v], bet[v], RES ? res[v] : 0.f);
@@ -1074,47 +1078,49 @@ hipError_t fwd(const GroupNorm& g, hipStream_t s) {
   return hipGetLastError();
 }
 
-template <typename T, int V, bool X8, bool RES>
+template <typename T, int V, bool X8, bool RES, bool RELU>
 hipError_t bwd_units(const P& p, unsigned grid, bool small, hipStream_t s) {
-  if (small) gn_bwd_k<T, V, 256, KEPT, X8, RES><<<grid, 256, 0, s>>>(p);
-  else gn_bwd_k<T, V, 512, KEPT, X8, RES><<<grid, 512, 0, s>>>(p);
+  if (small) gn_bwd_k<T, V, 256, KEPT, X8, RES, RELU><<<grid, 256, 0, s>>>(p);
+  else gn_bwd_k<T, V, 512, KEPT, X8, RES, RELU><<<grid, 512, 0, s>>>(p);
   return hipGetLastError();
 }
 
 // the sums of the chunks, of the groups, then dx
-template <typename T, int V, bool X8, bool RES>
+template <typename T, int V, bool X8, bool RES, bool RELU>
 hipError_t bwd_split(const P& p, hipStream_t s) {
-  gn_bwd_split_k<T, V, X8, false, RES><<<split_grid(p), ST, 0, s>>>(p);
+  gn_bwd_split_k<T, V, X8, false, RES, RELU><<<split_grid(p), ST, 0, s>>>(p);
   hipError_t err = hipGetLastError();
   if (err != hipSuccess) return err;
   gn_bwd_group_k<<<group_grid(p), GT, 0, s>>>(p);
   err = hipGetLastError();
   if (err != hipSuccess) return err;
-  gn_bwd_split_k<T, V, X8, true, RES><<<split_grid(p), ST, 0, s>>>(p);
+  gn_bwd_split_k<T, V, X8, true, RES, RELU><<<split_grid(p), ST, 0, s>>>(p);
   return hipGetLastError();
 }
+
+template <typename F> hipError_t either(bool b, F f) { return b ? f(std::true_type{}) : f(std::false_type{}); }
 
 template <typename T, int V>
 hipError_t bwd(const GroupNorm& g, hipStream_t s) {
   P p = base(g);
   unsigned grid;
   bool small;
-  long long rows;
-  hipError_t err;
   p.part = g.work;
-  if (by_units(&p, V, sizeof(T), &grid, &small)) {
-    rows = p.units_p;
-    if (g.resid) err = g.x ? bwd_units<T, V, false, true>(p, grid, small, s) : bwd_units<T, V, true, true>(p, grid, small, s);
-    else err = g.x ? bwd_units<T, V, false, false>(p, grid, small, s) : bwd_units<T, V, true, false>(p, grid, small, s);
-  } else {
+  const bool units = by_units(&p, V, sizeof(T), &grid, &small);
+  if (!units) {
     split_plan(g.s, V, &p);
-    rows = p.n * p.chunks;
     p.sums = g.work + part_floats(g.s);
-    if (g.resid) err = g.x ? bwd_split<T, V, false, true>(p, s) : bwd_split<T, V, true, true>(p, s);
-    else err = g.x ? bwd_split<T, V, false, false>(p, s) : bwd_split<T, V, true, false>(p, s);
   }
+  const hipError_t err = either(!g.x, [&](auto x8) {
+    return either(g.resid, [&](auto res) {
+      return either(g.s.act == SLIDE_ACT_RELU, [&](auto relu) {
+        constexpr bool X8 = decltype(x8)::value, RES = decltype(res)::value, RELU = decltype(relu)::value;
+        return units ? bwd_units<T, V, X8, RES, RELU>(p, grid, small, s) : bwd_split<T, V, X8, RES, RELU>(p, s);
+      });
+    });
+  });
   if (err != hipSuccess) return err;
-  gn_sum_k<<<(p.C + 15) / 16, 1024, 0, s>>>(p.part, rows, p.C, g.dgamma, g.dbeta, g.accumulate);
+  gn_sum_k<<<(p.C + 15) / 16, 1024, 0, s>>>(p.part, units ? p.units_p : p.n * p.chunks, p.C, g.dgamma, g.dbeta, g.accumulate);
   return hipGetLastError();
 }
 
