@@ -2,7 +2,8 @@
 //
 // Pack: 16 lanes take a block of 128 columns of one row, 8 columns each: largest finite magnitude over the 16 (within
 // a DPP row), the block's power of two, one exact multiplication and one rounding per value.  One pass, 16-byte loads, 8-byte
-// stores; bound by memory: es + 1 + 1/128 bytes a value (es: 2 or 4).
+// stores; bound by memory: es + 1 + 1/128 bytes a value (es: 2 or 4).  403456 x 384 of bfloat16: 94 us there, 79 us back, 5.0 and
+// 5.9 TB/s (the way back finds codes in the last-level cache).
 #include "act8_internal.h"
 
 namespace sl {

@@ -6,6 +6,8 @@
 // eight consecutive rows of a column per lane, are read with the transposing LDS reads.
 // The rows are split into slabs: a work item is (slab, output tile), writes its partial tile once, and a second kernel adds the slabs
 // in a fixed order.
+// Bound by what feeds the matrix cores, not by bytes: 403456 x 384 -> 1536 takes 540 to 620 us, 0.8 to 0.9 PFLOP/s (a library product of
+// 8192 reaches 1.46; the bytes alone take 271 us).
 #include "act8_internal.h"
 #include "lds_dma.h"
 #include "split_f32.h"
