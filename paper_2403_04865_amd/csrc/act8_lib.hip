@@ -20,6 +20,11 @@ bool dtype_ok(int dt) { return dt == DT_F32 || dt == DT_BF16; }
 bool matrix_ok(const void* p, int dt, int64_t ld, int64_t cols) {
   return p && ((uintptr_t)p & (elem_size(dt) - 1)) == 0 && ld >= cols && ld <= LD_MAX;
 }
+// two matrices of `rows` rows that share no memory
+bool apart(const void* a, int64_t lda, int64_t ca, const void* b, int64_t ldb, int64_t cb, int64_t rows, size_t es) {
+  const uintptr_t a0 = (uintptr_t)a, b0 = (uintptr_t)b, a1 = a0 + ((rows - 1) * lda + ca) * es, b1 = b0 + ((rows - 1) * ldb + cb) * es;
+  return a1 <= b0 || b1 <= a0;
+}
 bool floats_ok(const void* p) { return p && ((uintptr_t)p & 3) == 0; }
 
 int work_ok(const void* work, size_t have, size_t need) {
@@ -64,7 +69,8 @@ int slide_act8_linear(const void* x, int dtype, int64_t ldx, const slide_act8* x
   if (residual && (!matrix_ok(residual, dtype, ldr, out) || (residual == y && ldr != ldy))) return SLIDE_EINVAL;
   if (out > A8_MAX_COLS) return SLIDE_EUNSUPPORTED;
   (void)hipGetLastError();
-  const bool fused = x && x8->rows <= A8_FEW;
+  // packed inside the product, every workgroup reads x for itself: not where y (a residual stream updated in place) lies on it
+  const bool fused = x && x8->rows <= A8_FEW && apart(x, ldx, x8->cols, y, ldy, out, x8->rows, elem_size(dtype));
   if (x && !fused) {
     const int rc = status(launch_act8_pack(x, dtype, ldx, false, *x8, (hipStream_t)stream));
     if (rc) return rc;

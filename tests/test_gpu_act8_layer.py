@@ -195,3 +195,24 @@ def test_two_at_once():
     torch.cuda.synchronize()
     for a, w in zip(pair, want):
         assert not _same(a.results(), w)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("rows,width", [(1, 4096), (5, 272), (16, 1040), (17, 1040), (300, 384)])
+def test_a_residual_stream_updated_in_place(rows, width, dtype):
+    """x, residual and y the same matrix: the same bits as apart, and the checkpoint of what x was."""
+    import torch
+    from paper_2403_04865_amd import Act8, Act8Lib
+    print("case", rows, width, dtype, flush=True)
+    t = {"fp32": torch.float32, "bf16": torch.bfloat16}[dtype]
+    rng = np.random.default_rng(rows + width)
+    x = torch.from_numpy(rng.standard_normal((rows, width)).astype(np.float32)).cuda().to(t)
+    w = torch.from_numpy((rng.standard_normal((width, width)) / width ** 0.5).astype(np.float32)).cuda().to(t)
+    L, w8 = Act8Lib(), Act8.empty(width, width)
+    L.slide_act8_pack(w, w8)
+    y, a, b = torch.empty_like(x), Act8.empty(rows, width), Act8.empty(rows, width)
+    L.slide_act8_pack(x, a)
+    L.slide_act8_linear(None, a, w8, y, act="silu", residual=x)
+    L.slide_act8_linear(x, b, w8, x, act="silu", residual=x)
+    assert torch.equal(a.codes, b.codes) and torch.equal(a.scales, b.scales)
+    assert torch.equal(x, y)
