@@ -103,7 +103,7 @@ hipError_t launch_act8_unpack(const slide_act8& a, void* y, int dt, long long ld
 
 constexpr int A8_FEW = 16;   // up to as many rows the product packs x itself
 struct A8Linear {
-  const void* xin; long long ldxin;   // x to be packed into `x` (M <= A8_FEW), or null: packed before
+  const void* xin; long long ldxin;   // x to be packed into `x` (shares no memory with y), or null: packed before
   A8 x, w;
   long long M; int N, K;
   const float* bias;

@@ -69,8 +69,8 @@ int slide_act8_linear(const void* x, int dtype, int64_t ldx, const slide_act8* x
   if (residual && (!matrix_ok(residual, dtype, ldr, out) || (residual == y && ldr != ldy))) return SLIDE_EINVAL;
   if (out > A8_MAX_COLS) return SLIDE_EUNSUPPORTED;
   (void)hipGetLastError();
-  // packed inside the product, every workgroup reads x for itself: not where y (a residual stream updated in place) lies on it
-  const bool fused = x && x8->rows <= A8_FEW && apart(x, ldx, x8->cols, y, ldy, out, x8->rows, elem_size(dtype));
+  // Packed inside the product, every workgroup reads x for itself: not where y (a residual stream updated in place) lies on it.
+  const bool fused = x && apart(x, ldx, x8->cols, y, ldy, out, x8->rows, elem_size(dtype));
   if (x && !fused) {
     const int rc = status(launch_act8_pack(x, dtype, ldx, false, *x8, (hipStream_t)stream));
     if (rc) return rc;

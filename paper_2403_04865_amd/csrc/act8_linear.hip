@@ -75,12 +75,20 @@ constexpr int SW = 8;   // wavefronts
 template <typename T>
 __device__ __forceinline__ Codes pack32(const T* x, int k, int K, bool vec, int* byte) {
   float v[32];
-  if (vec && k + 32 <= K) {
-    typedef T vec16 __attribute__((ext_vector_type(16 / sizeof(T))));
-    constexpr int E = 16 / sizeof(T);
+  constexpr int E = 16 / sizeof(T);
+  typedef T vec16 __attribute__((ext_vector_type(E)));
+  if (vec && K % A8_BLOCK == 0 && k < K) {   // (k < K in all lanes of a block)
 #pragma unroll
     for (int h = 0; h < 32 / E; ++h) {
       const vec16 q = *reinterpret_cast<const vec16*>(x + k + h * E);
+#pragma unroll
+      for (int e = 0; e < E; ++e) v[h * E + e] = to_f(q[e]);
+    }
+  } else if (vec && K % E == 0) {
+#pragma unroll
+    for (int h = 0; h < 32 / E; ++h) {
+      vec16 q = {};
+      if (k + h * E < K) q = *reinterpret_cast<const vec16*>(x + k + h * E);
 #pragma unroll
       for (int e = 0; e < E; ++e) v[h * E + e] = to_f(q[e]);
     }
@@ -106,6 +114,13 @@ __device__ __forceinline__ Codes pack32(const T* x, int k, int K, bool vec, int*
   for (int w = 0; w < 8; ++w) c[w] = (int)a8_code4(v[4 * w] * s, v[4 * w + 1] * s, v[4 * w + 2] * s, v[4 * w + 3] * s);
   *byte = (int)b;
   return c;
+}
+
+// what pack32 gave, as the checkpoint
+__device__ __forceinline__ void leave32(const Codes& c, int byte, uint8_t* row, uint8_t* scale, int k, int k16) {
+  if (k < k16) *reinterpret_cast<i32x4*>(row + k) = __builtin_shufflevector(c, c, 0, 1, 2, 3);
+  if (k + 16 < k16) *reinterpret_cast<i32x4*>(row + k + 16) = __builtin_shufflevector(c, c, 4, 5, 6, 7);
+  if ((k & (A8_BLOCK - 1)) == 0) *scale = (uint8_t)byte;
 }
 
 template <int MT, int ACT, typename T, bool PACK>
@@ -149,12 +164,7 @@ __global__ void __launch_bounds__(64 * SW) linear_few_k(A8Linear g, bool vec) {
         const int b = b0 + u * SW, k = b * A8_BLOCK + kg;
         if (b >= nb) { cx[u][0] = Codes{}; sx[u][0] = 127; continue; }   // uniform
         cx[u][0] = pack32((const T*)g.xin + mr[0] * g.ldxin, k, g.K, vec, &sx[u][0]);
-        if (leave) {
-          uint8_t* to = const_cast<uint8_t*>(xp[0]) + k;
-          if (k < k16) *reinterpret_cast<i32x4*>(to) = __builtin_shufflevector(cx[u][0], cx[u][0], 0, 1, 2, 3);
-          if (k + 16 < k16) *reinterpret_cast<i32x4*>(to + 16) = __builtin_shufflevector(cx[u][0], cx[u][0], 4, 5, 6, 7);
-          if (kg == 0) const_cast<uint8_t*>(xs[0])[b] = (uint8_t)sx[u][0];
-        }
+        if (leave) leave32(cx[u][0], sx[u][0], const_cast<uint8_t*>(xp[0]), const_cast<uint8_t*>(xs[0]) + b, k, k16);
       }
     }
 #pragma unroll
@@ -484,8 +494,8 @@ constexpr int RN = 64, RCOLS = 1024;   // rows of w per stage; most columns of y
 constexpr int RWAVES = 4;              // two such workgroups per compute unit
 template <int KB> constexpr int rows_fm() { return KB <= 2 ? 4 : 3; }   // what fits 256 registers
 
-template <int KB, int ACT>
-__global__ void __launch_bounds__(64 * RWAVES, 2) linear_rows_k(A8Linear g, int TM, int TN, int ncols, bool vec, bool stream) {
+template <int KB, int ACT, bool PACK>
+__global__ void __launch_bounds__(64 * RWAVES, 2) linear_rows_k(A8Linear g, int TM, int TN, int ncols, bool vec, bool stream, bool xvec) {
   constexpr int FM = rows_fm<KB>(), NW = RWAVES, STAGE = RN * KB * STEP, LOADS = RN / 8 * KB / NW;
   static_assert(LOADS * NW * 8 == RN * KB, "loads are dealt evenly");
   __shared__ __attribute__((aligned(16))) uint8_t ring0[STAGE], ring1[STAGE], wsc[RCOLS * 4], patch[NW][16 * patch_row<bf16>()];
@@ -526,11 +536,23 @@ __global__ void __launch_bounds__(64 * RWAVES, 2) linear_rows_k(A8Linear g, int 
   for (int i = 0; i < FM; ++i) {
     const long long m = m0 + 16 * i + r < g.M ? m0 + 16 * i + r : g.M - 1;
     const uint8_t *p = g.x.codes + m * g.x.ldc, *q = g.x.scales + m * g.x.lds;
-#pragma unroll
-    for (int b = 0; b < KB; ++b) x[i][b] = load_codes(p, b * A8_BLOCK + 32 * kg, k16);
     sx[i] = 0;
+    if constexpr (PACK) {
+      const bool leave = tn == 0 && m0 + 16 * i + r < g.M;
 #pragma unroll
-    for (int b = 0; b < KB; ++b) sx[i] |= (unsigned)q[b] << (8 * b);
+      for (int b = 0; b < KB; ++b) {
+        int byte;
+        const int k = b * A8_BLOCK + 32 * kg;
+        x[i][b] = pack32((const bf16*)g.xin + m * g.ldxin, k, g.K, xvec, &byte);
+        sx[i] |= (unsigned)byte << (8 * b);
+        if (leave) leave32(x[i][b], byte, const_cast<uint8_t*>(p), const_cast<uint8_t*>(q) + b, k, k16);
+      }
+    } else {
+#pragma unroll
+      for (int b = 0; b < KB; ++b) x[i][b] = load_codes(p, b * A8_BLOCK + 32 * kg, k16);
+#pragma unroll
+      for (int b = 0; b < KB; ++b) sx[i] |= (unsigned)q[b] << (8 * b);
+    }
   }
 
   const int have = (int)(g.M - m0 < 16 * FM ? g.M - m0 : 16 * FM);   // may be negative
@@ -594,11 +616,13 @@ hipError_t rows_kb(const A8Linear& g, hipStream_t s) {
   long long tn = (8LL * SLOTS + TM - 1) / TM;
   if (tn > st) tn = st;
   const int least = (st + RCOLS / RN - 1) / (RCOLS / RN);
-  if (tn < least) tn = least;
+  if (tn < least || g.xin) tn = least;   // (x is packed again for every piece of columns)
   const int per = (int)((st + tn - 1) / tn), TN = (st + per - 1) / per;
   auto ok = [&](const void* p, long long ld) { return !p || (((uintptr_t)p & 15) == 0 && ld % 8 == 0); };
-  linear_rows_k<KB, ACT><<<(unsigned)((TM + 7) / 8 * 8 * TN), 64 * RWAVES, 0, s>>>(
-      g, (int)TM, TN, per * RN, ok(g.y, g.ldy) && ok(g.resid, g.ldr), g.M * g.N * 2 >= STREAM_BYTES);
+  const unsigned grid = (unsigned)((TM + 7) / 8 * 8 * TN);
+  const bool vec = ok(g.y, g.ldy) && ok(g.resid, g.ldr), stream = g.M * g.N * 2 >= STREAM_BYTES;
+  if (g.xin) linear_rows_k<KB, ACT, true><<<grid, 64 * RWAVES, 0, s>>>(g, (int)TM, TN, per * RN, vec, stream, ok(g.xin, g.ldxin));
+  else linear_rows_k<KB, ACT, false><<<grid, 64 * RWAVES, 0, s>>>(g, (int)TM, TN, per * RN, vec, stream, false);
   return hipGetLastError();
 }
 
@@ -610,15 +634,32 @@ hipError_t rows(const A8Linear& g, hipStream_t s) {
 }
 
 template <int ACT, typename T>
-hipError_t run(const A8Linear& g, hipStream_t s) {
+hipError_t run(const A8Linear& given, hipStream_t s) {
+  A8Linear g = given;
   const long long t128 = ((g.M + 127) / 128) * ((g.N + 127) / 128), t256 = ((g.M + 255) / 256) * ((g.N + 255) / 256);
   // 32-bit offsets within a tile's rows; the launch's threads within 2^32
   const bool near = g.x.ldc <= (1 << 22) && g.w.ldc <= (1 << 22) && g.ldy <= (1 << 21) && g.ldr <= (1 << 21) && t128 < (1 << 22);
-  if (!near || g.M <= 64 || t128 < 64) return few<ACT, T>(g, s);
+  const bool fewer = !near || g.M <= 64 || t128 < 64;
+  // The few-rows kernel packs up to 16 rows itself, the rows kernel (bfloat16) where every compute unit has rows and no row is packed
+  // twice: from 32768 rows on, up to 384 columns (40000 x 384 -> 64, 256, 384, 768: 21.6, 23.8, 33.7, 35.7 us with the packing before, 14.3,
+  // 20.7, 24.4, 35.5 so; 120000: 47.8, 52, 74, 102 and 32, 44, 53, 75; 403456: 157, 169, 189, 260 and 116, 152, 180, 250; 16384 x 384 -> 256
+  // 15.3 and 17.8; 403456 x 384 -> 1152 323 and 368).  Without packing it wants several stages of w per workgroup (16384 x 384 -> 384: 13.7 us,
+  // 10.2 by tiles of 128; 7289 x 384 -> 1152: 13.1, 14.6 and by tiles of 256 12.6).
+  bool rows_k = false, packs = fewer && g.M <= A8_FEW;
   if constexpr (sizeof(T) == 2) {
-    // the rows kernel wants several stages of w per workgroup (16384 x 384 -> 384: 13.7 us, 10.2 by tiles of 128; 7289 x 384 -> 1152: 13.1,
-    // 14.6 and by tiles of 256 12.6)
-    if (g.K <= 3 * A8_BLOCK && g.M * g.N >= (1LL << 25)) return rows<ACT>(g, s);
+    const bool ok = !fewer && g.K <= 3 * A8_BLOCK;
+    packs = packs || (ok && g.M >= (1 << 15) && g.N <= 384);
+    rows_k = ok && ((g.xin && packs) || g.M * g.N >= (1LL << 25));
+  }
+  if (g.xin && !packs) {
+    const slide_act8 o{const_cast<uint8_t*>(g.x.codes), g.x.ldc, const_cast<uint8_t*>(g.x.scales), g.x.lds, g.M, g.K};
+    const hipError_t e = launch_act8_pack(g.xin, g.dt, g.ldxin, false, o, s);
+    if (e != hipSuccess) return e;
+    g.xin = nullptr;
+  }
+  if (fewer) return few<ACT, T>(g, s);
+  if constexpr (sizeof(T) == 2) {
+    if (rows_k) return rows<ACT>(g, s);
     if (t256 >= 144) return tiles<256, 256, 8, ACT, T>(g, s);
   }
   return tiles<128, 128, 4, ACT, T>(g, s);

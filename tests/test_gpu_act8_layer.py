@@ -198,7 +198,7 @@ def test_two_at_once():
 
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
-@pytest.mark.parametrize("rows,width", [(1, 4096), (5, 272), (16, 1040), (17, 1040), (300, 384)])
+@pytest.mark.parametrize("rows,width", [(1, 4096), (5, 272), (16, 1040), (17, 1040), (300, 384), (33000, 384)])
 def test_a_residual_stream_updated_in_place(rows, width, dtype):
     """x, residual and y the same matrix: the same bits as apart, and the checkpoint of what x was."""
     import torch
@@ -216,3 +216,35 @@ def test_a_residual_stream_updated_in_place(rows, width, dtype):
     L.slide_act8_linear(x, b, w8, x, act="silu", residual=x)
     assert torch.equal(a.codes, b.codes) and torch.equal(a.scales, b.scales)
     assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("rows,cin,cout,extra", [(7, 384, 40, 0), (16, 333, 64, 5), (33000, 384, 384, 0), (40000, 333, 64, 0), (33001, 200, 100, 8),
+                                                 (32768, 128, 8, 3), (32770, 1, 384, 0), (50000, 256, 129, 16), (32999, 384, 385, 0)])
+def test_packing_inside_the_product(rows, cin, cout, extra):
+    """As packing first does: the checkpoint bit for bit, with its zeros behind the last column and nothing else touched, and y."""
+    import torch
+    from paper_2403_04865_amd import Act8, Act8Lib
+    print("case", rows, cin, cout, extra, flush=True)
+    gen = torch.Generator(device="cuda").manual_seed(rows + cin)
+    x = torch.randn(rows, cin + extra, generator=gen, device="cuda").bfloat16()[:, :cin]
+    x[rows // 2, cin // 2] = float("nan")
+    x[rows - 1] = 0
+    w = torch.randn(cout, cin, generator=gen, device="cuda").bfloat16()
+    bias = torch.randn(cout, generator=gen, device="cuda")
+    L, w8 = Act8Lib(), Act8.empty(cout, cin)
+    L.slide_act8_pack(w, w8)
+    k16, nb = -(-cin // 16) * 16, -(-cin // 128)
+
+    def guarded():
+        codes, scales = torch.full((rows + 1, k16 + 16), 0x5a, dtype=torch.uint8, device="cuda"), torch.full((rows + 1, nb + 1), 0x5a, dtype=torch.uint8, device="cuda")
+        return Act8(rows, cin, codes[:rows, :k16], scales[:rows, :nb]), codes, scales
+    (a, ac, as_), (b, bc, bs) = guarded(), guarded()
+    y, z = (torch.full((rows + 1, cout), 7.0, device="cuda", dtype=torch.bfloat16) for _ in range(2))
+    L.slide_act8_pack(x, a)
+    L.slide_act8_linear(None, a, w8, y[:rows], bias=bias, act="relu")
+    L.slide_act8_linear(x, b, w8, z[:rows], bias=bias, act="relu")
+    assert torch.equal(ac, bc) and torch.equal(as_, bs)
+    same = (y == z) | (y.isnan() & z.isnan())
+    # with another kernel the 8-bit products may be added in another order: half a step's rounding of results, nothing more
+    assert same.float().mean() > 0.99 and torch.allclose(y.float(), z.float(), rtol=2.0 ** -7, atol=1e-2, equal_nan=True)
+    assert bool((z[rows] == 7).all()) and bool(z[rows // 2].isnan().all()) and int(z.isnan().sum()) == cout
