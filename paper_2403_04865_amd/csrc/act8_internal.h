@@ -101,7 +101,6 @@ inline A8 a8_view(const slide_act8& a) { return A8{a.codes, a.ldc, a.scales, a.l
 hipError_t launch_act8_pack(const void* x, int dt, long long ldx, bool transpose, const slide_act8& out, hipStream_t s);
 hipError_t launch_act8_unpack(const slide_act8& a, void* y, int dt, long long ldy, hipStream_t s);
 
-constexpr int A8_FEW = 16;   // up to as many rows the product packs x itself
 struct A8Linear {
   const void* xin; long long ldxin;   // x to be packed into `x` (shares no memory with y), or null: packed before
   A8 x, w;

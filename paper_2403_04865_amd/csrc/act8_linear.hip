@@ -66,7 +66,7 @@ __device__ __forceinline__ Codes load_codes(const uint8_t* p, int k, int k16) { 
 
 // ---- few rows -------------------------------------------------------------------------------------------------------
 // A workgroup takes 16 output columns and 16 MT rows; its wavefronts share out the blocks of k and their partial products are added in
-// LDS, in a fixed order.  PACK (up to 16 rows): x comes as it is and every workgroup makes the codes it multiplies for itself, the first one
+// LDS, in a fixed order.  PACK: x comes as it is and every workgroup makes the codes it multiplies for itself, the first one
 // leaves them as the checkpoint: one launch instead of two (1 x 4096 -> 4096: 12.2 us a call with a launch for the packing, 8.5 so).
 constexpr int SW = 8;   // wavefronts
 
@@ -141,7 +141,6 @@ __global__ void __launch_bounds__(64 * SW) linear_few_k(A8Linear g, bool vec) {
     mr[i] = m0 + 16 * i + r < g.M ? m0 + 16 * i + r : g.M - 1;
     xp[i] = g.x.codes + mr[i] * g.x.ldc; xs[i] = g.x.scales + mr[i] * g.x.lds;
   }
-  const bool leave = PACK && blockIdx.x == 0 && m0 + r < g.M;   // this lane's codes are the checkpoint's
   f32x4 acc[MT];
 #pragma unroll
   for (int i = 0; i < MT; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -162,9 +161,13 @@ __global__ void __launch_bounds__(64 * SW) linear_few_k(A8Linear g, bool vec) {
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const int b = b0 + u * SW, k = b * A8_BLOCK + kg;
-        if (b >= nb) { cx[u][0] = Codes{}; sx[u][0] = 127; continue; }   // uniform
-        cx[u][0] = pack32((const T*)g.xin + mr[0] * g.ldxin, k, g.K, vec, &sx[u][0]);
-        if (leave) leave32(cx[u][0], sx[u][0], const_cast<uint8_t*>(xp[0]), const_cast<uint8_t*>(xs[0]) + b, k, k16);
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+          if (b >= nb) { cx[u][i] = Codes{}; sx[u][i] = 127; continue; }   // uniform
+          cx[u][i] = pack32((const T*)g.xin + mr[i] * g.ldxin, k, g.K, vec, &sx[u][i]);
+          if (blockIdx.x == 0 && m0 + 16 * i + r < g.M)   // this lane's codes are the checkpoint's
+            leave32(cx[u][i], sx[u][i], const_cast<uint8_t*>(xp[i]), const_cast<uint8_t*>(xs[i]) + b, k, k16);
+        }
       }
     }
 #pragma unroll
@@ -200,11 +203,7 @@ __global__ void __launch_bounds__(64 * SW) linear_few_k(A8Linear g, bool vec) {
 template <int ACT, typename T>
 hipError_t few(const A8Linear& g, hipStream_t s) {
   const int mt = g.M <= 16 ? 1 : g.M <= 32 ? 2 : 4;
-  if (g.xin) {   // M <= 16
-    const bool vec = ((uintptr_t)g.xin & 15) == 0 && g.ldxin * sizeof(T) % 16 == 0;
-    linear_few_k<1, ACT, T, true><<<(g.N + 15) / 16, 64 * SW, 0, s>>>(g, vec);
-    return hipGetLastError();
-  }
+  const bool vec = ((uintptr_t)g.xin & 15) == 0 && g.ldxin * sizeof(T) % 16 == 0;
   A8Linear p = g;
   // grid.y is limited to 65535: the rows go in pieces
   const long long most = 16LL * mt * 65535;
@@ -212,11 +211,17 @@ hipError_t few(const A8Linear& g, hipStream_t s) {
     p.M = g.M - m < most ? g.M - m : most;
     p.x.codes = g.x.codes + m * g.x.ldc; p.x.scales = g.x.scales + m * g.x.lds;
     p.y = (T*)g.y + m * g.ldy;
+    if (g.xin) p.xin = (const T*)g.xin + m * g.ldxin;
     if (g.resid) p.resid = (const T*)g.resid + m * g.ldr;
     const dim3 grid((g.N + 15) / 16, (unsigned)((p.M + 16 * mt - 1) / (16 * mt)));
-    if (mt == 1) linear_few_k<1, ACT, T, false><<<grid, 64 * SW, 0, s>>>(p, false);
-    else if (mt == 2) linear_few_k<2, ACT, T, false><<<grid, 64 * SW, 0, s>>>(p, false);
-    else linear_few_k<4, ACT, T, false><<<grid, 64 * SW, 0, s>>>(p, false);
+    auto go = [&](auto pack) {
+      constexpr bool PACK = decltype(pack)::value;
+      if (mt == 1) linear_few_k<1, ACT, T, PACK><<<grid, 64 * SW, 0, s>>>(p, vec);
+      else if (mt == 2) linear_few_k<2, ACT, T, PACK><<<grid, 64 * SW, 0, s>>>(p, vec);
+      else linear_few_k<4, ACT, T, PACK><<<grid, 64 * SW, 0, s>>>(p, vec);
+    };
+    if (g.xin) go(std::true_type{});
+    else go(std::false_type{});
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
@@ -640,12 +645,19 @@ hipError_t run(const A8Linear& given, hipStream_t s) {
   // 32-bit offsets within a tile's rows; the launch's threads within 2^32
   const bool near = g.x.ldc <= (1 << 22) && g.w.ldc <= (1 << 22) && g.ldy <= (1 << 21) && g.ldr <= (1 << 21) && t128 < (1 << 22);
   const bool fewer = !near || g.M <= 64 || t128 < 64;
-  // The few-rows kernel packs up to 16 rows itself, the rows kernel (bfloat16) where every compute unit has rows and no row is packed
-  // twice: from 32768 rows on, up to 384 columns (40000 x 384 -> 64, 256, 384, 768: 21.6, 23.8, 33.7, 35.7 us with the packing before, 14.3,
-  // 20.7, 24.4, 35.5 so; 120000: 47.8, 52, 74, 102 and 32, 44, 53, 75; 403456: 157, 169, 189, 260 and 116, 152, 180, 250; 16384 x 384 -> 256
+  // Who packs x (two launches otherwise).  The few-rows kernel, every workgroup for itself, up to 16 rows; beyond, where its workgroups are there
+  // at once, x comes in 16-byte pieces and a wavefront has one block of 128 bfloat16 columns, or two of up to 32 rows (with the packing before and
+  // so: 64 x 384 -> 384 9.5 and 7.0 us, 64 x 1024 9.3 and 8.2, 64 x 1280 9.5 and 10.4, 32 x 2048 9.4 and 8.3, 17 x 4096 10.6 and 11.9; 400 x 384
+  // -> 384 9.2 and 6.9, 1152 9.4 and 9.8; 256 x 1024 -> 1152
+  // 10.6 and 13.2; 64 x 333 8.9 and 14; float32, 64 x 384 -> 384 8.8 and 7.0, 64 x 1024 8.8 and 12).  The rows kernel (bfloat16) where every compute unit has rows and no row is
+  // packed twice: from 32768 rows on, up to 384 columns (40000 x 384 -> 64, 256, 384, 768: 21.6, 23.8, 33.7, 35.7 us with the packing before,
+  // 14.3, 20.7, 24.4, 35.5 so; 120000: 47.8, 52, 74, 102 and 32, 44, 53, 75; 403456: 157, 169, 189, 260 and 116, 152, 180, 250; 16384 x 384 -> 256
   // 15.3 and 17.8; 403456 x 384 -> 1152 323 and 368).  Without packing it wants several stages of w per workgroup (16384 x 384 -> 384: 13.7 us,
   // 10.2 by tiles of 128; 7289 x 384 -> 1152: 13.1, 14.6 and by tiles of 256 12.6).
-  bool rows_k = false, packs = fewer && g.M <= A8_FEW;
+  const int nb = (g.K + A8_BLOCK - 1) / A8_BLOCK;
+  const bool pieces = ((uintptr_t)g.xin & 15) == 0 && g.ldxin * sizeof(T) % 16 == 0 && g.K * sizeof(T) % 16 == 0;
+  bool rows_k = false, packs = fewer && (g.M <= 16 || (pieces && nb * (int)sizeof(T) <= (g.M <= 32 ? 4 * SW : 2 * SW) &&
+                                                       (g.N + 15LL) / 16 * ((g.M + 63) / 64) <= 256));
   if constexpr (sizeof(T) == 2) {
     const bool ok = !fewer && g.K <= 3 * A8_BLOCK;
     packs = packs || (ok && g.M >= (1 << 15) && g.N <= 384);

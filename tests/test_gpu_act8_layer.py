@@ -218,7 +218,8 @@ def test_a_residual_stream_updated_in_place(rows, width, dtype):
     assert torch.equal(x, y)
 
 
-@pytest.mark.parametrize("rows,cin,cout,extra", [(7, 384, 40, 0), (16, 333, 64, 5), (33000, 384, 384, 0), (40000, 333, 64, 0), (33001, 200, 100, 8),
+@pytest.mark.parametrize("rows,cin,cout,extra", [(17, 2048, 40, 0), (32, 2040, 4096, 8), (33, 1024, 72, 0), (64, 136, 333, 8), (200, 384, 1024, 0),
+                                                 (257, 8, 64, 8), (1000, 640, 64, 0), (7, 384, 40, 0), (16, 333, 64, 5), (33000, 384, 384, 0), (40000, 333, 64, 0), (33001, 200, 100, 8),
                                                  (32768, 128, 8, 3), (32770, 1, 384, 0), (50000, 256, 129, 16), (32999, 384, 385, 0)])
 def test_packing_inside_the_product(rows, cin, cout, extra):
     """As packing first does: the checkpoint bit for bit, with its zeros behind the last column and nothing else touched, and y."""
