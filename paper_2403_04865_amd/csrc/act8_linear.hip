@@ -70,32 +70,35 @@ __device__ __forceinline__ Codes load_codes(const uint8_t* p, int k, int k16) { 
 // leaves them as the checkpoint: one launch instead of two (1 x 4096 -> 4096: 12.2 us a call with a launch for the packing, 8.5 so).
 constexpr int SW = 8;   // wavefronts
 
-// 32 values of row `x` from column k on (zeros from K on) -> codes and the scale byte of their block, which the four lanes that differ in
-// bits 4 and 5 hold together
-template <typename T>
-__device__ __forceinline__ Codes pack32(const T* x, int k, int K, bool vec, int* byte) {
-  float v[32];
-  constexpr int E = 16 / sizeof(T);
+// 32 values of row `x` from column k on (zeros from K on)
+template <typename T> struct Raw {
+  static constexpr int E = 16 / sizeof(T);
   typedef T vec16 __attribute__((ext_vector_type(E)));
-  if (vec && K % A8_BLOCK == 0 && k < K) {   // (k < K in all lanes of a block)
+  vec16 q[32 / E];
+  __device__ __forceinline__ void load(const T* x, int k, int K, bool vec) {
+    if (vec && K % A8_BLOCK == 0 && k < K) {   // (k < K in all lanes of a block)
 #pragma unroll
-    for (int h = 0; h < 32 / E; ++h) {
-      const vec16 q = *reinterpret_cast<const vec16*>(x + k + h * E);
+      for (int h = 0; h < 32 / E; ++h) q[h] = *reinterpret_cast<const vec16*>(x + k + h * E);
+    } else if (vec && K % E == 0) {
 #pragma unroll
-      for (int e = 0; e < E; ++e) v[h * E + e] = to_f(q[e]);
+      for (int h = 0; h < 32 / E; ++h) {
+        q[h] = vec16{};
+        if (k + h * E < K) q[h] = *reinterpret_cast<const vec16*>(x + k + h * E);
+      }
+    } else {
+#pragma unroll
+      for (int h = 0; h < 32 / E; ++h)
+#pragma unroll
+        for (int e = 0; e < E; ++e) q[h][e] = k + h * E + e < K ? x[k + h * E + e] : (T)0.f;
     }
-  } else if (vec && K % E == 0) {
-#pragma unroll
-    for (int h = 0; h < 32 / E; ++h) {
-      vec16 q = {};
-      if (k + h * E < K) q = *reinterpret_cast<const vec16*>(x + k + h * E);
-#pragma unroll
-      for (int e = 0; e < E; ++e) v[h * E + e] = to_f(q[e]);
-    }
-  } else {
-#pragma unroll
-    for (int e = 0; e < 32; ++e) v[e] = k + e < K ? to_f(x[k + e]) : 0.f;
   }
+};
+// ... -> codes and the scale byte of their block, which the four lanes that differ in bits 4 and 5 hold together
+template <typename T>
+__device__ __forceinline__ Codes pack32(const Raw<T>& w, int* byte) {
+  float v[32];
+#pragma unroll
+  for (int e = 0; e < 32; ++e) v[e] = to_f(w.q[e / Raw<T>::E][e % Raw<T>::E]);
   auto most = [](float m) { m = fmaxf(m, __shfl_xor(m, 16, 64)); return fmaxf(m, __shfl_xor(m, 32, 64)); };
   float m = 0.f;
 #pragma unroll
@@ -111,7 +114,7 @@ __device__ __forceinline__ Codes pack32(const T* x, int k, int K, bool vec, int*
   const float s = a8_inverse(b);
   Codes c;
 #pragma unroll
-  for (int w = 0; w < 8; ++w) c[w] = (int)a8_code4(v[4 * w] * s, v[4 * w + 1] * s, v[4 * w + 2] * s, v[4 * w + 3] * s);
+  for (int j = 0; j < 8; ++j) c[j] = (int)a8_code4(v[4 * j] * s, v[4 * j + 1] * s, v[4 * j + 2] * s, v[4 * j + 3] * s);
   *byte = (int)b;
   return c;
 }
@@ -164,7 +167,9 @@ __global__ void __launch_bounds__(64 * SW) linear_few_k(A8Linear g, bool vec) {
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
           if (b >= nb) { cx[u][i] = Codes{}; sx[u][i] = 127; continue; }   // uniform
-          cx[u][i] = pack32((const T*)g.xin + mr[i] * g.ldxin, k, g.K, vec, &sx[u][i]);
+          Raw<T> raw;
+          raw.load((const T*)g.xin + mr[i] * g.ldxin, k, g.K, vec);
+          cx[u][i] = pack32(raw, &sx[u][i]);
           if (blockIdx.x == 0 && m0 + 16 * i + r < g.M)   // this lane's codes are the checkpoint's
             leave32(cx[u][i], sx[u][i], const_cast<uint8_t*>(xp[i]), const_cast<uint8_t*>(xs[i]) + b, k, k16);
         }
@@ -537,24 +542,35 @@ __global__ void __launch_bounds__(64 * RWAVES, 2) linear_rows_k(A8Linear g, int 
   // this wavefront's rows (behind the last: the last one again, nothing of it is stored)
   Codes x[FM][KB];
   unsigned sx[FM];   // a byte per block
+  auto row_of = [&](int i) { return m0 + 16 * i + r < g.M ? m0 + 16 * i + r : g.M - 1; };
+  if constexpr (PACK) {
+    Raw<bf16> raw[FM][KB];   // all of them on their way before the first is looked at
 #pragma unroll
-  for (int i = 0; i < FM; ++i) {
-    const long long m = m0 + 16 * i + r < g.M ? m0 + 16 * i + r : g.M - 1;
-    const uint8_t *p = g.x.codes + m * g.x.ldc, *q = g.x.scales + m * g.x.lds;
-    sx[i] = 0;
-    if constexpr (PACK) {
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+      for (int b = 0; b < KB; ++b) raw[i][b].load((const bf16*)g.xin + row_of(i) * g.ldxin, b * A8_BLOCK + 32 * kg, g.K, xvec);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < FM; ++i) {
       const bool leave = tn == 0 && m0 + 16 * i + r < g.M;
+      uint8_t* const to = const_cast<uint8_t*>(g.x.codes) + row_of(i) * g.x.ldc;
+      uint8_t* const scale = const_cast<uint8_t*>(g.x.scales) + row_of(i) * g.x.lds;
+      sx[i] = 0;
 #pragma unroll
       for (int b = 0; b < KB; ++b) {
         int byte;
-        const int k = b * A8_BLOCK + 32 * kg;
-        x[i][b] = pack32((const bf16*)g.xin + m * g.ldxin, k, g.K, xvec, &byte);
+        x[i][b] = pack32(raw[i][b], &byte);
         sx[i] |= (unsigned)byte << (8 * b);
-        if (leave) leave32(x[i][b], byte, const_cast<uint8_t*>(p), const_cast<uint8_t*>(q) + b, k, k16);
+        if (leave) leave32(x[i][b], byte, to, scale + b, b * A8_BLOCK + 32 * kg, k16);
       }
-    } else {
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < FM; ++i) {
+      const uint8_t *p = g.x.codes + row_of(i) * g.x.ldc, *q = g.x.scales + row_of(i) * g.x.lds;
 #pragma unroll
       for (int b = 0; b < KB; ++b) x[i][b] = load_codes(p, b * A8_BLOCK + 32 * kg, k16);
+      sx[i] = 0;
 #pragma unroll
       for (int b = 0; b < KB; ++b) sx[i] |= (unsigned)q[b] << (8 * b);
     }
