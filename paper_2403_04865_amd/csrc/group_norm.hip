@@ -302,7 +302,7 @@ template <int V> __device__ __forceinline__ void mine(const float* ch, int c, fl
 // KG: groups of RG rows of a thread that stay in registers
 template <typename T, int V, int TH, int KG>
 __global__ void __launch_bounds__(TH, 4) gn_fwd_k(P p) {
-  __shared__ float red[TH * V], gs[1][SMAX], cm[SMAX], ca[SMAX], cb[SMAX];
+  __shared__ float red[TH * V], gs[1][SMAX], cm[SMAX], cg[SMAX], ca[SMAX], cb[SMAX];
   const GroupNorm& g = p.g;
   const Own<V> o(p.S, TH);
   const int j = blockIdx.x >> 3, slice = j % p.slices, first = (int)(blockIdx.x & 7) + 8 * (j / p.slices);
@@ -312,7 +312,7 @@ __global__ void __launch_bounds__(TH, 4) gn_fwd_k(P p) {
   constexpr int es = sizeof(T);
   const int ldx = (int)g.ldx * es, ldy = (int)g.ldy * es, ldr = (int)g.ldr * es;
   const int vx = o.on ? o.tr * ldx + tc * es : DMA_ABSENT, vy = o.on ? o.tr * ldy + tc * es : DMA_ABSENT, vr = o.on ? o.tr * ldr + tc * es : DMA_ABSENT;
-  for (int c = threadIdx.x; c < p.S; c += TH) cb[c] = g.beta[s0 + c];
+  for (int c = threadIdx.x; c < p.S; c += TH) { cg[c] = g.gamma[s0 + c]; cb[c] = g.beta[s0 + c]; }
   for (long long tile = first; tile < p.n; tile += p.units_p) {
     const long long r0 = tile * p.hw;
     const __amdgpu_buffer_rsrc_t xb = tile_buffer((const T*)g.x + r0 * g.ldx + s0, g.ldx, es, p.hw, p.S);
@@ -410,7 +410,7 @@ __global__ void __launch_bounds__(TH, 4) gn_fwd_k(P p) {
 #pragma unroll
     for (int v = 0; v < V; ++v) { const float d = m[v] - mean[v]; s[0][v] = fmaf(d * d, n, q[0][v]); }
     group_sums<TH, V, 1>(s, o, p.S, per, red, gs);
-    for (int c = threadIdx.x; c < p.S; c += TH) ca[c] = g.gamma[s0 + c] * (1.0f / sqrtf(gs[0][c / per] / count + g.s.eps));
+    for (int c = threadIdx.x; c < p.S; c += TH) ca[c] = cg[c] * (1.0f / sqrtf(gs[0][c / per] / count + g.s.eps));
     if ((int)threadIdx.x < gl) g.rstd[tile * p.G + slice * gl + threadIdx.x] = 1.0f / sqrtf(gs[0][threadIdx.x] / count + g.s.eps);
     __syncthreads();
     // ---- the result
