@@ -1001,7 +1001,10 @@ size_t part_floats(const slide_group_norm& s) {
 //     fetch cache lines that other units want too) and, where there are units enough, PIECES pieces in all (a unit costs some
 //     microseconds of barriers), or all of them.
 //   * 256 threads up to sixteen rows of a thread, else 512.
-//   * With fewer units than half the compute units a longer unit is split instead.
+//   * With fewer units than half the compute units (float32: three quarters) a longer unit is split instead (9 x 3136 x 512 float32, 144 units:
+//     forward 46 us, split 37; backward 73 and 58; 130 x 3136 x 64, 260 units: 64 and 73, 119 and 113), and a float32 unit of 1.5 MB
+//     (140 x 12544 x 64, units of 1.6 MB: 383 us and 327, 544 and 483; 1024: 2001 and 2030, 3233 and 3092; 256 x 6272 x 64, 0.8 MB: 266
+//     and 295, 426 and 430; bfloat16, 500 x 12544 x 64, 1.6 MB: 475 and 539, 779 and 817; 256 x 25088 x 64, 3.2 MB: 480 and 530, 775 and 870).
 constexpr int PIECES = 2048;
 bool by_units(P* p, int V, int es, unsigned* grid, bool* small) {
   const slide_group_norm& s = p->g.s;
@@ -1026,7 +1029,8 @@ bool by_units(P* p, int V, int es, unsigned* grid, bool* small) {
   const int rpp = (*small ? 256 : 512) / vpr;
   p->slices = p->C / p->S;
   p->rows = (int)((s.hw + rpp - 1) / rpp);
-  if (s.n * p->slices < 128 && p->rows > 16) return false;
+  if (s.n * p->slices < (es == 4 ? 192 : 128) && p->rows > 16) return false;
+  if (es == 4 && s.hw * p->S * es >= 3 << 19) return false;
   p->units_p = (int)(s.n < MOST_P ? s.n : MOST_P);
   *grid = (unsigned)((p->units_p + 7) / 8 * 8 * p->slices);
   return true;
