@@ -690,9 +690,10 @@ __global__ void __launch_bounds__(ST) gn_stat_k(P p) {
   for (long long unit = blockIdx.x; unit < p.n * p.chunks * p.slices; unit += gridDim.x) {
     const Where w = where(p, unit);
     const int S = p.C - w.slice * p.S < p.S ? p.C - w.slice * p.S : p.S;   // the last slice may be short
-    // (with a checkpoint the pieces of a row are padded to whole DPP rows of 16 lanes, which hold a block of its columns)
-    Own<V> o(p.pack ? (S / V + 15) / 16 * 16 * V : S, ST);
-    o.on = o.on && o.tc * V < S;
+    // With a checkpoint the pieces of a row are padded to whole DPP rows of 16 lanes, which hold a block of its columns.  Lanes behind the last
+    // column go along with zeros: left out, they would cut the exchange of the block's maximum between the others.
+    const Own<V> o(p.pack ? (S / V + 15) / 16 * 16 * V : S, ST);
+    const bool have_cols = o.tc * V < S;
     const int c0 = w.slice * p.S + o.tc * V;
     const T* x = (const T*)g.x + w.tile * p.hw * g.ldx + c0;
     float n = 0.f, m[V], q[V];
@@ -705,7 +706,8 @@ __global__ void __launch_bounds__(ST) gn_stat_k(P p) {
 #pragma unroll
         for (int e = 0; e < SE; ++e) {
           const int k = r + e * o.rpp;
-          if (k < w.hi) { buf[e].load(x + (long long)k * g.ldx); ++have; }
+          have += k < w.hi;
+          if (k < w.hi && have_cols) buf[e].load(x + (long long)k * g.ldx);
           else buf[e].zero();
         }
         float s[V], d2[V];
@@ -718,15 +720,15 @@ __global__ void __launch_bounds__(ST) gn_stat_k(P p) {
 #pragma unroll
           for (int v = 0; v < V; ++v) s[v] += t[v];
           if constexpr (V == 8) {
-            if (p.pack && r + e * o.rpp < w.hi) {   // (lanes behind the last column take no part: nothing)
+            if (p.pack && r + e * o.rpp < w.hi) {   // (alike in the lanes of a row)
               const unsigned sc = a8_block_byte(t, 16);
               const float inv = a8_inverse(sc);
               const long long row = w.tile * p.hw + r + e * o.rpp;
               u32x2 z;
               z[0] = a8_code4(t[0] * inv, t[1] * inv, t[2] * inv, t[3] * inv);
               z[1] = a8_code4(t[4] * inv, t[5] * inv, t[6] * inv, t[7] * inv);
-              *reinterpret_cast<u32x2*>(const_cast<uint8_t*>(p.x8.codes) + row * p.x8.ldc + c0) = z;
-              if ((o.tc & 15) == 0) const_cast<uint8_t*>(p.x8.scales)[row * p.x8.lds + (c0 >> 7)] = (uint8_t)sc;
+              if (have_cols) *reinterpret_cast<u32x2*>(const_cast<uint8_t*>(p.x8.codes) + row * p.x8.ldc + c0) = z;
+              if (have_cols && (o.tc & 15) == 0) const_cast<uint8_t*>(p.x8.scales)[row * p.x8.lds + (c0 >> 7)] = (uint8_t)sc;
             }
           }
         }
@@ -745,7 +747,7 @@ __global__ void __launch_bounds__(ST) gn_stat_k(P p) {
         for (int v = 0; v < V; ++v) { float k = n0; merge(k, m[v], q[v], (float)have, s[v], d2[v]); }
         n = n0 + (float)have;
       }
-    if (o.on) {
+    if (o.on && have_cols) {
       if (o.tc == 0) sn[o.tr] = n;
 #pragma unroll
       for (int v = 0; v < V; ++v) { sm[o.tr * S + o.tc * V + v] = m[v]; sq[o.tr * S + o.tc * V + v] = q[v]; }
