@@ -403,7 +403,7 @@ __global__ void __launch_bounds__(TH, 4) gn_fwd_k(P p) {
     for (int v = 0; v < V; ++v) s[0][v] = n * m[v];
     group_sums<TH, V, 1>(s, o, p.S, per, red, gs);
     for (int c = threadIdx.x; c < p.S; c += TH) cm[c] = gs[0][c / per] / count;
-    if ((int)threadIdx.x < gl) g.mean[tile * p.G + slice * gl + threadIdx.x] = gs[0][threadIdx.x] / count;
+    for (int k = threadIdx.x; k < gl; k += TH) g.mean[tile * p.G + slice * gl + k] = gs[0][k] / count;   // (more groups than threads: a channel each)
     __syncthreads();
     float mean[V];
     mine<V>(cm, at, mean);
@@ -411,7 +411,7 @@ __global__ void __launch_bounds__(TH, 4) gn_fwd_k(P p) {
     for (int v = 0; v < V; ++v) { const float d = m[v] - mean[v]; s[0][v] = fmaf(d * d, n, q[0][v]); }
     group_sums<TH, V, 1>(s, o, p.S, per, red, gs);
     for (int c = threadIdx.x; c < p.S; c += TH) ca[c] = cg[c] * (1.0f / sqrtf(gs[0][c / per] / count + g.s.eps));
-    if ((int)threadIdx.x < gl) g.rstd[tile * p.G + slice * gl + threadIdx.x] = 1.0f / sqrtf(gs[0][threadIdx.x] / count + g.s.eps);
+    for (int k = threadIdx.x; k < gl; k += TH) g.rstd[tile * p.G + slice * gl + k] = 1.0f / sqrtf(gs[0][k] / count + g.s.eps);
     __syncthreads();
     // ---- the result
     const __amdgpu_buffer_rsrc_t yb = tile_buffer((T*)g.y + r0 * g.ldy + s0, g.ldy, es, p.hw, p.S);
