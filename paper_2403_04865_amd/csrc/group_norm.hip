@@ -670,15 +670,18 @@ __global__ void __launch_bounds__(1024) gn_sum_k(const float* __restrict__ part,
 
 constexpr int ST = 256, SE = 8;   // threads; rows of a thread whose loads are in flight together
 
-struct Where { long long tile; int slice, chunk, lo, hi; };
+// row0: the chunk's first row, of the whole matrix.  Rows are counted within the chunk: a tile may have 2^31 - 1 of them, and a chunk's count with
+// what a thread strides beyond it stays far below that.
+struct Where { long long tile, row0; int slice, chunk, rows; };
 __device__ __forceinline__ Where where(const P& p, long long unit) {
   Where w;
   w.slice = (int)(unit % p.slices);
   const long long k = unit / p.slices;
   w.chunk = (int)(k % p.chunks);
   w.tile = k / p.chunks;
-  w.lo = w.chunk * p.rows_chunk;
-  w.hi = w.lo + p.rows_chunk < p.hw ? w.lo + p.rows_chunk : p.hw;
+  const int lo = w.chunk * p.rows_chunk;   // < hw
+  w.rows = p.hw - lo < p.rows_chunk ? p.hw - lo : p.rows_chunk;
+  w.row0 = w.tile * p.hw + lo;
   return w;
 }
 
@@ -695,19 +698,19 @@ __global__ void __launch_bounds__(ST) gn_stat_k(P p) {
     const Own<V> o(p.pack ? (S / V + 15) / 16 * 16 * V : S, ST);
     const bool have_cols = o.tc * V < S;
     const int c0 = w.slice * p.S + o.tc * V;
-    const T* x = (const T*)g.x + w.tile * p.hw * g.ldx + c0;
+    const T* x = (const T*)g.x + w.row0 * g.ldx + c0;
     float n = 0.f, m[V], q[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) m[v] = q[v] = 0.f;
     if (o.on)
-      for (int r = w.lo + o.tr; r < w.hi; r += SE * o.rpp) {
+      for (int r = o.tr; r < w.rows; r += SE * o.rpp) {
         Vec<T, V> buf[SE];
         int have = 0;
 #pragma unroll
         for (int e = 0; e < SE; ++e) {
           const int k = r + e * o.rpp;
-          have += k < w.hi;
-          if (k < w.hi && have_cols) buf[e].load(x + (long long)k * g.ldx);
+          have += k < w.rows;
+          if (k < w.rows && have_cols) buf[e].load(x + (long long)k * g.ldx);
           else buf[e].zero();
         }
         float s[V], d2[V];
@@ -720,10 +723,10 @@ __global__ void __launch_bounds__(ST) gn_stat_k(P p) {
 #pragma unroll
           for (int v = 0; v < V; ++v) s[v] += t[v];
           if constexpr (V == 8) {
-            if (p.pack && r + e * o.rpp < w.hi) {   // (alike in the lanes of a row)
+            if (p.pack && r + e * o.rpp < w.rows) {   // (alike in the lanes of a row)
               const unsigned sc = a8_block_byte(t, 16);
               const float inv = a8_inverse(sc);
-              const long long row = w.tile * p.hw + r + e * o.rpp;
+              const long long row = w.row0 + r + e * o.rpp;
               u32x2 z;
               z[0] = a8_code4(t[0] * inv, t[1] * inv, t[2] * inv, t[3] * inv);
               z[1] = a8_code4(t[4] * inv, t[5] * inv, t[6] * inv, t[7] * inv);
@@ -736,7 +739,7 @@ __global__ void __launch_bounds__(ST) gn_stat_k(P p) {
         for (int v = 0; v < V; ++v) s[v] /= (float)have;
 #pragma unroll
         for (int e = 0; e < SE; ++e) {
-          if (r + e * o.rpp >= w.hi) continue;
+          if (r + e * o.rpp >= w.rows) continue;
           float t[V];
           buf[e].get(t);
 #pragma unroll
@@ -832,8 +835,8 @@ __global__ void __launch_bounds__(ST) gn_apply_k(P p) {
 #pragma unroll
     for (int v = 0; v < V; ++v) { a[v] *= g.gamma[c0 + v]; bet[v] = g.beta[c0 + v]; }
 #pragma unroll 4
-    for (int r = w.lo + o.tr; r < w.hi; r += o.rpp) {
-      const long long row = w.tile * p.hw + r;
+    for (int r = o.tr; r < w.rows; r += o.rpp) {
+      const long long row = w.row0 + r;
       Vec<T, V> b;
       float t[V], u[V];
       b.load((const T*)g.x + row * g.ldx + c0);
@@ -879,21 +882,21 @@ __global__ void __launch_bounds__(ST) gn_bwd_split_k(P p) {
           s[v] = gsum[1] * inv * rstd[v];             // of du gamma
         }
       }
-      for (int r = w.lo + o.tr; r < w.hi; r += RG * o.rpp) {
+      for (int r = o.tr; r < w.rows; r += RG * o.rpp) {
         typename Input<T, V, X8>::type bx[RG];
         Vec<T, V> bd[RG], br[RG];
 #pragma unroll
         for (int k = 0; k < RG; ++k) {   // (rows behind the last: the last one's values, left out below)
           const int at = r + k * o.rpp;
-          const long long row = w.tile * p.hw + (at < w.hi ? at : w.hi - 1);
+          const long long row = w.row0 + (at < w.rows ? at : w.rows - 1);
           load_in(bx[k], p, row, c0);
           bd[k].load((const T*)g.dy + row * g.lddy + c0);
           if constexpr (RES) br[k].load((const T*)g.resid + row * g.ldr + c0);
         }
 #pragma unroll
         for (int k = 0; k < RG; ++k) {
-          if (r + k * o.rpp >= w.hi) break;
-          const long long row = w.tile * p.hw + r + k * o.rpp;
+          if (r + k * o.rpp >= w.rows) break;
+          const long long row = w.row0 + r + k * o.rpp;
           float dy[V], res[V], d[V], du[V];
           less_of<>(bx[k], mean, d);
           bd[k].get(dy);
