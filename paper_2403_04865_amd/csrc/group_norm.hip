@@ -959,6 +959,7 @@ __global__ void __launch_bounds__(GT) gn_bwd_group_k(P p) {
 constexpr int WANT = 1024;              // workgroups of a split launch
 constexpr int SPLIT_SMAX = 2048;
 constexpr long long MOST_P = 4096;      // rows of partial sums that the unit kernels leave
+constexpr long long MOST_WGS = 1 << 22; // workgroups of a unit launch, but for the rounding up to eight tiles (channels <= 65536: 64 tiles of slices at least)
 
 int gcd(int a, int b) { while (b) { const int t = a % b; a = b; b = t; } return a; }
 
@@ -1036,7 +1037,9 @@ bool by_units(P* p, int V, int es, unsigned* grid, bool* small) {
   p->rows = (int)((s.hw + rpp - 1) / rpp);
   if (s.n * p->slices < (es == 4 ? 192 : 128) && p->rows > 16) return false;
   if (es == 4 && s.hw * p->S * es >= 3 << 19) return false;
-  p->units_p = (int)(s.n < MOST_P ? s.n : MOST_P);
+  // A launch may have 2^32 - 1 threads: with thousands of slices (a prime number of channels, each a group of its own) a workgroup takes more tiles
+  const long long most_p = MOST_WGS / p->slices < MOST_P ? MOST_WGS / p->slices : MOST_P;
+  p->units_p = (int)(s.n < most_p ? s.n : most_p);
   *grid = (unsigned)((p->units_p + 7) / 8 * 8 * p->slices);
   return true;
 }

@@ -21,3 +21,32 @@ def test_checkpoints_of_split_rows(n, hw, c, groups, dtype):
 def test_more_groups_than_threads(n, hw, c, groups, dtype):
     _run(n, hw, c, groups, dtype, "silu")
     _run(n, hw, c, groups, dtype, "gelu", checkpoint=True)
+
+
+# 4099 slices of one channel (a prime number of groups) of 4104 tiles: more than 2^32 threads as a workgroup each
+def test_more_units_than_a_launch_has_workgroups():
+    import torch
+    from paper_2403_04865_amd import Act8Lib
+    n, c = 4104, 4099
+    L = Act8Lib()
+    x, dy = torch.randn(n, 2, c, device="cuda"), torch.randn(n, 2, c, device="cuda")
+    gamma, beta = torch.rand(c, device="cuda") + 0.5, torch.randn(c, device="cuda")
+    y, dx = torch.full_like(x, float("nan")), torch.full_like(x, float("nan"))
+    mean, rstd, dg, db = torch.empty(n, c, device="cuda"), torch.empty(n, c, device="cuda"), torch.empty(c, device="cuda"), torch.empty(c, device="cuda")
+    work = torch.empty(L.slide_group_norm_workspace_bytes(n, 2, c, c, torch.float32), dtype=torch.uint8, device="cuda")
+    L.slide_group_norm_fwd(x, gamma, beta, c, y, mean, rstd, eps=0.1, workspace=work)
+    L.slide_group_norm_bwd(dy, x, gamma, beta, mean, rstd, c, dx, dg, db, workspace=work)
+    X, DY, G = x.double(), dy.double(), gamma.double()
+    m = X.mean(1, keepdim=True)
+    r = 1 / torch.sqrt((X - m).square().mean(1, keepdim=True) + 0.1)     # <= 3.2, xhat <= 1
+    h = (X - m) * r
+    U = 2.0 ** -24      # a dozen roundings of parts that are |x|, |xhat|, |dy|, the gain and shift in size, times rstd
+    assert ((y - (h * G + beta)).abs() <= 16 * U * (4 * X.abs().amax(1, keepdim=True) + 2 + beta.abs())).all()
+    assert ((mean - m[:, 0]).abs() <= 4 * U * X.abs().amax(1)).all()
+    t = DY * G
+    want = r * (t - t.mean(1, keepdim=True) - h * (t * h).mean(1, keepdim=True))
+    top = DY.abs().amax(1, keepdim=True)
+    assert ((dx - want).abs() <= 16 * U * r * 1.5 * 3 * top * (1 + 4 * r * X.abs().amax(1, keepdim=True))).all()
+    # a thread adds the four to eight tiles that it takes, 4104 partial sums go together in 64 bits
+    assert ((db - DY.sum((0, 1))).abs() <= 32 * U * DY.abs().sum((0, 1))).all()
+    assert ((dg - (DY * h).sum((0, 1))).abs() <= (32 * U * (DY.abs() * (1 + 4 * r * X.abs().amax(1, keepdim=True)))).sum((0, 1))).all()
