@@ -436,7 +436,9 @@ ACTS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3}
 
 
 class Act8:
-    """A matrix [rows, cols] in 8 bits (include/act8.h): codes [rows, >= cols] uint8, scales [rows, >= ceil(cols / 128)] uint8."""
+    """A matrix [rows, cols] in 8 bits (include/act8.h): codes [rows, >= cols] uint8, scales [rows, >= ceil(cols / 128)] uint8.  The calls write
+    and read every row of codes up to the next multiple of 16 columns: a single row must have them, and the last of several rows' must lie in
+    the tensor's memory."""
 
     def __init__(self, rows, cols, codes, scales):
         if codes.dim() != 2 or scales.dim() != 2 or codes.element_size() != 1 or scales.element_size() != 1:
@@ -447,9 +449,12 @@ class Act8:
             raise ValueError("codes and scales: rows must be contiguous")
         if codes.device != scales.device:
             raise ValueError("codes and scales are on different devices")
+        whole = -(-cols // 16) * 16
+        if codes.shape[1] < whole and (rows == 1 or codes.storage_offset() + (rows - 1) * codes.stride(0) + whole > codes.untyped_storage().nbytes()):
+            raise ValueError(f"codes {tuple(codes.shape)}: a row of {cols} takes {whole} bytes")
         self.rows, self.cols, self.codes, self.scales = rows, cols, codes, scales
         # (the stride that torch reports of a single row says nothing)
-        self._c = _CAct8(codes.data_ptr(), codes.stride(0) if rows > 1 else -(-cols // 16) * 16, scales.data_ptr(),
+        self._c = _CAct8(codes.data_ptr(), codes.stride(0) if rows > 1 else whole, scales.data_ptr(),
                          scales.stride(0) if rows > 1 else max(scales.shape[1], 1), rows, cols)
         self._ref = C.byref(self._c)
 

@@ -1,0 +1,24 @@
+"""What the binding of include/act8.h takes and refuses before a call reaches the library (no GPU)."""
+import pytest
+
+
+def test_rows_of_codes_reach_a_multiple_of_16():
+    import torch
+    from paper_2403_04865_amd import Act8
+    new = lambda *s: torch.zeros(s, dtype=torch.uint8)   # noqa: E731
+    one = new(1, 1)
+    for codes in (new(1, 100), new(1, 111), new(400)[:100].view(1, 100), new(1, 112)[:, :100]):
+        with pytest.raises(ValueError, match="112 bytes"):      # what lies behind 100 is not the row's to write
+            Act8(1, 100, codes, one)
+    assert Act8(1, 100, new(1, 112), one)._c.ldc == 112
+    assert Act8(1, 100, new(1, 128), one)._c.ldc == 112
+    assert Act8(1, 96, new(1, 96), one)._c.ldc == 96
+    # between rows the bytes are the matrix's, behind the last row they have to be there
+    assert Act8(3, 100, new(3, 112)[:, :100], new(3, 1))._c.ldc == 112
+    assert Act8(2, 100, new(3, 112)[1:, :100], new(2, 1))._c.ldc == 112
+    assert Act8(3, 100, new(2 * 112 + 112).as_strided((3, 100), (112, 1)), new(3, 1))._c.ldc == 112
+    for short in (100, 111):
+        with pytest.raises(ValueError, match="112 bytes"):
+            Act8(3, 100, new(2 * 112 + short).as_strided((3, 100), (112, 1)), new(3, 1))
+        with pytest.raises(ValueError, match="112 bytes"):
+            Act8(3, 100, new(5 + 2 * 112 + short).as_strided((3, 100), (112, 1), 5), new(3, 1))
