@@ -334,6 +334,9 @@ class ResNetLib:
     def __init__(self, cfg: ResNetConfig):
         self.lib = load_cdll()
         self.cfg = cfg
+        for v in (cfg.norm_groups, cfg.checkpoint8):
+            if not -2 ** 15 <= v < 2 ** 15:     # their 16 bits would hold another number
+                raise SlideError(-1, "resnet_ctx_create")
         cc = _CResNetConfig(cfg.tile, cfg.block, (C.c_int32 * 4)(*cfg.depths), cfg.width, cfg.mil_hidden, cfg.n_classes,
                             cfg.bn_eps, cfg.norm_groups, cfg.checkpoint8)
         h = C.c_void_p()
