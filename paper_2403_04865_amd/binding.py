@@ -164,6 +164,9 @@ _SYMS.update({
 })
 
 
+_loaded = {}   # the file as it was -> the library with its functions declared (190 us to do again for every Act8Lib)
+
+
 def load_cdll():
     p = lib_path()
     if not os.path.exists(p):
@@ -172,12 +175,16 @@ def load_cdll():
     # loaded first, its own dependency brings up a second runtime and every launch on torch's pointers fails
     # (hipErrorNoDevice).
     import torch  # noqa: F401
-    lib = C.CDLL(p)
-    for name, (res, args) in _SYMS.items():
-        f = getattr(lib, name)
-        f.restype = res
-        f.argtypes = args
-    return lib
+    at = os.stat(p)
+    key = (p, at.st_dev, at.st_ino, at.st_mtime_ns, at.st_size)
+    if key not in _loaded:
+        lib = C.CDLL(p)
+        for name, (res, args) in _SYMS.items():
+            f = getattr(lib, name)
+            f.restype = res
+            f.argtypes = args
+        _loaded[key] = lib
+    return _loaded[key]
 
 
 def _ptr(t):

@@ -22,3 +22,23 @@ def test_rows_of_codes_reach_a_multiple_of_16():
             Act8(3, 100, new(2 * 112 + short).as_strided((3, 100), (112, 1)), new(3, 1))
         with pytest.raises(ValueError, match="112 bytes"):
             Act8(3, 100, new(5 + 2 * 112 + short).as_strided((3, 100), (112, 1), 5), new(3, 1))
+
+
+def test_the_library_is_declared_once():
+    from paper_2403_04865_amd import Act8Lib
+    from paper_2403_04865_amd.binding import load_cdll
+    assert load_cdll() is load_cdll() and Act8Lib().lib is Act8Lib().lib
+
+
+def test_a_library_built_again_is_loaded_again(monkeypatch, tmp_path):
+    import shutil
+
+    from paper_2403_04865_amd import binding
+    at = tmp_path / "libslide.so"
+    shutil.copy(binding.lib_path(), at)
+    monkeypatch.setattr(binding, "lib_path", lambda: str(at))
+    first = binding.load_cdll()
+    again = tmp_path / "new"
+    shutil.copy(at, again)
+    again.rename(at)
+    assert binding.load_cdll() is not first
