@@ -567,7 +567,11 @@ class Act8Lib:
             raise SlideError(rc, what, self.lib.slide_last_hip_error())
 
     def _work(self, t):
-        return (None, 0) if t is None else (t.data_ptr(), t.numel() * t.element_size())
+        if t is None:
+            return None, 0
+        if not t.is_contiguous():
+            raise ValueError("workspace: a contiguous tensor")
+        return t.data_ptr(), t.numel() * t.element_size()
 
     # ---- calls
     def slide_act8_pack(self, x, out, transpose=False, stream=None):

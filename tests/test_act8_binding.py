@@ -42,3 +42,16 @@ def test_a_library_built_again_is_loaded_again(monkeypatch, tmp_path):
     shutil.copy(at, again)
     again.rename(at)
     assert binding.load_cdll() is not first
+
+
+def test_work_space_is_as_large_as_it_says():
+    import torch
+    from paper_2403_04865_amd import Act8, Act8Lib
+    L = Act8Lib()
+    need = L.slide_act8_wgrad_workspace_bytes(1000, 8, 32)
+    with pytest.raises(ValueError, match="contiguous"):      # one byte of memory
+        L.slide_act8_wgrad(torch.zeros(1000, 8), Act8.empty(1000, 32, "cpu"), torch.zeros(8, 32), workspace=torch.zeros(1, dtype=torch.uint8).expand(need))
+    t, f = torch.zeros(2, 9, 24), torch.zeros(2, 4)
+    need = L.slide_group_norm_workspace_bytes(2, 9, 24, 4, torch.float32)
+    with pytest.raises(ValueError, match="contiguous"):
+        L.slide_group_norm_fwd(t, torch.ones(24), torch.zeros(24), 4, t, f, f, workspace=torch.zeros(1).expand(need // 4))
