@@ -61,7 +61,8 @@ int slide_act8_linear(const void* x, int dtype, int64_t ldx, const slide_act8* x
 
 /* Weight gradient of the layer out of the checkpoint of its input: dW[n][k] = sum_m dy[m][n] x8[m][k], db[n] = sum_m dy[m][n],
  * written (accumulate == 0) or added to what is there.  dy: [x8.rows][out] of dtype; dW: float32, lddw between rows; db: [out]
- * float32 or NULL.  Sums in float32, over slabs of rows that are then added in a fixed order: the same bits on every run.
+ * float32 or NULL.  Sums in float32, over slabs of rows that are then added in a fixed order: the same bits on every run.  float32 gradients count
+ * with all their bits, whatever their size; where a result is not finite, or past 2^80 on the way, its part is summed again, more slowly.
  * work: slide_act8_wgrad_workspace_bytes(x8.rows, out, x8.cols) bytes (0 for sizes that are refused).  SLIDE_EUNSUPPORTED for those and
  * where rows of x8's codes or scales are more than 2^24 bytes apart. */
 size_t slide_act8_wgrad_workspace_bytes(int64_t rows, int64_t out, int64_t in);

@@ -1,8 +1,8 @@
 // Weight gradient out of an 8-bit activation checkpoint (gfx950): dW[n][k] = sum_m dy[m][n] x8[m][k], db[n] = sum_m dy[m][n].
 //
-// A code times its power of two is exactly a bfloat16, so the checkpoint is decoded on its way into LDS and the products are the
-// matrix cores' bfloat16 ones with float32 sums; float32 gradients go in as three bfloat16 terms (split_f32.h), which are
-// all of their bits.  The contraction runs over the rows of both operands: 64-row slices lie in LDS as they are in memory and the fragments,
+// A code times its power of two is exactly a bfloat16 (from 2^-133 on), so the checkpoint is decoded on its way into LDS and the products are the
+// matrix cores' bfloat16 ones with float32 sums; float32 gradients go in as three bfloat16 terms of 2^48 times their value (split_f32.h), which
+// are all of their bits, and blocks that come out infinite that way are taken again.  The contraction runs over the rows of both operands: 64-row slices lie in LDS as they are in memory and the fragments,
 // eight consecutive rows of a column per lane, are read with the transposing LDS reads.
 // The rows are split into slabs: a work item is (slab, output tile), writes its partial tile once, and a second kernel adds the slabs
 // in a fixed order.
@@ -72,6 +72,7 @@ __global__ void __launch_bounds__(NTH) wgrad_k(Item it) {
   if (id >= tiles * it.slabs) return;
   const int slab = id / tiles, tile = id % tiles;
   const int x0 = tile / it.TY * BX, y0 = tile % it.TY * BY;
+  const float up = TERMS > 1 ? split_up(slab) : 1.f;   // (slabs of either sign)
   const long long lo = slab * it.per;
   const int span = lo >= g.M ? 0 : (int)(g.M - lo < it.per ? g.M - lo : it.per);
   const int steps = (span + BK - 1) / BK;
@@ -140,7 +141,7 @@ __global__ void __launch_bounds__(NTH) wgrad_k(Item it) {
     float f[8];
     if constexpr (TERMS > 1) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) f[e] = to_f(R.x[i][e]);
+      for (int e = 0; e < 8; ++e) f[e] = to_f(R.x[i][e]) * up;
     }
 #pragma unroll
     for (int t = 0; t < TERMS; ++t) {
@@ -150,7 +151,7 @@ __global__ void __launch_bounds__(NTH) wgrad_k(Item it) {
         if constexpr (TERMS == 1) o[e] = R.x[i][e];
         else {
           o[e] = (bf16)f[e];
-          f[e] = a8_mag((float)o[e]) ? f[e] - (float)o[e] : 0.f;   // (what rounds to an infinity, or is none, has no further terms)
+          f[e] -= (float)o[e];   // (no number behind what rounds to an infinity: such blocks are taken again)
         }
       }
       *reinterpret_cast<bf16x8*>(p + t * BX) = o;
@@ -261,6 +262,38 @@ __global__ void __launch_bounds__(NTH) wgrad_k(Item it) {
     if (s + 1 < steps) step(s + 1, ring1, ring0, r1, s1);
   }
 
+  // Float32: back from 2^48.  A block with a result that is not finite (a gradient of 2^80 or more, a result as large, an infinity, a NaN) is taken
+  // again from memory, in sums of double: 403456 x 384 -> 1536 with one NaN in it 106 ms, 2 without.
+  if constexpr (TERMS > 1) {
+    if (not_finite(acc)) {   // of this wavefront
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < WBN; ++j) {
+          const int n0 = x0 + (wm * 2 + i) * 32 + 4 * (lane >> 5), k0 = y0 + (wn * WBN + j) * 32 + (lane & 31), k = k0 < g.K ? k0 : g.K - 1;
+          const long long n_last = g.N - 1;   // (what is not there: the last one again; it is not stored)
+          double a[16];
+#pragma unroll
+          for (int r = 0; r < 16; ++r) a[r] = 0.0;
+#pragma unroll 4
+          for (int m = 0; m < span; ++m) {
+            const T* d = (const T*)g.dy + (lo + m) * g.lddy;
+            const double v = __builtin_amdgcn_cvt_f32_fp8(g.x.codes[(lo + m) * g.x.ldc + k], 0) * a8_scale(g.x.scales[(lo + m) * g.x.lds + (k >> 7)]);
+            float t[16];
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+              const long long n = n0 + 8 * (r >> 2) + (r & 3);
+              t[r] = to_f(d[n < n_last ? n : n_last]);
+            }
+#pragma unroll
+            for (int r = 0; r < 16; ++r) a[r] = fma((double)t[r], v, a[r]);
+          }
+#pragma unroll
+          for (int r = 0; r < 16; ++r) acc[i][j][r] = (float)a[r];
+        }
+    } else scale_down(acc, up);
+  }
+
   // lane: column l % 32, rows 8 (r / 4) + 4 (l / 32) + r % 4
   const bool direct = it.slabs == 1;
   float* out = direct ? g.dW : it.part + (long long)slab * g.N * g.K;
@@ -290,7 +323,16 @@ __global__ void __launch_bounds__(NTH) wgrad_k(Item it) {
     }
     __syncthreads();
     if (tid < BX && x0 + tid < g.N) {
-      const float v = (red[tid] + red[BX + tid]) + (red[2 * BX + tid] + red[3 * BX + tid]);
+      float v = (red[tid] + red[BX + tid]) + (red[2 * BX + tid] + red[3 * BX + tid]);
+      if constexpr (TERMS > 1) {
+        if (a8_mag(v) || v == 0.f) v *= 1.0f / SPLIT_UP / SPLIT_UP * up;
+        else {   // not finite: as above
+          double a = 0.0;
+#pragma unroll 1
+          for (int m = 0; m < span; ++m) a += to_f(((const T*)g.dy)[(lo + m) * g.lddy + x0 + tid]);
+          v = (float)a;
+        }
+      }
       if (direct) g.db[x0 + tid] = g.accumulate ? g.db[x0 + tid] + v : v;
       else it.cpart[(long long)slab * g.N + x0 + tid] = v;
     }
