@@ -27,8 +27,8 @@ that is the plain batch statistic over every tile of the slide).
 
 Group normalisation (cfg.norm_groups > 0) stands in the same places, with the statistics of a tile's group of channels
 instead of the batch's.  With cfg.checkpoint8 its backward sees the convolution's output as its 8-bit
-checkpoint holds it (act8_oracle.pack), under the forward's statistics; ReLU decisions in front of
-which such a normalisation stands are taken there too.
+checkpoint holds it (act8_oracle.pack), under the forward's statistics; the ReLUs' decisions are the
+forward's.
 
 Storage precision.  The paper trains these encoders with 16-bit mixed precision (Method, the
 tiles-per-device figures with automatic mixed precision), and a ReLU or a max pooling turns a
@@ -117,14 +117,13 @@ def _group_mean(x, groups):
 
 def gn_fwd(x, g, b, eps, groups, kept=None):
     """Group normalisation (biased variance over a tile's group of channels and all positions).  kept: what the backward
-    sees in x's place.  Also returned: the output that the kept values give."""
+    sees in x's place."""
     mu = _group_mean(x, groups)
     rstd = 1.0 / np.sqrt(_group_mean((x - mu) ** 2, groups) + eps)
     gg, bb = g[None, :, None, None], b[None, :, None, None]
     y = (x - mu) * rstd * gg + bb
-    xh = (x if kept is None else kept) - mu
-    xh = xh * rstd
-    return y, (xh, rstd, groups), y if kept is None else xh * gg + bb
+    xh = ((x if kept is None else kept) - mu) * rstd
+    return y, (xh, rstd, groups)
 
 
 def gn_bwd(dy, g, cache):
@@ -187,16 +186,15 @@ def _identity(a):
 
 
 def _conv_bn(P, x, conv, bn, stride, pad, cfg, store):
-    """Output behind the normalisation, the cache, and the output on which the backward takes a ReLU's decisions
-    (None: the stored activation)."""
+    """Output behind the normalisation, and the cache."""
     c = store(conv2d_fwd(x, P[conv + ".W"], stride, pad))
     groups = getattr(cfg, "norm_groups", 0)
     if not groups:
         y, bc = bn_fwd(c, P[bn + ".g"], P[bn + ".b"], cfg.bn_eps)
-        return y, (x, conv, bn, stride, pad, bc), None
-    kept = checkpoint_values(c) if cfg.checkpoint8 else None
-    y, bc, u = gn_fwd(c, P[bn + ".g"], P[bn + ".b"], cfg.bn_eps, groups, kept)
-    return y, (x, conv, bn, stride, pad, bc), u if cfg.checkpoint8 else None
+    else:
+        kept = checkpoint_values(c) if cfg.checkpoint8 else None
+        y, bc = gn_fwd(c, P[bn + ".g"], P[bn + ".b"], cfg.bn_eps, groups, kept)
+    return y, (x, conv, bn, stride, pad, bc)
 
 
 def _conv_bn_bwd(P, g, dy, cache):
@@ -206,18 +204,18 @@ def _conv_bn_bwd(P, g, dy, cache):
     return dx
 
 
-def _relu(y, u, store):
+def _relu(y, store):
     """The stored activation and where its backward lets a gradient pass."""
     r = store(np.maximum(y, 0.0))
-    return r, (r if u is None else u) > 0.0
+    return r, r > 0.0
 
 
 def encoder_fwd(prm, X, cfg, dtype=np.float64, store=_identity):
     """Tile features H [n, dim] and the cache for encoder_bwd.  X: [n,3,S,S] normalised pixels."""
     P = {k: np.asarray(v, dtype=dtype) for k, v in prm.items() if not k.startswith(("mil.", "head."))}
     x = np.asarray(X, dtype=dtype)
-    y, c0, u = _conv_bn(P, x, "stem.conv", "stem.bn", 2, 3, cfg, store)
-    r0, on0 = _relu(y, u, store)
+    y, c0 = _conv_bn(P, x, "stem.conv", "stem.bn", 2, 3, cfg, store)
+    r0, on0 = _relu(y, store)
     x, mp = maxpool_fwd(r0)
     caches = []
     for name, stride, down in _blocks(cfg):
@@ -229,18 +227,18 @@ def encoder_fwd(prm, X, cfg, dtype=np.float64, store=_identity):
             convs = [("conv1", "bn1", 1, 0), ("conv2", "bn2", stride, 1), ("conv3", "bn3", 1, 0)]
         ks, on, r = [], [], x0
         for i, (cv, bn, st, pad) in enumerate(convs):
-            body, k, u = _conv_bn(P, r, p + cv, p + bn, st, pad, cfg, store)
+            body, k = _conv_bn(P, r, p + cv, p + bn, st, pad, cfg, store)
             ks.append(k)
             if i + 1 < len(convs):
-                r, m = _relu(body, u, store)
+                r, m = _relu(body, store)
                 on.append(m)
         if down:
-            sc, kd, _ = _conv_bn(P, x0, p + "down.conv", p + "down.bn", stride, 0, cfg, store)
+            sc, kd = _conv_bn(P, x0, p + "down.conv", p + "down.bn", stride, 0, cfg, store)
             if getattr(cfg, "norm_groups", 0):
                 sc = store(sc)     # written on its own there
         else:
             sc, kd = x0, None
-        x, m = _relu(body + sc, None if u is None else u + sc, store)
+        x, m = _relu(body + sc, store)
         caches.append((ks, on, kd, m))
     H = x.mean(axis=(2, 3))
     return H, {"P": P, "stem": (c0, on0, mp), "blocks": caches, "last_shape": x.shape}

@@ -129,6 +129,7 @@ struct GroupNorm {
   const void* x; long long ldx;       // bwd: null = from x8
   const float *gamma, *beta;
   const void* resid; long long ldr;
+  const void* out; long long ldo;     // bwd of a rectifier from x8, bfloat16: what the forward put out (resid is not read then), or null
   void* y; long long ldy;             // bwd: dx
   const slide_act8* x8;               // fwd: written (may be null); bwd: read where x is null
   float *mean, *rstd;

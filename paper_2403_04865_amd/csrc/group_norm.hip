@@ -449,12 +449,21 @@ __global__ void __launch_bounds__(TH, 4) gn_fwd_k(P p) {
   }
 }
 
+// The third matrix that a backward reads: none, the residual, or (rectifiers only) what the forward put out, which says where it let
+// values through.  Then du = dy where that is positive, and neither the sum nor its residual is formed.
+enum Third { NONE, RESID, OUT };
+
 // du = dy act'(u) of V values, u = (x - mean) (rstd gamma) + beta + residual.  A rectifier asks which side of zero u is on: where float32
 // cannot tell, it is formed again in double (mean and rstd are what the forward stored).  The kernels of that branch are their own
 // (RELU): in the others it would cost up to 50 registers (1024 tiles of 56 x 56 x 64, SiLU out of a checkpoint: 340 us with it, 310 without).
-template <bool RES, bool RELU, int V, typename F>
+template <Third RES, bool RELU, int V, typename F>
 __device__ __forceinline__ void du_vec(const float (&d)[V], const float (&dy)[V], const float (&rg)[V], const float (&bet)[V], const float (&res)[V],
                                        int act, float (&du)[V], F exactly) {
+  if constexpr (RES == OUT) {
+#pragma unroll
+    for (int v = 0; v < V; ++v) du[v] = res[v] > 0.f ? dy[v] : 0.f * dy[v];
+    return;
+  }
   if (!RELU && act == SLIDE_ACT_NONE) {
 #pragma unroll
     for (int v = 0; v < V; ++v) du[v] = dy[v];
@@ -463,7 +472,7 @@ __device__ __forceinline__ void du_vec(const float (&d)[V], const float (&dy)[V]
   float u[V];
 #pragma unroll
   for (int v = 0; v < V; ++v) u[v] = fmaf(d[v], rg[v], bet[v]);
-  if constexpr (RES) {
+  if constexpr (RES != NONE) {
 #pragma unroll
     for (int v = 0; v < V; ++v) u[v] += res[v];
   }
@@ -471,7 +480,7 @@ __device__ __forceinline__ void du_vec(const float (&d)[V], const float (&dy)[V]
     // u is off by less than 1e-6 of its parts' magnitudes; where it is as small as that, the first part is as large as the others
     bool near = false;
 #pragma unroll
-    for (int v = 0; v < V; ++v) near |= fabsf(u[v]) <= 2.1e-6f * (RES ? fabsf(bet[v]) + fabsf(res[v]) : fabsf(bet[v]));
+    for (int v = 0; v < V; ++v) near |= fabsf(u[v]) <= 2.1e-6f * (RES != NONE ? fabsf(bet[v]) + fabsf(res[v]) : fabsf(bet[v]));
     if (near) {
 #pragma unroll
       for (int v = 0; v < V; ++v) { u[v] = exactly(v); __builtin_amdgcn_sched_barrier(0); }
@@ -508,7 +517,7 @@ __device__ __forceinline__ float side(double x, double mean, double rstd, double
   return u > 0.0 ? 1.f : u < 0.0 ? -1.f : (float)u;
 }
 
-template <typename T, int V, int TH, int KG, bool X8, bool RES, bool RELU>
+template <typename T, int V, int TH, int KG, bool X8, Third RES, bool RELU>
 __global__ void __launch_bounds__(TH, 2) gn_bwd_k(P p) {
   __shared__ float red[2 * TH * V], gs[2][SMAX], cm[SMAX], cr[SMAX], crg[SMAX], cbet[SMAX], red2[TH];
   const GroupNorm& g = p.g;
@@ -533,9 +542,9 @@ __global__ void __launch_bounds__(TH, 2) gn_bwd_k(P p) {
                                          : tile_buffer((const T*)g.x + r0 * g.ldx + s0, g.ldx, es, p.hw, p.S);
     const __amdgpu_buffer_rsrc_t sb = tile_buffer(X8 ? p.x8.scales + r0 * p.x8.lds : nullptr, p.x8.lds, 1, p.hw, (p.C + 127) >> 7);
     const __amdgpu_buffer_rsrc_t db = tile_buffer((const T*)g.dy + r0 * g.lddy + s0, g.lddy, es, p.hw, p.S);
-    const __amdgpu_buffer_rsrc_t rb = tile_buffer(RES ? (const T*)g.resid + r0 * g.ldr + s0 : nullptr, g.ldr, es, p.hw, p.S);
+    const __amdgpu_buffer_rsrc_t rb = tile_buffer(RES != NONE ? (const T*)g.resid + r0 * g.ldr + s0 : nullptr, g.ldr, es, p.hw, p.S);
     typedef typename Input<T, V, X8>::type In;
-    struct Rows { In x[RG]; Vec<T, V> d[RG], w[RES ? RG : 1]; } kept[KG];
+    struct Rows { In x[RG]; Vec<T, V> d[RG], w[RES != NONE ? RG : 1]; } kept[KG];
     auto load = [&](Rows& b, int e) __attribute__((always_inline)) {
 #pragma unroll
       for (int k = 0; k < RG; ++k) {
@@ -543,7 +552,7 @@ __global__ void __launch_bounds__(TH, 2) gn_bwd_k(P p) {
         if constexpr (X8) b.x[k].load(xb, vx, row * ldx, sb, vs, row * lds);
         else b.x[k].load(xb, vx, row * ldx);
         b.d[k].load(db, vd, row * ldd);
-        if constexpr (RES) b.w[k].load(rb, vr, row * ldr);
+        if constexpr (RES != NONE) b.w[k].load(rb, vr, row * ldr);
       }
     };
 #pragma unroll
@@ -566,11 +575,11 @@ __global__ void __launch_bounds__(TH, 2) gn_bwd_k(P p) {
         float dy[V], res[V], d[V], du[V];
         less_of<>(b.x[k], m, d);
         b.d[k].get(dy);
-        if constexpr (RES) b.w[k].get(res);
+        if constexpr (RES != NONE) b.w[k].get(res);
         du_vec<RES, RELU, V>(d, dy, rg, bet, res, act, du, [&](int v) __attribute__((always_inline)) {
           float x[V];
           b.x[k].get(x);
-          return side(x[v], m[v], cr[at + v], g.gamma[s0 + at + v], bet[v], RES ? res[v] : 0.f);
+          return side(x[v], m[v], cr[at + v], g.gamma[s0 + at + v], bet[v], RES != NONE ? res[v] : 0.f);
         });
         f(d, du, e + k);
         row_end();
@@ -856,7 +865,7 @@ __global__ void __launch_bounds__(ST) gn_apply_k(P p) {
 }
 
 // DX false: the chunk's sums of du xhat and du per channel -> part; true: dx (and dresidual) out of the groups' sums
-template <typename T, int V, bool X8, bool DX, bool RES, bool RELU>
+template <typename T, int V, bool X8, bool DX, Third RES, bool RELU>
 __global__ void __launch_bounds__(ST) gn_bwd_split_k(P p) {
   __shared__ __attribute__((aligned(16))) float red[DX ? 1 : ST * V];
   __shared__ float red2[DX ? 1 : ST], ch[DX ? 1 : ST * V];
@@ -891,7 +900,7 @@ __global__ void __launch_bounds__(ST) gn_bwd_split_k(P p) {
           const long long row = w.row0 + (at < w.rows ? at : w.rows - 1);
           load_in(bx[k], p, row, c0);
           bd[k].load((const T*)g.dy + row * g.lddy + c0);
-          if constexpr (RES) br[k].load((const T*)g.resid + row * g.ldr + c0);
+          if constexpr (RES != NONE) br[k].load((const T*)g.resid + row * g.ldr + c0);
         }
 #pragma unroll
         for (int k = 0; k < RG; ++k) {
@@ -900,11 +909,11 @@ __global__ void __launch_bounds__(ST) gn_bwd_split_k(P p) {
           float dy[V], res[V], d[V], du[V];
           less_of<>(bx[k], mean, d);
           bd[k].get(dy);
-          if constexpr (RES) br[k].get(res);
+          if constexpr (RES != NONE) br[k].get(res);
           du_vec<RES, RELU, V>(d, dy, rg, bet, res, act, du, [&](int v) __attribute__((always_inline)) {
             float x[V];
             bx[k].get(x);
-            return side(x[v], mean[v], rstd[v], g.gamma[c0 + v], bet[v], RES ? res[v] : 0.f);
+            return side(x[v], mean[v], rstd[v], g.gamma[c0 + v], bet[v], RES != NONE ? res[v] : 0.f);
           });
           if constexpr (DX) {
             if (g.dresid) store_vec((T*)g.dresid + row * g.lddr + c0, du);
@@ -1094,7 +1103,7 @@ hipError_t fwd(const GroupNorm& g, hipStream_t s) {
   return hipGetLastError();
 }
 
-template <typename T, int V, bool X8, bool RES, bool RELU>
+template <typename T, int V, bool X8, Third RES, bool RELU>
 hipError_t bwd_units(const P& p, unsigned grid, bool small, hipStream_t s) {
   if (small) gn_bwd_k<T, V, 256, KEPT, X8, RES, RELU><<<grid, 256, 0, s>>>(p);
   else gn_bwd_k<T, V, 512, KEPT, X8, RES, RELU><<<grid, 512, 0, s>>>(p);
@@ -1102,7 +1111,7 @@ hipError_t bwd_units(const P& p, unsigned grid, bool small, hipStream_t s) {
 }
 
 // the sums of the chunks, of the groups, then dx
-template <typename T, int V, bool X8, bool RES, bool RELU>
+template <typename T, int V, bool X8, Third RES, bool RELU>
 hipError_t bwd_split(const P& p, hipStream_t s) {
   gn_bwd_split_k<T, V, X8, false, RES, RELU><<<split_grid(p), ST, 0, s>>>(p);
   hipError_t err = hipGetLastError();
@@ -1127,14 +1136,22 @@ hipError_t bwd(const GroupNorm& g, hipStream_t s) {
     split_plan(g.s, V, &p);
     p.sums = g.work + part_floats(g.s);
   }
-  const hipError_t err = either(!g.x, [&](auto x8) {
-    return either(g.resid, [&](auto res) {
+  auto run = [&](auto x8, auto third, auto relu) {
+    constexpr bool X8 = decltype(x8)::value, RELU = decltype(relu)::value;
+    constexpr Third RES = decltype(third)::value;
+    return units ? bwd_units<T, V, X8, RES, RELU>(p, grid, small, s) : bwd_split<T, V, X8, RES, RELU>(p, s);
+  };
+  hipError_t err;
+  if (g.out) {
+    if constexpr (sizeof(T) == 2 && V == 8) err = run(std::true_type{}, std::integral_constant<Third, OUT>{}, std::true_type{});
+    else return hipErrorInvalidValue;   // the convolutional encoder's rows are whole pieces
+  } else {
+    err = either(!g.x, [&](auto x8) {
       return either(g.s.act == SLIDE_ACT_RELU, [&](auto relu) {
-        constexpr bool X8 = decltype(x8)::value, RES = decltype(res)::value, RELU = decltype(relu)::value;
-        return units ? bwd_units<T, V, X8, RES, RELU>(p, grid, small, s) : bwd_split<T, V, X8, RES, RELU>(p, s);
+        return g.resid ? run(x8, std::integral_constant<Third, RESID>{}, relu) : run(x8, std::integral_constant<Third, NONE>{}, relu);
       });
     });
-  });
+  }
   if (err != hipSuccess) return err;
   gn_sum_k<<<(p.C + 15) / 16, 1024, 0, s>>>(p.part, units ? p.units_p : p.n * p.chunks, p.C, g.dgamma, g.dbeta, g.accumulate);
   return hipGetLastError();
@@ -1152,7 +1169,9 @@ hipError_t launch_group_norm_fwd(const GroupNorm& g, hipStream_t s) {
   return V == 8 ? fwd<bf16, 8>(g, s) : fwd<bf16, 1>(g, s);
 }
 
-hipError_t launch_group_norm_bwd(const GroupNorm& g, hipStream_t s) {
+hipError_t launch_group_norm_bwd(const GroupNorm& given, hipStream_t s) {
+  GroupNorm g = given;
+  if (g.out) { g.resid = g.out; g.ldr = g.ldo; }   // read in the residual's place
   const int V = pieces(g, true);
   if (g.s.dtype == DT_F32) return V == 8 ? bwd<float, 8>(g, s) : bwd<float, 1>(g, s);
   return V == 8 ? bwd<bf16, 8>(g, s) : bwd<bf16, 1>(g, s);

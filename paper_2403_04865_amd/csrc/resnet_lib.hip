@@ -296,18 +296,22 @@ void gn_fwd(Run& r, int id, long long n, int resid, int act_, int t_out) {
          [&] { return launch_group_norm_fwd(g, r.s); });
 }
 
-// dx (rows of the convolution's output) from dy through ReLU and group normalisation; dresid (may be null): the gradient behind the
-// ReLU, which is the residual's
-void gn_bwd(Run& r, int id, long long n, const bf16* dy, int resid, int act_, bf16* dx, bf16* dresid, int accumulate) {
+// dx (rows of the convolution's output) from dy through ReLU (t_relu: its output; -1: none) and group normalisation; dresid (may be null): the
+// gradient behind the ReLU, which is the residual's.  With 8-bit checkpoints the ReLU's decisions are read from its output, which the arena holds: taken
+// again on the rounded values they were other ones now and then, and gradients 0.15 to 0.3 off.
+void gn_bwd(Run& r, int id, long long n, const bf16* dy, int resid, int t_relu, bf16* dx, bf16* dresid, int accumulate) {
   resnet_ctx* c = r.c;
   const ConvL& L = c->convs[id];
-  GroupNorm g = norm_call(c, L, n, resid, act_);
+  const bool kept = c->cfg.checkpoint8 && t_relu >= 0;
+  if (kept) resid = -1;
+  GroupNorm g = norm_call(c, L, n, resid, t_relu >= 0 ? SLIDE_ACT_RELU : SLIDE_ACT_NONE);
   const slide_act8 x8 = act8_of(c, L.t_conv, n);
+  if (kept) { g.out = act(c, t_relu); g.ldo = L.Cout; }
   if (c->cfg.checkpoint8) g.x8 = &x8;
   else { g.x = act(c, L.t_conv); g.ldx = L.Cout; }
   g.dy = dy; g.lddy = L.Cout; g.y = dx; g.ldy = L.Cout; g.dresid = dresid; g.lddr = L.Cout;
   g.dgamma = c->grads + L.og; g.dbeta = c->grads + L.ob; g.accumulate = accumulate != 0;
-  launch(r, RK_BN_BWD, 0, (double)rows_of(c, L.t_conv, n) * L.Cout * ((g.x ? 6 : 5) + (resid >= 0 ? 2 : 0) + (dresid ? 2 : 0)),
+  launch(r, RK_BN_BWD, 0, (double)rows_of(c, L.t_conv, n) * L.Cout * ((g.x ? 6 : 5) + (resid >= 0 || kept ? 2 : 0) + (dresid ? 2 : 0)),
          [&] { return launch_group_norm_bwd(g, r.s); });
 }
 
@@ -467,15 +471,15 @@ int enc_bwd(resnet_ctx* c, const void* dfeats, long long n, int accumulate, hipS
     if (gn) {
       // gA: gradient at the block's output, in its place then the gradient of the sum (behind the ReLU); an identity shortcut ends
       // there: the residual branch is added to it
-      gn_bwd(r, b.conv[b.nconv - 1], n, gA, shortcut(c, b), SLIDE_ACT_RELU, gB, gA, accumulate);
+      gn_bwd(r, b.conv[b.nconv - 1], n, gA, shortcut(c, b), b.t_out, gB, gA, accumulate);
       for (int k = b.nconv - 1; k >= 0; --k) {
         conv_wgrad(sums, b.conv[k], n, gB, accumulate);
         if (k == 0 && b.down < 0) conv_dgrad(r, b.conv[k], n, gB, gA, 1);
         else conv_dgrad(r, b.conv[k], n, gB, gC, 0);
-        if (k > 0) gn_bwd(r, b.conv[k - 1], n, gC, -1, SLIDE_ACT_RELU, gB, nullptr, accumulate);
+        if (k > 0) gn_bwd(r, b.conv[k - 1], n, gC, -1, b.t_r[k - 1], gB, nullptr, accumulate);
       }
       if (b.down >= 0) {
-        gn_bwd(r, b.down, n, gA, -1, SLIDE_ACT_NONE, gB, nullptr, accumulate);
+        gn_bwd(r, b.down, n, gA, -1, -1, gB, nullptr, accumulate);
         conv_wgrad(sums, b.down, n, gB, accumulate);
         conv_dgrad(r, b.down, n, gB, gC, 1);
         bf16* t = gA; gA = gC; gC = t;
@@ -507,7 +511,7 @@ int enc_bwd(resnet_ctx* c, const void* dfeats, long long n, int accumulate, hipS
     launch(r, RK_POOLING, 0, (double)rows_of(c, c->t_r0, n) * a.C * 2 * 1.375, [&] {
       return launch_maxpool_bwd((const unsigned char*)(c->arena + c->lay.parg), gA, gB, n, a.H, a.H, a.C, s);
     });
-    if (gn) gn_bwd(r, 0, n, gB, -1, SLIDE_ACT_RELU, gC, nullptr, accumulate);
+    if (gn) gn_bwd(r, 0, n, gB, -1, c->t_r0, gC, nullptr, accumulate);
     else bn_bwd(r, 0, n, gB, act_bits(c, c->t_r0), gC, accumulate);
     conv_wgrad(sums, 0, n, gC, accumulate);
   }
