@@ -694,17 +694,19 @@ __device__ __forceinline__ Where where(const P& p, long long unit) {
   return w;
 }
 
-// partial statistics of a chunk: part[tile * chunks + chunk][0 mean, 1 squared distances][C]
-template <typename T, int V>
+// Partial statistics of a chunk: part[tile * chunks + chunk][0 mean, 1 squared distances][C].
+// A checkpoint may be written on the way (p.pack).  NARROW: all 2, 4 or 8 lanes of a row hold its only block of columns.  Else sixteen lanes hold a
+// block; rows that are not whole sixteens are padded to them, and the lanes behind the last column go along with zeros (left out, they would cut the
+// exchange of the block's maximum between the others).  Unpadded, a checkpoint leaves the order of the statistics' sums, and so their last
+// bits, as they are without.
+template <typename T, int V, bool NARROW>
 __global__ void __launch_bounds__(ST) gn_stat_k(P p) {
   __shared__ float sn[ST], sm[ST * V], sq[ST * V];
   const GroupNorm& g = p.g;
   for (long long unit = blockIdx.x; unit < p.n * p.chunks * p.slices; unit += gridDim.x) {
     const Where w = where(p, unit);
     const int S = p.C - w.slice * p.S < p.S ? p.C - w.slice * p.S : p.S;   // the last slice may be short
-    // With a checkpoint the pieces of a row are padded to whole DPP rows of 16 lanes, which hold a block of its columns.  Lanes behind the last
-    // column go along with zeros: left out, they would cut the exchange of the block's maximum between the others.
-    const Own<V> o(p.pack ? (S / V + 15) / 16 * 16 * V : S, ST);
+    const Own<V> o(!NARROW && p.pack ? (S / V + 15) / 16 * 16 * V : S, ST);
     const bool have_cols = o.tc * V < S;
     const int c0 = w.slice * p.S + o.tc * V;
     const T* x = (const T*)g.x + w.row0 * g.ldx + c0;
@@ -733,14 +735,14 @@ __global__ void __launch_bounds__(ST) gn_stat_k(P p) {
           for (int v = 0; v < V; ++v) s[v] += t[v];
           if constexpr (V == 8) {
             if (p.pack && r + e * o.rpp < w.rows) {   // (alike in the lanes of a row)
-              const unsigned sc = a8_block_byte(t, 16);
+              const unsigned sc = a8_block_byte(t, NARROW ? p.pack : 16);
               const float inv = a8_inverse(sc);
               const long long row = w.row0 + r + e * o.rpp;
               u32x2 z;
               z[0] = a8_code4(t[0] * inv, t[1] * inv, t[2] * inv, t[3] * inv);
               z[1] = a8_code4(t[4] * inv, t[5] * inv, t[6] * inv, t[7] * inv);
               if (have_cols) *reinterpret_cast<u32x2*>(const_cast<uint8_t*>(p.x8.codes) + row * p.x8.ldc + c0) = z;
-              if (have_cols && (o.tc & 15) == 0) const_cast<uint8_t*>(p.x8.scales)[row * p.x8.lds + (c0 >> 7)] = (uint8_t)sc;
+              if (have_cols && (o.tc & (NARROW ? p.pack - 1 : 15)) == 0) const_cast<uint8_t*>(p.x8.scales)[row * p.x8.lds + (c0 >> 7)] = (uint8_t)sc;
             }
           }
         }
@@ -1084,8 +1086,8 @@ hipError_t fwd(const GroupNorm& g, hipStream_t s) {
   // the last column is to be cleared.
   if (g.x8) {
     const int vpr = p.S / 8;
-    if (V == 8 && p.C % A8_GRAIN == 0 && (!units || p.S % A8_BLOCK == 0)) p.pack = 16;
-    else if (V == 8 && p.C % A8_GRAIN == 0 && p.S == p.C && p.C < A8_BLOCK && (vpr & (vpr - 1)) == 0) p.pack = vpr;
+    if (V == 8 && p.C % A8_GRAIN == 0 && p.S == p.C && p.C < A8_BLOCK && (vpr & (vpr - 1)) == 0) p.pack = vpr;
+    else if (V == 8 && p.C % A8_GRAIN == 0 && (!units || p.S % A8_BLOCK == 0)) p.pack = 16;
     else {
       const hipError_t e = launch_act8_pack(g.x, g.s.dtype, g.ldx, false, *g.x8, s);   // before y, which may be x, is written
       if (e != hipSuccess) return e;
@@ -1093,7 +1095,8 @@ hipError_t fwd(const GroupNorm& g, hipStream_t s) {
   }
   if (units) return fwd_units<T, V>(p, grid, small, s);
   p.part = g.work;
-  gn_stat_k<T, V><<<split_grid(p), ST, 0, s>>>(p);
+  if (V == 8 && p.pack && p.pack < 16) gn_stat_k<T, V, V == 8><<<split_grid(p), ST, 0, s>>>(p);
+  else gn_stat_k<T, V, false><<<split_grid(p), ST, 0, s>>>(p);
   hipError_t err = hipGetLastError();
   if (err != hipSuccess) return err;
   gn_stat_group_k<<<group_grid(p), GT, 0, s>>>(p);

@@ -50,3 +50,29 @@ def test_more_units_than_a_launch_has_workgroups():
     # a thread adds the four to eight tiles that it takes, 4104 partial sums go together in 64 bits
     assert ((db - DY.sum((0, 1))).abs() <= 32 * U * DY.abs().sum((0, 1))).all()
     assert ((dg - (DY * h).sum((0, 1))).abs() <= (32 * U * (DY.abs() * (1 + 4 * r * X.abs().amax(1, keepdim=True)))).sum((0, 1))).all()
+
+
+# A checkpoint is written on the way: where a row's lanes need no padding (2, 4, 8 or a multiple of 16 of them, rows of up to 2048 channels or a multiple of
+# that) the results keep their bits
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("n,hw,c,groups", [(1, 9001, 16, 4), (1, 9001, 32, 8), (3, 12544, 64, 32), (2, 5000, 128, 32), (1, 3000, 384, 32), (1, 700, 2048, 32),
+                                           (1, 90, 4096, 64), (40, 784, 64, 32), (30, 49, 96, 8)])
+def test_a_checkpoint_leaves_the_results_as_they_are(n, hw, c, groups, dtype):
+    import torch
+    from paper_2403_04865_amd import Act8, Act8Lib
+    t = {"bf16": torch.bfloat16, "fp32": torch.float32}[dtype]
+    print("case", n, hw, c, groups, dtype, flush=True)
+    gen = torch.Generator(device="cuda").manual_seed(c)
+    x = (torch.randn(n, hw, c, device="cuda", generator=gen) * torch.exp(torch.randn(c, device="cuda", generator=gen)) + 1).to(t)
+    gamma, beta = torch.randn(c, device="cuda", generator=gen), torch.randn(c, device="cuda", generator=gen)
+    L = Act8Lib()
+    work = torch.empty(L.slide_group_norm_workspace_bytes(n, hw, c, groups, t), dtype=torch.uint8, device="cuda")
+    outs = []
+    for x8 in (None, Act8.empty(n * hw, c)):
+        y, mean, rstd = torch.full_like(x, float("nan")), torch.empty(n, groups, device="cuda"), torch.empty(n, groups, device="cuda")
+        L.slide_group_norm_fwd(x, gamma, beta, groups, y, mean, rstd, act="silu", x8=x8, workspace=work)
+        outs.append((y, mean, rstd))
+    assert all(torch.equal(a, b) for a, b in zip(*outs))
+    alone = Act8.empty(n * hw, c)
+    L.slide_act8_pack(x.view(n * hw, c), alone)
+    assert torch.equal(alone.codes, x8.codes) and torch.equal(alone.scales, x8.scales)

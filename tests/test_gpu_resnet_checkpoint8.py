@@ -18,7 +18,7 @@ pytestmark = pytest.mark.gpu
 
 @pytest.mark.timeout(300)
 @pytest.mark.parametrize("name,n,tile,groups", [("rn_tiny", 6, None, 32), ("rn_tiny_bneck", 5, None, 8), ("rn_tiny", 7, 96, 1), ("rn_tiny", 3, None, 64),
-                                                ("rn_tiny", 40, None, 16)])
+                                                ("rn_tiny", 40, None, 16), ("rn18_small", 3, None, 32)])
 def test_gradients_are_those_without(name, n, tile, groups):
     cfg, prm, X, label = resnet_inputs(name, n, None, tile)
     cfg = replace(cfg, norm_groups=groups)
