@@ -657,7 +657,7 @@ hipError_t rows(const A8Linear& g, hipStream_t s) {
 template <int ACT, typename T>
 hipError_t run(const A8Linear& given, hipStream_t s) {
   A8Linear g = given;
-  const long long t128 = ((g.M + 127) / 128) * ((g.N + 127) / 128), t256 = ((g.M + 255) / 256) * ((g.N + 255) / 256);
+  const long long t128 = ((g.M + 127) / 128) * ((g.N + 127) / 128);
   // 32-bit offsets within a tile's rows; the launch's threads within 2^32
   const bool near = g.x.ldc <= (1 << 22) && g.w.ldc <= (1 << 22) && g.ldy <= (1 << 21) && g.ldr <= (1 << 21) && t128 < (1 << 22);
   const bool fewer = !near || g.M <= 64 || t128 < 64;
@@ -688,7 +688,14 @@ hipError_t run(const A8Linear& given, hipStream_t s) {
   if (fewer) return few<ACT, T>(g, s);
   if constexpr (sizeof(T) == 2) {
     if (rows_k) return rows<ACT>(g, s);
-    if (t256 >= 144) return tiles<256, 256, 8, ACT, T>(g, s);
+    // Tiles of 256 or of 128, by rounds of an XCD's workgroups: it takes every eighth row of tiles, 32 large or 64 small tiles at once.  A round of
+    // the large ones takes 54 to 60 us with K = 4096, one of the small ones 42, the last, which is rarely full, ten less (x packed before, 128
+    // and 256, rounds in brackets: 6000 x 1152 39.7 [1] and 55.0 us [1]; 7289 64.2 [2] and 55.9 [1]; 14000 78.0 [2] and 110 [2]; 20000 112 [3] and
+    // 112 [2]; 28000 151 [4] and 165 [3]; 2304 x 4096 66.5 [2] and 56.8 [1]; 6000 125 [3] and 118 [2]; 33000 x 384 73.0 [2] and 108 [2]; 50000 102
+    // [3] and 111 [2].  Shorter ones likewise: 7289 x 256 -> 1152 12.7 and 11.5; 14000 15.3 and 20.2; 28000 26.4 and 28.8; 403456 x 1536 -> 384
+    // 368 [19] and 350 [13]; 600 x 512 -> 20000 25.5 [3] and 37.4 [3]).
+    auto rounds = [&](int b, int at_once) { return (((g.M + b - 1) / b + 7) / 8 * ((g.N + b - 1) / b) + at_once - 1) / at_once; };
+    if (54 * rounds(256, 32) <= 42 * rounds(128, 64) - 10) return tiles<256, 256, 8, ACT, T>(g, s);
   }
   return tiles<128, 128, 4, ACT, T>(g, s);
 }
