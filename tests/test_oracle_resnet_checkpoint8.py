@@ -10,7 +10,7 @@ import gen
 # Of weights and shifts.  A norm adds 0.0325 of the gradient at most, 1.25 times the 2.6e-2 that four significant bits leave in the mean square, independently
 # of the others; a gain's own gradient is a sum of du xhat, which may cancel to anything.
 @pytest.mark.parametrize("block", ["basic", "bottleneck"])
-@pytest.mark.parametrize("groups", [4, 16])
+@pytest.mark.parametrize("groups", [1, 4, 8])
 def test_decisions_and_gradients(block, groups):
     from oracle import resnet_oracle as ro
     cfg, n = gen.RESNET_CONFIGS["rn_probe"]
