@@ -2,8 +2,9 @@
 //
 // Pack: 16 lanes take a block of 128 columns of one row, 8 columns each: largest finite magnitude over the 16 (within
 // a DPP row), the block's power of two, one exact multiplication and one rounding per value.  One pass, 16-byte loads, 8-byte
-// stores; bound by memory: es + 1 + 1/128 bytes a value (es: 2 or 4).  403456 x 384 of bfloat16: 94 us there, 79 us back, 5.0 and
-// 5.9 TB/s (the way back finds codes in the last-level cache).
+// stores; bound by memory: es + 1 + 1/128 bytes a value (es: 2 or 4).  403456 x 384 of bfloat16: 92 us there, 75 us back, 5.1 and
+// 6.3 TB/s (the way back finds codes in the last-level cache).  The transpose (weights, once per update) reads 64 bytes of a row at a
+// time: 1536 x 384 5.5 us (5.5 untransposed), 4096 x 4096 20 (10), 403456 x 384 212 (84).
 #include "act8_internal.h"
 
 namespace sl {

@@ -8,8 +8,8 @@
 //   * Few large units are split over rows: partial statistics per channel (count, mean, sum of squared distances: merged, never a
 //     difference of large sums), one small kernel for the groups, one pass for the result.
 // Measured (bfloat16, us; in brackets the bytes that must move at the 5.16 TB/s of a copy): 1024 x 56 x 56 x 64 with SiLU: forward with
-// checkpoint 252 (199), backward out of it 315 (199), a unit of 0.6 MB being read twice, 5 TB/s in all; 1024 x 28 x 28 x 128, ReLU and
-// residual, backward 277 (199); split, 2 x 300 x 301 x 320 with GELU: 47 + 10 + 59 forward (79), 62 + 7 + 67 backward (56; GELU's slope twice).
+// checkpoint 259 (199), backward out of it 303 (199), a unit of 0.6 MB being read twice, 5 TB/s in all; 1024 x 28 x 28 x 128, ReLU and
+// residual, backward 269 (199); split, 2 x 300 x 301 x 320 with GELU: 45 + 9 + 53 forward (79), 53 + 7 + 58 backward (56; GELU's slope twice).
 // Keeping more of a unit (in LDS: a third of the second reading) gained 3 %, more workgroups per unit of the chip lost 15 %.
 // A thread owns V neighbouring channels (16 bytes of bfloat16) and strides over rows.  All statistics and sums are float32; the
 // gradients of gain and shift add the workgroups' sums in double, in a fixed order.
