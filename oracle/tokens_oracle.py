@@ -1,0 +1,145 @@
+"""Transformers over the tiles of slides in 64 bits (numpy): norm and rotation of heads, attention over packed slides, their
+gradients, and how far the gradients of operands rounded on the way may be off.  Written from the formulas of include/tokens.h."""
+from __future__ import annotations
+
+import numpy as np
+
+
+# ---- norm and rotation of heads ------------------------------------------------------------------
+
+def rotation(pos, pairs, head_dim, theta):
+    """cos, sin [rows, 1, head_dim / 2]; the phase is taken modulo a turn in extended precision."""
+    rows, half = pos.shape[0], head_dim // 2
+    phi = np.zeros((rows, half), dtype=np.longdouble)
+    at = 0
+    for a, n in enumerate(pairs):
+        for j in range(n):
+            phi[:, at + j] = pos[:, a].astype(np.longdouble) * np.longdouble(theta) ** (-np.longdouble(j) / n)
+        at += n
+    turn = 2 * np.longdouble("3.14159265358979323846264338327950288")
+    phi = (phi - np.floor(phi / turn) * turn).astype(np.float64)
+    return np.cos(phi)[:, None], np.sin(phi)[:, None]
+
+
+def columns(head_dim, pairing):
+    p = np.arange(head_dim // 2)
+    return (p, p + head_dim // 2) if pairing == "halves" else (2 * p, 2 * p + 1)
+
+
+def turned(x, cos, sin, pairing):
+    a, b = columns(x.shape[-1], pairing)
+    y = np.empty_like(x)
+    y[..., a] = x[..., a] * cos - x[..., b] * sin
+    y[..., b] = x[..., b] * cos + x[..., a] * sin
+    return y
+
+
+def rope_fwd(x, gain, cos, sin, pairing, eps):
+    if gain is not None:
+        x = x / np.sqrt((x * x).mean(-1, keepdims=True) + eps) * gain
+    return turned(x, cos, sin, pairing)
+
+
+def rope_bwd(dy, x, gain, cos, sin, pairing, eps):
+    """dx, dgain."""
+    dn = turned(dy, cos, -sin, pairing)
+    if gain is None:
+        return dn, None
+    r = 1 / np.sqrt((x * x).mean(-1, keepdims=True) + eps)
+    h = x * r
+    u = dn * gain
+    return r * (u - h * (u * h).mean(-1, keepdims=True)), (dn * h).sum((0, 1))
+
+
+# ---- attention ------------------------------------------------------------------------------------
+
+def slides(q_start, k_start):
+    return [(slice(q_start[i], q_start[i + 1]), slice(k_start[i], k_start[i + 1])) for i in range(len(q_start) - 1)]
+
+
+def _scores(q, k, scale, cap, dist, slope):
+    x = scale * (q @ k.T)
+    t = np.tanh(x / cap) if cap else None
+    s = cap * t if cap else x
+    return s - slope * dist if dist is not None else s, t
+
+
+def _distance(pos_q, pos_k, lead_q, lead_k):
+    d = np.hypot(pos_q[:, None, 0] - pos_k[None, :, 0], pos_q[:, None, 1] - pos_k[None, :, 1])
+    d[:lead_q] = 0
+    d[:, :lead_k] = 0
+    return d
+
+
+def attn(q, k, v, q_start, k_start, scale, cap=0.0, pos_q=None, pos_k=None, slopes=None, lead_q=0, lead_k=0, do=None,
+         half_step=0.0, operand=0.0):
+    """Outputs of the forward and, where `do` is given, the gradients; behind each name `name_off`: the bound on what comes out where
+    results are rounded with `half_step` and probabilities and score gradients are rounded with `operand` before a product, both relative,
+    beside float32 arithmetic.  Rows of no slide are NaN."""
+    hq, hk = q.shape[1], k.shape[1]
+    group = hq // hk
+    out = {"o": np.full_like(q, np.nan), "lse": np.full((hq, q.shape[0]), np.nan)}
+    if do is not None:
+        out.update(dq=np.full_like(q, np.nan), dk=np.full_like(k, np.nan), dv=np.full_like(v, np.nan))
+    out.update({n + "_off": np.full_like(a, np.nan) for n, a in list(out.items())})
+    for rq, rk in slides(q_start, k_start):
+        if do is not None:
+            for n in ("dk", "dv", "dk_off", "dv_off"):
+                out[n][rk] = 0
+        dist = _distance(pos_q[rq], pos_k[rk], lead_q, lead_k) if slopes is not None else None
+        for h in range(hq):
+            _one(out, q[rq, h], k[rk, h // group], v[rk, h // group], None if do is None else do[rq, h], scale, cap, dist,
+                 0.0 if slopes is None else slopes[h], rq, rk, h, h // group, half_step, operand)
+    for n in ("dk", "dv"):
+        if do is not None:
+            out[n + "_off"] += half_step * np.abs(out[n])
+    return out
+
+
+def _one(out, q, k, v, do, scale, cap, dist, slope, rq, rk, h, hk, half_step, operand):
+    n, m, dim = q.shape[0], k.shape[0], q.shape[1]
+    if n == 0:
+        return
+    if m == 0:
+        out["o"][rq, h], out["lse"][h, rq] = 0, -np.inf
+        out["o_off"][rq, h] = out["lse_off"][h, rq] = 0
+        if do is not None:
+            out["dq"][rq, h] = out["dq_off"][rq, h] = 0
+        return
+    s, t = _scores(q, k, scale, cap, dist, slope)
+    top = s.max(1, keepdims=True)
+    e = np.exp(s - top)
+    z = e.sum(1, keepdims=True)
+    p = e / z
+    lse = (top + np.log(z))[:, 0]
+    o = p @ v
+    # float32: a score is off by a unit (2^-24) for every product in it and a few for cap, bias, exponent and the maximum; sums of m terms
+    u = 2.0 ** -24
+    size = scale * (np.abs(q) @ np.abs(k).T)
+    far = np.abs(slope) * dist if dist is not None else 0.0
+    off = u * ((dim + 8) * size + 8 * (cap + np.abs(s) + far + np.abs(lse)[:, None]) + 16)     # of a score, so relative of exp(score)
+    worst = off.max(1, keepdims=True)
+    rel = 2 * worst + (m + 8) * u                                                             # of a probability
+    a = p @ np.abs(v)
+    o_off = half_step * np.abs(o) + (operand + rel) * a
+    out["o"][rq, h], out["lse"][h, rq] = o, lse
+    out["o_off"][rq, h] = o_off
+    out["lse_off"][h, rq] = worst[:, 0] + u * (m + 8 + 4 * np.abs(lse))
+    if do is None:
+        return
+    dp = do @ v.T
+    delta = (do * o).sum(1, keepdims=True)
+    slope_t = 1 - t * t if cap else 1.0
+    ds = p * (dp - delta) * slope_t
+    delta_off = (np.abs(do) * o_off).sum(1, keepdims=True) + dim * u * (np.abs(do) * np.abs(o)).sum(1, keepdims=True)
+    dp_off = (dim + 8) * u * (np.abs(do) @ np.abs(v).T)
+    # 1 - tanh^2 is off by twice the tanh's error where it is not small, relative else
+    ds_off = operand * np.abs(ds) + p * ((delta_off + dp_off) * np.abs(slope_t) + (rel + 16 * u + (2 * off / cap if cap else 0.0)) * np.abs(dp - delta))
+    terms = (m + 8) * u
+    out["dq"][rq, h] = scale * (ds @ k)
+    out["dq_off"][rq, h] = scale * ((ds_off + terms * np.abs(ds)) @ np.abs(k)) + half_step * np.abs(out["dq"][rq, h])
+    terms = (n + 8) * u
+    out["dk"][rk, hk] += scale * (ds.T @ q)
+    out["dk_off"][rk, hk] += scale * ((ds_off + terms * np.abs(ds)).T @ np.abs(q))
+    out["dv"][rk, hk] += p.T @ do
+    out["dv_off"][rk, hk] += ((operand + rel + terms) * p).T @ np.abs(do)

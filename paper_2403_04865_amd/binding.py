@@ -164,6 +164,29 @@ _SYMS.update({
 })
 
 
+class _CHeadRope(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("heads_q", C.c_int32), ("heads_k", C.c_int32), ("head_dim", C.c_int32), ("dtype", C.c_int32),
+                ("axes", C.c_int32), ("pairing", C.c_int32), ("pairs", C.c_int32 * 3), ("eps", C.c_float), ("theta", C.c_double)]
+
+
+class _CTokensAttn(C.Structure):
+    _fields_ = [("rows_q", C.c_int64), ("rows_k", C.c_int64), ("docs", C.c_int32), ("heads_q", C.c_int32), ("heads_k", C.c_int32),
+                ("head_dim", C.c_int32), ("dtype", C.c_int32), ("lead_q", C.c_int32), ("lead_k", C.c_int32), ("scale", C.c_float),
+                ("cap", C.c_float), ("reserved", C.c_int32)]
+
+
+_RP, _TP = C.POINTER(_CHeadRope), C.POINTER(_CTokensAttn)
+_SYMS.update({
+    "slide_head_rope_fwd": (C.c_int, [_RP, _VP, _I64, _VP, _I64, _VP, _VP, _VP, _VP, _I64, _VP, _I64, _VP]),
+    "slide_head_rope_workspace_bytes": (C.c_size_t, [_RP]),
+    "slide_head_rope_bwd": (C.c_int, [_RP, _VP, _I64, _VP, _I64, _VP, _I64, _VP, _I64, _VP, _VP, _VP, _VP, _I64, _VP, _I64, _VP, _VP,
+                                      C.c_int, _VP, C.c_size_t, _VP]),
+    "slide_tokens_attn_workspace_bytes": (C.c_size_t, [_TP, C.c_int]),
+    "slide_tokens_attn_fwd": (C.c_int, [_TP] + [_VP, _I64] * 3 + [_VP] * 5 + [_VP, _I64, _VP, _VP, C.c_size_t, _VP]),
+    "slide_tokens_attn_bwd": (C.c_int, [_TP] + [_VP, _I64] * 5 + [_VP] * 6 + [_VP, _I64] * 3 + [_VP, C.c_size_t, _VP]),
+})
+
+
 _loaded = {}   # the file as it was -> the library with its functions declared (190 us to do again for every Act8Lib)
 
 
@@ -478,9 +501,9 @@ class Act8:
         return self.codes.get_device()
 
 
-class Act8Lib:
-    """The calls of include/act8.h on torch tensors, whose shapes, strides and types they take; no context.  A call runs on the
-    tensors' device, on `stream` (default: that device's current stream)."""
+class _TensorCalls:
+    """What the classes share whose calls take torch tensors: types, the device, the stream."""
+    ENTRIES = ()
 
     def __init__(self):
         import torch
@@ -490,43 +513,13 @@ class Act8Lib:
         self._shapes = {}
         # the raw handle of a device's current stream, where this torch has it without building a Stream
         self._raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
-        self._entry = {n: getattr(self.lib, n) for n in ("slide_act8_pack", "slide_act8_unpack", "slide_act8_linear", "slide_act8_wgrad",
-                                                         "slide_group_norm_fwd", "slide_group_norm_bwd")}
+        self._entry = {n: getattr(self.lib, n) for n in self.ENTRIES}
 
-    # ---- marshalling
     def _type(self, t):
         try:
             return self._types[t.dtype]
         except KeyError:
             raise ValueError(f"float32 or bfloat16, not {t.dtype}") from None
-
-    def _matrix(self, t, rows, cols, dtype, what):
-        """(pointer, elements between rows) of a [rows, cols] matrix of dtype, or of tiles [n, hw, cols] whose rows lie at one stride.
-        (None, 0) for None."""
-        if t is None:
-            return None, 0
-        if t.dtype != dtype:
-            raise ValueError(f"{what}: {t.dtype}, expected {dtype}")
-        shape = t.shape
-        if len(shape) in (2, 3) and shape[-1] == cols and t.numel() == rows * cols and t.is_contiguous():   # most of them
-            return t.data_ptr(), cols
-        stride = t.stride()
-        if len(shape) == 2:
-            have, last = shape
-            ld = stride[0]
-        elif len(shape) == 3:
-            n, hw, last = shape
-            if n > 1 and hw > 1 and stride[0] != hw * stride[1]:
-                raise ValueError(f"{what}: tiles must follow one another at one row stride")
-            have = n * hw
-            ld = stride[1] if hw > 1 else stride[0]
-        else:
-            raise ValueError(f"{what}: a matrix, or tiles of rows")
-        if have != rows or last != cols:
-            raise ValueError(f"{what}: {tuple(shape)}, expected {rows} rows of {cols}")
-        if last > 1 and stride[-1] != 1:
-            raise ValueError(f"{what}: rows must be contiguous")
-        return t.data_ptr(), ld if have > 1 else max(ld, cols)
 
     def _floats(self, t, n, what):
         if t is None:
@@ -534,14 +527,6 @@ class Act8Lib:
         if t.dtype != self._torch.float32 or t.numel() != n or not t.is_contiguous():
             raise ValueError(f"{what}: {n} contiguous float32 values")
         return t.data_ptr()
-
-    def _act(self, act):
-        if isinstance(act, str):
-            try:
-                return ACTS[act]
-            except KeyError:
-                raise ValueError(f"activation {act!r}: one of {', '.join(ACTS)}") from None
-        return int(act)
 
     def _call(self, what, first, others, args, stream):
         """Run the entry point on the device of `first`, which all of `others` must be on."""
@@ -572,6 +557,50 @@ class Act8Lib:
         if not t.is_contiguous():
             raise ValueError("workspace: a contiguous tensor")
         return t.data_ptr(), t.numel() * t.element_size()
+
+
+class Act8Lib(_TensorCalls):
+    """The calls of include/act8.h on torch tensors, whose shapes, strides and types they take; no context.  A call runs on the
+    tensors' device, on `stream` (default: that device's current stream)."""
+
+    ENTRIES = ("slide_act8_pack", "slide_act8_unpack", "slide_act8_linear", "slide_act8_wgrad", "slide_group_norm_fwd", "slide_group_norm_bwd")
+
+    # ---- marshalling
+    def _matrix(self, t, rows, cols, dtype, what):
+        """(pointer, elements between rows) of a [rows, cols] matrix of dtype, or of tiles [n, hw, cols] whose rows lie at one stride.
+        (None, 0) for None."""
+        if t is None:
+            return None, 0
+        if t.dtype != dtype:
+            raise ValueError(f"{what}: {t.dtype}, expected {dtype}")
+        shape = t.shape
+        if len(shape) in (2, 3) and shape[-1] == cols and t.numel() == rows * cols and t.is_contiguous():   # most of them
+            return t.data_ptr(), cols
+        stride = t.stride()
+        if len(shape) == 2:
+            have, last = shape
+            ld = stride[0]
+        elif len(shape) == 3:
+            n, hw, last = shape
+            if n > 1 and hw > 1 and stride[0] != hw * stride[1]:
+                raise ValueError(f"{what}: tiles must follow one another at one row stride")
+            have = n * hw
+            ld = stride[1] if hw > 1 else stride[0]
+        else:
+            raise ValueError(f"{what}: a matrix, or tiles of rows")
+        if have != rows or last != cols:
+            raise ValueError(f"{what}: {tuple(shape)}, expected {rows} rows of {cols}")
+        if last > 1 and stride[-1] != 1:
+            raise ValueError(f"{what}: rows must be contiguous")
+        return t.data_ptr(), ld if have > 1 else max(ld, cols)
+
+    def _act(self, act):
+        if isinstance(act, str):
+            try:
+                return ACTS[act]
+            except KeyError:
+                raise ValueError(f"activation {act!r}: one of {', '.join(ACTS)}") from None
+        return int(act)
 
     # ---- calls
     def slide_act8_pack(self, x, out, transpose=False, stream=None):
@@ -649,3 +678,146 @@ class Act8Lib:
                     self._floats(rstd, n * groups, "rstd"), *m(dx, n * hw, c, t, "dx"), *m(dresidual, n * hw, c, t, "dresidual"),
                     self._floats(dgamma, c, "dgamma"), self._floats(dbeta, c, "dbeta"), int(accumulate), *self._work(workspace)),
                    stream)
+
+
+PAIRINGS = {"halves": 0, "neighbours": 1}
+
+
+class HeadRope:
+    """Rotation of a head's columns by positions of len(pairs) axes (slide_head_rope in include/tokens.h): `pairs` columns' pairs of each axis."""
+
+    def __init__(self, head_dim, pairs, theta=10000.0, pairing="halves", eps=1e-6):
+        pairs = tuple(int(n) for n in pairs)
+        if len(pairs) > 3:
+            raise ValueError("pairs: of three axes at most")
+        if any(n < 0 or 2 * n > head_dim for n in pairs):
+            raise ValueError(f"pairs {pairs}: at most {head_dim // 2} in all")
+        if pairing not in PAIRINGS:
+            raise ValueError(f"pairing {pairing!r}: one of {', '.join(PAIRINGS)}")
+        self.head_dim, self.pairs, self.theta, self.pairing, self.eps = int(head_dim), pairs, float(theta), pairing, float(eps)
+        self._made = {}
+
+    def _c(self, rows, heads_q, heads_k, dtype):
+        """The C description, kept by its values."""
+        key = (rows, heads_q, heads_k, dtype, self.head_dim, self.pairs, self.pairing, self.eps, self.theta)
+        s = self._made.get(key)
+        if s is None:
+            if len(self._made) > 256:
+                self._made.clear()
+            s = self._made[key] = C.pointer(_CHeadRope(rows, heads_q, heads_k, self.head_dim, dtype, len(self.pairs), PAIRINGS[self.pairing],
+                                                       (C.c_int32 * 3)(*self.pairs), self.eps, self.theta))
+        return s
+
+
+class TokensLib(_TensorCalls):
+    """The calls of include/tokens.h on torch tensors, whose shapes, strides and types they take; no context.  Queries, keys and values are
+    [rows, heads, head_dim] with a row's heads beside each other: views of one matrix that a layer wrote will do.  A call runs on the tensors'
+    device, on `stream` (default: that device's current stream)."""
+    ENTRIES = ("slide_head_rope_fwd", "slide_head_rope_bwd", "slide_tokens_attn_fwd", "slide_tokens_attn_bwd")
+
+    def _heads(self, t, rows, heads, dim, dtype, what):
+        """(pointer, elements between rows) of [rows, heads, dim]; (None, 0) for None."""
+        if t is None:
+            return None, 0
+        if t.dtype != dtype:
+            raise ValueError(f"{what}: {t.dtype}, expected {dtype}")
+        if tuple(t.shape) != (rows, heads, dim):
+            raise ValueError(f"{what}: {tuple(t.shape)}, expected {(rows, heads, dim)}")
+        ld, between, one = t.stride()
+        if (dim > 1 and one != 1) or (heads > 1 and between != dim):
+            raise ValueError(f"{what}: a row's heads must lie beside each other")
+        return t.data_ptr(), ld if rows > 1 else heads * dim
+
+    def _ints(self, t, shape, what):
+        if t is None:
+            return None
+        if t.dtype != self._torch.int32 or tuple(t.shape) != shape or not t.is_contiguous():
+            raise ValueError(f"{what}: contiguous int32 {shape}")
+        return t.data_ptr()
+
+    def _shape3(self, t, what):
+        if t.dim() != 3:
+            raise ValueError(f"{what}: [rows, heads, head_dim]")
+        return t.shape
+
+    # ---- norm and rotation of heads
+    def slide_head_rope_workspace_bytes(self, rope, rows, heads_q, heads_k):
+        """Of the backward; 0 for a shape that is refused."""
+        return int(self.lib.slide_head_rope_workspace_bytes(rope._c(rows, heads_q, heads_k, 0)))
+
+    def _rope_sizes(self, rope, q, k):
+        rows, hq, dim = self._shape3(q, "q")
+        if dim != rope.head_dim:
+            raise ValueError(f"heads of {dim} columns for a rotation of {rope.head_dim}")
+        hk = 0 if k is None else self._shape3(k, "k")[1]
+        return rows, hq, hk, dim, rope._c(rows, hq, hk, self._type(q))
+
+    def slide_head_rope_fwd(self, rope, q, k, pos, q_out, k_out, gq=None, gk=None, stream=None):
+        """q_out, k_out = q, k of every head, normalised where there is a gain and rotated by pos [rows, axes].  k may be None."""
+        rows, hq, hk, dim, s = self._rope_sizes(rope, q, k)
+        h, t = self._heads, q.dtype
+        self._call("slide_head_rope_fwd", q, (k, pos, q_out, k_out, gq, gk),
+                   (s, *h(q, rows, hq, dim, t, "q"), *h(k, rows, hk, dim, t, "k"), self._floats(gq, dim, "gq"), self._floats(gk, dim, "gk"),
+                    self._ints(pos, (rows, len(rope.pairs)), "pos"), *h(q_out, rows, hq, dim, t, "q_out"), *h(k_out, rows, hk, dim, t, "k_out")),
+                   stream)
+
+    def slide_head_rope_bwd(self, rope, dq_out, dk_out, q, k, pos, dq, dk, gq=None, gk=None, dgq=None, dgk=None, accumulate=False,
+                            workspace=None, stream=None):
+        """dq, dk (and the gains' dgq, dgk) out of the gradients dq_out, dk_out of the rotated heads; q, k: the forward's inputs (None where
+        there is no gain)."""
+        rows, hq, hk, dim, s = self._rope_sizes(rope, dq_out, dk_out)
+        h, t, f = self._heads, dq_out.dtype, self._floats
+        self._call("slide_head_rope_bwd", dq_out, (dk_out, q, k, pos, dq, dk, gq, gk, dgq, dgk, workspace),
+                   (s, *h(dq_out, rows, hq, dim, t, "dq_out"), *h(dk_out, rows, hk, dim, t, "dk_out"), *h(q, rows, hq, dim, t, "q"),
+                    *h(k, rows, hk, dim, t, "k"), f(gq, dim, "gq"), f(gk, dim, "gk"), self._ints(pos, (rows, len(rope.pairs)), "pos"),
+                    *h(dq, rows, hq, dim, t, "dq"), *h(dk, rows, hk, dim, t, "dk"), f(dgq, dim, "dgq"), f(dgk, dim, "dgk"),
+                    int(accumulate), *self._work(workspace)), stream)
+
+    # ---- attention
+    def _attn(self, *key):
+        """The C description of an attention, kept by its values: its fields in order."""
+        s = self._shapes.get(key)
+        if s is None:
+            if len(self._shapes) > 256:
+                self._shapes.clear()
+            s = self._shapes[key] = C.pointer(_CTokensAttn(*key, 0))
+        return s
+
+    def slide_tokens_attn_workspace_bytes(self, rows_q, rows_k, docs, heads_q, heads_k, head_dim, dtype, backward=False):
+        """For the forward, or for both directions; 0 where none is needed and for a shape that is refused."""
+        s = self._attn(rows_q, rows_k, docs, heads_q, heads_k, head_dim, self._types.get(dtype, -1), 0, 0, 1.0, 0.0)
+        return int(self.lib.slide_tokens_attn_workspace_bytes(s, int(backward)))
+
+    def _attn_args(self, q, k, v, q_start, k_start, lse, scale, cap, pos_q, pos_k, slopes, lead_q, lead_k):
+        rows_q, hq, dim = self._shape3(q, "q")
+        rows_k, hk, _ = self._shape3(k, "k")
+        docs = q_start.numel() - 1
+        if not (0 <= lead_q < 1 << 31 and 0 <= lead_k < 1 << 31):
+            raise ValueError("lead_q, lead_k: rows without a place, not negative")
+        s = self._attn(rows_q, rows_k, docs, hq, hk, dim, self._type(q), lead_q, lead_k, scale, cap)
+        for t, rows, what in ((pos_q, rows_q, "pos_q"), (pos_k, rows_k, "pos_k")):
+            if t is not None and tuple(t.shape) != (rows, 2):
+                raise ValueError(f"{what}: {tuple(t.shape)}, expected {(rows, 2)}")
+        h, t, f = self._heads, q.dtype, self._floats
+        if lse.dtype != self._torch.float32 or tuple(lse.shape) != (hq, rows_q) or not lse.is_contiguous():
+            raise ValueError(f"lse: contiguous float32 {(hq, rows_q)}")
+        qkv = (*h(q, rows_q, hq, dim, t, "q"), *h(k, rows_k, hk, dim, t, "k"), *h(v, rows_k, hk, dim, t, "v"))
+        where = (self._ints(q_start, (docs + 1,), "q_start"), self._ints(k_start, (docs + 1,), "k_start"), f(pos_q, 2 * rows_q, "pos_q"),
+                 f(pos_k, 2 * rows_k, "pos_k"), f(slopes, hq, "slopes"))
+        return s, (rows_q, hq, dim, t), (rows_k, hk, dim, t), qkv, where
+
+    def slide_tokens_attn_fwd(self, q, k, v, q_start, k_start, o, lse, scale, cap=0.0, pos_q=None, pos_k=None, slopes=None, lead_q=0,
+                              lead_k=0, workspace=None, stream=None):
+        """o = softmax(scores) v inside every slide, lse [heads, rows] the log of the sums; q_start, k_start: [slides + 1] int32."""
+        s, a, _, qkv, where = self._attn_args(q, k, v, q_start, k_start, lse, scale, cap, pos_q, pos_k, slopes, lead_q, lead_k)
+        self._call("slide_tokens_attn_fwd", q, (k, v, q_start, k_start, o, lse, pos_q, pos_k, slopes, workspace),
+                   (s, *qkv, *where, *self._heads(o, *a, "o"), lse.data_ptr(), *self._work(workspace)), stream)
+
+    def slide_tokens_attn_bwd(self, do, q, k, v, o, lse, q_start, k_start, dq, dk, dv, scale, cap=0.0, pos_q=None, pos_k=None, slopes=None,
+                              lead_q=0, lead_k=0, workspace=None, stream=None):
+        """dq, dk, dv out of the output's gradient and the o and lse that the forward left."""
+        s, a, b, qkv, where = self._attn_args(q, k, v, q_start, k_start, lse, scale, cap, pos_q, pos_k, slopes, lead_q, lead_k)
+        h = self._heads
+        self._call("slide_tokens_attn_bwd", q, (do, k, v, o, lse, q_start, k_start, dq, dk, dv, pos_q, pos_k, slopes, workspace),
+                   (s, *h(do, *a, "do"), *qkv, *h(o, *a, "o"), lse.data_ptr(), *where, *h(dq, *a, "dq"), *h(dk, *b, "dk"), *h(dv, *b, "dv"),
+                    *self._work(workspace)), stream)

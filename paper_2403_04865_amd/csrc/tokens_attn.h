@@ -1,0 +1,259 @@
+// Device parts that the passes of the attention over packed slides share (tokens_attn_fwd / _dq / _dkv .hip).
+//
+// Every pass is a workgroup's 32 columns a wavefront against blocks of rows that pass through LDS.  Forward and dq: columns are queries, the heads that
+// share a key head packed beside each other (column c of a slide is its query c / group, head c % group of the group), rows are keys.
+// dk, dv: columns are keys, rows are such packed queries.  A block of scores is made transposed, rows down the registers of an
+// accumulator and one column a lane, so a row statistic of the columns is a reduction inside a lane and one exchange between the halves of the
+// wavefront, and the probabilities are in the layout in which the next product takes its second operand.
+#pragma once
+#include <type_traits>
+
+#include "lds_dma.h"
+#include "tokens_internal.h"
+
+namespace sl {
+
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr float TOK_LOG2E = 1.4426950408889634f, TOK_LN2 = 0.69314718055994531f;
+
+template <typename T> struct TokType;
+template <> struct TokType<bf16>  { static constexpr int EPC = 8, KB = 64; };   // elements of 16 bytes, rows of a block in LDS
+template <> struct TokType<float> { static constexpr int EPC = 4, KB = 32; };
+
+template <typename T, int DP> constexpr int tok_ldr() { return DP + TokType<T>::EPC; }   // elements between rows in LDS: 16-byte reads of eight rows meet no bank twice
+
+// ---- which slide ----------------------------------------------------------------------------------
+// Slots of `width` columns are dealt to the slides without a table: slide i's begin at start[i] * group / width + i, which leaves each
+// as many as its columns take, whatever the lengths, of total / width + docs in all.
+struct TokDoc { int doc, lo, hi, tile; };   // rows lo .. hi - 1; the slot's first column is tile * width; doc < 0: none
+__device__ __forceinline__ int tok_clamp(int v, int rows) { return v < 0 ? 0 : v > rows ? rows : v; }
+__device__ __forceinline__ TokDoc tok_find(const int* __restrict__ start, int docs, int rows, int group, int width, int slot) {
+  const int lane = threadIdx.x & 63;
+  // the last slide whose first slot is `slot` or before; 64 candidates at a time
+  int lo = 0, n = docs;
+  while (n > 0) {   // candidates lo .. lo + n - 1; n shrinks to an n / 64 (rounded up) with every turn
+    const int step = (n + 63) >> 6;
+    const int i = lo + lane * step;
+    const bool in = lane * step < n;
+    const long long first = in ? (long long)tok_clamp(start[in ? i : 0], rows) * group / width + i : 0;
+    const unsigned long long m = __builtin_amdgcn_ballot_w64(in && first <= slot);
+    if (!m) return {-1, 0, 0, 0};
+    const int l = 63 - __builtin_clzll(m);
+    lo += l * step;
+    n = step == 1 ? 0 : (n - l * step < step ? n - l * step : step);
+  }
+  const int doc = __builtin_amdgcn_readfirstlane(lo);
+  const int a = tok_clamp(__builtin_amdgcn_readfirstlane(start[doc]), rows), b = tok_clamp(__builtin_amdgcn_readfirstlane(start[doc + 1]), rows);
+  return {doc, a, b > a ? b : a, slot - (int)((long long)a * group / width) - doc};
+}
+// Where a workgroup is in a grid of `slots` x `splits` x `heads`, as many of one head as possible on one XCD (workgroups are dealt to the eight in
+// turn), whose L2 then holds that head's rows.  false: past the end.
+struct TokWork { int slot, split, head; };
+__device__ __forceinline__ bool tok_work(int slots, int splits, int heads, TokWork* w) {
+  const unsigned per = gridDim.x >> 3, at = (blockIdx.x & 7) * per + (blockIdx.x >> 3), all = (unsigned)slots * splits * heads;
+  if (at >= all) return false;
+  w->slot = at % (unsigned)slots;
+  const unsigned r = at / (unsigned)slots;
+  w->split = r % (unsigned)splits;
+  w->head = r / (unsigned)splits;
+  return true;
+}
+inline unsigned tok_grid(TokCut c, int heads) { return (unsigned)(((long long)c.slots * c.splits * heads + 7) / 8 * 8); }
+
+// ---- blocks of rows into LDS ----------------------------------------------------------------------
+__device__ __forceinline__ u32x4 tok_load16(__amdgpu_buffer_rsrc_t b, int voff) { return __builtin_amdgcn_raw_buffer_load_b128(b, voff, 0, 0); }
+
+// A thread's pieces of a block of KB rows of `dim` columns: NTHR threads, 16 bytes each, rows one behind the other.  Columns from dim
+// to DP and rows past the block's last are zeros (outside of the buffer).
+template <typename T, int DP, int NTHR>
+struct TokTile {
+  static constexpr int EPC = TokType<T>::EPC, KB = TokType<T>::KB, CH = DP / EPC, TOTAL = KB * CH, ITER = (TOTAL + NTHR - 1) / NTHR, LDR = tok_ldr<T, DP>();
+  static_assert(TOTAL % NTHR == 0, "every thread has as many pieces");
+  u32x4 v[ITER];
+  // rows 0 .. rows - 1 of p at ld
+  __device__ __forceinline__ void load(const T* p, int rows, int ld, int dim) {
+    rows = rows < KB ? rows : KB;
+    const __amdgpu_buffer_rsrc_t b = dma_rows(p, rows, ld, dim);
+#pragma unroll
+    for (int i = 0; i < ITER; ++i) {
+      const int c = threadIdx.x + i * NTHR, row = c / CH, col = c % CH * EPC;
+      v[i] = tok_load16(b, col < dim ? (row * ld + col) * (int)sizeof(T) : DMA_ABSENT);
+    }
+  }
+  // packed queries c0 .. c0 + KB - 1 of a slide with `cols` of them: p is its first query's first head of the group
+  __device__ __forceinline__ void load_packed(const T* p, int c0, int cols, int ld, int dim, int group, unsigned magic) {
+    const int r0 = c0 / group, phase = c0 - r0 * group;
+    const __amdgpu_buffer_rsrc_t b = dma_buffer(p + (long long)r0 * ld, DMA_MAX);
+#pragma unroll
+    for (int i = 0; i < ITER; ++i) {
+      const int c = threadIdx.x + i * NTHR, row = c / CH, col = c % CH * EPC;
+      const unsigned x = row + phase, r = x * magic >> 16, h = x - r * group;
+      v[i] = tok_load16(b, col < dim && c0 + row < cols ? (int)((r * ld + h * dim + col) * sizeof(T)) : DMA_ABSENT);
+    }
+  }
+  __device__ __forceinline__ void store(T* s) const {
+#pragma unroll
+    for (int i = 0; i < ITER; ++i) {
+      const int c = threadIdx.x + i * NTHR, row = c / CH, col = c % CH * EPC;
+      *reinterpret_cast<u32x4*>(s + row * LDR + col) = v[i];
+    }
+  }
+};
+// x / group for x < 64 + group as a product and a shift (group <= 128: the error x (group - 1) / (65536 group) is below 1 / group)
+__device__ __forceinline__ unsigned tok_magic(int group) { return (65536u + group - 1) / group; }
+
+// ---- products -------------------------------------------------------------------------------------
+template <typename T, int DP> struct TokFrag { u32x4 v[DP / TokType<T>::EPC / 2]; };   // a column's DP values: the pieces 2 i + (lane / 32)
+template <typename T, int DP>
+__device__ __forceinline__ void tok_load_frag(TokFrag<T, DP>& f, const T* row, bool valid, int dim) {
+  const int h2 = (threadIdx.x >> 5) & 1;
+#pragma unroll
+  for (int i = 0; i < DP / TokType<T>::EPC / 2; ++i) {
+    const int col = (2 * i + h2) * TokType<T>::EPC;
+    f.v[i] = u32x4{0, 0, 0, 0};
+    if (valid && col < dim) f.v[i] = *reinterpret_cast<const u32x4*>(row + col);
+  }
+}
+// acc[rows j0 .. j0 + 31][columns] += X f: contraction over the DP columns of X
+template <typename T, int DP>
+__device__ __forceinline__ void tok_mul(f32x16& acc, const T* X, int j0, const TokFrag<T, DP>& f) {
+  const int li = threadIdx.x & 31, h2 = (threadIdx.x >> 5) & 1;
+  const T* p = X + (j0 + li) * tok_ldr<T, DP>() + h2 * TokType<T>::EPC;
+#pragma unroll
+  for (int i = 0; i < DP / TokType<T>::EPC / 2; ++i) {
+    const u32x4 a = *reinterpret_cast<const u32x4*>(p + 2 * i * TokType<T>::EPC);
+    if constexpr (sizeof(T) == 2) {
+      acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, f.v[i]), acc, 0, 0, 0);
+    } else {
+      const f32x4 fa = __builtin_bit_cast(f32x4, a), fb = __builtin_bit_cast(f32x4, f.v[i]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(fa[e], fb[e], acc, 0, 0, 0);
+    }
+  }
+}
+// acc[DP][columns] += (rows j0 .. j0 + 31 of X)^T p: contraction over rows, p as the scores lie.  bfloat16: p is rounded to it (half a step, 2^-9 of each
+// probability and of either sign, where the result's own rounding is as large); the matrix cores take no wider operand beside bfloat16.
+template <typename T, int DP>
+__device__ __forceinline__ void tok_mul_t(f32x16 (&acc)[DP / 32], const T* X, int j0, const f32x16& p) {
+  constexpr int LDR = tok_ldr<T, DP>();
+  const int lane = threadIdx.x & 63, li = lane & 31, h2 = lane >> 5;
+  if constexpr (sizeof(T) == 2) {
+    // LDS transpose reads: within 16 lanes, lane s addresses four columns of row s / 4 and receives column s of the four rows
+    typedef short s16x4 __attribute__((ext_vector_type(4)));
+    typedef short s16x8 __attribute__((ext_vector_type(8)));
+    const int g = lane >> 4, s = lane & 15;
+    const T* q = X + (j0 + 4 * (g >> 1) + (s >> 2)) * LDR + 16 * (g & 1) + (s & 3) * 4;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      bf16x8 b;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) b[i] = (bf16)p[8 * t + i];
+#pragma unroll
+      for (int d = 0; d < DP / 32; ++d) {
+        const T* at = q + 16 * t * LDR + d * 32;
+        const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)at);
+        const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(at + 8 * LDR));
+        const s16x8 a = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+        acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), b, acc[d], 0, 0, 0);
+      }
+    }
+  } else {
+    const T* q = X + (j0 + 4 * h2) * LDR + li;
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+#pragma unroll
+      for (int d = 0; d < DP / 32; ++d)
+        acc[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(q[((r >> 2) * 8 + (r & 3)) * LDR + d * 32], p[r], acc[d], 0, 0, 0);
+  }
+}
+// row of a block of 32 that register r of this lane holds
+__device__ __forceinline__ int tok_row(int r) { return (r >> 2) * 8 + ((threadIdx.x >> 5) & 1) * 4 + (r & 3); }
+__device__ __forceinline__ f32x16 tok_zero() {
+  f32x16 z;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) z[r] = 0.f;
+  return z;
+}
+template <int N>
+__device__ __forceinline__ void tok_zero_all(f32x16 (&a)[N]) {
+#pragma unroll
+  for (int d = 0; d < N; ++d) a[d] = tok_zero();
+}
+// a column's DP results (down the registers) times f to `dim` elements at `row`
+template <typename O, int N>
+__device__ __forceinline__ void tok_store(const f32x16 (&a)[N], float f, O* row, int dim) {
+  const int h2 = (threadIdx.x >> 5) & 1;
+  typedef O O4 __attribute__((ext_vector_type(4)));
+#pragma unroll
+  for (int d = 0; d < N; ++d)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const int col = d * 32 + g * 8 + h2 * 4;
+      O4 v;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = (O)(a[d][g * 4 + i] * f);
+      if (col < dim) *reinterpret_cast<O4*>(row + col) = v;
+    }
+}
+
+// ---- scores ---------------------------------------------------------------------------------------
+// Everything is in units of log2(e): y = c1 qk - slope d without a cap, c2 tanh(c1 qk) - slope d with one.
+struct TokScore { float c1, c2; };
+template <bool CAP>
+__device__ __forceinline__ TokScore tok_score_of(float scale, float cap) {
+  return CAP ? TokScore{scale / cap, cap * TOK_LOG2E} : TokScore{scale * TOK_LOG2E, 0.f};
+}
+// tanh(u) and, where wanted, its derivative, from e = exp(-2 |u|): (1 - e) / (1 + e) and 4 e / (1 + e)^2, which lose nothing for large
+// |u|.  For small |u| 1 - e has e's rounding, 2^-25 of one: float32 takes the series there (next term 2^-27 of u at 1/4).
+template <typename T, bool SLOPE>
+__device__ __forceinline__ float tok_tanh(float u, float* slope) {
+  const float e = __builtin_amdgcn_exp2f(-2.f * TOK_LOG2E * fabsf(u));
+  const float r = __builtin_amdgcn_rcpf(1.f + e);
+  float t = (1.f - e) * r;
+  if (SLOPE) *slope = 4.f * e * r * r;
+  if (sizeof(T) == 4) {
+    const float w = u * u, a = fabsf(u);
+    const float series = a * fmaf(w, fmaf(w, fmaf(w, fmaf(w, 62.f / 2835.f, -17.f / 315.f), 2.f / 15.f), -1.f / 3.f), 1.f);
+    t = a < 0.25f ? series : t;
+  }
+  return copysignf(t, u);
+}
+template <typename T, bool BIAS, bool CAP, bool SLOPE>
+__device__ __forceinline__ float tok_score(float qk, float d, float slope, TokScore c, float* dt) {
+  float y = CAP ? c.c2 * tok_tanh<T, SLOPE>(qk * c.c1, dt) : qk * c.c1;
+  if (BIAS) y = fmaf(-slope, d, y);
+  return y;
+}
+__device__ __forceinline__ float tok_dist(float ax, float ay, float bx, float by) {
+  const float x = ax - bx, y = ay - by;
+  return __builtin_amdgcn_sqrtf(fmaf(x, x, y * y));   // within an ulp
+}
+
+// Positions of a block's keys in LDS, x and y apart, 0 for keys without a place and behind the last
+template <int KB>
+__device__ __forceinline__ void tok_put_places(float* px, float* py, const float* pos, int lo, int k0, int n, int lead) {
+  if (threadIdx.x < KB) {
+    const int j = k0 + threadIdx.x;
+    float x = 0.f, y = 0.f;
+    if (j < n && j >= lead) {
+      const float2 p = *reinterpret_cast<const float2*>(pos + 2LL * (lo + j));
+      x = p.x; y = p.y;
+    }
+    px[threadIdx.x] = x;
+    py[threadIdx.x] = y;
+  }
+}
+
+// dispatch on the padded head width, bias and cap
+template <typename T, typename F>
+hipError_t tok_dispatch(const TokAttn& g, F f) {
+  auto by_cap = [&](auto dp, auto bias) { return g.cap > 0.f ? f(dp, bias, std::true_type{}) : f(dp, bias, std::false_type{}); };
+  auto by_bias = [&](auto dp) { return g.slopes ? by_cap(dp, std::true_type{}) : by_cap(dp, std::false_type{}); };
+  if (g.dim <= 32) return by_bias(std::integral_constant<int, 32>{});
+  if (g.dim <= 64) return by_bias(std::integral_constant<int, 64>{});
+  if (g.dim <= 96) return by_bias(std::integral_constant<int, 96>{});
+  return by_bias(std::integral_constant<int, 128>{});
+}
+
+}  // namespace sl

@@ -1,0 +1,57 @@
+// Internal declarations of the operators over tokens (include/tokens.h; gfx950 only).
+#pragma once
+#include "../../include/tokens.h"
+#include "slide_internal.h"
+
+namespace sl {
+
+constexpr int64_t TOK_LD_MAX = (1 << 21) - 1;   // 64 rows of 4-byte elements within a buffer's 32-bit offsets
+constexpr int64_t TOK_ROWS_MAX = (1LL << 31) - 1 - 256;
+
+// ---- norm and rotation of heads ------------------------------------------------------------------
+constexpr int ROPE_PAIRS = 128;
+struct HeadRope {
+  long long rows;
+  int hq, hk, dim, axes, neighbours;
+  int bound[2];                       // first pair of axis 1, of axis 2
+  float eps;
+  const void *q, *k; long long ldq, ldk;        // forward: inputs; backward: the forward's inputs
+  const void *dyq, *dyk; long long lddyq, lddyk;
+  void *yq, *yk; long long ldyq, ldyk;          // outputs: values, or gradients
+  const float *gq, *gk;
+  const int* pos;
+  float *dgq, *dgk; int accumulate;
+  float* work;
+  unsigned long long freq[ROPE_PAIRS];          // a pair's turns for a step of its position, as a fraction of 2^64
+};
+size_t head_rope_work_bytes(const slide_head_rope& s);
+hipError_t launch_head_rope_fwd(int dt, const HeadRope& g, hipStream_t s);
+hipError_t launch_head_rope_bwd(int dt, const HeadRope& g, hipStream_t s);
+
+// ---- attention -----------------------------------------------------------------------------------
+struct TokAttn {
+  int rows_q, rows_k, docs, hq, hk, group, dim;
+  int lead_q, lead_k;
+  float scale, cap;
+  const void *q, *k, *v, *o_in, *dout;
+  int ldq, ldk, ldv, ldo, lddo, lddq, lddk, lddv;
+  const int *q_start, *k_start;
+  const float *pos_q, *pos_k, *slopes;
+  void *o, *dq, *dk, *dv;
+  float* lse;           // [hq][rows_q]
+  float* delta;         // [hq][rows_q]: dout . o
+  // partial results of `splits` ranges of the other side's rows, one behind the other (splits > 1)
+  int splits;
+  float *part, *part2;
+};
+// How a pass is cut: workgroups of `waves` wavefronts with 32 columns (packed queries, or keys) each, `slots` of them a key head and range
+struct TokCut { int waves, slots, splits; };
+TokCut tok_cut(long long cols, long long other, int docs, int heads, int dt, int dim);
+hipError_t launch_tok_fwd(int dt, const TokAttn& g, TokCut c, hipStream_t s);
+hipError_t launch_tok_delta(int dt, const TokAttn& g, hipStream_t s);
+hipError_t launch_tok_dq(int dt, const TokAttn& g, TokCut c, hipStream_t s);
+hipError_t launch_tok_dkv(int dt, const TokAttn& g, TokCut c, hipStream_t s);
+// sums of partial gradients, in the order of the ranges; rows of slides only
+hipError_t launch_tok_sum(int dt, const float* part, int splits, int rows, int cols, const int* start, int docs, void* out, int ld, hipStream_t s);
+
+}  // namespace sl

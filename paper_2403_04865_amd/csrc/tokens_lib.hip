@@ -1,0 +1,223 @@
+// C entry points of include/tokens.h: checks of the arguments, then the launches.
+#include "run_internal.h"
+#include "tokens_internal.h"
+
+#include <cmath>
+
+using namespace sl;
+
+namespace {
+
+bool dtype_ok(int dt) { return dt == DT_F32 || dt == DT_BF16; }
+// rows of `cols` elements that 16-byte accesses reach
+bool matrix_ok(const void* p, int dt, int64_t ld, int64_t cols) {
+  return p && ((uintptr_t)p & 15) == 0 && ld >= cols && ld <= TOK_LD_MAX && ld % (16 / (int64_t)elem_size(dt)) == 0;
+}
+bool aligned(const void* p, unsigned n) { return ((uintptr_t)p & (n - 1)) == 0; }
+int work_ok(const void* work, size_t have, size_t need) {
+  if (!need) return SLIDE_OK;
+  if (!work || have < need) return SLIDE_EARENA;
+  return aligned(work, 256) ? SLIDE_OK : SLIDE_EINVAL;
+}
+int status(hipError_t e) {
+  if (e == hipSuccess) return SLIDE_OK;
+  g_last_hip = (int)e;
+  return SLIDE_EHIP;
+}
+
+int rope_ok(const slide_head_rope* s) {
+  if (!s || s->rows < 1 || s->rows > TOK_ROWS_MAX || s->heads_q < 1 || s->heads_q > 4096 || s->heads_k < 0 || s->heads_k > 4096 || s->head_dim < 1 ||
+      !dtype_ok(s->dtype) || s->axes < 0 || s->axes > 3 || (s->pairing != SLIDE_ROPE_HALVES && s->pairing != SLIDE_ROPE_NEIGHBOURS) ||
+      !(s->eps > 0.f) || !std::isfinite(s->eps) || !(s->theta > 0.0) || !std::isfinite(s->theta))
+    return SLIDE_EINVAL;
+  int64_t pairs = 0;
+  for (int a = 0; a < s->axes; ++a) {
+    if (s->pairs[a] < 0) return SLIDE_EINVAL;
+    pairs += s->pairs[a];
+  }
+  if (2 * pairs > s->head_dim) return SLIDE_EINVAL;
+  return s->head_dim % 16 || s->head_dim > 2 * ROPE_PAIRS ? SLIDE_EUNSUPPORTED : SLIDE_OK;
+}
+HeadRope rope_of(const slide_head_rope& s) {
+  HeadRope g{};
+  g.rows = s.rows; g.hq = s.heads_q; g.hk = s.heads_k; g.dim = s.head_dim; g.axes = s.axes; g.neighbours = s.pairing; g.eps = s.eps;
+  int at = 0;
+  for (int a = 0; a < s.axes; ++a) {
+    const int n = s.pairs[a];
+    // theta^(-j / n) / 2 pi modulo 1 as a fraction of 2^64, 64-bit mantissas
+    const long double step = n ? -std::log((long double)s.theta) / n : 0;
+    for (int j = 0; j < n; ++j) {
+      const long double turns = std::exp(step * j) * 0.159154943091895335768883763372514362L;
+      g.freq[at++] = (unsigned long long)((turns - std::floor(turns)) * 18446744073709551616.0L);
+    }
+    if (a < 2) g.bound[a] = at;
+  }
+  for (int a = s.axes; a < 2; ++a) g.bound[a] = at;
+  return g;
+}
+
+int attn_ok(const slide_tokens_attn* s) {
+  if (!s || s->rows_q < 1 || s->rows_q > TOK_ROWS_MAX || s->rows_k < 1 || s->rows_k > TOK_ROWS_MAX || s->docs < 1 || s->docs > (1 << 20) ||
+      s->heads_q < 1 || s->heads_q > 4096 || s->heads_k < 1 || s->heads_q % s->heads_k || s->head_dim < 1 || !dtype_ok(s->dtype) || s->lead_q < 0 ||
+      s->lead_k < 0 || !std::isfinite(s->scale) || !std::isfinite(s->cap) || s->cap < 0.f || s->reserved != 0)
+    return SLIDE_EINVAL;
+  const int64_t group = s->heads_q / s->heads_k;
+  if (s->head_dim % 16 || s->head_dim > 128 || group > 128) return SLIDE_EUNSUPPORTED;
+  // launches of 2^32 threads at most; 32 columns a wavefront
+  const int64_t most = s->rows_q * group > s->rows_k ? s->rows_q * group : s->rows_k;
+  if (most >= (1LL << 31) || (most / 32 + s->docs) * 64 * s->heads_k >= (1LL << 31) || s->rows_q * s->heads_q >= (1LL << 32)) return SLIDE_EUNSUPPORTED;
+  return SLIDE_OK;
+}
+TokCut cut_q(const slide_tokens_attn& s) {
+  return tok_cut(s.rows_q * (s.heads_q / s.heads_k), s.rows_k, s.docs, s.heads_k, s.dtype, s.head_dim);
+}
+TokCut cut_k(const slide_tokens_attn& s) {
+  return tok_cut(s.rows_k, s.rows_q * (s.heads_q / s.heads_k), s.docs, s.heads_k, s.dtype, s.head_dim);
+}
+size_t up256(size_t n) { return (n + 255) / 256 * 256; }
+// work space: the forward's partial outputs and their maxima and sums; the backward's deltas, partial dq, then in the same place partial dk and dv
+struct AttnWork { size_t fwd_part, fwd, delta, dq_part, k_part, bwd; };
+AttnWork attn_work(const slide_tokens_attn& s) {
+  const size_t q = (size_t)s.rows_q * s.heads_q, k = (size_t)s.rows_k * s.heads_k;
+  const TokCut cq = cut_q(s), ck = cut_k(s);
+  AttnWork w{};
+  w.fwd_part = cq.splits > 1 ? up256(cq.splits * q * s.head_dim * 4) : 0;
+  w.fwd = w.fwd_part + (cq.splits > 1 ? up256(cq.splits * q * 8) : 0);
+  w.delta = up256(q * 4);
+  w.dq_part = w.fwd_part;
+  w.k_part = ck.splits > 1 ? up256(ck.splits * k * s.head_dim * 4) : 0;
+  w.bwd = w.delta + (w.dq_part > 2 * w.k_part ? w.dq_part : 2 * w.k_part);
+  return w;
+}
+// pos_q, pos_k, slopes: all or none
+bool bias_ok(const float* a, const float* b, const float* slopes) {
+  if (!a && !b && !slopes) return true;
+  return a && b && slopes && aligned(a, 8) && aligned(b, 8) && aligned(slopes, 4);
+}
+TokAttn attn_of(const slide_tokens_attn& s) {
+  TokAttn g{};
+  g.rows_q = (int)s.rows_q; g.rows_k = (int)s.rows_k; g.docs = s.docs; g.hq = s.heads_q; g.hk = s.heads_k; g.group = s.heads_q / s.heads_k;
+  g.dim = s.head_dim; g.lead_q = s.lead_q; g.lead_k = s.lead_k; g.scale = s.scale; g.cap = s.cap;
+  return g;
+}
+
+}  // namespace
+
+extern "C" {
+
+int slide_head_rope_fwd(const slide_head_rope* s, const void* q, int64_t ldq, const void* k, int64_t ldk, const float* gq,
+                        const float* gk, const int32_t* pos, void* yq, int64_t ldyq, void* yk, int64_t ldyk, void* stream) {
+  const int rc = rope_ok(s);
+  if (rc) return rc;
+  const int64_t cq = (int64_t)s->heads_q * s->head_dim, ck = (int64_t)s->heads_k * s->head_dim;
+  if (!matrix_ok(q, s->dtype, ldq, cq) || !matrix_ok(yq, s->dtype, ldyq, cq) || (yq == q && ldyq != ldq) || !aligned(gq, 16)) return SLIDE_EINVAL;
+  if (s->heads_k ? !matrix_ok(k, s->dtype, ldk, ck) || !matrix_ok(yk, s->dtype, ldyk, ck) || (yk == k && ldyk != ldk) || yk == yq || !aligned(gk, 16)
+                 : k || yk || gk)
+    return SLIDE_EINVAL;
+  if (s->axes ? !pos || !aligned(pos, 4) : pos != nullptr) return SLIDE_EINVAL;
+  (void)hipGetLastError();
+  HeadRope g = rope_of(*s);
+  g.q = q; g.ldq = ldq; g.k = k; g.ldk = ldk; g.gq = gq; g.gk = gk; g.pos = pos; g.yq = yq; g.ldyq = ldyq; g.yk = yk; g.ldyk = ldyk;
+  return status(launch_head_rope_fwd(s->dtype, g, (hipStream_t)stream));
+}
+
+size_t slide_head_rope_workspace_bytes(const slide_head_rope* s) { return rope_ok(s) == SLIDE_OK ? head_rope_work_bytes(*s) : 0; }
+
+int slide_head_rope_bwd(const slide_head_rope* s, const void* dyq, int64_t lddyq, const void* dyk, int64_t lddyk, const void* q,
+                        int64_t ldq, const void* k, int64_t ldk, const float* gq, const float* gk, const int32_t* pos, void* dq,
+                        int64_t lddq, void* dk, int64_t lddk, float* dgq, float* dgk, int accumulate, void* work,
+                        size_t work_bytes, void* stream) {
+  int rc = rope_ok(s);
+  if (rc) return rc;
+  const int64_t cq = (int64_t)s->heads_q * s->head_dim, ck = (int64_t)s->heads_k * s->head_dim;
+  if (!matrix_ok(dyq, s->dtype, lddyq, cq) || !matrix_ok(dq, s->dtype, lddq, cq) || (dq == dyq && lddq != lddyq)) return SLIDE_EINVAL;
+  if (gq ? !matrix_ok(q, s->dtype, ldq, cq) || !aligned(gq, 16) || !dgq || !aligned(dgq, 4) || dq == q : dgq != nullptr) return SLIDE_EINVAL;
+  if (s->heads_k) {
+    if (!matrix_ok(dyk, s->dtype, lddyk, ck) || !matrix_ok(dk, s->dtype, lddk, ck) || (dk == dyk && lddk != lddyk) || dk == dq) return SLIDE_EINVAL;
+    if (gk ? !matrix_ok(k, s->dtype, ldk, ck) || !aligned(gk, 16) || !dgk || !aligned(dgk, 4) || dk == k || dgk == dgq : dgk != nullptr) return SLIDE_EINVAL;
+  } else if (dyk || dk || k || gk || dgk) {
+    return SLIDE_EINVAL;
+  }
+  if (s->axes ? !pos || !aligned(pos, 4) : pos != nullptr) return SLIDE_EINVAL;
+  rc = work_ok(work, work_bytes, head_rope_work_bytes(*s));
+  if (rc) return rc;
+  (void)hipGetLastError();
+  HeadRope g = rope_of(*s);
+  g.dyq = dyq; g.lddyq = lddyq; g.dyk = dyk; g.lddyk = lddyk; g.q = q; g.ldq = ldq; g.k = k; g.ldk = ldk; g.gq = gq; g.gk = gk; g.pos = pos;
+  g.yq = dq; g.ldyq = lddq; g.yk = dk; g.ldyk = lddk; g.dgq = dgq; g.dgk = dgk; g.accumulate = accumulate != 0; g.work = (float*)work;
+  return status(launch_head_rope_bwd(s->dtype, g, (hipStream_t)stream));
+}
+
+size_t slide_tokens_attn_workspace_bytes(const slide_tokens_attn* s, int backward) {
+  if (attn_ok(s) != SLIDE_OK) return 0;
+  const AttnWork w = attn_work(*s);
+  return backward && w.bwd > w.fwd ? w.bwd : w.fwd;
+}
+
+int slide_tokens_attn_fwd(const slide_tokens_attn* s, const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v,
+                          int64_t ldv, const int32_t* q_start, const int32_t* k_start, const float* pos_q, const float* pos_k,
+                          const float* slopes, void* o, int64_t ldo, float* lse, void* work, size_t work_bytes, void* stream) {
+  int rc = attn_ok(s);
+  if (rc) return rc;
+  const int64_t cq = (int64_t)s->heads_q * s->head_dim, ck = (int64_t)s->heads_k * s->head_dim;
+  if (!matrix_ok(q, s->dtype, ldq, cq) || !matrix_ok(k, s->dtype, ldk, ck) || !matrix_ok(v, s->dtype, ldv, ck) || !matrix_ok(o, s->dtype, ldo, cq) ||
+      !q_start || !k_start || !aligned(q_start, 4) || !aligned(k_start, 4) || !lse || !aligned(lse, 4) || !bias_ok(pos_q, pos_k, slopes) || o == q || o == k || o == v)
+    return SLIDE_EINVAL;
+  const AttnWork w = attn_work(*s);
+  rc = work_ok(work, work_bytes, w.fwd);
+  if (rc) return rc;
+  (void)hipGetLastError();
+  const TokCut c = cut_q(*s);
+  TokAttn g = attn_of(*s);
+  g.q = q; g.ldq = (int)ldq; g.k = k; g.ldk = (int)ldk; g.v = v; g.ldv = (int)ldv; g.q_start = q_start; g.k_start = k_start;
+  g.pos_q = pos_q; g.pos_k = pos_k; g.slopes = slopes; g.o = o; g.ldo = (int)ldo; g.lse = lse;
+  g.splits = c.splits; g.part = (float*)work; g.part2 = (float*)((char*)work + w.fwd_part);
+  return status(launch_tok_fwd(s->dtype, g, c, (hipStream_t)stream));
+}
+
+int slide_tokens_attn_bwd(const slide_tokens_attn* s, const void* dout, int64_t lddo, const void* q, int64_t ldq, const void* k,
+                          int64_t ldk, const void* v, int64_t ldv, const void* o, int64_t ldo, const float* lse,
+                          const int32_t* q_start, const int32_t* k_start, const float* pos_q, const float* pos_k,
+                          const float* slopes, void* dq, int64_t lddq, void* dk, int64_t lddk, void* dv, int64_t lddv, void* work,
+                          size_t work_bytes, void* stream) {
+  int rc = attn_ok(s);
+  if (rc) return rc;
+  const int64_t cq = (int64_t)s->heads_q * s->head_dim, ck = (int64_t)s->heads_k * s->head_dim;
+  const int dt = s->dtype;
+  if (!matrix_ok(dout, dt, lddo, cq) || !matrix_ok(q, dt, ldq, cq) || !matrix_ok(k, dt, ldk, ck) || !matrix_ok(v, dt, ldv, ck) || !matrix_ok(o, dt, ldo, cq) ||
+      !matrix_ok(dq, dt, lddq, cq) || !matrix_ok(dk, dt, lddk, ck) || !matrix_ok(dv, dt, lddv, ck) || !lse || !aligned(lse, 4) || !q_start || !k_start ||
+      !aligned(q_start, 4) || !aligned(k_start, 4) || !bias_ok(pos_q, pos_k, slopes))
+    return SLIDE_EINVAL;
+  const void* const in[5] = {dout, q, k, v, o};
+  for (const void* p : in)
+    if (p == dq || p == dk || p == dv) return SLIDE_EINVAL;
+  if (dq == dk || dq == dv || dk == dv) return SLIDE_EINVAL;
+  const AttnWork w = attn_work(*s);
+  rc = work_ok(work, work_bytes, w.bwd);
+  if (rc) return rc;
+  (void)hipGetLastError();
+  const hipStream_t st = (hipStream_t)stream;
+  TokAttn g = attn_of(*s);
+  g.q = q; g.ldq = (int)ldq; g.k = k; g.ldk = (int)ldk; g.v = v; g.ldv = (int)ldv; g.o_in = o; g.ldo = (int)ldo; g.dout = dout; g.lddo = (int)lddo;
+  g.q_start = q_start; g.k_start = k_start; g.pos_q = pos_q; g.pos_k = pos_k; g.slopes = slopes; g.lse = const_cast<float*>(lse);
+  g.dq = dq; g.lddq = (int)lddq; g.dk = dk; g.lddk = (int)lddk; g.dv = dv; g.lddv = (int)lddv;
+  g.delta = (float*)work;
+  g.part = (float*)((char*)work + w.delta);
+  hipError_t e = launch_tok_delta(dt, g, st);
+  if (e != hipSuccess) return status(e);
+  const TokCut a = cut_q(*s), b = cut_k(*s);
+  g.splits = a.splits;
+  e = launch_tok_dq(dt, g, a, st);
+  if (e == hipSuccess && a.splits > 1) e = launch_tok_sum(dt, g.part, a.splits, g.rows_q, (int)cq, q_start, g.docs, dq, g.lddq, st);
+  if (e != hipSuccess) return status(e);
+  g.splits = b.splits;
+  g.part2 = (float*)((char*)g.part + w.k_part);
+  e = launch_tok_dkv(dt, g, b, st);
+  if (e == hipSuccess && b.splits > 1) {
+    e = launch_tok_sum(dt, g.part, b.splits, g.rows_k, (int)ck, k_start, g.docs, dk, g.lddk, st);
+    if (e == hipSuccess) e = launch_tok_sum(dt, g.part2, b.splits, g.rows_k, (int)ck, k_start, g.docs, dv, g.lddv, st);
+  }
+  return status(e);
+}
+
+}  // extern "C"
