@@ -64,7 +64,7 @@ typedef struct slide_tokens_attn {
   int32_t docs;                                /* 1 to 2^20 */
   int32_t heads_q, heads_k, head_dim, dtype;
   int32_t lead_q, lead_k;
-  float scale, cap;                            /* finite; cap 0: none */
+  float scale, cap;                            /* scale, and cap where it is not 0 (none): 2^-40 to 2^40 */
   int32_t reserved;                            /* 0 */
 } slide_tokens_attn;
 
@@ -75,7 +75,7 @@ size_t slide_tokens_attn_workspace_bytes(const slide_tokens_attn* s, int backwar
  * o = 0 and lse = -infinity.  q_start, k_start: [docs + 1], not decreasing, from 0 to rows_q / rows_k; rows before the first slide and behind the last
  * one are neither read nor written.  (What does not fit is taken as if cut to that range: never out of the matrices.)
  * pos_q [rows_q][2], pos_k [rows_k][2] float32, 8-byte aligned, finite and
- * below 2^60, and slopes [heads_q] float32, finite: all of them or none. */
+ * below 2^60, and slopes [heads_q] float32, below 2^40: all of them or none. */
 int slide_tokens_attn_fwd(const slide_tokens_attn* s, const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v,
                           int64_t ldv, const int32_t* q_start, const int32_t* k_start, const float* pos_q, const float* pos_k,
                           const float* slopes, void* o, int64_t ldo, float* lse, void* work, size_t work_bytes, void* hip_stream);

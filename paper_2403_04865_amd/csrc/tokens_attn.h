@@ -23,6 +23,9 @@ template <> struct TokType<float> { static constexpr int EPC = 4, KB = 32; };
 
 template <typename T, int DP> constexpr int tok_ldr() { return DP + TokType<T>::EPC; }   // elements between rows in LDS: 16-byte reads of eight rows meet no bank twice
 
+// Two wavefronts a SIMD where 256 registers hold what a wavefront keeps: their matrix instructions then take vector registers, without copies
+template <typename T, int DP, int NW> constexpr int tok_waves() { return NW == 4 ? (DP <= 64 || sizeof(T) == 2 ? 2 : 1) : (DP <= 64 ? 2 : 1); }
+
 // ---- which slide ----------------------------------------------------------------------------------
 // Slots of `width` columns are dealt to the slides without a table: slide i's begin at start[i] * group / width + i, which leaves each
 // as many as its columns take, whatever the lengths, of total / width + docs in all.
@@ -198,32 +201,42 @@ __device__ __forceinline__ void tok_store(const f32x16 (&a)[N], float f, O* row,
 }
 
 // ---- scores ---------------------------------------------------------------------------------------
-// Everything is in units of log2(e): y = c1 qk - slope d without a cap, c2 tanh(c1 qk) - slope d with one.
-struct TokScore { float c1, c2; };
+// A score is kept as z, a probability is 2^(ex z - ex max z): without a cap z = qk - slope / scale * d, so that the scale costs nothing beside
+// the maximum; with one z = c2 tanh(c1 qk) - slope d, all in units of log2(e), and ex is 1.
+struct TokScore { float c1, c2, ex, per_slope; };
 template <bool CAP>
 __device__ __forceinline__ TokScore tok_score_of(float scale, float cap) {
-  return CAP ? TokScore{scale / cap, cap * TOK_LOG2E} : TokScore{scale * TOK_LOG2E, 0.f};
+  return CAP ? TokScore{scale / cap, cap * TOK_LOG2E, 1.f, TOK_LOG2E} : TokScore{0.f, 0.f, scale * TOK_LOG2E, 1.f / scale};
 }
-// tanh(u) and, where wanted, its derivative, from e = exp(-2 |u|): (1 - e) / (1 + e) and 4 e / (1 + e)^2, which lose nothing for large
-// |u|.  For small |u| 1 - e has e's rounding, 2^-25 of one: float32 takes the series there (next term 2^-27 of u at 1/4).
+// tanh(u) and a quarter of its derivative.  float32: e = exp(-2 |u|), (1 - e) / (1 + e) and e / (1 + e)^2, which lose nothing for large |u|; for small
+// |u| 1 - e has e's rounding, 2^-25 of one, and the series is taken (next term 2^-27 of u at 1/4).
+// bfloat16: r = 1 / (1 + exp(2 u)), 1 - 2 r and r (1 - r), four operations fewer; off by 2^-24 of one, which is 2^-19 of a score at
+// a cap of 50, where a probability is rounded to 2^-9 of itself.
 template <typename T, bool SLOPE>
-__device__ __forceinline__ float tok_tanh(float u, float* slope) {
-  const float e = __builtin_amdgcn_exp2f(-2.f * TOK_LOG2E * fabsf(u));
-  const float r = __builtin_amdgcn_rcpf(1.f + e);
-  float t = (1.f - e) * r;
-  if (SLOPE) *slope = 4.f * e * r * r;
-  if (sizeof(T) == 4) {
-    const float w = u * u, a = fabsf(u);
+__device__ __forceinline__ float tok_cap(float qk, const TokScore& c, float* slope) {
+  if constexpr (sizeof(T) == 2) {
+    const float r = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(qk * (c.c1 * (2.f * TOK_LOG2E))));
+    if (SLOPE) *slope = fmaf(-r, r, r);
+    return fmaf(r, -2.f * c.c2, c.c2);
+  } else {
+    const float u = qk * c.c1, a = fabsf(u);
+    const float e = __builtin_amdgcn_exp2f(-2.f * TOK_LOG2E * a), r = __builtin_amdgcn_rcpf(1.f + e);
+    if (SLOPE) *slope = e * r * r;
+    const float w = u * u;
     const float series = a * fmaf(w, fmaf(w, fmaf(w, fmaf(w, 62.f / 2835.f, -17.f / 315.f), 2.f / 15.f), -1.f / 3.f), 1.f);
-    t = a < 0.25f ? series : t;
+    return c.c2 * copysignf(a < 0.25f ? series : (1.f - e) * r, u);
   }
-  return copysignf(t, u);
 }
+// slope: times c.per_slope
 template <typename T, bool BIAS, bool CAP, bool SLOPE>
-__device__ __forceinline__ float tok_score(float qk, float d, float slope, TokScore c, float* dt) {
-  float y = CAP ? c.c2 * tok_tanh<T, SLOPE>(qk * c.c1, dt) : qk * c.c1;
-  if (BIAS) y = fmaf(-slope, d, y);
-  return y;
+__device__ __forceinline__ float tok_score(float qk, float d, float slope, const TokScore& c, float* dt) {
+  const float z = CAP ? tok_cap<T, SLOPE>(qk, c, dt) : qk;
+  return BIAS ? fmaf(-slope, d, z) : z;
+}
+// 2^(ex z - at)
+template <bool CAP>
+__device__ __forceinline__ float tok_exp(float z, float at, const TokScore& c) {
+  return __builtin_amdgcn_exp2f(CAP ? z - at : fmaf(z, c.ex, -at));
 }
 __device__ __forceinline__ float tok_dist(float ax, float ay, float bx, float by) {
   const float x = ax - bx, y = ay - by;

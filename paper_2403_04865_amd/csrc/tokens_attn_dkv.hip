@@ -7,7 +7,7 @@ namespace sl {
 namespace {
 
 template <typename T, int DP, int NW, bool BIAS, bool CAP>
-__global__ void __launch_bounds__(NW * 64) tok_dkv_k(const TokAttn g, const int slots) {
+__global__ void __launch_bounds__(NW * 64, DP <= 64 && NW == 4 ? 2 : 1) tok_dkv_k(const TokAttn g, const int slots) {
   constexpr int KB = TokType<T>::KB, LDR = tok_ldr<T, DP>(), NB = KB / 32, W = NW * 32;
   __shared__ __attribute__((aligned(16))) T Qs[KB * LDR], Os[KB * LDR];
   __shared__ __attribute__((aligned(16))) float px[KB], py[KB], ps[KB], pl[KB], pd[KB];
@@ -46,74 +46,91 @@ __global__ void __launch_bounds__(NW * 64) tok_dkv_k(const TokAttn g, const int 
     qt.load_packed(qp, t0 * KB, cols, g.ldq, g.dim, g.group, magic);
     ot.load_packed(op, t0 * KB, cols, g.lddo, g.dim, g.group, magic);
   }
+  // keys without a place are among the first workgroups' only, whose loop is a copy of its own
+  auto pass = [&](auto lead) __attribute__((always_inline)) {
+    constexpr bool LEADS = decltype(lead)::value;
 #pragma unroll 1
-  for (int t = t0; t < t1; ++t) {
-    const int c0 = t * KB;
-    __syncthreads();
-    qt.store(Qs);
-    ot.store(Os);
-    if (threadIdx.x < KB) {
-      const int c = c0 + threadIdx.x;
-      float x = 0.f, y = 0.f, slope = 0.f, lse = INFINITY, delta = 0.f;   // a query that is not there: probabilities of zero
-      if (c < cols) {
-        const int qi = c / g.group, head = w.head * g.group + (c - qi * g.group);
-        const long long row = qlo + qi;
-        lse = g.lse[(long long)head * g.rows_q + row] * TOK_LOG2E;
-        delta = g.delta[(long long)head * g.rows_q + row];
-        if (BIAS && qi >= g.lead_q) {
-          const float2 p = *reinterpret_cast<const float2*>(g.pos_q + 2 * row);
-          x = p.x; y = p.y;
-          slope = g.slopes[head] * TOK_LOG2E;
+    for (int t = t0; t < t1; ++t) {
+      const int c0 = t * KB;
+      __syncthreads();
+      qt.store(Qs);
+      ot.store(Os);
+      if (threadIdx.x < KB) {
+        const int c = c0 + threadIdx.x;
+        float x = 0.f, y = 0.f, slope = 0.f, lse = INFINITY, delta = 0.f;   // a query that is not there: probabilities of zero
+        if (c < cols) {
+          const int qi = c / g.group, head = w.head * g.group + (c - qi * g.group);
+          const long long row = qlo + qi;
+          lse = g.lse[(long long)head * g.rows_q + row] * TOK_LOG2E;
+          delta = -g.delta[(long long)head * g.rows_q + row];
+          if (BIAS && qi >= g.lead_q) {
+            const float2 p = *reinterpret_cast<const float2*>(g.pos_q + 2 * row);
+            x = p.x; y = p.y;
+            slope = g.slopes[head] * sc.per_slope;
+          }
         }
+        if (BIAS) { px[threadIdx.x] = x; py[threadIdx.x] = y; ps[threadIdx.x] = slope; }
+        pl[threadIdx.x] = lse;
+        pd[threadIdx.x] = delta;
       }
-      if (BIAS) { px[threadIdx.x] = x; py[threadIdx.x] = y; ps[threadIdx.x] = slope; }
-      pl[threadIdx.x] = lse;
-      pd[threadIdx.x] = delta;
-    }
-    __syncthreads();
-    if (t + 1 < t1) {
-      qt.load_packed(qp, c0 + KB, cols, g.ldq, g.dim, g.group, magic);
-      ot.load_packed(op, c0 + KB, cols, g.lddo, g.dim, g.group, magic);
-    }
-#pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      f32x16 s = tok_zero(), dp = tok_zero();
-      tok_mul<T, DP>(s, Qs, b * 32, fk);
-      tok_mul<T, DP>(dp, Os, b * 32, fv);
-      f32x16 p;
-#pragma unroll
-      for (int q4 = 0; q4 < 4; ++q4) {
-        const int r0 = b * 32 + tok_row(q4 * 4);
-        f32x4 qx, qy, slope;
-        if (BIAS) {
-          qx = *reinterpret_cast<const f32x4*>(px + r0);
-          qy = *reinterpret_cast<const f32x4*>(py + r0);
-          slope = *reinterpret_cast<const f32x4*>(ps + r0);
-        }
-        const f32x4 lse = *reinterpret_cast<const f32x4*>(pl + r0), delta = *reinterpret_cast<const f32x4*>(pd + r0);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int r = q4 * 4 + i;
-          float d = BIAS ? tok_dist(qx[i], qy[i], kx, ky) : 0.f, dt = 1.f;
-          if (leads && !placed) d = 0.f;
-          const float y = tok_score<T, BIAS, CAP, true>(s[r], d, BIAS ? slope[i] : 0.f, sc, &dt);
-          p[r] = __builtin_amdgcn_exp2f(y - lse[i]);
-          float ds = p[r] * (dp[r] - delta[i]);
-          if (CAP) ds *= dt;
-          s[r] = ds;
-        }
+      __syncthreads();
+      if (t + 1 < t1) {
+        qt.load_packed(qp, c0 + KB, cols, g.ldq, g.dim, g.group, magic);
+        ot.load_packed(op, c0 + KB, cols, g.lddo, g.dim, g.group, magic);
       }
-      tok_mul_t<T, DP>(dv, Os, b * 32, p);
-      tok_mul_t<T, DP>(dk, Qs, b * 32, s);
+      auto block = [&](int b) __attribute__((always_inline)) {
+        f32x16 s = tok_zero(), dp, p;
+#pragma unroll
+        for (int q4 = 0; q4 < 4; ++q4) {   // the product starts from -delta
+          const f32x4 d = *reinterpret_cast<const f32x4*>(pd + b * 32 + tok_row(q4 * 4));
+#pragma unroll
+          for (int i = 0; i < 4; ++i) dp[q4 * 4 + i] = d[i];
+        }
+        tok_mul<T, DP>(s, Qs, b * 32, fk);
+        tok_mul<T, DP>(dp, Os, b * 32, fv);
+#pragma unroll
+        for (int q4 = 0; q4 < 4; ++q4) {
+          const int r0 = b * 32 + tok_row(q4 * 4);
+          f32x4 qx, qy, slope;
+          if (BIAS) {
+            qx = *reinterpret_cast<const f32x4*>(px + r0);
+            qy = *reinterpret_cast<const f32x4*>(py + r0);
+            slope = *reinterpret_cast<const f32x4*>(ps + r0);
+          }
+          const f32x4 lse = *reinterpret_cast<const f32x4*>(pl + r0);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int r = q4 * 4 + i;
+            float d = BIAS ? tok_dist(qx[i], qy[i], kx, ky) : 0.f, dt = 1.f;
+            if (LEADS && !placed) d = 0.f;
+            const float z = tok_score<T, BIAS, CAP, true>(s[r], d, BIAS ? slope[i] : 0.f, sc, &dt);
+            p[r] = tok_exp<CAP>(z, lse[i], sc);
+            float ds = p[r] * dp[r];
+            if (CAP) ds *= dt;
+            s[r] = ds;
+          }
+        }
+        tok_mul_t<T, DP>(dv, Os, b * 32, p);
+        tok_mul_t<T, DP>(dk, Qs, b * 32, s);
+      };
+#pragma unroll
+      for (int b = 0; b < NB; ++b) block(b);
     }
+  };
+  if constexpr (BIAS) {
+    if (leads) pass(std::true_type{});
+    else pass(std::false_type{});
+  } else {
+    pass(std::false_type{});
   }
   if (!valid) return;
+  const float f = CAP ? 4.f * g.scale : g.scale;   // scores' gradients carry a quarter of the cap's derivative
   if (g.splits > 1) {
     const long long at = ((w.split * (long long)g.rows_k + krow) * g.hk + w.head) * g.dim;
-    tok_store(dk, g.scale, g.part + at, g.dim);
+    tok_store(dk, f, g.part + at, g.dim);
     tok_store(dv, 1.f, g.part2 + at, g.dim);
   } else {
-    tok_store(dk, g.scale, (T*)g.dk + krow * g.lddk + w.head * g.dim, g.dim);
+    tok_store(dk, f, (T*)g.dk + krow * g.lddk + w.head * g.dim, g.dim);
     tok_store(dv, 1.f, (T*)g.dv + krow * g.lddv + w.head * g.dim, g.dim);
   }
 }

@@ -32,7 +32,7 @@ __global__ void __launch_bounds__(256) tok_delta_k(const TokAttn g) {
 }
 
 template <typename T, int DP, int NW, bool BIAS, bool CAP>
-__global__ void __launch_bounds__(NW * 64) tok_dq_k(const TokAttn g, const int slots) {
+__global__ void __launch_bounds__(NW * 64, (tok_waves<T, DP, NW>())) tok_dq_k(const TokAttn g, const int slots) {
   constexpr int KB = TokType<T>::KB, LDR = tok_ldr<T, DP>(), NB = KB / 32, W = NW * 32;
   __shared__ __attribute__((aligned(16))) T Ks[KB * LDR], Vs[KB * LDR];
   __shared__ __attribute__((aligned(16))) float px[KB], py[KB];
@@ -55,12 +55,12 @@ __global__ void __launch_bounds__(NW * 64) tok_dq_k(const TokAttn g, const int s
   // a column that is not there: infinite, so its probabilities are zero
   const float lse = valid ? g.lse[(long long)head * g.rows_q + qrow] * TOK_LOG2E : INFINITY;
   const float delta = valid ? g.delta[(long long)head * g.rows_q + qrow] : 0.f;
+  const TokScore sc = tok_score_of<CAP>(g.scale, g.cap);
   float qx = 0.f, qy = 0.f, slope = 0.f;
   if (BIAS && valid && qi >= g.lead_q) {
     qx = g.pos_q[2 * qrow]; qy = g.pos_q[2 * qrow + 1];
-    slope = g.slopes[head] * TOK_LOG2E;
+    slope = g.slopes[head] * sc.per_slope;
   }
-  const TokScore sc = tok_score_of<CAP>(g.scale, g.cap);
 
   const int tiles = (nk + KB - 1) / KB, per = (tiles + g.splits - 1) / g.splits;
   const int t0 = w.split * per, t1 = t0 + per < tiles ? t0 + per : tiles;
@@ -85,9 +85,8 @@ __global__ void __launch_bounds__(NW * 64) tok_dq_k(const TokAttn g, const int s
       kt.load(kp + (long long)(k0 + KB) * g.ldk, nk - k0 - KB, g.ldk, g.dim);
       vt.load(vp + (long long)(k0 + KB) * g.ldv, nk - k0 - KB, g.ldv, g.dim);
     }
-    const bool leads = BIAS && k0 < g.lead_k, last = k0 + KB > nk;   // uniform
-#pragma unroll
-    for (int b = 0; b < NB; ++b) {
+    auto block = [&](auto edge, int b) __attribute__((always_inline)) {
+      constexpr bool EDGE = decltype(edge)::value;
       f32x16 s = tok_zero(), dp = tok_zero();
       tok_mul<T, DP>(s, Ks, b * 32, fq);
       tok_mul<T, DP>(dp, Vs, b * 32, fo);
@@ -103,20 +102,27 @@ __global__ void __launch_bounds__(NW * 64) tok_dq_k(const TokAttn g, const int s
         for (int i = 0; i < 4; ++i) {
           const int r = q4 * 4 + i;
           float d = BIAS ? tok_dist(qx, qy, kx[i], ky[i]) : 0.f, dt = 1.f;
-          if (leads && k0 + r0 + i < g.lead_k) d = 0.f;
-          const float y = tok_score<T, BIAS, CAP, true>(s[r], d, slope, sc, &dt);
-          float ds = __builtin_amdgcn_exp2f(y - lse) * (dp[r] - delta);
+          if (EDGE && BIAS && k0 + r0 + i < g.lead_k) d = 0.f;
+          const float z = tok_score<T, BIAS, CAP, true>(s[r], d, slope, sc, &dt);
+          float ds = tok_exp<CAP>(z, lse, sc) * (dp[r] - delta);
           if (CAP) ds *= dt;
-          if (last && k0 + r0 + i >= nk) ds = 0.f;   // there K is zeros, but a probability may be no number
+          if (EDGE && k0 + r0 + i >= nk) ds = 0.f;   // there K is zeros, but a probability may be no number
           s[r] = ds;
         }
       }
       tok_mul_t<T, DP>(dq, Ks, b * 32, s);
+    };
+    const bool edge = (BIAS && k0 < g.lead_k) || k0 + KB > nk;   // uniform
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      if (edge) block(std::true_type{}, b);
+      else block(std::false_type{}, b);
     }
   }
   if (!valid) return;
-  if (g.splits > 1) tok_store(dq, g.scale, g.part + ((w.split * (long long)g.rows_q + qrow) * g.hq + head) * g.dim, g.dim);
-  else tok_store(dq, g.scale, (T*)g.dq + qrow * g.lddq + head * g.dim, g.dim);
+  const float f = CAP ? 4.f * g.scale : g.scale;   // scores' gradients carry a quarter of the cap's derivative
+  if (g.splits > 1) tok_store(dq, f, g.part + ((w.split * (long long)g.rows_q + qrow) * g.hq + head) * g.dim, g.dim);
+  else tok_store(dq, f, (T*)g.dq + qrow * g.lddq + head * g.dim, g.dim);
 }
 
 template <typename T>

@@ -6,7 +6,7 @@ namespace sl {
 namespace {
 
 template <typename T, int DP, int NW, bool BIAS, bool CAP>
-__global__ void __launch_bounds__(NW * 64) tok_fwd_k(const TokAttn g, const int slots) {
+__global__ void __launch_bounds__(NW * 64, (tok_waves<T, DP, NW>())) tok_fwd_k(const TokAttn g, const int slots) {
   constexpr int KB = TokType<T>::KB, LDR = tok_ldr<T, DP>(), NB = KB / 32, W = NW * 32;
   __shared__ __attribute__((aligned(16))) T Ks[KB * LDR], Vs[KB * LDR];
   __shared__ __attribute__((aligned(16))) float px[KB], py[KB];
@@ -25,12 +25,12 @@ __global__ void __launch_bounds__(NW * 64) tok_fwd_k(const TokAttn g, const int 
   const long long qrow = doc.lo + qi;
   TokFrag<T, DP> fq;
   tok_load_frag<T, DP>(fq, (const T*)g.q + qrow * g.ldq + head * g.dim, valid, g.dim);
+  const TokScore sc = tok_score_of<CAP>(g.scale, g.cap);
   float qx = 0.f, qy = 0.f, slope = 0.f;
   if (BIAS && valid && qi >= g.lead_q) {
     qx = g.pos_q[2 * qrow]; qy = g.pos_q[2 * qrow + 1];
-    slope = g.slopes[head] * TOK_LOG2E;
+    slope = g.slopes[head] * sc.per_slope;
   }
-  const TokScore sc = tok_score_of<CAP>(g.scale, g.cap);
 
   const int tiles = (nk + KB - 1) / KB, per = (tiles + g.splits - 1) / g.splits;
   const int t0 = w.split * per, t1 = t0 + per < tiles ? t0 + per : tiles;
@@ -62,41 +62,46 @@ __global__ void __launch_bounds__(NW * 64) tok_fwd_k(const TokAttn g, const int 
       s[b] = tok_zero();
       tok_mul<T, DP>(s[b], Ks, b * 32, fq);
     }
-    const bool leads = BIAS && k0 < g.lead_k, last = k0 + KB > nk;   // uniform
+    // the first and the last blocks hold keys without a place and keys that are not there: a copy of the loop of their own
+    auto scores = [&](auto edge) __attribute__((always_inline)) {
+      constexpr bool EDGE = decltype(edge)::value;
 #pragma unroll
-    for (int b = 0; b < NB; ++b)
+      for (int b = 0; b < NB; ++b)
 #pragma unroll
-      for (int q4 = 0; q4 < 4; ++q4) {
-        const int r0 = b * 32 + tok_row(q4 * 4);
-        f32x4 kx, ky;
-        if (BIAS) {
-          kx = *reinterpret_cast<const f32x4*>(px + r0);
-          ky = *reinterpret_cast<const f32x4*>(py + r0);
+        for (int q4 = 0; q4 < 4; ++q4) {
+          const int r0 = b * 32 + tok_row(q4 * 4);
+          f32x4 kx, ky;
+          if (BIAS) {
+            kx = *reinterpret_cast<const f32x4*>(px + r0);
+            ky = *reinterpret_cast<const f32x4*>(py + r0);
+          }
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            float d = BIAS ? tok_dist(qx, qy, kx[i], ky[i]) : 0.f;
+            if (EDGE && BIAS && k0 + r0 + i < g.lead_k) d = 0.f;
+            float z = tok_score<T, BIAS, CAP, false>(s[b][q4 * 4 + i], d, slope, sc, nullptr);
+            if (EDGE && k0 + r0 + i >= nk) z = -INFINITY;
+            s[b][q4 * 4 + i] = z;
+          }
         }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          float d = BIAS ? tok_dist(qx, qy, kx[i], ky[i]) : 0.f;
-          if (leads && k0 + r0 + i < g.lead_k) d = 0.f;
-          float y = tok_score<T, BIAS, CAP, false>(s[b][q4 * 4 + i], d, slope, sc, nullptr);
-          if (last && k0 + r0 + i >= nk) y = -INFINITY;
-          s[b][q4 * 4 + i] = y;
-        }
-      }
+    };
+    if ((BIAS && k0 < g.lead_k) || k0 + KB > nk) scores(std::true_type{});   // uniform
+    else scores(std::false_type{});
     float mn = m;
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
       for (int r = 0; r < 16; ++r) mn = fmaxf(mn, s[b][r]);
     mn = fmaxf(mn, __shfl_xor(mn, 32, 64));
-    const float ms = mn == -INFINITY ? 0.f : mn;
-    const float resc = __builtin_amdgcn_exp2f(m - ms);   // 0 at the first block
+    const float ms = mn == -INFINITY ? 0.f : mn * sc.ex;
+    const float resc = tok_exp<CAP>(m, ms, sc);   // 0 at the first block
     m = mn;
     float ls = 0.f;
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        s[b][r] = __builtin_amdgcn_exp2f(s[b][r] - ms);
+        s[b][r] = tok_exp<CAP>(s[b][r], ms, sc);
         ls += s[b][r];
       }
     l = fmaf(l, resc, ls);
@@ -110,6 +115,7 @@ __global__ void __launch_bounds__(NW * 64) tok_fwd_k(const TokAttn g, const int 
     for (int b = 0; b < NB; ++b) tok_mul_t<T, DP>(o, Vs, b * 32, s[b]);
   }
   l += __shfl_xor(l, 32, 64);
+  m *= sc.ex;
   if (!valid) return;
   const bool none = t0 >= t1;
   if (g.splits > 1) {

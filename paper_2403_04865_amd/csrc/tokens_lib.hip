@@ -8,6 +8,8 @@ using namespace sl;
 
 namespace {
 
+constexpr float FACTOR_MIN = 0x1p-40f, FACTOR_MAX = 0x1p40f;   // their quotients, and slopes over them, stay within float32
+
 bool dtype_ok(int dt) { return dt == DT_F32 || dt == DT_BF16; }
 // rows of `cols` elements that 16-byte accesses reach
 bool matrix_ok(const void* p, int dt, int64_t ld, int64_t cols) {
@@ -59,7 +61,7 @@ HeadRope rope_of(const slide_head_rope& s) {
 int attn_ok(const slide_tokens_attn* s) {
   if (!s || s->rows_q < 1 || s->rows_q > TOK_ROWS_MAX || s->rows_k < 1 || s->rows_k > TOK_ROWS_MAX || s->docs < 1 || s->docs > (1 << 20) ||
       s->heads_q < 1 || s->heads_q > 4096 || s->heads_k < 1 || s->heads_q % s->heads_k || s->head_dim < 1 || !dtype_ok(s->dtype) || s->lead_q < 0 ||
-      s->lead_k < 0 || !std::isfinite(s->scale) || !std::isfinite(s->cap) || s->cap < 0.f || s->reserved != 0)
+      s->lead_k < 0 || !(s->scale >= FACTOR_MIN && s->scale <= FACTOR_MAX) || !(s->cap == 0.f || (s->cap >= FACTOR_MIN && s->cap <= FACTOR_MAX)) || s->reserved != 0)
     return SLIDE_EINVAL;
   const int64_t group = s->heads_q / s->heads_k;
   if (s->head_dim % 16 || s->head_dim > 128 || group > 128) return SLIDE_EUNSUPPORTED;

@@ -101,7 +101,7 @@ def bwd(lib, s=None, **kw):
 
 INF, NAN = float("inf"), float("nan")
 BAD_ATTN = [dict(rows_q=0), dict(rows_k=0), dict(rows_q=1 << 31), dict(rows_k=(1 << 31) - 1), dict(docs=0), dict(docs=(1 << 20) + 1), dict(heads_q=0), dict(heads_k=0),
-            dict(heads_k=3), dict(heads_q=5000, heads_k=50), dict(head_dim=0), dict(dtype=2), dict(lead_q=-1), dict(lead_k=-1), dict(scale=INF), dict(scale=NAN),
+            dict(heads_k=3), dict(heads_q=5000, heads_k=50), dict(head_dim=0), dict(dtype=2), dict(lead_q=-1), dict(lead_k=-1), dict(scale=INF), dict(scale=NAN), dict(scale=0.0), dict(scale=-0.1), dict(scale=2.0 ** -41), dict(scale=2.0 ** 41), dict(cap=2.0 ** -41), dict(cap=2.0 ** 41),
             dict(cap=-1.0), dict(cap=INF), dict(cap=NAN), dict(reserved=1)]
 
 
