@@ -68,7 +68,7 @@ typedef struct slide_tokens_attn {
   int32_t reserved;                            /* 0 */
 } slide_tokens_attn;
 
-/* For the forward, or for both directions. */
+/* For the forward, or for both directions; 0 for what is refused. */
 size_t slide_tokens_attn_workspace_bytes(const slide_tokens_attn* s, int backward);
 
 /* o [rows_q][heads_q * head_dim] = softmax(scores) v, lse [heads_q][rows_q] float32 = log of the sum of exp(scores).  A slide without keys has

@@ -784,7 +784,7 @@ class TokensLib(_TensorCalls):
         return s
 
     def slide_tokens_attn_workspace_bytes(self, rows_q, rows_k, docs, heads_q, heads_k, head_dim, dtype, backward=False):
-        """For the forward, or for both directions; 0 where none is needed and for a shape that is refused."""
+        """For the forward, or for both directions; 0 for a shape that is refused."""
         s = self._attn(rows_q, rows_k, docs, heads_q, heads_k, head_dim, self._types.get(dtype, -1), 0, 0, 1.0, 0.0)
         return int(self.lib.slide_tokens_attn_workspace_bytes(s, int(backward)))
 

@@ -26,43 +26,105 @@ template <typename T, int DP> constexpr int tok_ldr() { return DP + TokType<T>::
 // Two wavefronts a SIMD where 256 registers hold what a wavefront keeps: their matrix instructions then take vector registers, without copies
 template <typename T, int DP, int NW> constexpr int tok_waves() { return NW == 4 ? (DP <= 64 || sizeof(T) == 2 ? 2 : 1) : (DP <= 64 ? 2 : 1); }
 
-// ---- which slide ----------------------------------------------------------------------------------
-// Slots of `width` columns are dealt to the slides without a table: slide i's begin at start[i] * group / width + i, which leaves each
-// as many as its columns take, whatever the lengths, of total / width + docs in all.
-struct TokDoc { int doc, lo, hi, tile; };   // rows lo .. hi - 1; the slot's first column is tile * width; doc < 0: none
+// ---- who does what --------------------------------------------------------------------------------
+// A pass is cut into units: `width` columns of a slide and key head against a block of KB rows.  They are numbered head by head, slide by slide,
+// column tile by column tile, block by block (a slide with columns and without rows has one for each tile, so that its results are
+// written), and every workgroup takes the same number of neighbouring ones, whatever the slides' lengths: no workgroup waits for the longest slide, and one
+// query against 50000 keys keeps the card as busy as 8000 against each other.  Column tiles that end up with several workgroups
+// leave partial results, which a second launch adds up in the order of the blocks.  (Before, a workgroup took a column tile, or every tile was
+// split alike: 65 tiles of 12 heads on 256 units were 4 rounds for the work of 3.05; 8193 rows, 12 heads of 64: 557 us.)
 __device__ __forceinline__ int tok_clamp(int v, int rows) { return v < 0 ? 0 : v > rows ? rows : v; }
-__device__ __forceinline__ TokDoc tok_find(const int* __restrict__ start, int docs, int rows, int group, int width, int slot) {
-  const int lane = threadIdx.x & 63;
-  // the last slide whose first slot is `slot` or before; 64 candidates at a time
-  int lo = 0, n = docs;
-  while (n > 0) {   // candidates lo .. lo + n - 1; n shrinks to an n / 64 (rounded up) with every turn
-    const int step = (n + 63) >> 6;
-    const int i = lo + lane * step;
-    const bool in = lane * step < n;
-    const long long first = in ? (long long)tok_clamp(start[in ? i : 0], rows) * group / width + i : 0;
-    const unsigned long long m = __builtin_amdgcn_ballot_w64(in && first <= slot);
-    if (!m) return {-1, 0, 0, 0};
-    const int l = 63 - __builtin_clzll(m);
-    lo += l * step;
-    n = step == 1 ? 0 : (n - l * step < step ? n - l * step : step);
+struct TokSide { const int* start; int rows, group, per; };   // rows of slides, `group` columns (or rows) each, `per` of them a tile (block)
+struct TokSpan { int lo, n; };                                // first row; packed columns (rows) of a slide
+__device__ __forceinline__ TokSpan tok_span(const TokSide& s, int doc) {
+  const int a = tok_clamp(s.start[doc], s.rows), b = tok_clamp(s.start[doc + 1], s.rows);
+  return {a, b > a ? (b - a) * s.group : 0};
+}
+__device__ __forceinline__ int tok_parts(int n, int per) { return (int)(((long long)n + per - 1) / per); }
+__device__ __forceinline__ long long tok_units(const TokSide& c, const TokSide& r, int doc) {
+  const int tiles = tok_parts(tok_span(c, doc).n, c.per), blocks = tok_parts(tok_span(r, doc).n, r.per);
+  return (long long)tiles * (blocks > 0 ? blocks : 1);
+}
+__device__ __forceinline__ long long tok_uniform(long long v) {
+  return (long long)(unsigned)__builtin_amdgcn_readfirstlane((int)v) | (long long)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32;
+}
+// The slides' first units: up to 64 slides a lane each, more in a table that a launch before has written ([docs + 1])
+struct TokIndex {
+  long long end, all;   // the lane's slide's last unit + 1 (docs <= 64); all units of a head
+  const long long* table;
+  int docs;
+  __device__ __forceinline__ TokIndex(const TokSide& c, const TokSide& r, int n, const long long* t) : end(0), table(t), docs(n) {
+    if (n > 64) {
+      all = tok_uniform(t[n]);
+      return;
+    }
+    const int lane = threadIdx.x & 63;
+    end = lane < n ? tok_units(c, r, lane) : 0;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const long long v = __shfl_up(end, o, 64);
+      if (lane >= o) end += v;
+    }
+    all = tok_uniform(__shfl(end, 63, 64));
   }
-  const int doc = __builtin_amdgcn_readfirstlane(lo);
-  const int a = tok_clamp(__builtin_amdgcn_readfirstlane(start[doc]), rows), b = tok_clamp(__builtin_amdgcn_readfirstlane(start[doc + 1]), rows);
-  return {doc, a, b > a ? b : a, slot - (int)((long long)a * group / width) - doc};
+  // the slide of unit u (below `all`), whose first unit goes to *first
+  __device__ __forceinline__ int find(long long u, long long* first) const {
+    const int lane = threadIdx.x & 63;
+    if (docs <= 64) {
+      const int l = __builtin_ctzll(__builtin_amdgcn_ballot_w64(end > u));
+      const long long before = __shfl(end, l > 0 ? l - 1 : 0, 64);
+      *first = l > 0 ? tok_uniform(before) : 0;
+      return l;
+    }
+    int lo = 0, n = docs;   // candidates lo .. lo + n - 1: the last one that begins at u or before; n shrinks to n / 64 with every turn
+    while (n > 1) {
+      const int step = (n + 63) >> 6;
+      const bool in = lane * step < n;
+      const unsigned long long m = __builtin_amdgcn_ballot_w64(in && table[in ? lo + lane * step : 0] <= u);
+      const int l = 63 - __builtin_clzll(m | 1);
+      lo += l * step;
+      n = n - l * step < step ? n - l * step : step;
+    }
+    *first = tok_uniform(table[lo]);
+    return lo;
+  }
+};
+// What a workgroup does of one column tile: rows' blocks a .. b - 1.  slot < 0: all of them; else the place of its partial results
+struct TokSeg { int head, doc, tile, a, b, slot; TokSpan c, r; };
+struct TokJoin { int pieces, head, doc, tile; };   // the tile that began in a workgroup and goes on in the next ones; pieces 0: none
+// Neighbouring workgroups (dealt to the eight XCDs in turn) are made neighbours within an XCD: its L2 holds a head's rows
+__device__ __forceinline__ int tok_block() { return (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3); }
+template <typename F>
+__device__ __forceinline__ void tok_walk(const TokSide& c, const TokSide& r, int docs, int heads, const long long* table, TokJoin* joins, F f) {
+  const TokIndex index(c, r, docs, table);
+  const int me = tok_block(), blocks = gridDim.x;
+  const long long all = index.all * heads;
+  long long per = (all + blocks - 1) / blocks;
+  per = per < TOK_LEAST ? TOK_LEAST : per;
+  long long u = me * per;
+  const long long end = u + per < all ? u + per : all;
+  TokJoin join = {0, 0, 0, 0};
+  while (u < end) {   // uniform
+    TokSeg s;
+    s.head = (int)(u / index.all);
+    long long first;
+    const long long v = u - s.head * index.all;
+    s.doc = index.find(v, &first);
+    s.c = tok_span(c, s.doc);
+    s.r = tok_span(r, s.doc);
+    s.c.lo = __builtin_amdgcn_readfirstlane(s.c.lo); s.c.n = __builtin_amdgcn_readfirstlane(s.c.n);
+    s.r.lo = __builtin_amdgcn_readfirstlane(s.r.lo); s.r.n = __builtin_amdgcn_readfirstlane(s.r.n);
+    const int n = tok_parts(s.r.n, r.per), rb = n > 0 ? n : 1;
+    s.tile = (int)((v - first) / rb);
+    s.a = (int)((v - first) - (long long)s.tile * rb);
+    s.b = end - u < rb - s.a ? s.a + (int)(end - u) : rb;
+    s.slot = s.a == 0 && s.b == rb ? -1 : s.a > 0 ? me : blocks + me;
+    if (s.a == 0 && s.b < rb) join = {(int)((u + rb - 1) / per) - me + 1, s.head, s.doc, s.tile};
+    f(s);
+    u += s.b - s.a;
+  }
+  if (threadIdx.x == 0) joins[me] = join;
 }
-// Where a workgroup is in a grid of `slots` x `splits` x `heads`, as many of one head as possible on one XCD (workgroups are dealt to the eight in
-// turn), whose L2 then holds that head's rows.  false: past the end.
-struct TokWork { int slot, split, head; };
-__device__ __forceinline__ bool tok_work(int slots, int splits, int heads, TokWork* w) {
-  const unsigned per = gridDim.x >> 3, at = (blockIdx.x & 7) * per + (blockIdx.x >> 3), all = (unsigned)slots * splits * heads;
-  if (at >= all) return false;
-  w->slot = at % (unsigned)slots;
-  const unsigned r = at / (unsigned)slots;
-  w->split = r % (unsigned)splits;
-  w->head = r / (unsigned)splits;
-  return true;
-}
-inline unsigned tok_grid(TokCut c, int heads) { return (unsigned)(((long long)c.slots * c.splits * heads + 7) / 8 * 8); }
 
 // ---- blocks of rows into LDS ----------------------------------------------------------------------
 __device__ __forceinline__ u32x4 tok_load16(__amdgpu_buffer_rsrc_t b, int voff) { return __builtin_amdgcn_raw_buffer_load_b128(b, voff, 0, 0); }
@@ -200,6 +262,16 @@ __device__ __forceinline__ void tok_store(const f32x16 (&a)[N], float f, O* row,
     }
 }
 
+// a value of the lane and of the other one of its column (lane ^ 32), without a way through LDS
+__device__ __forceinline__ float tok_other_max(float v) {
+  const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
+}
+__device__ __forceinline__ float tok_other_sum(float v) {
+  const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(x[0]) + __uint_as_float(x[1]);
+}
+
 // ---- scores ---------------------------------------------------------------------------------------
 // A score is kept as z, a probability is 2^(ex z - ex max z): without a cap z = qk - slope / scale * d, so that the scale costs nothing beside
 // the maximum; with one z = c2 tanh(c1 qk) - slope d, all in units of log2(e), and ex is 1.
@@ -257,6 +329,10 @@ __device__ __forceinline__ void tok_put_places(float* px, float* py, const float
     py[threadIdx.x] = y;
   }
 }
+
+// the sides of a pass: queries packed with the heads of a group, and keys
+__device__ __forceinline__ TokSide tok_queries(const TokAttn& g, int per) { return {g.q_start, g.rows_q, g.group, per}; }
+__device__ __forceinline__ TokSide tok_keys(const TokAttn& g, int per) { return {g.k_start, g.rows_k, 1, per}; }
 
 // dispatch on the padded head width, bias and cap
 template <typename T, typename F>

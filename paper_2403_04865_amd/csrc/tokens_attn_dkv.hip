@@ -7,132 +7,122 @@ namespace sl {
 namespace {
 
 template <typename T, int DP, int NW, bool BIAS, bool CAP>
-__global__ void __launch_bounds__(NW * 64, DP <= 64 && NW == 4 ? 2 : 1) tok_dkv_k(const TokAttn g, const int slots) {
+__global__ void __launch_bounds__(NW * 64, DP <= 64 && NW == 4 ? 2 : 1) tok_dkv_k(const TokAttn g) {
   constexpr int KB = TokType<T>::KB, LDR = tok_ldr<T, DP>(), NB = KB / 32, W = NW * 32;
   __shared__ __attribute__((aligned(16))) T Qs[KB * LDR], Os[KB * LDR];
   __shared__ __attribute__((aligned(16))) float px[KB], py[KB], ps[KB], pl[KB], pd[KB];
-  TokWork w;
-  if (!tok_work(slots, g.splits, g.hk, &w)) return;
-  const TokDoc doc = tok_find(g.k_start, g.docs, g.rows_k, 1, W, w.slot);
-  if (doc.doc < 0) return;
-  const int nk = doc.hi - doc.lo;
-  if ((long long)doc.tile * W >= nk) return;
-  const int qlo = tok_clamp(g.q_start[doc.doc], g.rows_q), qhi = tok_clamp(g.q_start[doc.doc + 1], g.rows_q);
-  const int cols = qhi > qlo ? (qhi - qlo) * g.group : 0;
-
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int j = doc.tile * W + wave * 32 + (lane & 31);
-  const bool valid = j < nk;
-  const long long krow = doc.lo + (valid ? j : 0);
-  TokFrag<T, DP> fk, fv;
-  tok_load_frag<T, DP>(fk, (const T*)g.k + krow * g.ldk + w.head * g.dim, valid, g.dim);
-  tok_load_frag<T, DP>(fv, (const T*)g.v + krow * g.ldv + w.head * g.dim, valid, g.dim);
-  const bool placed = BIAS && valid && j >= g.lead_k;
-  const bool leads = BIAS && doc.tile * W < g.lead_k;   // uniform
-  float kx = 0.f, ky = 0.f;
-  if (placed) { kx = g.pos_k[2 * krow]; ky = g.pos_k[2 * krow + 1]; }
   const TokScore sc = tok_score_of<CAP>(g.scale, g.cap);
-
-  const int tiles = (cols + KB - 1) / KB, per = (tiles + g.splits - 1) / g.splits;
-  const int t0 = w.split * per, t1 = t0 + per < tiles ? t0 + per : tiles;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const unsigned magic = tok_magic(g.group);
-  const T* const qp = (const T*)g.q + (long long)qlo * g.ldq + w.head * g.group * g.dim;
-  const T* const op = (const T*)g.dout + (long long)qlo * g.lddo + w.head * g.group * g.dim;
-  TokTile<T, DP, NW * 64> qt, ot;
-  f32x16 dk[DP / 32], dv[DP / 32];
-  tok_zero_all(dk);
-  tok_zero_all(dv);
-  if (t0 < t1) {
-    qt.load_packed(qp, t0 * KB, cols, g.ldq, g.dim, g.group, magic);
-    ot.load_packed(op, t0 * KB, cols, g.lddo, g.dim, g.group, magic);
-  }
-  // keys without a place are among the first workgroups' only, whose loop is a copy of its own
-  auto pass = [&](auto lead) __attribute__((always_inline)) {
-    constexpr bool LEADS = decltype(lead)::value;
+  tok_walk(tok_keys(g, W), tok_queries(g, KB), g.docs, g.hk, g.table, (TokJoin*)g.joins, [&](const TokSeg& w) __attribute__((always_inline)) {
+    const int cols = w.r.n, nk = w.c.n, qlo = w.r.lo;
+    const int j = w.tile * W + wave * 32 + (lane & 31);
+    const bool valid = j < nk, idle = w.tile * W + wave * 32 >= nk;
+    const long long krow = w.c.lo + (valid ? j : 0);
+    TokFrag<T, DP> fk, fv;
+    tok_load_frag<T, DP>(fk, (const T*)g.k + krow * g.ldk + w.head * g.dim, valid, g.dim);
+    tok_load_frag<T, DP>(fv, (const T*)g.v + krow * g.ldv + w.head * g.dim, valid, g.dim);
+    const bool placed = BIAS && valid && j >= g.lead_k;
+    float kx = 0.f, ky = 0.f;
+    if (placed) { kx = g.pos_k[2 * krow]; ky = g.pos_k[2 * krow + 1]; }
+    const T* const qp = (const T*)g.q + (long long)qlo * g.ldq + w.head * g.group * g.dim;
+    const T* const op = (const T*)g.dout + (long long)qlo * g.lddo + w.head * g.group * g.dim;
+    TokTile<T, DP, NW * 64> qt, ot;
+    f32x16 dk[DP / 32], dv[DP / 32];
+    tok_zero_all(dk);
+    tok_zero_all(dv);
+    // keys without a place are among the first tiles' only, whose loop is a copy of its own
+    auto pass = [&](auto lead) __attribute__((always_inline)) {
+      constexpr bool LEADS = decltype(lead)::value;
+      qt.load_packed(qp, w.a * KB, cols, g.ldq, g.dim, g.group, magic);
+      ot.load_packed(op, w.a * KB, cols, g.lddo, g.dim, g.group, magic);
 #pragma unroll 1
-    for (int t = t0; t < t1; ++t) {
-      const int c0 = t * KB;
-      __syncthreads();
-      qt.store(Qs);
-      ot.store(Os);
-      if (threadIdx.x < KB) {
-        const int c = c0 + threadIdx.x;
-        float x = 0.f, y = 0.f, slope = 0.f, lse = INFINITY, delta = 0.f;   // a query that is not there: probabilities of zero
-        if (c < cols) {
-          const int qi = c / g.group, head = w.head * g.group + (c - qi * g.group);
-          const long long row = qlo + qi;
-          lse = g.lse[(long long)head * g.rows_q + row] * TOK_LOG2E;
-          delta = -g.delta[(long long)head * g.rows_q + row];
-          if (BIAS && qi >= g.lead_q) {
-            const float2 p = *reinterpret_cast<const float2*>(g.pos_q + 2 * row);
-            x = p.x; y = p.y;
-            slope = g.slopes[head] * sc.per_slope;
+      for (int t = w.a; t < w.b; ++t) {
+        const int c0 = t * KB;
+        __syncthreads();
+        qt.store(Qs);
+        ot.store(Os);
+        if (threadIdx.x < KB) {
+          const int c = c0 + threadIdx.x;
+          float x = 0.f, y = 0.f, slope = 0.f, lse = INFINITY, delta = 0.f;   // a query that is not there: probabilities of zero
+          if (c < cols) {
+            const int qi = c / g.group, head = w.head * g.group + (c - qi * g.group);
+            const long long row = qlo + qi;
+            lse = g.lse[(long long)head * g.rows_q + row] * TOK_LOG2E;
+            delta = -g.delta[(long long)head * g.rows_q + row];
+            if (BIAS && qi >= g.lead_q) {
+              const float2 p = *reinterpret_cast<const float2*>(g.pos_q + 2 * row);
+              x = p.x; y = p.y;
+              slope = g.slopes[head] * sc.per_slope;
+            }
           }
+          if (BIAS) { px[threadIdx.x] = x; py[threadIdx.x] = y; ps[threadIdx.x] = slope; }
+          pl[threadIdx.x] = lse;
+          pd[threadIdx.x] = delta;
         }
-        if (BIAS) { px[threadIdx.x] = x; py[threadIdx.x] = y; ps[threadIdx.x] = slope; }
-        pl[threadIdx.x] = lse;
-        pd[threadIdx.x] = delta;
+        __syncthreads();
+        if (t + 1 < w.b) {
+          qt.load_packed(qp, c0 + KB, cols, g.ldq, g.dim, g.group, magic);
+          ot.load_packed(op, c0 + KB, cols, g.lddo, g.dim, g.group, magic);
+        }
+        if (idle) continue;   // uniform in a wavefront: none of its columns is there
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+          f32x16 s = tok_zero(), dp, p;
+#pragma unroll
+          for (int q4 = 0; q4 < 4; ++q4) {   // the product starts from -delta
+            const f32x4 d = *reinterpret_cast<const f32x4*>(pd + b * 32 + tok_row(q4 * 4));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) dp[q4 * 4 + i] = d[i];
+          }
+          tok_mul<T, DP>(s, Qs, b * 32, fk);
+          tok_mul<T, DP>(dp, Os, b * 32, fv);
+#pragma unroll
+          for (int q4 = 0; q4 < 4; ++q4) {
+            const int r0 = b * 32 + tok_row(q4 * 4);
+            f32x4 qx, qy, slope;
+            if (BIAS) {
+              qx = *reinterpret_cast<const f32x4*>(px + r0);
+              qy = *reinterpret_cast<const f32x4*>(py + r0);
+              slope = *reinterpret_cast<const f32x4*>(ps + r0);
+            }
+            const f32x4 lse = *reinterpret_cast<const f32x4*>(pl + r0);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int r = q4 * 4 + i;
+              float d = BIAS ? tok_dist(qx[i], qy[i], kx, ky) : 0.f, dt = 1.f;
+              if (LEADS && !placed) d = 0.f;
+              const float z = tok_score<T, BIAS, CAP, true>(s[r], d, BIAS ? slope[i] : 0.f, sc, &dt);
+              p[r] = tok_exp<CAP>(z, lse[i], sc);
+              float ds = p[r] * dp[r];
+              if (CAP) ds *= dt;
+              s[r] = ds;
+            }
+          }
+          tok_mul_t<T, DP>(dv, Os, b * 32, p);
+          tok_mul_t<T, DP>(dk, Qs, b * 32, s);
+        }
       }
-      __syncthreads();
-      if (t + 1 < t1) {
-        qt.load_packed(qp, c0 + KB, cols, g.ldq, g.dim, g.group, magic);
-        ot.load_packed(op, c0 + KB, cols, g.lddo, g.dim, g.group, magic);
+    };
+    if (cols > 0) {
+      if constexpr (BIAS) {
+        if (w.tile * W < g.lead_k) pass(std::true_type{});   // uniform
+        else pass(std::false_type{});
+      } else {
+        pass(std::false_type{});
       }
-      auto block = [&](int b) __attribute__((always_inline)) {
-        f32x16 s = tok_zero(), dp, p;
-#pragma unroll
-        for (int q4 = 0; q4 < 4; ++q4) {   // the product starts from -delta
-          const f32x4 d = *reinterpret_cast<const f32x4*>(pd + b * 32 + tok_row(q4 * 4));
-#pragma unroll
-          for (int i = 0; i < 4; ++i) dp[q4 * 4 + i] = d[i];
-        }
-        tok_mul<T, DP>(s, Qs, b * 32, fk);
-        tok_mul<T, DP>(dp, Os, b * 32, fv);
-#pragma unroll
-        for (int q4 = 0; q4 < 4; ++q4) {
-          const int r0 = b * 32 + tok_row(q4 * 4);
-          f32x4 qx, qy, slope;
-          if (BIAS) {
-            qx = *reinterpret_cast<const f32x4*>(px + r0);
-            qy = *reinterpret_cast<const f32x4*>(py + r0);
-            slope = *reinterpret_cast<const f32x4*>(ps + r0);
-          }
-          const f32x4 lse = *reinterpret_cast<const f32x4*>(pl + r0);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int r = q4 * 4 + i;
-            float d = BIAS ? tok_dist(qx[i], qy[i], kx, ky) : 0.f, dt = 1.f;
-            if (LEADS && !placed) d = 0.f;
-            const float z = tok_score<T, BIAS, CAP, true>(s[r], d, BIAS ? slope[i] : 0.f, sc, &dt);
-            p[r] = tok_exp<CAP>(z, lse[i], sc);
-            float ds = p[r] * dp[r];
-            if (CAP) ds *= dt;
-            s[r] = ds;
-          }
-        }
-        tok_mul_t<T, DP>(dv, Os, b * 32, p);
-        tok_mul_t<T, DP>(dk, Qs, b * 32, s);
-      };
-#pragma unroll
-      for (int b = 0; b < NB; ++b) block(b);
     }
-  };
-  if constexpr (BIAS) {
-    if (leads) pass(std::true_type{});
-    else pass(std::false_type{});
-  } else {
-    pass(std::false_type{});
-  }
-  if (!valid) return;
-  const float f = CAP ? 4.f * g.scale : g.scale;   // scores' gradients carry a quarter of the cap's derivative
-  if (g.splits > 1) {
-    const long long at = ((w.split * (long long)g.rows_k + krow) * g.hk + w.head) * g.dim;
-    tok_store(dk, f, g.part + at, g.dim);
-    tok_store(dv, 1.f, g.part2 + at, g.dim);
-  } else {
-    tok_store(dk, f, (T*)g.dk + krow * g.lddk + w.head * g.dim, g.dim);
-    tok_store(dv, 1.f, (T*)g.dv + krow * g.lddv + w.head * g.dim, g.dim);
-  }
+    if (!valid) return;
+    const float f = CAP ? 4.f * g.scale : g.scale;   // scores' gradients carry a quarter of the cap's derivative
+    if (w.slot >= 0) {
+      const long long at = ((long long)w.slot * W + wave * 32 + (lane & 31)) * g.dim;
+      tok_store(dk, f, g.part + at, g.dim);
+      tok_store(dv, 1.f, g.part2 + at, g.dim);
+    } else {
+      tok_store(dk, f, (T*)g.dk + krow * g.lddk + w.head * g.dim, g.dim);
+      tok_store(dv, 1.f, (T*)g.dv + krow * g.lddv + w.head * g.dim, g.dim);
+    }
+  });
 }
 
 template <typename T>
@@ -140,8 +130,8 @@ hipError_t run_dkv(const TokAttn& g, TokCut c, hipStream_t s) {
   return tok_dispatch<T>(g, [&](auto dp, auto bias, auto cap) {
     constexpr int DP = decltype(dp)::value;
     constexpr bool BIAS = decltype(bias)::value, CAP = decltype(cap)::value;
-    if (c.waves == 4) tok_dkv_k<T, DP, 4, BIAS, CAP><<<tok_grid(c, g.hk), 256, 0, s>>>(g, c.slots);
-    else tok_dkv_k<T, DP, 1, BIAS, CAP><<<tok_grid(c, g.hk), 64, 0, s>>>(g, c.slots);
+    if (c.waves == 4) tok_dkv_k<T, DP, 4, BIAS, CAP><<<c.blocks, 256, 0, s>>>(g);
+    else tok_dkv_k<T, DP, 1, BIAS, CAP><<<c.blocks, 64, 0, s>>>(g);
     return hipGetLastError();
   });
 }

@@ -40,18 +40,26 @@ struct TokAttn {
   void *o, *dq, *dk, *dv;
   float* lse;           // [hq][rows_q]
   float* delta;         // [hq][rows_q]: dout . o
-  // partial results of `splits` ranges of the other side's rows, one behind the other (splits > 1)
-  int splits;
-  float *part, *part2;
+  const long long* table;   // first units of the slides, where there are more than 64
+  void* joins;              // column tiles of several workgroups
+  float *part, *part2;      // their partial results: two tiles a workgroup
 };
-// How a pass is cut: workgroups of `waves` wavefronts with 32 columns (packed queries, or keys) each, `slots` of them a key head and range
-struct TokCut { int waves, slots, splits; };
-TokCut tok_cut(long long cols, long long other, int docs, int heads, int dt, int dim);
+constexpr int TOK_LEAST = 4;   // units of a workgroup at least: its start costs as much as two or three
+// How a pass is cut: `blocks` workgroups of `waves` wavefronts with 32 columns each (packed queries, or keys)
+struct TokCut { int waves, blocks; };
+TokCut tok_cut(long long cols, long long rows, int docs, int heads, int dt);
+inline size_t tok_table_bytes(int docs) { return docs > 64 ? ((size_t)docs + 1) * 8 : 0; }
+inline size_t tok_joins_bytes(TokCut c) { return (size_t)c.blocks * 16; }
+inline size_t tok_part_bytes(TokCut c, int dim) { return (size_t)2 * c.blocks * c.waves * 32 * dim * 4; }
+inline size_t tok_sums_bytes(TokCut c) { return (size_t)2 * c.blocks * c.waves * 32 * 8; }
+enum { TOK_FWD = 0, TOK_DQ = 1, TOK_DKV = 2 };
+// first units of the slides of a pass, where a table is used
+hipError_t launch_tok_table(int pass, int dt, const TokAttn& g, TokCut c, long long* table, hipStream_t s);
 hipError_t launch_tok_fwd(int dt, const TokAttn& g, TokCut c, hipStream_t s);
 hipError_t launch_tok_delta(int dt, const TokAttn& g, hipStream_t s);
 hipError_t launch_tok_dq(int dt, const TokAttn& g, TokCut c, hipStream_t s);
 hipError_t launch_tok_dkv(int dt, const TokAttn& g, TokCut c, hipStream_t s);
-// sums of partial gradients, in the order of the ranges; rows of slides only
-hipError_t launch_tok_sum(int dt, const float* part, int splits, int rows, int cols, const int* start, int docs, void* out, int ld, hipStream_t s);
+// results of the column tiles that several workgroups share, out of their parts
+hipError_t launch_tok_join(int pass, int dt, const TokAttn& g, TokCut c, hipStream_t s);
 
 }  // namespace sl

@@ -17,7 +17,6 @@ bool matrix_ok(const void* p, int dt, int64_t ld, int64_t cols) {
 }
 bool aligned(const void* p, unsigned n) { return ((uintptr_t)p & (n - 1)) == 0; }
 int work_ok(const void* work, size_t have, size_t need) {
-  if (!need) return SLIDE_OK;
   if (!work || have < need) return SLIDE_EARENA;
   return aligned(work, 256) ? SLIDE_OK : SLIDE_EINVAL;
 }
@@ -65,31 +64,38 @@ int attn_ok(const slide_tokens_attn* s) {
     return SLIDE_EINVAL;
   const int64_t group = s->heads_q / s->heads_k;
   if (s->head_dim % 16 || s->head_dim > 128 || group > 128) return SLIDE_EUNSUPPORTED;
-  // launches of 2^32 threads at most; 32 columns a wavefront
-  const int64_t most = s->rows_q * group > s->rows_k ? s->rows_q * group : s->rows_k;
-  if (most >= (1LL << 31) || (most / 32 + s->docs) * 64 * s->heads_k >= (1LL << 31) || s->rows_q * s->heads_q >= (1LL << 32)) return SLIDE_EUNSUPPORTED;
+  // packed columns are counted in 32 bits, and a launch has 2^32 threads at most: eight a row and head
+  if (s->rows_q * group > TOK_ROWS_MAX || s->rows_q * s->heads_q >= (1LL << 29)) return SLIDE_EUNSUPPORTED;
   return SLIDE_OK;
 }
-TokCut cut_q(const slide_tokens_attn& s) {
-  return tok_cut(s.rows_q * (s.heads_q / s.heads_k), s.rows_k, s.docs, s.heads_k, s.dtype, s.head_dim);
-}
-TokCut cut_k(const slide_tokens_attn& s) {
-  return tok_cut(s.rows_k, s.rows_q * (s.heads_q / s.heads_k), s.docs, s.heads_k, s.dtype, s.head_dim);
-}
+TokCut cut_q(const slide_tokens_attn& s) { return tok_cut(s.rows_q * (s.heads_q / s.heads_k), s.rows_k, s.docs, s.heads_k, s.dtype); }
+TokCut cut_k(const slide_tokens_attn& s) { return tok_cut(s.rows_k, s.rows_q * (s.heads_q / s.heads_k), s.docs, s.heads_k, s.dtype); }
 size_t up256(size_t n) { return (n + 255) / 256 * 256; }
-// work space: the forward's partial outputs and their maxima and sums; the backward's deltas, partial dq, then in the same place partial dk and dv
-struct AttnWork { size_t fwd_part, fwd, delta, dq_part, k_part, bwd; };
-AttnWork attn_work(const slide_tokens_attn& s) {
-  const size_t q = (size_t)s.rows_q * s.heads_q, k = (size_t)s.rows_k * s.heads_k;
-  const TokCut cq = cut_q(s), ck = cut_k(s);
-  AttnWork w{};
-  w.fwd_part = cq.splits > 1 ? up256(cq.splits * q * s.head_dim * 4) : 0;
-  w.fwd = w.fwd_part + (cq.splits > 1 ? up256(cq.splits * q * 8) : 0);
-  w.delta = up256(q * 4);
-  w.dq_part = w.fwd_part;
-  w.k_part = ck.splits > 1 ? up256(ck.splits * k * s.head_dim * 4) : 0;
-  w.bwd = w.delta + (w.dq_part > 2 * w.k_part ? w.dq_part : 2 * w.k_part);
+// Work space of a pass: the slides' table, the shared tiles, their parts and what goes with them (maxima and sums, or the values' parts).  The
+// backward's passes follow one another in the same place, behind the deltas.
+struct PassWork { size_t joins, part, part2, bytes; };
+PassWork pass_work(const slide_tokens_attn& s, int pass) {
+  const TokCut c = pass == TOK_DKV ? cut_k(s) : cut_q(s);
+  PassWork w;
+  w.joins = up256(tok_table_bytes(s.docs));
+  w.part = w.joins + up256(tok_joins_bytes(c));
+  w.part2 = w.part + up256(tok_part_bytes(c, s.head_dim));
+  w.bytes = w.part2 + (pass == TOK_FWD ? up256(tok_sums_bytes(c)) : pass == TOK_DKV ? up256(tok_part_bytes(c, s.head_dim)) : 0);
   return w;
+}
+size_t delta_bytes(const slide_tokens_attn& s) { return up256((size_t)s.rows_q * s.heads_q * 4); }
+size_t bwd_bytes(const slide_tokens_attn& s) {
+  const size_t a = pass_work(s, TOK_DQ).bytes, b = pass_work(s, TOK_DKV).bytes;
+  return delta_bytes(s) + (a > b ? a : b);
+}
+hipError_t run_pass(int pass, const slide_tokens_attn& s, TokAttn g, char* work, hipStream_t st) {
+  const TokCut c = pass == TOK_DKV ? cut_k(s) : cut_q(s);
+  const PassWork w = pass_work(s, pass);
+  g.table = (const long long*)work; g.joins = work + w.joins; g.part = (float*)(work + w.part); g.part2 = (float*)(work + w.part2);
+  hipError_t e = launch_tok_table(pass, s.dtype, g, c, (long long*)work, st);
+  if (e != hipSuccess) return e;
+  e = pass == TOK_FWD ? launch_tok_fwd(s.dtype, g, c, st) : pass == TOK_DQ ? launch_tok_dq(s.dtype, g, c, st) : launch_tok_dkv(s.dtype, g, c, st);
+  return e != hipSuccess ? e : launch_tok_join(pass, s.dtype, g, c, st);
 }
 // pos_q, pos_k, slopes: all or none
 bool bias_ok(const float* a, const float* b, const float* slopes) {
@@ -152,8 +158,8 @@ int slide_head_rope_bwd(const slide_head_rope* s, const void* dyq, int64_t lddyq
 
 size_t slide_tokens_attn_workspace_bytes(const slide_tokens_attn* s, int backward) {
   if (attn_ok(s) != SLIDE_OK) return 0;
-  const AttnWork w = attn_work(*s);
-  return backward && w.bwd > w.fwd ? w.bwd : w.fwd;
+  const size_t f = pass_work(*s, TOK_FWD).bytes, b = backward ? bwd_bytes(*s) : 0;
+  return b > f ? b : f;
 }
 
 int slide_tokens_attn_fwd(const slide_tokens_attn* s, const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v,
@@ -165,16 +171,13 @@ int slide_tokens_attn_fwd(const slide_tokens_attn* s, const void* q, int64_t ldq
   if (!matrix_ok(q, s->dtype, ldq, cq) || !matrix_ok(k, s->dtype, ldk, ck) || !matrix_ok(v, s->dtype, ldv, ck) || !matrix_ok(o, s->dtype, ldo, cq) ||
       !q_start || !k_start || !aligned(q_start, 4) || !aligned(k_start, 4) || !lse || !aligned(lse, 4) || !bias_ok(pos_q, pos_k, slopes) || o == q || o == k || o == v)
     return SLIDE_EINVAL;
-  const AttnWork w = attn_work(*s);
-  rc = work_ok(work, work_bytes, w.fwd);
+  rc = work_ok(work, work_bytes, pass_work(*s, TOK_FWD).bytes);
   if (rc) return rc;
   (void)hipGetLastError();
-  const TokCut c = cut_q(*s);
   TokAttn g = attn_of(*s);
   g.q = q; g.ldq = (int)ldq; g.k = k; g.ldk = (int)ldk; g.v = v; g.ldv = (int)ldv; g.q_start = q_start; g.k_start = k_start;
   g.pos_q = pos_q; g.pos_k = pos_k; g.slopes = slopes; g.o = o; g.ldo = (int)ldo; g.lse = lse;
-  g.splits = c.splits; g.part = (float*)work; g.part2 = (float*)((char*)work + w.fwd_part);
-  return status(launch_tok_fwd(s->dtype, g, c, (hipStream_t)stream));
+  return status(run_pass(TOK_FWD, *s, g, (char*)work, (hipStream_t)stream));
 }
 
 int slide_tokens_attn_bwd(const slide_tokens_attn* s, const void* dout, int64_t lddo, const void* q, int64_t ldq, const void* k,
@@ -194,8 +197,7 @@ int slide_tokens_attn_bwd(const slide_tokens_attn* s, const void* dout, int64_t 
   for (const void* p : in)
     if (p == dq || p == dk || p == dv) return SLIDE_EINVAL;
   if (dq == dk || dq == dv || dk == dv) return SLIDE_EINVAL;
-  const AttnWork w = attn_work(*s);
-  rc = work_ok(work, work_bytes, w.bwd);
+  rc = work_ok(work, work_bytes, bwd_bytes(*s));
   if (rc) return rc;
   (void)hipGetLastError();
   const hipStream_t st = (hipStream_t)stream;
@@ -204,21 +206,10 @@ int slide_tokens_attn_bwd(const slide_tokens_attn* s, const void* dout, int64_t 
   g.q_start = q_start; g.k_start = k_start; g.pos_q = pos_q; g.pos_k = pos_k; g.slopes = slopes; g.lse = const_cast<float*>(lse);
   g.dq = dq; g.lddq = (int)lddq; g.dk = dk; g.lddk = (int)lddk; g.dv = dv; g.lddv = (int)lddv;
   g.delta = (float*)work;
-  g.part = (float*)((char*)work + w.delta);
+  char* const rest = (char*)work + delta_bytes(*s);
   hipError_t e = launch_tok_delta(dt, g, st);
-  if (e != hipSuccess) return status(e);
-  const TokCut a = cut_q(*s), b = cut_k(*s);
-  g.splits = a.splits;
-  e = launch_tok_dq(dt, g, a, st);
-  if (e == hipSuccess && a.splits > 1) e = launch_tok_sum(dt, g.part, a.splits, g.rows_q, (int)cq, q_start, g.docs, dq, g.lddq, st);
-  if (e != hipSuccess) return status(e);
-  g.splits = b.splits;
-  g.part2 = (float*)((char*)g.part + w.k_part);
-  e = launch_tok_dkv(dt, g, b, st);
-  if (e == hipSuccess && b.splits > 1) {
-    e = launch_tok_sum(dt, g.part, b.splits, g.rows_k, (int)ck, k_start, g.docs, dk, g.lddk, st);
-    if (e == hipSuccess) e = launch_tok_sum(dt, g.part2, b.splits, g.rows_k, (int)ck, k_start, g.docs, dv, g.lddv, st);
-  }
+  if (e == hipSuccess) e = run_pass(TOK_DQ, *s, g, rest, st);
+  if (e == hipSuccess) e = run_pass(TOK_DKV, *s, g, rest, st);
   return status(e);
 }
 

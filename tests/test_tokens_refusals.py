@@ -148,13 +148,11 @@ def test_attention_work_space(lib):
         if b > f:
             assert bwd(lib, s, bytes=b - 1) == EARENA
         assert bwd(lib, s, work=AT + 64) == EINVAL
-        if f:
-            assert fwd(lib, s, bytes=f) == EHIP and fwd(lib, s, bytes=f - 1) == EARENA and fwd(lib, s, work=None, bytes=0) == EARENA
-        else:
-            assert fwd(lib, s, work=None, bytes=0) == EHIP
-    # one query, many keys: the keys are split; as many rows as fill the card: nothing is
-    assert lib.slide_tokens_attn_workspace_bytes(C.byref(attn(rows_q=1, rows_k=50000, docs=1)), 0) > 0
-    assert lib.slide_tokens_attn_workspace_bytes(C.byref(attn(rows_q=100000, rows_k=100000, docs=1)), 0) == 0
+        assert fwd(lib, s, bytes=f) == EHIP and fwd(lib, s, bytes=f - 1) == EARENA and fwd(lib, s, work=None, bytes=0) == EARENA
+        assert fwd(lib, s, work=AT + 64) == EINVAL
+    # what a workgroup may leave is bounded, whatever the sizes
+    assert lib.slide_tokens_attn_workspace_bytes(C.byref(attn(rows_q=1 << 24, rows_k=1 << 24, docs=1)), 0) < 1 << 26
+    assert lib.slide_tokens_attn_workspace_bytes(C.byref(attn(rows_q=10, rows_k=10, docs=1)), 0) < 1 << 20
 
 
 def test_binding():
