@@ -17,7 +17,7 @@ namespace sl {
 namespace {
 
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
-constexpr int ROPE_BLOCKS = 1024;   // workgroups of the backward, each of which leaves its part of the gains' gradients
+constexpr int ROPE_BLOCKS = 512;   // workgroups of the backward's queries, and of its keys, each of which leaves its part of the gains' gradients
 
 __device__ __forceinline__ void load8(const float* p, float (&v)[8]) {
   const f32x4 a = *reinterpret_cast<const f32x4*>(p), b = *reinterpret_cast<const f32x4*>(p + 4);
@@ -117,47 +117,76 @@ __device__ __forceinline__ float inverse_rms(const Pairs& v, int dim, float eps)
   return 1.f / sqrtf(ss / (float)dim + eps);
 }
 
-// Head h of a row: queries first, then keys
-struct Place { bool key; int head; };
-__device__ __forceinline__ Place place_of(int h, int hq) { return h < hq ? Place{false, h} : Place{true, h - hq}; }
+// a thread's 16 values of a head as they lie in memory
+template <typename T> struct Raw { u32x4 v[sizeof(T)]; };
+template <typename T>
+__device__ __forceinline__ Raw<T> get_raw(const T* p, int apart) {
+  constexpr int H = sizeof(T) / 2;
+  Raw<T> r;
+#pragma unroll
+  for (int i = 0; i < H; ++i) {
+    r.v[i] = *reinterpret_cast<const u32x4*>(p + i * 4);
+    r.v[H + i] = *reinterpret_cast<const u32x4*>(p + apart + i * 4);
+  }
+  return r;
+}
+template <bool NEIGHBOURS, typename T>
+__device__ __forceinline__ Pairs pairs_of(const Raw<T>& r) {
+  T e[16];
+  __builtin_memcpy(e, &r, sizeof(r));
+  Pairs v;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    v.a[i] = to_f(e[NEIGHBOURS ? 2 * i : i]);
+    v.b[i] = to_f(e[NEIGHBOURS ? 2 * i + 1 : 8 + i]);
+  }
+  return v;
+}
 
-// BACKWARD: the gradients.  A thread's row is item / slices; it goes over heads item % slices, + slices, ...
-template <typename T, int LANES, bool NEIGHBOURS, bool BACKWARD>
-__global__ void __launch_bounds__(256) head_rope_k(const HeadRope g, const int slices, const long long items) {
+// blockIdx.y: queries or keys.  A thread's row is item / slices; it goes over heads item % slices, + slices, ..., the next one's values on
+// their way while it works.
+template <typename T, int LANES, bool NEIGHBOURS, bool BACKWARD, bool NORM>
+__device__ __forceinline__ void rope_side(const HeadRope& g, bool key, int slices, long long items) {
   constexpr int PER = 256 / LANES;
   const int sub = threadIdx.x % LANES, p0 = sub * 8;
   const bool mine = sub * 16 < g.dim;                 // head widths that are no power of two leave lanes over
   const int first = mine ? (NEIGHBOURS ? 2 * p0 : p0) : 0, apart = NEIGHBOURS ? 8 : g.dim / 2;
-  const int heads = g.hq + g.hk, turns = (heads + slices - 1) / slices;
-  Pairs gq, gk;
+  const int heads = key ? g.hk : g.hq, turns = (heads + slices - 1) / slices;
+  const T* const xs = (const T*)(key ? g.k : g.q);
+  const T* const ds = (const T*)(key ? g.dyk : g.dyq);
+  T* const ys = (T*)(key ? g.yk : g.yq);
+  const long long ldx = key ? g.ldk : g.ldq, ldd = key ? g.lddyk : g.lddyq, ldy = key ? g.ldyk : g.ldyq;
+  Pairs w, sum;   // the gain, and this thread's part of its gradient
 #pragma unroll
-  for (int i = 0; i < 8; ++i) gq.a[i] = gq.b[i] = gk.a[i] = gk.b[i] = 1.f;
-  if (g.gq) gq = get_pairs<NEIGHBOURS>(g.gq + first, apart);
-  if (g.gk) gk = get_pairs<NEIGHBOURS>(g.gk + first, apart);
-  Pairs sq, sk;   // this thread's part of the gains' gradients
-#pragma unroll
-  for (int i = 0; i < 8; ++i) sq.a[i] = sq.b[i] = sk.a[i] = sk.b[i] = 0.f;
+  for (int i = 0; i < 8; ++i) sum.a[i] = sum.b[i] = 0.f;
+  if (NORM) w = get_pairs<NEIGHBOURS>((key ? g.gk : g.gq) + first, apart);
 
   for (long long base = blockIdx.x * (long long)PER; base < items; base += (long long)gridDim.x * PER) {   // alike in a workgroup
     const long long item = base + threadIdx.x / LANES;
     const bool there = item < items;
     const long long row = there ? item / slices : 0;
     const int slice = there ? (int)(item - row * slices) : 0;
+    Raw<T> nx = {}, nd = {};
+    auto ask = [&](int h) __attribute__((always_inline)) {
+      if (there && mine && h < heads) {
+        if (!BACKWARD || NORM) nx = get_raw(xs + row * ldx + (long long)h * g.dim + first, apart);
+        if (BACKWARD) nd = get_raw(ds + row * ldd + (long long)h * g.dim + first, apart);
+      }
+    };
+    ask(slice);
     float c[8], s[8];
     angles(g, row, mine ? p0 : 0, c, s);
     for (int t = 0; t < turns; ++t) {
       const int h = slice + t * slices;
-      const bool on = there && h < heads, work = on && mine;
-      const Place at = place_of(on ? h : 0, g.hq);
-      const float* const gain = at.key ? g.gk : g.gq;
-      const Pairs& w = at.key ? gk : gq;
-      const long long col = at.head * g.dim + first;
-      Pairs x, y;
+      const bool work = there && mine && h < heads;
+      Pairs x = pairs_of<NEIGHBOURS>(nx), d = pairs_of<NEIGHBOURS>(nd), y;
+      ask(h + slices);
+      if (NORM && !mine) {   // lanes left over count for nothing
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x.a[i] = x.b[i] = y.a[i] = y.b[i] = 0.f;
-      if (work && (!BACKWARD || gain)) x = get_pairs<NEIGHBOURS>((const T*)(at.key ? g.k : g.q) + row * (at.key ? g.ldk : g.ldq) + col, apart);
+        for (int i = 0; i < 8; ++i) x.a[i] = x.b[i] = d.a[i] = d.b[i] = 0.f;
+      }
       if (!BACKWARD) {
-        if (gain) {
+        if (NORM) {
           const float r = inverse_rms<LANES>(x, g.dim, g.eps);
 #pragma unroll
           for (int i = 0; i < 8; ++i) { x.a[i] *= r * w.a[i]; x.b[i] *= r * w.b[i]; }
@@ -168,24 +197,19 @@ __global__ void __launch_bounds__(256) head_rope_k(const HeadRope g, const int s
           y.b[i] = fmaf(x.b[i], c[i], x.a[i] * s[i]);
         }
       } else {
-        Pairs d;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) d.a[i] = d.b[i] = 0.f;
-        if (work) d = get_pairs<NEIGHBOURS>((const T*)(at.key ? g.dyk : g.dyq) + row * (at.key ? g.lddyk : g.lddyq) + col, apart);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           y.a[i] = fmaf(d.a[i], c[i], d.b[i] * s[i]);
           y.b[i] = fmaf(d.b[i], c[i], -d.a[i] * s[i]);
         }
-        if (gain) {
+        if (NORM) {
           const float r = inverse_rms<LANES>(x, g.dim, g.eps);
           float dot = 0.f;
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
             x.a[i] *= r; x.b[i] *= r;
-            const float da = work ? y.a[i] * x.a[i] : 0.f, db = work ? y.b[i] * x.b[i] : 0.f;
-            if (at.key) { sk.a[i] += da; sk.b[i] += db; }
-            else { sq.a[i] += da; sq.b[i] += db; }
+            const float da = y.a[i] * x.a[i], db = y.b[i] * x.b[i];
+            if (work) { sum.a[i] += da; sum.b[i] += db; }
             dot = fmaf(da, w.a[i], fmaf(db, w.b[i], dot));
           }
           dot = group_sum<LANES>(dot) / (float)g.dim;
@@ -196,44 +220,51 @@ __global__ void __launch_bounds__(256) head_rope_k(const HeadRope g, const int s
           }
         }
       }
-      if (work) put_pairs<NEIGHBOURS>((T*)(at.key ? g.yk : g.yq) + row * (at.key ? g.ldyk : g.ldyq) + col, apart, y);
+      if (work) put_pairs<NEIGHBOURS>(ys + row * ldy + (long long)h * g.dim + first, apart, y);
     }
   }
-  if (!BACKWARD || (!g.gq && !g.gk)) return;
-  // over the rows of a wavefront, then of the workgroup's four; work[workgroup][queries, keys][columns of a head]
-  __shared__ float red[4][LANES][32];
+  if (!BACKWARD || !NORM) return;
+  // over the rows of a wavefront, then of the workgroup's four; work[queries, keys][workgroup][columns of a head]
+  __shared__ float red[4][LANES][16];
 #pragma unroll
-  for (int i = 0; i < 32; ++i) {
-    float v = i < 8 ? sq.a[i] : i < 16 ? sq.b[i - 8] : i < 24 ? sk.a[i - 16] : sk.b[i - 24];
+  for (int i = 0; i < 16; ++i) {
+    float v = i < 8 ? sum.a[i] : sum.b[i - 8];
 #pragma unroll
     for (int o = LANES; o < 64; o <<= 1) v += __shfl_xor(v, o, 64);
     if ((threadIdx.x & 63) < LANES) red[threadIdx.x >> 6][sub][i] = v;
   }
   __syncthreads();
-  for (int e = threadIdx.x; e < LANES * 32; e += 256) {
-    const int l = e / 32, i = e % 32, pair = l * 8 + (i & 7), second = (i >> 3) & 1;
+  for (int e = threadIdx.x; e < LANES * 16; e += 256) {
+    const int l = e / 16, i = e % 16, pair = l * 8 + (i & 7), second = i >> 3;
     if (l * 16 >= g.dim) continue;
     const int col = NEIGHBOURS ? 2 * pair + second : pair + second * (g.dim / 2);
-    g.work[((long long)blockIdx.x * 2 + (i >> 4)) * g.dim + col] = (red[0][l][i] + red[1][l][i]) + (red[2][l][i] + red[3][l][i]);
+    g.work[((long long)key * gridDim.x + blockIdx.x) * g.dim + col] = (red[0][l][i] + red[1][l][i]) + (red[2][l][i] + red[3][l][i]);
   }
 }
+template <typename T, int LANES, bool NEIGHBOURS, bool BACKWARD>
+__global__ void __launch_bounds__(256) head_rope_k(const HeadRope g, const int slices, const long long items) {
+  const bool key = blockIdx.y == 1;
+  if (key ? g.gk != nullptr : g.gq != nullptr) rope_side<T, LANES, NEIGHBOURS, BACKWARD, true>(g, key, slices, items);
+  else rope_side<T, LANES, NEIGHBOURS, BACKWARD, false>(g, key, slices, items);
+}
 
-// gains' gradients: 8 columns a workgroup, 32 threads each
+// gains' gradients: 4 columns a workgroup, 64 threads each; blockIdx.y: of the queries or of the keys
 __global__ void __launch_bounds__(256) rope_gain_k(const float* __restrict__ work, int blocks, int dim, float* dgq, float* dgk, int accumulate) {
-  __shared__ float red[32][9];
-  const int c = threadIdx.x & 7, part = threadIdx.x >> 3, col = blockIdx.x * 8 + c;
+  float* const out = blockIdx.y ? dgk : dgq;
+  if (!out) return;
+  __shared__ float red[64][5];
+  const int c = threadIdx.x & 3, part = threadIdx.x >> 2, col = blockIdx.x * 4 + c;
+  const float* const at = work + (long long)blockIdx.y * blocks * dim + col;
   float v = 0.f;
-  for (int b = part; b < blocks; b += 32) v += work[(long long)b * 2 * dim + col];
+#pragma unroll 8
+  for (int b = part; b < blocks; b += 64) v += at[(long long)b * dim];
   red[part][c] = v;
   __syncthreads();
-  if (threadIdx.x >= 8) return;
+  if (threadIdx.x >= 4) return;
   v = 0.f;
 #pragma unroll
-  for (int i = 0; i < 32; ++i) v += red[i][threadIdx.x];
-  float* const out = col < dim ? dgq : dgk;
-  if (!out) return;
-  float* const at = out + (col < dim ? col : col - dim);
-  *at = accumulate ? *at + v : v;
+  for (int i = 0; i < 64; ++i) v += red[i][threadIdx.x];
+  out[col] = accumulate ? out[col] + v : v;
 }
 
 int lanes_of(int dim) { int l = 1; while (l * 16 < dim) l *= 2; return l; }
@@ -242,23 +273,19 @@ int slices_of(long long rows, int heads, int lanes) {
   const long long want = 256 * 1024, have = rows * lanes, n = (want + have - 1) / have;
   return (int)(n > heads ? heads : n);
 }
-long long backward_blocks(long long rows, int heads, int dim) {
-  const int lanes = lanes_of(dim), per = 256 / lanes;
-  const long long n = (rows * slices_of(rows, heads, lanes) + per - 1) / per;
-  return n < ROPE_BLOCKS ? n : ROPE_BLOCKS;
-}
+int slices_of(const HeadRope& g) { return slices_of(g.rows, g.hq > g.hk ? g.hq : g.hk, lanes_of(g.dim)); }
 
 template <typename T, bool BACKWARD>
 hipError_t run(const HeadRope& g, hipStream_t s) {
-  const int lanes = lanes_of(g.dim), slices = slices_of(g.rows, g.hq + g.hk, lanes), per = 256 / lanes;
+  const int lanes = lanes_of(g.dim), slices = slices_of(g), per = 256 / lanes;
   const long long items = g.rows * slices;
   long long blocks = (items + per - 1) / per;
   const long long most = BACKWARD ? ROPE_BLOCKS : 1 << 20;
   if (blocks > most) blocks = most;
   auto go = [&](auto l) {
     constexpr int L = decltype(l)::value;
-    if (g.neighbours) head_rope_k<T, L, true, BACKWARD><<<(unsigned)blocks, 256, 0, s>>>(g, slices, items);
-    else head_rope_k<T, L, false, BACKWARD><<<(unsigned)blocks, 256, 0, s>>>(g, slices, items);
+    if (g.neighbours) head_rope_k<T, L, true, BACKWARD><<<dim3((unsigned)blocks, g.hk ? 2 : 1), 256, 0, s>>>(g, slices, items);
+    else head_rope_k<T, L, false, BACKWARD><<<dim3((unsigned)blocks, g.hk ? 2 : 1), 256, 0, s>>>(g, slices, items);
   };
   switch (lanes) {
     case 1: go(std::integral_constant<int, 1>{}); break;
@@ -269,14 +296,14 @@ hipError_t run(const HeadRope& g, hipStream_t s) {
   }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || !BACKWARD || (!g.gq && !g.gk)) return e;
-  rope_gain_k<<<g.dim / 4, 256, 0, s>>>(g.work, (int)blocks, g.dim, g.gq ? g.dgq : nullptr, g.gk ? g.dgk : nullptr, g.accumulate);
+  rope_gain_k<<<dim3(g.dim / 4, g.hk ? 2 : 1), 256, 0, s>>>(g.work, (int)blocks, g.dim, g.gq ? g.dgq : nullptr, g.gk ? g.dgk : nullptr, g.accumulate);
   return hipGetLastError();
 }
 
 }  // namespace
 
 size_t head_rope_work_bytes(const slide_head_rope& s) {
-  const size_t n = (size_t)backward_blocks(s.rows, s.heads_q + s.heads_k, s.head_dim) * 2 * s.head_dim * sizeof(float);
+  const size_t n = (size_t)2 * ROPE_BLOCKS * s.head_dim * sizeof(float);
   return (n + 255) / 256 * 256;
 }
 hipError_t launch_head_rope_fwd(int dt, const HeadRope& g, hipStream_t s) { return dt == DT_F32 ? run<float, false>(g, s) : run<bf16, false>(g, s); }

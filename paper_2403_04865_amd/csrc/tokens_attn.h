@@ -26,6 +26,9 @@ template <typename T, int DP> constexpr int tok_ldr() { return DP + TokType<T>::
 // Two wavefronts a SIMD where 256 registers hold what a wavefront keeps: their matrix instructions then take vector registers, without copies
 template <typename T, int DP, int NW> constexpr int tok_waves() { return NW == 4 ? (DP <= 64 || sizeof(T) == 2 ? 2 : 1) : (DP <= 64 ? 2 : 1); }
 
+// where the kernels for two heads at a time are built (what it takes of the call: tok_cut)
+template <typename T, int DP, bool BIAS> constexpr bool tok_pairs() { return BIAS && DP == 64 && sizeof(T) == 2; }
+
 // ---- who does what --------------------------------------------------------------------------------
 // A pass is cut into units: `width` columns of a slide and key head against a block of KB rows.  They are numbered head by head, slide by slide,
 // column tile by column tile, block by block (a slide with columns and without rows has one for each tile, so that its results are
@@ -99,8 +102,7 @@ __device__ __forceinline__ void tok_walk(const TokSide& c, const TokSide& r, int
   const TokIndex index(c, r, docs, table);
   const int me = tok_block(), blocks = gridDim.x;
   const long long all = index.all * heads;
-  long long per = (all + blocks - 1) / blocks;
-  per = per < TOK_LEAST ? TOK_LEAST : per;
+  const long long per = (all + blocks - 1) / blocks;
   long long u = me * per;
   const long long end = u + per < all ? u + per : all;
   TokJoin join = {0, 0, 0, 0};
@@ -130,31 +132,47 @@ __device__ __forceinline__ void tok_walk(const TokSide& c, const TokSide& r, int
 __device__ __forceinline__ u32x4 tok_load16(__amdgpu_buffer_rsrc_t b, int voff) { return __builtin_amdgcn_raw_buffer_load_b128(b, voff, 0, 0); }
 
 // A thread's pieces of a block of KB rows of `dim` columns: NTHR threads, 16 bytes each, rows one behind the other.  Columns from dim
-// to DP and rows past the block's last are zeros (outside of the buffer).
-template <typename T, int DP, int NTHR>
+// to DP and rows past the last are zeros (outside of the buffer).
+template <typename T, int DP, int NTHR, int KB = TokType<T>::KB>
 struct TokTile {
-  static constexpr int EPC = TokType<T>::EPC, KB = TokType<T>::KB, CH = DP / EPC, TOTAL = KB * CH, ITER = (TOTAL + NTHR - 1) / NTHR, LDR = tok_ldr<T, DP>();
+  static constexpr int EPC = TokType<T>::EPC, CH = DP / EPC, TOTAL = KB * CH, ITER = (TOTAL + NTHR - 1) / NTHR, LDR = tok_ldr<T, DP>();
   static_assert(TOTAL % NTHR == 0, "every thread has as many pieces");
   u32x4 v[ITER];
-  // rows 0 .. rows - 1 of p at ld
-  __device__ __forceinline__ void load(const T* p, int rows, int ld, int dim) {
-    rows = rows < KB ? rows : KB;
-    const __amdgpu_buffer_rsrc_t b = dma_rows(p, rows, ld, dim);
+  int at[ITER];   // where the pieces are, from the block's first row on
+  __device__ __forceinline__ TokTile() {}
+  __device__ __forceinline__ TokTile(int ld, int dim) {
 #pragma unroll
     for (int i = 0; i < ITER; ++i) {
       const int c = threadIdx.x + i * NTHR, row = c / CH, col = c % CH * EPC;
-      v[i] = tok_load16(b, col < dim ? (row * ld + col) * (int)sizeof(T) : DMA_ABSENT);
+      at[i] = col < dim ? (row * ld + col) * (int)sizeof(T) : DMA_ABSENT;
     }
+  }
+  // rows 0 .. rows - 1 of p at ld
+  __device__ __forceinline__ void load(const T* p, int rows, int ld, int dim) {
+    const __amdgpu_buffer_rsrc_t b = dma_rows(p, rows < KB ? rows : KB, ld, dim);
+#pragma unroll
+    for (int i = 0; i < ITER; ++i) v[i] = tok_load16(b, at[i]);
+  }
+  // the same rows' columns of another head, with that tile's offsets
+  __device__ __forceinline__ void load_as(const TokTile& o, const T* p, int rows, int ld, int dim) {
+    const __amdgpu_buffer_rsrc_t b = dma_rows(p, rows < KB ? rows : KB, ld, dim);
+#pragma unroll
+    for (int i = 0; i < ITER; ++i) v[i] = tok_load16(b, o.at[i]);
   }
   // packed queries c0 .. c0 + KB - 1 of a slide with `cols` of them: p is its first query's first head of the group
   __device__ __forceinline__ void load_packed(const T* p, int c0, int cols, int ld, int dim, int group, unsigned magic) {
+    if (group == 1) {   // uniform
+      load(p + (long long)c0 * ld, cols - c0, ld, dim);
+      return;
+    }
     const int r0 = c0 / group, phase = c0 - r0 * group;
     const __amdgpu_buffer_rsrc_t b = dma_buffer(p + (long long)r0 * ld, DMA_MAX);
 #pragma unroll
     for (int i = 0; i < ITER; ++i) {
       const int c = threadIdx.x + i * NTHR, row = c / CH, col = c % CH * EPC;
       const unsigned x = row + phase, r = x * magic >> 16, h = x - r * group;
-      v[i] = tok_load16(b, col < dim && c0 + row < cols ? (int)((r * ld + h * dim + col) * sizeof(T)) : DMA_ABSENT);
+      const int to = (int)((r * ld + h * dim + col) * sizeof(T));
+      v[i] = tok_load16(b, col < dim && c0 + row < cols ? to : DMA_ABSENT);
     }
   }
   __device__ __forceinline__ void store(T* s) const {
@@ -180,57 +198,78 @@ __device__ __forceinline__ void tok_load_frag(TokFrag<T, DP>& f, const T* row, b
     if (valid && col < dim) f.v[i] = *reinterpret_cast<const u32x4*>(row + col);
   }
 }
-// acc[rows j0 .. j0 + 31][columns] += X f: contraction over the DP columns of X
+// Operands of a product out of LDS.  They are asked for all together and ahead of what comes between (left to the compiler, every product waited for
+// a read of its own).
+// rows j0 .. j0 + 31 of X, contraction over the DP columns
+template <typename T, int DP> struct TokRows { u32x4 v[DP / TokType<T>::EPC / 2]; };
 template <typename T, int DP>
-__device__ __forceinline__ void tok_mul(f32x16& acc, const T* X, int j0, const TokFrag<T, DP>& f) {
+__device__ __forceinline__ void tok_get(TokRows<T, DP>& x, const T* X, int j0) {
   const int li = threadIdx.x & 31, h2 = (threadIdx.x >> 5) & 1;
   const T* p = X + (j0 + li) * tok_ldr<T, DP>() + h2 * TokType<T>::EPC;
 #pragma unroll
+  for (int i = 0; i < DP / TokType<T>::EPC / 2; ++i) x.v[i] = *reinterpret_cast<const u32x4*>(p + 2 * i * TokType<T>::EPC);
+}
+// acc[rows][columns] += X f
+template <typename T, int DP>
+__device__ __forceinline__ void tok_mul(f32x16& acc, const TokRows<T, DP>& x, const TokFrag<T, DP>& f) {
+#pragma unroll
   for (int i = 0; i < DP / TokType<T>::EPC / 2; ++i) {
-    const u32x4 a = *reinterpret_cast<const u32x4*>(p + 2 * i * TokType<T>::EPC);
     if constexpr (sizeof(T) == 2) {
-      acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, f.v[i]), acc, 0, 0, 0);
+      acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x.v[i]), __builtin_bit_cast(bf16x8, f.v[i]), acc, 0, 0, 0);
     } else {
-      const f32x4 fa = __builtin_bit_cast(f32x4, a), fb = __builtin_bit_cast(f32x4, f.v[i]);
+      const f32x4 fa = __builtin_bit_cast(f32x4, x.v[i]), fb = __builtin_bit_cast(f32x4, f.v[i]);
 #pragma unroll
       for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(fa[e], fb[e], acc, 0, 0, 0);
     }
   }
 }
-// acc[DP][columns] += (rows j0 .. j0 + 31 of X)^T p: contraction over rows, p as the scores lie.  bfloat16: p is rounded to it (half a step, 2^-9 of each
-// probability and of either sign, where the result's own rounding is as large); the matrix cores take no wider operand beside bfloat16.
-template <typename T, int DP>
-__device__ __forceinline__ void tok_mul_t(f32x16 (&acc)[DP / 32], const T* X, int j0, const f32x16& p) {
-  constexpr int LDR = tok_ldr<T, DP>();
-  const int lane = threadIdx.x & 63, li = lane & 31, h2 = lane >> 5;
-  if constexpr (sizeof(T) == 2) {
-    // LDS transpose reads: within 16 lanes, lane s addresses four columns of row s / 4 and receives column s of the four rows
-    typedef short s16x4 __attribute__((ext_vector_type(4)));
-    typedef short s16x8 __attribute__((ext_vector_type(8)));
-    const int g = lane >> 4, s = lane & 15;
-    const T* q = X + (j0 + 4 * (g >> 1) + (s >> 2)) * LDR + 16 * (g & 1) + (s & 3) * 4;
+// the transpose of rows j0 .. j0 + 31 of X, contraction over the rows in the order in which an accumulator holds them
+template <typename T, int DP> struct TokCols;
+template <int DP> struct TokCols<bf16, DP> { bf16x8 v[2][DP / 32]; };
+template <int DP> struct TokCols<float, DP> { const float* at; };   // read one by one at the products, whose 64 cycles cover it
+template <int DP>
+__device__ __forceinline__ void tok_get_t(TokCols<bf16, DP>& x, const bf16* X, int j0) {
+  // LDS transpose reads: within 16 lanes, lane s addresses four columns of row s / 4 and receives column s of the four rows
+  typedef short s16x4 __attribute__((ext_vector_type(4)));
+  typedef short s16x8 __attribute__((ext_vector_type(8)));
+  constexpr int LDR = tok_ldr<bf16, DP>();
+  const int lane = threadIdx.x & 63, g = lane >> 4, s = lane & 15;
+  const bf16* q = X + (j0 + 4 * (g >> 1) + (s >> 2)) * LDR + 16 * (g & 1) + (s & 3) * 4;
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      bf16x8 b;
+  for (int t = 0; t < 2; ++t)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) b[i] = (bf16)p[8 * t + i];
-#pragma unroll
-      for (int d = 0; d < DP / 32; ++d) {
-        const T* at = q + 16 * t * LDR + d * 32;
-        const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)at);
-        const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(at + 8 * LDR));
-        const s16x8 a = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
-        acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), b, acc[d], 0, 0, 0);
-      }
+    for (int d = 0; d < DP / 32; ++d) {
+      const bf16* at = q + 16 * t * LDR + d * 32;
+      const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)at);
+      const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(at + 8 * LDR));
+      const s16x8 v = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+      x.v[t][d] = __builtin_bit_cast(bf16x8, v);
     }
-  } else {
-    const T* q = X + (j0 + 4 * h2) * LDR + li;
+}
+template <int DP>
+__device__ __forceinline__ void tok_get_t(TokCols<float, DP>& x, const float* X, int j0) {
+  x.at = X + (j0 + 4 * ((threadIdx.x >> 5) & 1)) * tok_ldr<float, DP>() + (threadIdx.x & 31);
+}
+// acc[DP][columns] += X^T p.  bfloat16: p is rounded to it (half a step, 2^-8 of each probability at most and of either sign, where the
+// result's own rounding is as large); the matrix cores take no wider operand beside bfloat16.
+template <int DP>
+__device__ __forceinline__ void tok_mul_t(f32x16 (&acc)[DP / 32], const TokCols<bf16, DP>& x, const f32x16& p) {
 #pragma unroll
-    for (int r = 0; r < 16; ++r)
+  for (int t = 0; t < 2; ++t) {
+    bf16x8 b;
 #pragma unroll
-      for (int d = 0; d < DP / 32; ++d)
-        acc[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(q[((r >> 2) * 8 + (r & 3)) * LDR + d * 32], p[r], acc[d], 0, 0, 0);
+    for (int i = 0; i < 8; ++i) b[i] = (bf16)p[8 * t + i];
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d) acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x.v[t][d], b, acc[d], 0, 0, 0);
   }
+}
+template <int DP>
+__device__ __forceinline__ void tok_mul_t(f32x16 (&acc)[DP / 32], const TokCols<float, DP>& x, const f32x16& p) {
+#pragma unroll
+  for (int r = 0; r < 16; ++r)
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d)
+      acc[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(x.at[((r >> 2) * 8 + (r & 3)) * tok_ldr<float, DP>() + d * 32], p[r], acc[d], 0, 0, 0);
 }
 // row of a block of 32 that register r of this lane holds
 __device__ __forceinline__ int tok_row(int r) { return (r >> 2) * 8 + ((threadIdx.x >> 5) & 1) * 4 + (r & 3); }
@@ -315,23 +354,30 @@ __device__ __forceinline__ float tok_dist(float ax, float ay, float bx, float by
   return __builtin_amdgcn_sqrtf(fmaf(x, x, y * y));   // within an ulp
 }
 
-// Positions of a block's keys in LDS, x and y apart, 0 for keys without a place and behind the last
+// Positions of a block's keys: 0 for keys without a place and behind the last.  Loaded a block ahead, like the tiles
+struct TokPlace { float x, y; };
 template <int KB>
-__device__ __forceinline__ void tok_put_places(float* px, float* py, const float* pos, int lo, int k0, int n, int lead) {
-  if (threadIdx.x < KB) {
-    const int j = k0 + threadIdx.x;
-    float x = 0.f, y = 0.f;
-    if (j < n && j >= lead) {
-      const float2 p = *reinterpret_cast<const float2*>(pos + 2LL * (lo + j));
-      x = p.x; y = p.y;
-    }
-    px[threadIdx.x] = x;
-    py[threadIdx.x] = y;
+__device__ __forceinline__ TokPlace tok_place(const float* pos, int lo, int k0, int n, int lead) {
+  const int j = k0 + threadIdx.x;
+  TokPlace p = {0.f, 0.f};
+  if (threadIdx.x < KB && j < n && j >= lead) {
+    const float2 v = *reinterpret_cast<const float2*>(pos + 2LL * (lo + j));
+    p.x = v.x; p.y = v.y;
   }
+  return p;
 }
 
+// Heads that a wavefront takes together where there is a bias, because the distances are then taken once for them: `heads` groups of NH, of
+// `pack` heads beside each other in the columns; the n-th of a group's is `step` heads on, its key head `kv_step` on.
+// One group a key head and all of its heads packed where NH is 1; half of them where 2 and they share a key head; two key heads else.
+struct TokHeads { int heads, pack, step, kv_step; };
+inline __host__ __device__ TokHeads tok_heads(const TokAttn& g, int nh) {
+  if (nh == 1) return {g.hk, g.group, 0, 0};
+  if (g.group == 1) return {g.hk / 2, 1, 1, 1};
+  return {g.hk, g.group / 2, g.group / 2, 0};
+}
 // the sides of a pass: queries packed with the heads of a group, and keys
-__device__ __forceinline__ TokSide tok_queries(const TokAttn& g, int per) { return {g.q_start, g.rows_q, g.group, per}; }
+__device__ __forceinline__ TokSide tok_queries(const TokAttn& g, int per, int pack) { return {g.q_start, g.rows_q, pack, per}; }
 __device__ __forceinline__ TokSide tok_keys(const TokAttn& g, int per) { return {g.k_start, g.rows_k, 1, per}; }
 
 // dispatch on the padded head width, bias and cap

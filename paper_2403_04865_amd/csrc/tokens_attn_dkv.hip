@@ -14,7 +14,7 @@ __global__ void __launch_bounds__(NW * 64, DP <= 64 && NW == 4 ? 2 : 1) tok_dkv_
   const TokScore sc = tok_score_of<CAP>(g.scale, g.cap);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const unsigned magic = tok_magic(g.group);
-  tok_walk(tok_keys(g, W), tok_queries(g, KB), g.docs, g.hk, g.table, (TokJoin*)g.joins, [&](const TokSeg& w) __attribute__((always_inline)) {
+  tok_walk(tok_keys(g, W), tok_queries(g, KB, g.group), g.docs, g.hk, g.table, (TokJoin*)g.joins, [&](const TokSeg& w) __attribute__((always_inline)) {
     const int cols = w.r.n, nk = w.c.n, qlo = w.r.lo;
     const int j = w.tile * W + wave * 32 + (lane & 31);
     const bool valid = j < nk, idle = w.tile * W + wave * 32 >= nk;
@@ -27,7 +27,25 @@ __global__ void __launch_bounds__(NW * 64, DP <= 64 && NW == 4 ? 2 : 1) tok_dkv_
     if (placed) { kx = g.pos_k[2 * krow]; ky = g.pos_k[2 * krow + 1]; }
     const T* const qp = (const T*)g.q + (long long)qlo * g.ldq + w.head * g.group * g.dim;
     const T* const op = (const T*)g.dout + (long long)qlo * g.lddo + w.head * g.group * g.dim;
-    TokTile<T, DP, NW * 64> qt, ot;
+    TokTile<T, DP, NW * 64> qt(g.ldq, g.dim), ot(g.lddo, g.dim);
+    // what belongs to a block's queries, loaded a block ahead like the tiles.  A query that is not there: probabilities of zero
+    struct Row { float x, y, slope, lse, delta; };
+    auto row_of = [&](int c0) __attribute__((always_inline)) {
+      Row r = {0.f, 0.f, 0.f, INFINITY, 0.f};
+      const int c = c0 + threadIdx.x;
+      if (threadIdx.x < KB && c < cols) {
+        const int qi = c / g.group, head = w.head * g.group + (c - qi * g.group);
+        const long long row = qlo + qi;
+        r.lse = g.lse[(long long)head * g.rows_q + row] * TOK_LOG2E;
+        r.delta = -g.delta[(long long)head * g.rows_q + row];
+        if (BIAS && qi >= g.lead_q) {
+          const float2 p = *reinterpret_cast<const float2*>(g.pos_q + 2 * row);
+          r.x = p.x; r.y = p.y;
+          r.slope = g.slopes[head] * sc.per_slope;
+        }
+      }
+      return r;
+    };
     f32x16 dk[DP / 32], dv[DP / 32];
     tok_zero_all(dk);
     tok_zero_all(dv);
@@ -36,6 +54,7 @@ __global__ void __launch_bounds__(NW * 64, DP <= 64 && NW == 4 ? 2 : 1) tok_dkv_
       constexpr bool LEADS = decltype(lead)::value;
       qt.load_packed(qp, w.a * KB, cols, g.ldq, g.dim, g.group, magic);
       ot.load_packed(op, w.a * KB, cols, g.lddo, g.dim, g.group, magic);
+      Row row = row_of(w.a * KB);
 #pragma unroll 1
       for (int t = w.a; t < w.b; ++t) {
         const int c0 = t * KB;
@@ -43,27 +62,15 @@ __global__ void __launch_bounds__(NW * 64, DP <= 64 && NW == 4 ? 2 : 1) tok_dkv_
         qt.store(Qs);
         ot.store(Os);
         if (threadIdx.x < KB) {
-          const int c = c0 + threadIdx.x;
-          float x = 0.f, y = 0.f, slope = 0.f, lse = INFINITY, delta = 0.f;   // a query that is not there: probabilities of zero
-          if (c < cols) {
-            const int qi = c / g.group, head = w.head * g.group + (c - qi * g.group);
-            const long long row = qlo + qi;
-            lse = g.lse[(long long)head * g.rows_q + row] * TOK_LOG2E;
-            delta = -g.delta[(long long)head * g.rows_q + row];
-            if (BIAS && qi >= g.lead_q) {
-              const float2 p = *reinterpret_cast<const float2*>(g.pos_q + 2 * row);
-              x = p.x; y = p.y;
-              slope = g.slopes[head] * sc.per_slope;
-            }
-          }
-          if (BIAS) { px[threadIdx.x] = x; py[threadIdx.x] = y; ps[threadIdx.x] = slope; }
-          pl[threadIdx.x] = lse;
-          pd[threadIdx.x] = delta;
+          if (BIAS) { px[threadIdx.x] = row.x; py[threadIdx.x] = row.y; ps[threadIdx.x] = row.slope; }
+          pl[threadIdx.x] = row.lse;
+          pd[threadIdx.x] = row.delta;
         }
         __syncthreads();
         if (t + 1 < w.b) {
           qt.load_packed(qp, c0 + KB, cols, g.ldq, g.dim, g.group, magic);
           ot.load_packed(op, c0 + KB, cols, g.lddo, g.dim, g.group, magic);
+          row = row_of(c0 + KB);
         }
         if (idle) continue;   // uniform in a wavefront: none of its columns is there
 #pragma unroll
@@ -75,8 +82,12 @@ __global__ void __launch_bounds__(NW * 64, DP <= 64 && NW == 4 ? 2 : 1) tok_dkv_
 #pragma unroll
             for (int i = 0; i < 4; ++i) dp[q4 * 4 + i] = d[i];
           }
-          tok_mul<T, DP>(s, Qs, b * 32, fk);
-          tok_mul<T, DP>(dp, Os, b * 32, fv);
+          TokRows<T, DP> qr, dr;
+          TokCols<T, DP> qc, dc;
+          tok_get<T, DP>(qr, Qs, b * 32);
+          tok_get<T, DP>(dr, Os, b * 32);
+          tok_mul<T, DP>(s, qr, fk);
+          tok_mul<T, DP>(dp, dr, fv);
 #pragma unroll
           for (int q4 = 0; q4 < 4; ++q4) {
             const int r0 = b * 32 + tok_row(q4 * 4);
@@ -99,8 +110,10 @@ __global__ void __launch_bounds__(NW * 64, DP <= 64 && NW == 4 ? 2 : 1) tok_dkv_
               s[r] = ds;
             }
           }
-          tok_mul_t<T, DP>(dv, Os, b * 32, p);
-          tok_mul_t<T, DP>(dk, Qs, b * 32, s);
+          tok_get_t(dc, Os, b * 32);
+          tok_mul_t<DP>(dv, dc, p);
+          tok_get_t(qc, Qs, b * 32);
+          tok_mul_t<DP>(dk, qc, s);
         }
       }
     };

@@ -32,13 +32,13 @@ __global__ void __launch_bounds__(256) tok_delta_k(const TokAttn g) {
 }
 
 template <typename T, int DP, int NW, bool BIAS, bool CAP>
-__global__ void __launch_bounds__(NW * 64, (tok_waves<T, DP, NW>())) tok_dq_k(const TokAttn g) {
+__global__ void __launch_bounds__(NW * 64, DP <= 64 && NW == 4 ? 2 : 1) tok_dq_k(const TokAttn g) {
   constexpr int KB = TokType<T>::KB, LDR = tok_ldr<T, DP>(), NB = KB / 32, W = NW * 32;
   __shared__ __attribute__((aligned(16))) T Ks[KB * LDR], Vs[KB * LDR];
   __shared__ __attribute__((aligned(16))) float px[KB], py[KB];
   const TokScore sc = tok_score_of<CAP>(g.scale, g.cap);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  tok_walk(tok_queries(g, W), tok_keys(g, KB), g.docs, g.hk, g.table, (TokJoin*)g.joins, [&](const TokSeg& w) __attribute__((always_inline)) {
+  tok_walk(tok_queries(g, W, g.group), tok_keys(g, KB), g.docs, g.hk, g.table, (TokJoin*)g.joins, [&](const TokSeg& w) __attribute__((always_inline)) {
     const int cols = w.c.n, nk = w.r.n, klo = w.r.lo;
     const int c = w.tile * W + wave * 32 + (lane & 31);
     const bool valid = c < cols, idle = w.tile * W + wave * 32 >= cols;
@@ -57,31 +57,38 @@ __global__ void __launch_bounds__(NW * 64, (tok_waves<T, DP, NW>())) tok_dq_k(co
     }
     const T* const kp = (const T*)g.k + (long long)klo * g.ldk + w.head * g.dim;
     const T* const vp = (const T*)g.v + (long long)klo * g.ldv + w.head * g.dim;
-    TokTile<T, DP, NW * 64> kt, vt;
+    TokTile<T, DP, NW * 64> kt(g.ldk, g.dim), vt(g.ldv, g.dim);
+    TokPlace place = {0.f, 0.f};
     f32x16 dq[DP / 32];
     tok_zero_all(dq);
     if (nk > 0) {
       kt.load(kp + (long long)w.a * KB * g.ldk, nk - w.a * KB, g.ldk, g.dim);
       vt.load(vp + (long long)w.a * KB * g.ldv, nk - w.a * KB, g.ldv, g.dim);
+      if (BIAS) place = tok_place<KB>(g.pos_k, klo, w.a * KB, nk, g.lead_k);
 #pragma unroll 1
       for (int t = w.a; t < w.b; ++t) {
         const int k0 = t * KB;
         __syncthreads();
         kt.store(Ks);
         vt.store(Vs);
-        if (BIAS) tok_put_places<KB>(px, py, g.pos_k, klo, k0, nk, g.lead_k);
+        if (BIAS && threadIdx.x < KB) { px[threadIdx.x] = place.x; py[threadIdx.x] = place.y; }
         __syncthreads();
         if (t + 1 < w.b) {
           kt.load(kp + (long long)(k0 + KB) * g.ldk, nk - k0 - KB, g.ldk, g.dim);
           vt.load(vp + (long long)(k0 + KB) * g.ldv, nk - k0 - KB, g.ldv, g.dim);
+          if (BIAS) place = tok_place<KB>(g.pos_k, klo, k0 + KB, nk, g.lead_k);
         }
         if (idle) continue;   // uniform in a wavefront: none of its columns is there
         // the first and the last blocks hold keys without a place and keys that are not there: a copy of the code of their own
         auto block = [&](auto edge, int b) __attribute__((always_inline)) {
           constexpr bool EDGE = decltype(edge)::value;
           f32x16 s = tok_zero(), dp = tok_zero();
-          tok_mul<T, DP>(s, Ks, b * 32, fq);
-          tok_mul<T, DP>(dp, Vs, b * 32, fo);
+          TokRows<T, DP> kr, vr;
+          TokCols<T, DP> kc;
+          tok_get<T, DP>(kr, Ks, b * 32);
+          tok_get<T, DP>(vr, Vs, b * 32);
+          tok_mul<T, DP>(s, kr, fq);
+          tok_mul<T, DP>(dp, vr, fo);
 #pragma unroll
           for (int q4 = 0; q4 < 4; ++q4) {
             const int r0 = b * 32 + tok_row(q4 * 4);
@@ -102,7 +109,8 @@ __global__ void __launch_bounds__(NW * 64, (tok_waves<T, DP, NW>())) tok_dq_k(co
               s[r] = ds;
             }
           }
-          tok_mul_t<T, DP>(dq, Ks, b * 32, s);
+          tok_get_t(kc, Ks, b * 32);
+          tok_mul_t<DP>(dq, kc, s);
         };
         const bool edge = (BIAS && k0 < g.lead_k) || k0 + KB > nk;   // uniform
 #pragma unroll

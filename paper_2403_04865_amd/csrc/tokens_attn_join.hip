@@ -34,20 +34,20 @@ __global__ void __launch_bounds__(1024) tok_table_k(const TokSide c, const TokSi
 }
 
 // A workgroup joins COLS columns of a tile.  A column's threads are groups of `lanes` with four of its values each, group z of them takes every
-// `zs`-th piece; the groups' results meet in LDS.  SOFTMAX: pieces are sums under maxima of their own.
+// `zs`-th piece; blockIdx.z is the head of a group; the groups' results meet in LDS.  SOFTMAX: pieces are sums under maxima of their own.
 template <typename T, int W, bool SOFTMAX>
-__global__ void __launch_bounds__(256) tok_join_k(const TokAttn g, const TokSide side, int blocks, const float* __restrict__ part,
-                                                  const float* __restrict__ stat, T* __restrict__ out, int ld) {
-  constexpr int COLS = 8;
-  __shared__ f32x4 sums[256];
-  __shared__ float2 stats[256];
+__global__ void __launch_bounds__(W == 32 ? 512 : 256) tok_join_k(const TokAttn g, const TokSide side, const TokHeads hs, int hstep, int blocks,
+                                                                  const float* __restrict__ part, const float* __restrict__ stat, T* __restrict__ out, int ld) {
+  constexpr int COLS = 8, NT = W == 32 ? 512 : 256;   // few columns mean many pieces
+  __shared__ f32x4 sums[NT];
+  __shared__ float2 stats[NT];
   const TokJoin j = ((const TokJoin*)g.joins)[blockIdx.x];
   if (j.pieces == 0) return;
   const TokSpan c = tok_span(side, j.doc);
   const int first = j.tile * W + blockIdx.y * COLS, here = c.n - first < COLS ? c.n - first : COLS;   // columns of this workgroup
   if (here <= 0) return;
   const int quads = g.dim >> 2, lanes = quads <= 4 ? 4 : quads <= 8 ? 8 : quads <= 16 ? 16 : 32;
-  const int cols = here <= 1 ? 1 : here <= 2 ? 2 : here <= 4 ? 4 : 8, zs = 256 / (lanes * cols);
+  const int cols = here <= 1 ? 1 : here <= 2 ? 2 : here <= 4 ? 4 : 8, zs = NT / (lanes * cols);
   const int quad = threadIdx.x & (lanes - 1), col = (threadIdx.x / lanes) & (cols - 1), z = threadIdx.x / (lanes * cols);
   const bool on = quad < quads && col < here;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
@@ -56,7 +56,7 @@ __global__ void __launch_bounds__(256) tok_join_k(const TokAttn g, const TokSide
 #pragma unroll 4
     for (int p = z; p < j.pieces; p += zs) {
       const long long slot = p == 0 ? blocks + (int)blockIdx.x : (int)blockIdx.x + p;   // the first piece is the end of its workgroup's units
-      const long long at = slot * W + blockIdx.y * COLS + col;
+      const long long at = (slot * gridDim.z + blockIdx.z) * W + blockIdx.y * COLS + col;
       const f32x4 v = *reinterpret_cast<const f32x4*>(part + at * g.dim + quad * 4);
       if (SOFTMAX) {
         const float2 s = *reinterpret_cast<const float2*>(stat + 2 * at);
@@ -93,7 +93,7 @@ __global__ void __launch_bounds__(256) tok_join_k(const TokAttn g, const TokSide
     }
   }
   if (!on) return;
-  const int at = first + col, qi = at / side.group, head = j.head * side.group + (at - qi * side.group);
+  const int at = first + col, qi = at / side.group, head = j.head * hstep + blockIdx.z * hs.step + (at - qi * side.group);
   const long long row = c.lo + qi;
   const float f = !SOFTMAX ? 1.f : l == 0.f ? 0.f : 1.f / l;
   typedef T T4 __attribute__((ext_vector_type(4)));
@@ -104,14 +104,18 @@ __global__ void __launch_bounds__(256) tok_join_k(const TokAttn g, const TokSide
   if (SOFTMAX && quad == 0) g.lse[head * (long long)g.rows_q + row] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * TOK_LN2;
 }
 
-TokSide side_of(const TokAttn& g, bool queries, int per) { return queries ? TokSide{g.q_start, g.rows_q, g.group, per} : TokSide{g.k_start, g.rows_k, 1, per}; }
+// rows of a block in LDS (the kernels' KB)
+int tok_block_rows(int dt, TokCut c) { return dt == DT_F32 || c.heads == 2 ? 32 : 64; }
+TokSide side_of(const TokAttn& g, bool queries, int pack, int per) { return queries ? TokSide{g.q_start, g.rows_q, pack, per} : TokSide{g.k_start, g.rows_k, 1, per}; }
 
 template <typename T, bool SOFTMAX>
 hipError_t join(const TokAttn& g, TokCut c, bool queries, const float* part, const float* stat, void* out, int ld, hipStream_t s) {
-  const dim3 grid(c.blocks, c.waves * 32 / 8);
-  const TokSide side = side_of(g, queries, c.waves * 32);
-  if (c.waves == 4) tok_join_k<T, 128, SOFTMAX><<<grid, 256, 0, s>>>(g, side, c.blocks, part, stat, (T*)out, ld);
-  else tok_join_k<T, 32, SOFTMAX><<<grid, 256, 0, s>>>(g, side, c.blocks, part, stat, (T*)out, ld);
+  const TokHeads hs = tok_heads(g, c.heads);
+  const TokSide side = side_of(g, queries, hs.pack, c.waves * 32);
+  const int hstep = !queries ? 1 : g.group * (hs.kv_step + 1);   // heads from one group to the next
+  const dim3 grid(c.blocks, c.waves * 32 / 8, c.heads);
+  if (c.waves == 4) tok_join_k<T, 128, SOFTMAX><<<grid, 256, 0, s>>>(g, side, hs, hstep, c.blocks, part, stat, (T*)out, ld);
+  else tok_join_k<T, 32, SOFTMAX><<<grid, 512, 0, s>>>(g, side, hs, hstep, c.blocks, part, stat, (T*)out, ld);
   return hipGetLastError();
 }
 template <typename T>
@@ -125,23 +129,34 @@ hipError_t join_pass(int pass, const TokAttn& g, TokCut c, hipStream_t s) {
 }  // namespace
 
 // Few columns a slide leave three of four wavefronts idle: a wavefront a workgroup then.  Two workgroups of four wavefronts are on each of 256 units
-// at a time, or eight of one; fewer where there is less to do.
-TokCut tok_cut(long long cols, long long rows, int docs, int heads, int dt) {
+// at a time, or eight of one; fewer where there is less to do.  (Where there is, down to one unit each: 12 slides' tokens against 1 to 8192 keys,
+// 12 heads: 27.7 us with four units at least, 20.9 with two, 17.9 with one.)
+// Two heads at a time: a key head's, or two key heads', where the kernels are built for it.
+TokCut tok_cut(int pass, const slide_tokens_attn& s, bool bias) {
+  const int group = s.heads_q / s.heads_k;
+  const bool queries = pass != TOK_DKV;
   TokCut c;
-  c.waves = cols <= 32LL * docs ? 1 : 4;
-  const long long width = 32 * c.waves, kb = dt == DT_F32 ? 32 : 64;
+  c.heads = pass == TOK_FWD && bias && s.dtype == DT_BF16 && s.head_dim > 32 && s.head_dim <= 64 && (group == 1 ? s.heads_k % 2 == 0 : group % 2 == 0) ? 2 : 1;
+  long long cols = queries ? s.rows_q * (group > 1 ? group / c.heads : 1) : s.rows_k;
+  c.waves = cols <= 32LL * s.docs ? 1 : 4;
+  if (c.waves == 1 && c.heads == 2) {   // built for four wavefronts
+    c.heads = 1;
+    cols = s.rows_q * group;
+    c.waves = cols <= 32LL * s.docs ? 1 : 4;
+  }
+  const long long rows = queries ? s.rows_k : s.rows_q * group, width = 32 * c.waves, kb = tok_block_rows(s.dtype, c);
   // no more units than these: a slide's last tile and block are partly empty
-  const double units = ((double)cols / width + docs) * ((double)rows / kb + 1) * heads;
-  const long long most = c.waves == 4 ? 512 : 2048, n = units / TOK_LEAST < (double)most ? (long long)(units / TOK_LEAST) + 1 : most;
+  const double units = ((double)cols / width + s.docs) * ((double)rows / kb + 1) * s.heads_k;
+  const long long most = c.waves == 4 ? 512 : 2048, n = units < (double)most ? (long long)units + 1 : most;
   c.blocks = (int)((n + 7) / 8 * 8);
   return c;
 }
 
 hipError_t launch_tok_table(int pass, int dt, const TokAttn& g, TokCut c, long long* table, hipStream_t s) {
   if (g.docs <= 64) return hipSuccess;
-  const int kb = dt == DT_F32 ? TokType<float>::KB : TokType<bf16>::KB;
+  const int kb = tok_block_rows(dt, c), pack = tok_heads(g, c.heads).pack;
   const bool queries = pass != TOK_DKV;
-  tok_table_k<<<1, 1024, 0, s>>>(side_of(g, queries, c.waves * 32), side_of(g, !queries, kb), g.docs, table);
+  tok_table_k<<<1, 1024, 0, s>>>(side_of(g, queries, pack, c.waves * 32), side_of(g, !queries, g.group, kb), g.docs, table);
   return hipGetLastError();
 }
 

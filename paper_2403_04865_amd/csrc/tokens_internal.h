@@ -44,15 +44,13 @@ struct TokAttn {
   void* joins;              // column tiles of several workgroups
   float *part, *part2;      // their partial results: two tiles a workgroup
 };
-constexpr int TOK_LEAST = 4;   // units of a workgroup at least: its start costs as much as two or three
-// How a pass is cut: `blocks` workgroups of `waves` wavefronts with 32 columns each (packed queries, or keys)
-struct TokCut { int waves, blocks; };
-TokCut tok_cut(long long cols, long long rows, int docs, int heads, int dt);
+// How a pass is cut: `blocks` workgroups of `waves` wavefronts with 32 columns each (packed queries, or keys) and `heads` heads at a time
+struct TokCut { int waves, blocks, heads; };
+enum { TOK_FWD = 0, TOK_DQ = 1, TOK_DKV = 2 };
+TokCut tok_cut(int pass, const slide_tokens_attn& s, bool bias);
 inline size_t tok_table_bytes(int docs) { return docs > 64 ? ((size_t)docs + 1) * 8 : 0; }
 inline size_t tok_joins_bytes(TokCut c) { return (size_t)c.blocks * 16; }
-inline size_t tok_part_bytes(TokCut c, int dim) { return (size_t)2 * c.blocks * c.waves * 32 * dim * 4; }
-inline size_t tok_sums_bytes(TokCut c) { return (size_t)2 * c.blocks * c.waves * 32 * 8; }
-enum { TOK_FWD = 0, TOK_DQ = 1, TOK_DKV = 2 };
+inline size_t tok_columns(TokCut c) { return (size_t)2 * c.blocks * c.waves * 32 * c.heads; }   // of partial results
 // first units of the slides of a pass, where a table is used
 hipError_t launch_tok_table(int pass, int dt, const TokAttn& g, TokCut c, long long* table, hipStream_t s);
 hipError_t launch_tok_fwd(int dt, const TokAttn& g, TokCut c, hipStream_t s);

@@ -68,29 +68,32 @@ int attn_ok(const slide_tokens_attn* s) {
   if (s->rows_q * group > TOK_ROWS_MAX || s->rows_q * s->heads_q >= (1LL << 29)) return SLIDE_EUNSUPPORTED;
   return SLIDE_OK;
 }
-TokCut cut_q(const slide_tokens_attn& s) { return tok_cut(s.rows_q * (s.heads_q / s.heads_k), s.rows_k, s.docs, s.heads_k, s.dtype); }
-TokCut cut_k(const slide_tokens_attn& s) { return tok_cut(s.rows_k, s.rows_q * (s.heads_q / s.heads_k), s.docs, s.heads_k, s.dtype); }
 size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 // Work space of a pass: the slides' table, the shared tiles, their parts and what goes with them (maxima and sums, or the values' parts).  The
 // backward's passes follow one another in the same place, behind the deltas.
 struct PassWork { size_t joins, part, part2, bytes; };
-PassWork pass_work(const slide_tokens_attn& s, int pass) {
-  const TokCut c = pass == TOK_DKV ? cut_k(s) : cut_q(s);
+PassWork pass_work(const slide_tokens_attn& s, int pass, TokCut c) {
+  const size_t part = up256(tok_columns(c) * s.head_dim * 4);
   PassWork w;
   w.joins = up256(tok_table_bytes(s.docs));
   w.part = w.joins + up256(tok_joins_bytes(c));
-  w.part2 = w.part + up256(tok_part_bytes(c, s.head_dim));
-  w.bytes = w.part2 + (pass == TOK_FWD ? up256(tok_sums_bytes(c)) : pass == TOK_DKV ? up256(tok_part_bytes(c, s.head_dim)) : 0);
+  w.part2 = w.part + part;
+  w.bytes = w.part2 + (pass == TOK_FWD ? up256(tok_columns(c) * 8) : pass == TOK_DKV ? part : 0);
   return w;
+}
+// for a call with a bias and for one without
+size_t pass_bytes(const slide_tokens_attn& s, int pass) {
+  const size_t a = pass_work(s, pass, tok_cut(pass, s, false)).bytes, b = pass_work(s, pass, tok_cut(pass, s, true)).bytes;
+  return a > b ? a : b;
 }
 size_t delta_bytes(const slide_tokens_attn& s) { return up256((size_t)s.rows_q * s.heads_q * 4); }
 size_t bwd_bytes(const slide_tokens_attn& s) {
-  const size_t a = pass_work(s, TOK_DQ).bytes, b = pass_work(s, TOK_DKV).bytes;
+  const size_t a = pass_bytes(s, TOK_DQ), b = pass_bytes(s, TOK_DKV);
   return delta_bytes(s) + (a > b ? a : b);
 }
 hipError_t run_pass(int pass, const slide_tokens_attn& s, TokAttn g, char* work, hipStream_t st) {
-  const TokCut c = pass == TOK_DKV ? cut_k(s) : cut_q(s);
-  const PassWork w = pass_work(s, pass);
+  const TokCut c = tok_cut(pass, s, g.slopes != nullptr);
+  const PassWork w = pass_work(s, pass, c);
   g.table = (const long long*)work; g.joins = work + w.joins; g.part = (float*)(work + w.part); g.part2 = (float*)(work + w.part2);
   hipError_t e = launch_tok_table(pass, s.dtype, g, c, (long long*)work, st);
   if (e != hipSuccess) return e;
@@ -158,7 +161,7 @@ int slide_head_rope_bwd(const slide_head_rope* s, const void* dyq, int64_t lddyq
 
 size_t slide_tokens_attn_workspace_bytes(const slide_tokens_attn* s, int backward) {
   if (attn_ok(s) != SLIDE_OK) return 0;
-  const size_t f = pass_work(*s, TOK_FWD).bytes, b = backward ? bwd_bytes(*s) : 0;
+  const size_t f = pass_bytes(*s, TOK_FWD), b = backward ? bwd_bytes(*s) : 0;
   return b > f ? b : f;
 }
 
@@ -171,7 +174,7 @@ int slide_tokens_attn_fwd(const slide_tokens_attn* s, const void* q, int64_t ldq
   if (!matrix_ok(q, s->dtype, ldq, cq) || !matrix_ok(k, s->dtype, ldk, ck) || !matrix_ok(v, s->dtype, ldv, ck) || !matrix_ok(o, s->dtype, ldo, cq) ||
       !q_start || !k_start || !aligned(q_start, 4) || !aligned(k_start, 4) || !lse || !aligned(lse, 4) || !bias_ok(pos_q, pos_k, slopes) || o == q || o == k || o == v)
     return SLIDE_EINVAL;
-  rc = work_ok(work, work_bytes, pass_work(*s, TOK_FWD).bytes);
+  rc = work_ok(work, work_bytes, pass_bytes(*s, TOK_FWD));
   if (rc) return rc;
   (void)hipGetLastError();
   TokAttn g = attn_of(*s);

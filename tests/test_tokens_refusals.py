@@ -151,7 +151,7 @@ def test_attention_work_space(lib):
         assert fwd(lib, s, bytes=f) == EHIP and fwd(lib, s, bytes=f - 1) == EARENA and fwd(lib, s, work=None, bytes=0) == EARENA
         assert fwd(lib, s, work=AT + 64) == EINVAL
     # what a workgroup may leave is bounded, whatever the sizes
-    assert lib.slide_tokens_attn_workspace_bytes(C.byref(attn(rows_q=1 << 24, rows_k=1 << 24, docs=1)), 0) < 1 << 26
+    assert lib.slide_tokens_attn_workspace_bytes(C.byref(attn(rows_q=1 << 24, rows_k=1 << 24, docs=1)), 0) < 1 << 27
     assert lib.slide_tokens_attn_workspace_bytes(C.byref(attn(rows_q=10, rows_k=10, docs=1)), 0) < 1 << 20
 
 
