@@ -15,6 +15,7 @@ namespace sl {
 
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 
+constexpr float TOK_NONE = -3e38f;   // below every score
 constexpr float TOK_LOG2E = 1.4426950408889634f, TOK_LN2 = 0.69314718055994531f;
 
 template <typename T> struct TokType;

@@ -36,12 +36,12 @@ __global__ void __launch_bounds__(NW * 64, (tok_waves<T, DP, NW>())) tok_fwd_k(c
     TokTile<T, DP, NW * 64, KB> kt[NH] = {TokTile<T, DP, NW * 64, KB>(g.ldk, g.dim)}, vt[NH] = {TokTile<T, DP, NW * 64, KB>(g.ldv, g.dim)};
     TokPlace place = {0.f, 0.f};
     f32x16 o[NH][DP / 32];
-    float m[NH], ms[NH], l[NH];   // running maximum of z, the same times ex (0 while there is none), sum
+    float top[NH], l[NH];   // what exponents are taken relative to, and their sum
 #pragma unroll
     for (int n = 0; n < NH; ++n) {
       tok_zero_all(o[n]);
-      m[n] = -INFINITY;
-      ms[n] = l[n] = 0.f;
+      top[n] = TOK_NONE;
+      l[n] = 0.f;
     }
     auto fetch = [&](int k0) __attribute__((always_inline)) {
       kt[0].load(kp + (long long)k0 * g.ldk, nk - k0, g.ldk, g.dim);
@@ -81,7 +81,7 @@ __global__ void __launch_bounds__(NW * 64, (tok_waves<T, DP, NW>())) tok_fwd_k(c
           }
         float mn[NH];
 #pragma unroll
-        for (int n = 0; n < NH; ++n) mn[n] = m[n];
+        for (int n = 0; n < NH; ++n) mn[n] = -INFINITY;
         // the first and the last blocks hold keys without a place and keys that are not there: a copy of the code of their own
         auto scores = [&](auto edge) __attribute__((always_inline)) {
           constexpr bool EDGE = decltype(edge)::value;
@@ -113,11 +113,12 @@ __global__ void __launch_bounds__(NW * 64, (tok_waves<T, DP, NW>())) tok_fwd_k(c
         else scores(std::false_type{});
 #pragma unroll
         for (int n = 0; n < NH; ++n) {
-          if (__builtin_amdgcn_ballot_w64(mn[n] > m[n]) != 0) {   // uniform: after the first blocks the maximum rarely moves
-            mn[n] = tok_other_max(mn[n]);
-            ms[n] = mn[n] == -INFINITY ? 0.f : mn[n] * sc.ex;
-            const float resc = tok_exp<CAP>(m[n], ms[n], sc);   // 0 at the first block
-            m[n] = mn[n];
+          // The reference is a maximum of before and moves when a score is 2^8 above it: sums keep their relative precision either way.  A branch for the
+          // lanes, not for the wavefront: behind a uniform one the compiler keeps the sums in two places and copies them every time.
+          const float mx = tok_other_max(mn[n]) * sc.ex;
+          if (mx > top[n] + 8.f) {
+            const float resc = __builtin_amdgcn_exp2f(top[n] - mx);   // 0 at the first block
+            top[n] = mx;
             l[n] *= resc;
 #pragma unroll
             for (int d = 0; d < DP / 32; ++d)
@@ -128,7 +129,7 @@ __global__ void __launch_bounds__(NW * 64, (tok_waves<T, DP, NW>())) tok_fwd_k(c
           for (int b = 0; b < NB; ++b)
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-              s[n][b][r] = tok_exp<CAP>(s[n][b][r], ms[n], sc);
+              s[n][b][r] = tok_exp<CAP>(s[n][b][r], top[n], sc);
               l[n] += s[n][b][r];
             }
 #pragma unroll
@@ -147,13 +148,13 @@ __global__ void __launch_bounds__(NW * 64, (tok_waves<T, DP, NW>())) tok_fwd_k(c
       const int h = head + n * hs.step;
       if (w.slot >= 0) {
         const long long at = ((long long)w.slot * NH + n) * W + wave * 32 + (lane & 31);
-        if (lane < 32) *reinterpret_cast<float2*>(g.part2 + 2 * at) = float2{m[n] * sc.ex, l[n]};
+        if (lane < 32) *reinterpret_cast<float2*>(g.part2 + 2 * at) = float2{top[n], l[n]};
         tok_store(o[n], 1.f, g.part + at * g.dim, g.dim);
         continue;
       }
       const bool nothing = l[n] == 0.f;   // no keys, or none within reach of a bias that is infinite
       tok_store(o[n], nothing ? 0.f : 1.f / l[n], (T*)g.o + qrow * g.ldo + h * g.dim, g.dim);
-      if (lane < 32) g.lse[(long long)h * g.rows_q + qrow] = nothing ? -INFINITY : (m[n] * sc.ex + __builtin_amdgcn_logf(l[n])) * TOK_LN2;
+      if (lane < 32) g.lse[(long long)h * g.rows_q + qrow] = nothing ? -INFINITY : (top[n] + __builtin_amdgcn_logf(l[n])) * TOK_LN2;
     }
   });
 }
