@@ -82,14 +82,17 @@ __device__ __forceinline__ void sin_cos(unsigned turn, float* s, float* c) {
   *s = quarter & 2 ? -a : a;
   *c = (quarter + 1) & 2 ? -b : b;
 }
-__device__ __forceinline__ void angles(const HeadRope& g, long long row, int p0, float (&c)[8], float (&s)[8]) {
+// the frequencies of as many pairs as a head's lanes hold: arguments of the kernel, of which a small call copies no more than it needs
+template <int LANES> struct Freq { unsigned long long f[8 * LANES]; };
+template <int LANES>
+__device__ __forceinline__ void angles(const HeadRope& g, const Freq<LANES>& freq, long long row, int p0, float (&c)[8], float (&s)[8]) {
   const int* pos = g.pos + row * g.axes;
   const long long x0 = g.axes > 0 ? pos[0] : 0, x1 = g.axes > 1 ? pos[1] : 0, x2 = g.axes > 2 ? pos[2] : 0;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const int p = p0 + i;
     const long long x = p < g.bound[0] ? x0 : p < g.bound[1] ? x1 : x2;   // frequencies behind the last axis' pairs are 0
-    sin_cos((unsigned)((unsigned long long)x * g.freq[p] >> 32), &s[i], &c[i]);
+    sin_cos((unsigned)((unsigned long long)x * freq.f[p] >> 32), &s[i], &c[i]);
   }
 }
 
@@ -146,7 +149,7 @@ __device__ __forceinline__ Pairs pairs_of(const Raw<T>& r) {
 // blockIdx.y: queries or keys.  A thread's row is item / slices; it goes over heads item % slices, + slices, ..., the next one's values on
 // their way while it works.
 template <typename T, int LANES, bool NEIGHBOURS, bool BACKWARD, bool NORM>
-__device__ __forceinline__ void rope_side(const HeadRope& g, bool key, int slices, long long items) {
+__device__ __forceinline__ void rope_side(const HeadRope& g, const Freq<LANES>& freq, bool key, int slices, long long items) {
   constexpr int PER = 256 / LANES;
   const int sub = threadIdx.x % LANES, p0 = sub * 8;
   const bool mine = sub * 16 < g.dim;                 // head widths that are no power of two leave lanes over
@@ -175,7 +178,7 @@ __device__ __forceinline__ void rope_side(const HeadRope& g, bool key, int slice
     };
     ask(slice);
     float c[8], s[8];
-    angles(g, row, mine ? p0 : 0, c, s);
+    angles<LANES>(g, freq, row, mine ? p0 : 0, c, s);
     for (int t = 0; t < turns; ++t) {
       const int h = slice + t * slices;
       const bool work = there && mine && h < heads;
@@ -242,10 +245,10 @@ __device__ __forceinline__ void rope_side(const HeadRope& g, bool key, int slice
   }
 }
 template <typename T, int LANES, bool NEIGHBOURS, bool BACKWARD>
-__global__ void __launch_bounds__(256) head_rope_k(const HeadRope g, const int slices, const long long items) {
+__global__ void __launch_bounds__(256) head_rope_k(const HeadRope g, const Freq<LANES> freq, const int slices, const long long items) {
   const bool key = blockIdx.y == 1;
-  if (key ? g.gk != nullptr : g.gq != nullptr) rope_side<T, LANES, NEIGHBOURS, BACKWARD, true>(g, key, slices, items);
-  else rope_side<T, LANES, NEIGHBOURS, BACKWARD, false>(g, key, slices, items);
+  if (key ? g.gk != nullptr : g.gq != nullptr) rope_side<T, LANES, NEIGHBOURS, BACKWARD, true>(g, freq, key, slices, items);
+  else rope_side<T, LANES, NEIGHBOURS, BACKWARD, false>(g, freq, key, slices, items);
 }
 
 // gains' gradients: 4 columns a workgroup, 64 threads each; blockIdx.y: of the queries or of the keys
@@ -268,9 +271,10 @@ __global__ void __launch_bounds__(256) rope_gain_k(const float* __restrict__ wor
 }
 
 int lanes_of(int dim) { int l = 1; while (l * 16 < dim) l *= 2; return l; }
-// Slices of a row's heads: all heads in one thread where the rows fill the card, else as many threads a row as do
+// Slices of a row's heads: all heads in one thread where the rows give a wavefront to each of the card's 1024 units that issue, else as many threads a
+// row as do (7289 rows of 6 + 6 heads of 64: 8.1 us with half as many threads, 8.4, 11.1 with twice, 10.5 with four times)
 int slices_of(long long rows, int heads, int lanes) {
-  const long long want = 256 * 1024, have = rows * lanes, n = (want + have - 1) / have;
+  const long long want = 64 * 1024, have = rows * lanes, n = (want + have - 1) / have;
   return (int)(n > heads ? heads : n);
 }
 int slices_of(const HeadRope& g) { return slices_of(g.rows, g.hq > g.hk ? g.hq : g.hk, lanes_of(g.dim)); }
@@ -284,8 +288,10 @@ hipError_t run(const HeadRope& g, hipStream_t s) {
   if (blocks > most) blocks = most;
   auto go = [&](auto l) {
     constexpr int L = decltype(l)::value;
-    if (g.neighbours) head_rope_k<T, L, true, BACKWARD><<<dim3((unsigned)blocks, g.hk ? 2 : 1), 256, 0, s>>>(g, slices, items);
-    else head_rope_k<T, L, false, BACKWARD><<<dim3((unsigned)blocks, g.hk ? 2 : 1), 256, 0, s>>>(g, slices, items);
+    Freq<L> f;
+    for (int i = 0; i < 8 * L; ++i) f.f[i] = g.freq[i];
+    if (g.neighbours) head_rope_k<T, L, true, BACKWARD><<<dim3((unsigned)blocks, g.hk ? 2 : 1), 256, 0, s>>>(g, f, slices, items);
+    else head_rope_k<T, L, false, BACKWARD><<<dim3((unsigned)blocks, g.hk ? 2 : 1), 256, 0, s>>>(g, f, slices, items);
   };
   switch (lanes) {
     case 1: go(std::integral_constant<int, 1>{}); break;

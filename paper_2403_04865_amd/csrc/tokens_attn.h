@@ -381,6 +381,29 @@ inline __host__ __device__ TokHeads tok_heads(const TokAttn& g, int nh) {
 __device__ __forceinline__ TokSide tok_queries(const TokAttn& g, int per, int pack) { return {g.q_start, g.rows_q, pack, per}; }
 __device__ __forceinline__ TokSide tok_keys(const TokAttn& g, int per) { return {g.k_start, g.rows_k, 1, per}; }
 
+// Distances of a block's 32 rows from the columns, as scores lie: the differences of each coordinate are a product of two terms, (row, 1) (1, -column), in
+// float32 on the matrix cores, which have nothing else to do while the vector unit works: one rounding, as the subtraction has.  px, py: the
+// rows' coordinates in LDS; cx, cy: the column's.  (Read row by row they were 8 of 28 reads of 16 bytes a block, and 2 of 13 operations a score.)
+template <typename T>
+__device__ __forceinline__ void tok_dists(f32x16& d, const float* px, const float* py, int j0, float cx, float cy) {
+  if constexpr (sizeof(T) == 4) {   // there the matrix cores are what is short
+#pragma unroll
+    for (int q4 = 0; q4 < 4; ++q4) {
+      const f32x4 x = *reinterpret_cast<const f32x4*>(px + j0 + tok_row(q4 * 4)), y = *reinterpret_cast<const f32x4*>(py + j0 + tok_row(q4 * 4));
+#pragma unroll
+      for (int i = 0; i < 4; ++i) d[q4 * 4 + i] = tok_dist(x[i], y[i], cx, cy);
+    }
+    return;
+  }
+  const bool second = (threadIdx.x & 32) != 0;   // the term that this half of the wavefront holds
+  const int row = j0 + (threadIdx.x & 31);
+  const float ax = second ? 1.f : px[row], ay = second ? 1.f : py[row];
+  const f32x16 x = __builtin_amdgcn_mfma_f32_32x32x2f32(ax, second ? -cx : 1.f, tok_zero(), 0, 0, 0);
+  const f32x16 y = __builtin_amdgcn_mfma_f32_32x32x2f32(ay, second ? -cy : 1.f, tok_zero(), 0, 0, 0);
+#pragma unroll
+  for (int r = 0; r < 16; ++r) d[r] = __builtin_amdgcn_sqrtf(fmaf(x[r], x[r], y[r] * y[r]));   // within an ulp
+}
+
 // dispatch on the padded head width, bias and cap
 template <typename T, typename F>
 hipError_t tok_dispatch(const TokAttn& g, F f) {

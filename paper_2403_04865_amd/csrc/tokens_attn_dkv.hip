@@ -75,7 +75,8 @@ __global__ void __launch_bounds__(NW * 64, DP <= 64 && NW == 4 ? 2 : 1) tok_dkv_
         if (idle) continue;   // uniform in a wavefront: none of its columns is there
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
-          f32x16 s = tok_zero(), dp, p;
+          f32x16 s = tok_zero(), dp, p, dist;
+          if (BIAS) tok_dists<T>(dist, px, py, b * 32, kx, ky);
 #pragma unroll
           for (int q4 = 0; q4 < 4; ++q4) {   // the product starts from -delta
             const f32x4 d = *reinterpret_cast<const f32x4*>(pd + b * 32 + tok_row(q4 * 4));
@@ -91,17 +92,13 @@ __global__ void __launch_bounds__(NW * 64, DP <= 64 && NW == 4 ? 2 : 1) tok_dkv_
 #pragma unroll
           for (int q4 = 0; q4 < 4; ++q4) {
             const int r0 = b * 32 + tok_row(q4 * 4);
-            f32x4 qx, qy, slope;
-            if (BIAS) {
-              qx = *reinterpret_cast<const f32x4*>(px + r0);
-              qy = *reinterpret_cast<const f32x4*>(py + r0);
-              slope = *reinterpret_cast<const f32x4*>(ps + r0);
-            }
+            f32x4 slope;
+            if (BIAS) slope = *reinterpret_cast<const f32x4*>(ps + r0);
             const f32x4 lse = *reinterpret_cast<const f32x4*>(pl + r0);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               const int r = q4 * 4 + i;
-              float d = BIAS ? tok_dist(qx[i], qy[i], kx, ky) : 0.f, dt = 1.f;
+              float d = BIAS ? dist[r] : 0.f, dt = 1.f;
               if (LEADS && !placed) d = 0.f;
               const float z = tok_score<T, BIAS, CAP, true>(s[r], d, BIAS ? slope[i] : 0.f, sc, &dt);
               p[r] = tok_exp<CAP>(z, lse[i], sc);

@@ -1,34 +1,24 @@
-// Attention over packed slides, backward: dout . o of every row, and the gradient of the queries (layout: tokens_attn.h).
+// Attention over packed slides, backward: the gradient of the queries, and dout . o of every row for the keys' pass (layout: tokens_attn.h).
 #include "tokens_attn.h"
 
 namespace sl {
 
 namespace {
 
-// delta[head][row] = dout . o in float32: a group of eight lanes a row and head
-template <typename T>
-__global__ void __launch_bounds__(256) tok_delta_k(const TokAttn g) {
+// sum of the products of two columns, over the lane and the other one of its column
+template <typename T, int DP>
+__device__ __forceinline__ float tok_dot(const TokFrag<T, DP>& a, const TokFrag<T, DP>& b) {
   constexpr int EPC = TokType<T>::EPC;
-  const long long item = blockIdx.x * 32LL + (threadIdx.x >> 3);
-  const int part = threadIdx.x & 7;
-  if (item >= (long long)g.rows_q * g.hq) return;
-  const long long row = item / g.hq;
-  const int head = (int)(item % g.hq);
-  if (row < tok_clamp(g.q_start[0], g.rows_q) || row >= tok_clamp(g.q_start[g.docs], g.rows_q)) return;
-  const T* a = (const T*)g.dout + row * g.lddo + head * g.dim;
-  const T* b = (const T*)g.o_in + row * g.ldo + head * g.dim;
   float sum = 0.f;
-  for (int c = part * EPC; c < g.dim; c += 8 * EPC) {
-    const u32x4 va = *reinterpret_cast<const u32x4*>(a + c), vb = *reinterpret_cast<const u32x4*>(b + c);
+#pragma unroll
+  for (int i = 0; i < DP / EPC / 2; ++i) {
     T ea[EPC], eb[EPC];
-    __builtin_memcpy(ea, &va, 16);
-    __builtin_memcpy(eb, &vb, 16);
+    __builtin_memcpy(ea, &a.v[i], 16);
+    __builtin_memcpy(eb, &b.v[i], 16);
 #pragma unroll
-    for (int i = 0; i < EPC; ++i) sum = fmaf(to_f(ea[i]), to_f(eb[i]), sum);
+    for (int e = 0; e < EPC; ++e) sum = fmaf(to_f(ea[e]), to_f(eb[e]), sum);
   }
-#pragma unroll
-  for (int o = 4; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
-  if (part == 0) g.delta[head * (long long)g.rows_q + row] = sum;
+  return tok_other_sum(sum);
 }
 
 template <typename T, int DP, int NW, bool BIAS, bool CAP>
@@ -49,7 +39,13 @@ __global__ void __launch_bounds__(NW * 64, DP <= 64 && NW == 4 ? 2 : 1) tok_dq_k
     tok_load_frag<T, DP>(fo, (const T*)g.dout + qrow * g.lddo + head * g.dim, valid, g.dim);
     // a column that is not there: infinite, so its probabilities are zero
     const float lse = valid ? g.lse[(long long)head * g.rows_q + qrow] * TOK_LOG2E : INFINITY;
-    const float delta = valid ? g.delta[(long long)head * g.rows_q + qrow] : 0.f;
+    float delta;   // dout . o, also for the keys' pass
+    {
+      TokFrag<T, DP> f;
+      tok_load_frag<T, DP>(f, (const T*)g.o_in + qrow * g.ldo + head * g.dim, valid, g.dim);
+      delta = tok_dot<T, DP>(fo, f);
+      if (valid && w.a == 0 && lane < 32) g.delta[(long long)head * g.rows_q + qrow] = delta;
+    }
     float qx = 0.f, qy = 0.f, slope = 0.f;
     if (BIAS && valid && qi >= g.lead_q) {
       qx = g.pos_q[2 * qrow]; qy = g.pos_q[2 * qrow + 1];
@@ -82,7 +78,8 @@ __global__ void __launch_bounds__(NW * 64, DP <= 64 && NW == 4 ? 2 : 1) tok_dq_k
         // the first and the last blocks hold keys without a place and keys that are not there: a copy of the code of their own
         auto block = [&](auto edge, int b) __attribute__((always_inline)) {
           constexpr bool EDGE = decltype(edge)::value;
-          f32x16 s = tok_zero(), dp = tok_zero();
+          f32x16 s = tok_zero(), dp = tok_zero(), dist;
+          if (BIAS) tok_dists<T>(dist, px, py, b * 32, qx, qy);
           TokRows<T, DP> kr, vr;
           TokCols<T, DP> kc;
           tok_get<T, DP>(kr, Ks, b * 32);
@@ -92,15 +89,10 @@ __global__ void __launch_bounds__(NW * 64, DP <= 64 && NW == 4 ? 2 : 1) tok_dq_k
 #pragma unroll
           for (int q4 = 0; q4 < 4; ++q4) {
             const int r0 = b * 32 + tok_row(q4 * 4);
-            f32x4 kx, ky;
-            if (BIAS) {
-              kx = *reinterpret_cast<const f32x4*>(px + r0);
-              ky = *reinterpret_cast<const f32x4*>(py + r0);
-            }
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               const int r = q4 * 4 + i;
-              float d = BIAS ? tok_dist(qx, qy, kx[i], ky[i]) : 0.f, dt = 1.f;
+              float d = BIAS ? dist[r] : 0.f, dt = 1.f;
               if (EDGE && BIAS && k0 + r0 + i < g.lead_k) d = 0.f;
               const float z = tok_score<T, BIAS, CAP, true>(s[r], d, slope, sc, &dt);
               float ds = tok_exp<CAP>(z, lse, sc) * (dp[r] - delta);
@@ -139,13 +131,6 @@ hipError_t run_dq(const TokAttn& g, TokCut c, hipStream_t s) {
 }
 
 }  // namespace
-
-hipError_t launch_tok_delta(int dt, const TokAttn& g, hipStream_t s) {
-  const unsigned blocks = (unsigned)(((long long)g.rows_q * g.hq + 31) / 32);
-  if (dt == DT_F32) tok_delta_k<float><<<blocks, 256, 0, s>>>(g);
-  else tok_delta_k<bf16><<<blocks, 256, 0, s>>>(g);
-  return hipGetLastError();
-}
 
 hipError_t launch_tok_dq(int dt, const TokAttn& g, TokCut c, hipStream_t s) { return dt == DT_F32 ? run_dq<float>(g, c, s) : run_dq<bf16>(g, c, s); }
 

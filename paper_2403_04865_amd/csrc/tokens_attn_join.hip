@@ -35,14 +35,19 @@ __global__ void __launch_bounds__(1024) tok_table_k(const TokSide c, const TokSi
 
 // A workgroup joins COLS columns of a tile.  A column's threads are groups of `lanes` with four of its values each, group z of them takes every
 // `zs`-th piece; blockIdx.z is the head of a group; the groups' results meet in LDS.  SOFTMAX: pieces are sums under maxima of their own.
-template <typename T, int W, bool SOFTMAX>
+// TWO: two results of the same columns, one after the other in blockIdx.z (keys' and values' gradients).
+template <typename T, int W, bool SOFTMAX, bool TWO>
 __global__ void __launch_bounds__(W == 32 ? 512 : 256) tok_join_k(const TokAttn g, const TokSide side, const TokHeads hs, int hstep, int blocks,
-                                                                  const float* __restrict__ part, const float* __restrict__ stat, T* __restrict__ out, int ld) {
+                                                                  const float* __restrict__ part0, const float* __restrict__ stat, T* __restrict__ out0, int ld0, T* __restrict__ out1, int ld1) {
   constexpr int COLS = 8, NT = W == 32 ? 512 : 256;   // few columns mean many pieces
   __shared__ f32x4 sums[NT];
   __shared__ float2 stats[NT];
   const TokJoin j = ((const TokJoin*)g.joins)[blockIdx.x];
   if (j.pieces == 0) return;
+  const int n = TWO ? 0 : blockIdx.z, heads = TWO ? 1 : gridDim.z;
+  const float* const part = TWO && blockIdx.z ? stat : part0;
+  T* const out = TWO && blockIdx.z ? out1 : out0;
+  const int ld = TWO && blockIdx.z ? ld1 : ld0;
   const TokSpan c = tok_span(side, j.doc);
   const int first = j.tile * W + blockIdx.y * COLS, here = c.n - first < COLS ? c.n - first : COLS;   // columns of this workgroup
   if (here <= 0) return;
@@ -56,7 +61,7 @@ __global__ void __launch_bounds__(W == 32 ? 512 : 256) tok_join_k(const TokAttn 
 #pragma unroll 4
     for (int p = z; p < j.pieces; p += zs) {
       const long long slot = p == 0 ? blocks + (int)blockIdx.x : (int)blockIdx.x + p;   // the first piece is the end of its workgroup's units
-      const long long at = (slot * gridDim.z + blockIdx.z) * W + blockIdx.y * COLS + col;
+      const long long at = (slot * heads + n) * W + blockIdx.y * COLS + col;
       const f32x4 v = *reinterpret_cast<const f32x4*>(part + at * g.dim + quad * 4);
       if (SOFTMAX) {
         const float2 s = *reinterpret_cast<const float2*>(stat + 2 * at);
@@ -93,7 +98,7 @@ __global__ void __launch_bounds__(W == 32 ? 512 : 256) tok_join_k(const TokAttn 
     }
   }
   if (!on) return;
-  const int at = first + col, qi = at / side.group, head = j.head * hstep + blockIdx.z * hs.step + (at - qi * side.group);
+  const int at = first + col, qi = at / side.group, head = j.head * hstep + n * hs.step + (at - qi * side.group);
   const long long row = c.lo + qi;
   const float f = !SOFTMAX ? 1.f : l == 0.f ? 0.f : 1.f / l;
   typedef T T4 __attribute__((ext_vector_type(4)));
@@ -108,22 +113,21 @@ __global__ void __launch_bounds__(W == 32 ? 512 : 256) tok_join_k(const TokAttn 
 int tok_block_rows(int dt, TokCut c) { return dt == DT_F32 || c.heads == 2 ? 32 : 64; }
 TokSide side_of(const TokAttn& g, bool queries, int pack, int per) { return queries ? TokSide{g.q_start, g.rows_q, pack, per} : TokSide{g.k_start, g.rows_k, 1, per}; }
 
-template <typename T, bool SOFTMAX>
-hipError_t join(const TokAttn& g, TokCut c, bool queries, const float* part, const float* stat, void* out, int ld, hipStream_t s) {
+template <typename T, bool SOFTMAX, bool TWO>
+hipError_t join(const TokAttn& g, TokCut c, void* out, int ld, void* out1, int ld1, hipStream_t s) {
+  const dim3 grid(c.blocks, c.waves * 32 / 8, TWO ? 2 : c.heads);
   const TokHeads hs = tok_heads(g, c.heads);
-  const TokSide side = side_of(g, queries, hs.pack, c.waves * 32);
-  const int hstep = !queries ? 1 : g.group * (hs.kv_step + 1);   // heads from one group to the next
-  const dim3 grid(c.blocks, c.waves * 32 / 8, c.heads);
-  if (c.waves == 4) tok_join_k<T, 128, SOFTMAX><<<grid, 256, 0, s>>>(g, side, hs, hstep, c.blocks, part, stat, (T*)out, ld);
-  else tok_join_k<T, 32, SOFTMAX><<<grid, 512, 0, s>>>(g, side, hs, hstep, c.blocks, part, stat, (T*)out, ld);
+  const TokSide side = side_of(g, !TWO, hs.pack, c.waves * 32);
+  const int hstep = TWO ? 1 : g.group * (hs.kv_step + 1);   // heads from one group to the next
+  if (c.waves == 4) tok_join_k<T, 128, SOFTMAX, TWO><<<grid, 256, 0, s>>>(g, side, hs, hstep, c.blocks, g.part, g.part2, (T*)out, ld, (T*)out1, ld1);
+  else tok_join_k<T, 32, SOFTMAX, TWO><<<grid, 512, 0, s>>>(g, side, hs, hstep, c.blocks, g.part, g.part2, (T*)out, ld, (T*)out1, ld1);
   return hipGetLastError();
 }
 template <typename T>
 hipError_t join_pass(int pass, const TokAttn& g, TokCut c, hipStream_t s) {
-  if (pass == TOK_FWD) return join<T, true>(g, c, true, g.part, g.part2, g.o, g.ldo, s);
-  if (pass == TOK_DQ) return join<T, false>(g, c, true, g.part, nullptr, g.dq, g.lddq, s);
-  const hipError_t e = join<T, false>(g, c, false, g.part, nullptr, g.dk, g.lddk, s);
-  return e != hipSuccess ? e : join<T, false>(g, c, false, g.part2, nullptr, g.dv, g.lddv, s);
+  if (pass == TOK_FWD) return join<T, true, false>(g, c, g.o, g.ldo, nullptr, 0, s);
+  if (pass == TOK_DQ) return join<T, false, false>(g, c, g.dq, g.lddq, nullptr, 0, s);
+  return join<T, false, true>(g, c, g.dk, g.lddk, g.dv, g.lddv, s);
 }
 
 }  // namespace

@@ -22,7 +22,7 @@ struct HeadRope {
   const int* pos;
   float *dgq, *dgk; int accumulate;
   float* work;
-  unsigned long long freq[ROPE_PAIRS];          // a pair's turns for a step of its position, as a fraction of 2^64
+  const unsigned long long* freq;               // host: a pair's turns for a step of its position, as a fraction of 2^64; [ROPE_PAIRS]
 };
 size_t head_rope_work_bytes(const slide_head_rope& s);
 hipError_t launch_head_rope_fwd(int dt, const HeadRope& g, hipStream_t s);
@@ -54,7 +54,6 @@ inline size_t tok_columns(TokCut c) { return (size_t)2 * c.blocks * c.waves * 32
 // first units of the slides of a pass, where a table is used
 hipError_t launch_tok_table(int pass, int dt, const TokAttn& g, TokCut c, long long* table, hipStream_t s);
 hipError_t launch_tok_fwd(int dt, const TokAttn& g, TokCut c, hipStream_t s);
-hipError_t launch_tok_delta(int dt, const TokAttn& g, hipStream_t s);
 hipError_t launch_tok_dq(int dt, const TokAttn& g, TokCut c, hipStream_t s);
 hipError_t launch_tok_dkv(int dt, const TokAttn& g, TokCut c, hipStream_t s);
 // results of the column tiles that several workgroups share, out of their parts
