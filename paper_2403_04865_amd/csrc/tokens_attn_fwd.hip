@@ -9,7 +9,10 @@ namespace {
 // takes 6.4 (four operations and a root), which two heads share where a wavefront has the registers.
 template <typename T, int DP, int NW, int NH, bool BIAS, bool CAP>
 __global__ void __launch_bounds__(NW * 64, (tok_waves<T, DP, NW>())) tok_fwd_k(const TokAttn g) {
-  constexpr int KB = NH == 2 ? 32 : TokType<T>::KB, LDR = tok_ldr<T, DP>(), NB = KB / 32, W = NW * 32;
+  // differences of coordinates on the matrix cores (tok_dists) for one head and four wavefronts: 16 slides, capped scores, 8 heads of 128 156 -> 152 us; with two
+  // heads, which share them, 383 -> 389, and with one wavefront, which waits for its loads, 38 -> 49
+  constexpr bool DISTS = BIAS && NH == 1 && NW == 4 && sizeof(T) == 2;
+  constexpr int KB = NH == 2 || DP == 128 ? 32 : TokType<T>::KB, LDR = tok_ldr<T, DP>(), NB = KB / 32, W = NW * 32;
   __shared__ __attribute__((aligned(16))) T Ks[NH][KB * LDR], Vs[NH][KB * LDR];
   __shared__ __attribute__((aligned(16))) float px[KB], py[KB];
   const TokScore sc = tok_score_of<CAP>(g.scale, g.cap);
@@ -79,6 +82,11 @@ __global__ void __launch_bounds__(NW * 64, (tok_waves<T, DP, NW>())) tok_fwd_k(c
             s[n][b] = tok_zero();
             tok_mul<T, DP>(s[n][b], kr, fq[n]);
           }
+        f32x16 dist[NB];
+        if (DISTS) {
+#pragma unroll
+          for (int b = 0; b < NB; ++b) tok_dists<T>(dist[b], px, py, b * 32, qx, qy);
+        }
         float mn[NH];
 #pragma unroll
         for (int n = 0; n < NH; ++n) mn[n] = -INFINITY;
@@ -91,13 +99,13 @@ __global__ void __launch_bounds__(NW * 64, (tok_waves<T, DP, NW>())) tok_fwd_k(c
             for (int q4 = 0; q4 < 4; ++q4) {
               const int r0 = b * 32 + tok_row(q4 * 4);
               f32x4 kx, ky;
-              if (BIAS) {
+              if (BIAS && !DISTS) {
                 kx = *reinterpret_cast<const f32x4*>(px + r0);
                 ky = *reinterpret_cast<const f32x4*>(py + r0);
               }
 #pragma unroll
               for (int i = 0; i < 4; ++i) {
-                float d = BIAS ? tok_dist(qx, qy, kx[i], ky[i]) : 0.f;
+                float d = DISTS ? dist[b][q4 * 4 + i] : BIAS ? tok_dist(qx, qy, kx[i], ky[i]) : 0.f;
                 if (EDGE && BIAS && k0 + r0 + i < g.lead_k) d = 0.f;
 #pragma unroll
                 for (int n = 0; n < NH; ++n) {

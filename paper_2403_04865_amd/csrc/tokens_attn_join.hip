@@ -110,7 +110,7 @@ __global__ void __launch_bounds__(W == 32 ? 512 : 256) tok_join_k(const TokAttn 
 }
 
 // rows of a block in LDS (the kernels' KB)
-int tok_block_rows(int dt, TokCut c) { return dt == DT_F32 || c.heads == 2 ? 32 : 64; }
+int tok_block_rows(int pass, int dt, int dim, TokCut c) { return dt == DT_F32 || c.heads == 2 || (pass == TOK_FWD && dim > 96) ? 32 : 64; }
 TokSide side_of(const TokAttn& g, bool queries, int pack, int per) { return queries ? TokSide{g.q_start, g.rows_q, pack, per} : TokSide{g.k_start, g.rows_k, 1, per}; }
 
 template <typename T, bool SOFTMAX, bool TWO>
@@ -148,7 +148,7 @@ TokCut tok_cut(int pass, const slide_tokens_attn& s, bool bias) {
     cols = s.rows_q * group;
     c.waves = cols <= 32LL * s.docs ? 1 : 4;
   }
-  const long long rows = queries ? s.rows_k : s.rows_q * group, width = 32 * c.waves, kb = tok_block_rows(s.dtype, c);
+  const long long rows = queries ? s.rows_k : s.rows_q * group, width = 32 * c.waves, kb = tok_block_rows(pass, s.dtype, s.head_dim, c);
   // no more units than these: a slide's last tile and block are partly empty
   const double units = ((double)cols / width + s.docs) * ((double)rows / kb + 1) * s.heads_k;
   const long long most = c.waves == 4 ? 512 : 2048, n = units < (double)most ? (long long)units + 1 : most;
@@ -158,7 +158,7 @@ TokCut tok_cut(int pass, const slide_tokens_attn& s, bool bias) {
 
 hipError_t launch_tok_table(int pass, int dt, const TokAttn& g, TokCut c, long long* table, hipStream_t s) {
   if (g.docs <= 64) return hipSuccess;
-  const int kb = tok_block_rows(dt, c), pack = tok_heads(g, c.heads).pack;
+  const int kb = tok_block_rows(pass, dt, g.dim, c), pack = tok_heads(g, c.heads).pack;
   const bool queries = pass != TOK_DKV;
   tok_table_k<<<1, 1024, 0, s>>>(side_of(g, queries, pack, c.waves * 32), side_of(g, !queries, g.group, kb), g.docs, table);
   return hipGetLastError();
