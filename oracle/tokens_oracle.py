@@ -120,8 +120,10 @@ def _one(out, q, k, v, do, scale, cap, dist, slope, rq, rk, h, hk, half_step, op
     off = u * ((dim + 8) * size + 8 * (cap + np.abs(s) + far + np.abs(lse)[:, None]) + 16)     # of a score, so relative of exp(score)
     worst = off.max(1, keepdims=True)
     rel = 2 * worst + (m + 8) * u                                                             # of a probability
+    # below 2^-126 there are no normal floats: a probability, a score's gradient, a product of either, a sum and a result may each be zero instead
+    tiny = 2.0 ** -126
     a = p @ np.abs(v)
-    o_off = half_step * np.abs(o) + (operand + rel) * a
+    o_off = half_step * np.abs(o) + (operand + rel) * a + tiny * (np.abs(v).sum(0) + m + 1)
     out["o"][rq, h], out["lse"][h, rq] = o, lse
     out["o_off"][rq, h] = o_off
     out["lse_off"][h, rq] = worst[:, 0] + u * (m + 8 + 4 * np.abs(lse))
@@ -134,12 +136,14 @@ def _one(out, q, k, v, do, scale, cap, dist, slope, rq, rk, h, hk, half_step, op
     delta_off = (np.abs(do) * o_off).sum(1, keepdims=True) + dim * u * (np.abs(do) * np.abs(o)).sum(1, keepdims=True)
     dp_off = (dim + 8) * u * (np.abs(do) @ np.abs(v).T)
     # 1 - tanh^2 is off by twice the tanh's error where it is not small, relative else
-    ds_off = operand * np.abs(ds) + p * ((delta_off + dp_off) * np.abs(slope_t) + (rel + 16 * u + (2 * off / cap if cap else 0.0)) * np.abs(dp - delta))
+    ds_off = operand * np.abs(ds) + p * ((delta_off + dp_off) * np.abs(slope_t) + (rel + 16 * u + (2 * off / cap if cap else 0.0)) * np.abs(dp - delta)) \
+        + tiny * (np.abs(dp - delta) + 2)
     terms = (m + 8) * u
     out["dq"][rq, h] = scale * (ds @ k)
-    out["dq_off"][rq, h] = scale * ((ds_off + terms * np.abs(ds)) @ np.abs(k)) + half_step * np.abs(out["dq"][rq, h])
+    out["dq_off"][rq, h] = scale * ((ds_off + terms * np.abs(ds)) @ np.abs(k)) + half_step * np.abs(out["dq"][rq, h]) \
+        + tiny * (m + 1)
     terms = (n + 8) * u
     out["dk"][rk, hk] += scale * (ds.T @ q)
-    out["dk_off"][rk, hk] += scale * ((ds_off + terms * np.abs(ds)).T @ np.abs(q))
+    out["dk_off"][rk, hk] += scale * ((ds_off + terms * np.abs(ds)).T @ np.abs(q)) + tiny * (n + 1)
     out["dv"][rk, hk] += p.T @ do
-    out["dv_off"][rk, hk] += ((operand + rel + terms) * p).T @ np.abs(do)
+    out["dv_off"][rk, hk] += ((operand + rel + terms) * p + tiny).T @ np.abs(do) + tiny * (n + 1)

@@ -118,11 +118,16 @@ __device__ __forceinline__ void tok_walk(const TokSide& c, const TokSide& r, int
     s.c.lo = __builtin_amdgcn_readfirstlane(s.c.lo); s.c.n = __builtin_amdgcn_readfirstlane(s.c.n);
     s.r.lo = __builtin_amdgcn_readfirstlane(s.r.lo); s.r.n = __builtin_amdgcn_readfirstlane(s.r.n);
     const int n = tok_parts(s.r.n, r.per), rb = n > 0 ? n : 1;
+    // never out of the matrices, whatever the starts are: those of a million slides that all begin and end anywhere have more units than 64 bits count
+    if (s.head >= heads || v < first || (v - first) / rb * c.per >= s.c.n) break;
     s.tile = (int)((v - first) / rb);
     s.a = (int)((v - first) - (long long)s.tile * rb);
     s.b = end - u < rb - s.a ? s.a + (int)(end - u) : rb;
     s.slot = s.a == 0 && s.b == rb ? -1 : s.a > 0 ? me : blocks + me;
-    if (s.a == 0 && s.b < rb) join = {(int)((u + rb - 1) / per) - me + 1, s.head, s.doc, s.tile};
+    if (s.a == 0 && s.b < rb) {
+      const long long last = (u + rb - 1) / per;
+      join = {(int)(last < blocks ? last : blocks - 1) - me + 1, s.head, s.doc, s.tile};
+    }
     f(s);
     u += s.b - s.a;
   }

@@ -109,6 +109,12 @@ SELF = [
     ([130], 2, 1, 112, "fp32", 1.0, True, 100),
     ([700, 900], 2, 1, 64, "bf16", 0.0, True, 1),
     ([1] * 70 + [3] * 5, 3, 3, 32, "bf16", 0.0, True, 1),
+    # two heads at a time: of one key head and of two, one slide after the other in a table
+    ([150, 33, 0, 257], 8, 2, 64, "bf16", 0.0, True, 3),
+    ([140, 161], 4, 4, 48, "bf16", 7.0, True, 1),
+    ([3, 90, 41] * 30, 4, 2, 64, "bf16", 0.0, True, 1),
+    ([3, 90, 41] * 30, 3, 1, 48, "fp32", 9.0, False, 0),
+    ([1, 200, 0] * 25, 2, 2, 128, "bf16", 9.0, True, 200),
     ([1] * 5000, 1, 1, 16, "fp32", 0.0, False, 0),
 ]
 
@@ -145,6 +151,39 @@ def test_few_queries_or_few_keys(lq, lk, hq, hk, dim, dtype, cap, bias, lead):
     c.forward(out)
     c.backward(out)
     _check(c, out)
+
+
+@pytest.mark.parametrize("heads,dim,dtype", [((4, 4), 64, "bf16"), ((3, 1), 64, "bf16"), ((2, 1), 128, "bf16"), ((2, 2), 48, "fp32")])
+def test_far_places_with_fractions(heads, dim, dtype):
+    """Distances are those of the float32 positions however far from the origin they lie."""
+    import torch
+    print(f"case far places {heads} {dim} {dtype}", flush=True)
+    c = Case([170, 61], [170, 61], *heads, dim, dtype, bias=True, lead_q=1, lead_k=1)
+    g = torch.Generator().manual_seed(9)
+    place = 123456.0 + 60 * torch.rand((231, 2), generator=g)
+    c.places.update(pos_q=place, pos_k=place)
+    c.dev_places = {n: x.cuda() for n, x in c.places.items()}
+    out = c.outputs()
+    c.forward(out)
+    c.backward(out)
+    _check(c, out)
+
+
+def test_scores_that_fall_and_rise_along_the_keys():
+    """A row's maximum far below and far above that of its first keys: sums are kept relative to it."""
+    import torch
+    print("case falling and rising scores", flush=True)
+    for order in (1, -1):
+        c = Case([96], [1200], 2, 2, 64, "fp32", backward=True)
+        ramp = torch.linspace(-6 * order, 6 * order, 1200)
+        c.host["k"].mul_(0.2).add_(ramp[:, None, None] * 0.5)
+        c.host["q"].mul_(0.2).add_(3.0)
+        c.k.copy_(c.host["k"].cuda())
+        c.q.copy_(c.host["q"].cuda())
+        out = c.outputs()
+        c.forward(out)
+        c.backward(out)
+        _check(c, out)
 
 
 def test_many_heads_share_a_key_head():
@@ -186,7 +225,7 @@ def test_an_infinite_value_stays_in_its_slide():
     assert torch.isnan(bad["o"][70:140]).any()
 
 
-@pytest.mark.parametrize("starts", [[0, 40, 20, 60], [-5, 10, 30, 1000], [60, 40, 20, 0], [70, 80, 90, 100]])
+@pytest.mark.parametrize("starts", [[0, 40, 20, 60], [0, 60, 0, 60], [-5, 10, 30, 1000], [60, 40, 20, 0], [70, 80, 90, 100]])
 def test_starts_that_do_not_fit_stay_inside(starts):
     """What a wrong table gives is unspecified; rows behind the matrices are never touched (outputs lie inside larger ones)."""
     import torch
