@@ -132,8 +132,8 @@ hipError_t join_pass(int pass, const TokAttn& g, TokCut c, hipStream_t s) {
 
 }  // namespace
 
-// Few columns a slide leave three of four wavefronts idle: a wavefront a workgroup then.  Two workgroups of four wavefronts are on each of 256 units
-// at a time, or eight of one; fewer where there is less to do.  (Where there is, down to one unit each: 12 slides' tokens against 1 to 8192 keys,
+// Few columns a slide leave three of four wavefronts idle: a wavefront a workgroup then.  As many workgroups as the card holds at a time: one or
+// two of four wavefronts on each of 256 units, four or eight of one; fewer where there is less to do.  (Where there is, down to one unit each: 12 slides' tokens against 1 to 8192 keys,
 // 12 heads: 27.7 us with four units at least, 20.9 with two, 17.9 with one.)
 // Two heads at a time: a key head's, or two key heads', where the kernels are built for it.
 TokCut tok_cut(int pass, const slide_tokens_attn& s, bool bias) {
@@ -151,7 +151,9 @@ TokCut tok_cut(int pass, const slide_tokens_attn& s, bool bias) {
   const long long rows = queries ? s.rows_k : s.rows_q * group, width = 32 * c.waves, kb = tok_block_rows(pass, s.dtype, s.head_dim, c);
   // no more units than these: a slide's last tile and block are partly empty
   const double units = ((double)cols / width + s.docs) * ((double)rows / kb + 1) * s.heads_k;
-  const long long most = c.waves == 4 ? 512 : 2048, n = units < (double)most ? (long long)units + 1 : most;
+  // two wavefronts a SIMD where 256 registers do, which is where the kernels' launch bounds say so; else one
+  const bool two = c.waves == 4 ? s.head_dim <= 64 || (pass == TOK_FWD && s.dtype == DT_BF16) : pass == TOK_FWD && s.head_dim <= 64;
+  const long long most = (c.waves == 4 ? 256 : 1024) * (two ? 2 : 1), n = units < (double)most ? (long long)units + 1 : most;
   c.blocks = (int)((n + 7) / 8 * 8);
   return c;
 }
