@@ -12,7 +12,8 @@
  * caller's, needs no clearing, is 256-byte aligned, holds nothing from one call to the next, and must not be shared by calls
  * that may run at the same time (two captured graphs that may).  Return value 0 or a negative SLIDE_E* code.  `dtype` is 0 = float32,
  * 1 = bfloat16; sums, norms, softmax statistics and angles are held in 32 bits or more, and results are the same bits on every run.
- * Matrices are 16-byte aligned and ld is a multiple of 8 (bfloat16) or 4 (float32), below 2^21.  Unless a comment allows it, outputs must not
+ * Matrices are 16-byte aligned and ld is a multiple of 8 (bfloat16) or 4 (float32), below 2^21.  bfloat16: products of bfloat16 operands with
+ * sums in float32; probabilities and the gradients of scores are rounded to bfloat16 where they are multiplied.  Unless a comment allows it, outputs must not
  * overlap inputs or each other.
  */
 #ifndef SLIDE_TOKENS_H_
@@ -30,7 +31,7 @@ extern "C" {
 
 /* Norm and rotation of a head's vector x (host).  head_dim: a multiple of 16 up to 256.  axes: 0 to 3 coordinates of a position;
  * axis a has pairs[a] >= 0 pairs, those of axis 0 first, at most head_dim / 2 in all (the others are not rotated).  The j-th pair of an axis with n
- * turns by position * theta^(-j / n) radians; theta > 0.  Angles are right to 2^-31 of a turn for every position that 32 bits hold.
+ * turns by position * theta^(-j / n) radians; theta >= 1.  Angles are right to 2^-31 of a turn for every position that 32 bits hold.
  * With a gain g:  n = x / sqrt(mean(x^2) + eps) * g, eps > 0; without: n = x.  Result: n, rotated. */
 typedef struct slide_head_rope {
   int64_t rows;
@@ -55,7 +56,7 @@ int slide_head_rope_bwd(const slide_head_rope* s, const void* dyq, int64_t lddyq
                         int64_t lddq, void* dk, int64_t lddk, float* dgq, float* dgk, int accumulate, void* work,
                         size_t work_bytes, void* hip_stream);
 
-/* Attention inside each of `docs` slides (host).  head_dim: a multiple of 16 up to 128; heads_q / heads_k up to 128.
+/* Attention inside each of `docs` slides (host).  head_dim: a multiple of 16 up to 128; heads_q / heads_k up to 128, times rows_q below 2^31 - 256.
  * Row i of slide b is rows q_start[b] + i of the queries and k_start[b] + i of the keys.  Score of a query and a key of the same slide:
  *     x = scale * q.k;   where cap > 0: x = cap * tanh(x / cap);   where there are slopes: x -= slopes[head] * distance(pos_q, pos_k)
  * The first lead_q queries and lead_k keys of a slide have no place (class tokens): their distances are 0 and their positions are not used. */
@@ -74,8 +75,8 @@ size_t slide_tokens_attn_workspace_bytes(const slide_tokens_attn* s, int backwar
 /* o [rows_q][heads_q * head_dim] = softmax(scores) v, lse [heads_q][rows_q] float32 = log of the sum of exp(scores).  A slide without keys has
  * o = 0 and lse = -infinity.  q_start, k_start: [docs + 1], not decreasing, from 0 to rows_q / rows_k; rows before the first slide and behind the last
  * one are neither read nor written.  (What does not fit is taken as if cut to that range: never out of the matrices.)
- * pos_q [rows_q][2], pos_k [rows_k][2] float32, 8-byte aligned, finite and
- * below 2^60, and slopes [heads_q] float32, below 2^40: all of them or none. */
+ * pos_q [rows_q][2], pos_k [rows_k][2] float32, 8-byte aligned, below 2^40 in size, and slopes [heads_q] float32, below 2^20 in size: all of them or
+ * none. */
 int slide_tokens_attn_fwd(const slide_tokens_attn* s, const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v,
                           int64_t ldv, const int32_t* q_start, const int32_t* k_start, const float* pos_q, const float* pos_k,
                           const float* slopes, void* o, int64_t ldo, float* lse, void* work, size_t work_bytes, void* hip_stream);

@@ -510,9 +510,12 @@ class _TensorCalls:
         self.lib = load_cdll()
         self._torch = torch
         self._types = {torch.float32: 0, torch.bfloat16: 1}
+        self._float32, self._int32 = torch.float32, torch.int32
         self._shapes = {}
         # the raw handle of a device's current stream, where this torch has it without building a Stream
         self._raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
+        # the current device, likewise without a check whether CUDA has been set up: there are tensors on it
+        self._device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
         self._entry = {n: getattr(self.lib, n) for n in self.ENTRIES}
 
     def _type(self, t):
@@ -524,7 +527,7 @@ class _TensorCalls:
     def _floats(self, t, n, what):
         if t is None:
             return None
-        if t.dtype != self._torch.float32 or t.numel() != n or not t.is_contiguous():
+        if t.dtype is not self._float32 or t.numel() != n or not t.is_contiguous():
             raise ValueError(f"{what}: {n} contiguous float32 values")
         return t.data_ptr()
 
@@ -543,7 +546,7 @@ class _TensorCalls:
             if stream.device.index != dev:
                 raise ValueError(f"{what}: a stream of {stream.device} for tensors on device {dev}")
             stream = stream.cuda_stream
-        if dev != cuda.current_device():
+        if dev != self._device():
             with cuda.device(dev):
                 rc = self._entry[what](*args, stream)
         else:
@@ -719,9 +722,9 @@ class TokensLib(_TensorCalls):
         """(pointer, elements between rows) of [rows, heads, dim]; (None, 0) for None."""
         if t is None:
             return None, 0
-        if t.dtype != dtype:
+        if t.dtype is not dtype:
             raise ValueError(f"{what}: {t.dtype}, expected {dtype}")
-        if tuple(t.shape) != (rows, heads, dim):
+        if t.shape != (rows, heads, dim):
             raise ValueError(f"{what}: {tuple(t.shape)}, expected {(rows, heads, dim)}")
         ld, between, one = t.stride()
         if (dim > 1 and one != 1) or (heads > 1 and between != dim):
@@ -731,7 +734,7 @@ class TokensLib(_TensorCalls):
     def _ints(self, t, shape, what):
         if t is None:
             return None
-        if t.dtype != self._torch.int32 or tuple(t.shape) != shape or not t.is_contiguous():
+        if t.dtype is not self._int32 or t.shape != shape or not t.is_contiguous():
             raise ValueError(f"{what}: contiguous int32 {shape}")
         return t.data_ptr()
 

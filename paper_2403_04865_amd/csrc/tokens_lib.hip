@@ -29,7 +29,7 @@ int status(hipError_t e) {
 int rope_ok(const slide_head_rope* s) {
   if (!s || s->rows < 1 || s->rows > TOK_ROWS_MAX || s->heads_q < 1 || s->heads_q > 4096 || s->heads_k < 0 || s->heads_k > 4096 || s->head_dim < 1 ||
       !dtype_ok(s->dtype) || s->axes < 0 || s->axes > 3 || (s->pairing != SLIDE_ROPE_HALVES && s->pairing != SLIDE_ROPE_NEIGHBOURS) ||
-      !(s->eps > 0.f) || !std::isfinite(s->eps) || !(s->theta > 0.0) || !std::isfinite(s->theta))
+      !(s->eps > 0.f) || !std::isfinite(s->eps) || !(s->theta >= 1.0) || !std::isfinite(s->theta))
     return SLIDE_EINVAL;
   int64_t pairs = 0;
   for (int a = 0; a < s->axes; ++a) {
@@ -46,13 +46,13 @@ HeadRope rope_of(const slide_head_rope& s, unsigned long long (&freq)[ROPE_PAIRS
   int at = 0;
   for (int a = 0; a < s.axes; ++a) {
     const int n = s.pairs[a];
-    // theta^(-j / n) / 2 pi modulo 1 as a fraction of 2^64, 64-bit mantissas: every eighth by itself, the others by products with the ratio
+    // theta^(-j / n) / 2 pi, below a sixth, as a fraction of 2^64, 64-bit mantissas: every eighth by itself, the others by products with the ratio
     // (2 us for 32 exponentials, a sixth of a small call)
     const long double step = n ? -std::log((long double)s.theta) / n : 0, ratio = std::exp(step);
     long double turns = 0;
     for (int j = 0; j < n; ++j) {
       turns = j % 8 == 0 ? std::exp(step * j) * 0.159154943091895335768883763372514362L : turns * ratio;
-      freq[at++] = (unsigned long long)((turns < 1 ? turns : turns - std::floor(turns)) * 18446744073709551616.0L);
+      freq[at++] = (unsigned long long)(turns * 18446744073709551616.0L);
     }
     if (a < 2) g.bound[a] = at;
   }

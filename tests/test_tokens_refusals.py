@@ -41,7 +41,7 @@ def rope_bwd(lib, s=None, **kw):
 
 BAD_ROPE = [dict(rows=0), dict(rows=-1), dict(rows=1 << 31), dict(heads_q=0), dict(heads_q=4097), dict(heads_k=-1), dict(head_dim=0), dict(dtype=2),
             dict(dtype=-1), dict(axes=-1), dict(axes=4), dict(pairing=2), dict(pairs=(17, 16, 0)), dict(pairs=(-1, 16, 0)), dict(eps=0.0),
-            dict(eps=float("nan")), dict(eps=float("inf")), dict(theta=0.0), dict(theta=float("nan")), dict(theta=-1.0), dict(theta=float("inf"))]
+            dict(eps=float("nan")), dict(eps=float("inf")), dict(theta=0.0), dict(theta=0.99), dict(theta=float("nan")), dict(theta=-1.0), dict(theta=float("inf"))]
 
 
 @pytest.mark.parametrize("bad", BAD_ROPE)
