@@ -257,19 +257,26 @@ __device__ __forceinline__ void tok_get_t(TokCols<float, DP>& x, const float* X,
   x.at = X + (j0 + 4 * ((threadIdx.x >> 5) & 1)) * tok_ldr<float, DP>() + (threadIdx.x & 31);
 }
 // acc[DP][columns] += X^T p.  bfloat16: p is rounded to it (half a step, 2^-8 of each probability at most and of either sign, where the
-// result's own rounding is as large); the matrix cores take no wider operand beside bfloat16.
-template <int DP>
+// result's own rounding is as large); the matrix cores take no wider operand beside bfloat16.  EXACT: p goes in as two terms, which leaves 2^-16 of it,
+// where that costs nothing: a wavefront that waits for memory.
+template <int DP, bool EXACT>
 __device__ __forceinline__ void tok_mul_t(f32x16 (&acc)[DP / 32], const TokCols<bf16, DP>& x, const f32x16& p) {
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
-    bf16x8 b;
+    bf16x8 b, rest;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) b[i] = (bf16)p[8 * t + i];
+    for (int i = 0; i < 8; ++i) {
+      b[i] = (bf16)p[8 * t + i];
+      if (EXACT) rest[i] = (bf16)(p[8 * t + i] - (float)b[i]);
+    }
 #pragma unroll
-    for (int d = 0; d < DP / 32; ++d) acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x.v[t][d], b, acc[d], 0, 0, 0);
+    for (int d = 0; d < DP / 32; ++d) {
+      acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x.v[t][d], b, acc[d], 0, 0, 0);
+      if (EXACT) acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x.v[t][d], rest, acc[d], 0, 0, 0);
+    }
   }
 }
-template <int DP>
+template <int DP, bool>
 __device__ __forceinline__ void tok_mul_t(f32x16 (&acc)[DP / 32], const TokCols<float, DP>& x, const f32x16& p) {
 #pragma unroll
   for (int r = 0; r < 16; ++r)

@@ -49,7 +49,7 @@ __global__ void __launch_bounds__(NW * 64, DP <= 64 && NW == 4 ? 2 : 1) tok_dkv_
     f32x16 dk[DP / 32], dv[DP / 32];
     tok_zero_all(dk);
     tok_zero_all(dv);
-    // keys without a place are among the first tiles' only, whose loop is a copy of its own
+    // keys without a place are among the first tiles' only, whose loop is a copy of its own.
     auto pass = [&](auto lead) __attribute__((always_inline)) {
       constexpr bool LEADS = decltype(lead)::value;
       qt.load_packed(qp, w.a * KB, cols, g.ldq, g.dim, g.group, magic);
@@ -108,9 +108,9 @@ __global__ void __launch_bounds__(NW * 64, DP <= 64 && NW == 4 ? 2 : 1) tok_dkv_
             }
           }
           tok_get_t(dc, Os, b * 32);
-          tok_mul_t<DP>(dv, dc, p);
+          tok_mul_t<DP, NW == 1>(dv, dc, p);
           tok_get_t(qc, Qs, b * 32);
-          tok_mul_t<DP>(dk, qc, s);
+          tok_mul_t<DP, NW == 1>(dk, qc, s);
         }
       }
     };

@@ -21,9 +21,14 @@ __device__ __forceinline__ float tok_dot(const TokFrag<T, DP>& a, const TokFrag<
   return tok_other_sum(sum);
 }
 
-template <typename T, int DP, int NW, bool BIAS, bool CAP>
+// dS = P (dP - delta) with delta = dout . o = sum P dP.  Out of an o that has been rounded to bfloat16 delta is off by some e, and every dS of the row by P e.  The
+// sum of a row's dS is -e up to float32, so e is known when the row has been passed: the keys' pass gets the right delta.  MEND: this one
+// gives e times sum P k back, for another product.  Where few keys count, dP - delta is small beside both and e decides (slides of 100 rows, head of 32, strong
+// bias: gradients 3.4e-3 off, 2.4e-3 mended); in longer ones it is 2e-4 to 6e-4 beside the 2.4e-3 of the roundings to bfloat16, and the product
+// not worth its time (8193 rows, 6 heads of 64, both directions: 731 us with an unmended delta, 764 with e for the keys, 860 with the product too).  float32 results need neither.
+template <typename T, int DP, int NW, bool BIAS, bool CAP, bool MEND>
 __global__ void __launch_bounds__(NW * 64, DP <= 64 && NW == 4 ? 2 : 1) tok_dq_k(const TokAttn g) {
-  constexpr int KB = TokType<T>::KB, LDR = tok_ldr<T, DP>(), NB = KB / 32, W = NW * 32;
+  constexpr int KB = DP == 128 ? 32 : TokType<T>::KB, LDR = tok_ldr<T, DP>(), NB = KB / 32, W = NW * 32;
   __shared__ __attribute__((aligned(16))) T Ks[KB * LDR], Vs[KB * LDR];
   __shared__ __attribute__((aligned(16))) float px[KB], py[KB];
   const TokScore sc = tok_score_of<CAP>(g.scale, g.cap);
@@ -39,7 +44,7 @@ __global__ void __launch_bounds__(NW * 64, DP <= 64 && NW == 4 ? 2 : 1) tok_dq_k
     tok_load_frag<T, DP>(fo, (const T*)g.dout + qrow * g.lddo + head * g.dim, valid, g.dim);
     // a column that is not there: infinite, so its probabilities are zero
     const float lse = valid ? g.lse[(long long)head * g.rows_q + qrow] * TOK_LOG2E : INFINITY;
-    float delta;   // dout . o, also for the keys' pass
+    float delta;   // dout . o, also for the keys' pass (where a tile is shared, its join adds e)
     {
       TokFrag<T, DP> f;
       tok_load_frag<T, DP>(f, (const T*)g.o_in + qrow * g.ldo + head * g.dim, valid, g.dim);
@@ -53,10 +58,13 @@ __global__ void __launch_bounds__(NW * 64, DP <= 64 && NW == 4 ? 2 : 1) tok_dq_k
     }
     const T* const kp = (const T*)g.k + (long long)klo * g.ldk + w.head * g.dim;
     const T* const vp = (const T*)g.v + (long long)klo * g.ldv + w.head * g.dim;
-    TokTile<T, DP, NW * 64> kt(g.ldk, g.dim), vt(g.ldv, g.dim);
+    TokTile<T, DP, NW * 64, KB> kt(g.ldk, g.dim), vt(g.ldv, g.dim);
     TokPlace place = {0.f, 0.f};
-    f32x16 dq[DP / 32];
+    constexpr bool ERR = sizeof(T) == 2;
+    f32x16 dq[DP / 32], pk[MEND ? DP / 32 : 1];
     tok_zero_all(dq);
+    tok_zero_all(pk);
+    float e = 0.f;   // sum of P (dP - delta)
     if (nk > 0) {
       kt.load(kp + (long long)w.a * KB * g.ldk, nk - w.a * KB, g.ldk, g.dim);
       vt.load(vp + (long long)w.a * KB * g.ldv, nk - w.a * KB, g.ldv, g.dim);
@@ -78,7 +86,7 @@ __global__ void __launch_bounds__(NW * 64, DP <= 64 && NW == 4 ? 2 : 1) tok_dq_k
         // the first and the last blocks hold keys without a place and keys that are not there: a copy of the code of their own
         auto block = [&](auto edge, int b) __attribute__((always_inline)) {
           constexpr bool EDGE = decltype(edge)::value;
-          f32x16 s = tok_zero(), dp = tok_zero(), dist;
+          f32x16 s = tok_zero(), dp = tok_zero(), dist, p;
           if (BIAS) tok_dists<T>(dist, px, py, b * 32, qx, qy);
           TokRows<T, DP> kr, vr;
           TokCols<T, DP> kc;
@@ -95,14 +103,20 @@ __global__ void __launch_bounds__(NW * 64, DP <= 64 && NW == 4 ? 2 : 1) tok_dq_k
               float d = BIAS ? dist[r] : 0.f, dt = 1.f;
               if (EDGE && BIAS && k0 + r0 + i < g.lead_k) d = 0.f;
               const float z = tok_score<T, BIAS, CAP, true>(s[r], d, slope, sc, &dt);
-              float ds = tok_exp<CAP>(z, lse, sc) * (dp[r] - delta);
-              if (CAP) ds *= dt;
-              if (EDGE && k0 + r0 + i >= nk) ds = 0.f;   // there K is zeros, but a probability may be no number
+              p[r] = tok_exp<CAP>(z, lse, sc);
+              if (EDGE && k0 + r0 + i >= nk) p[r] = 0.f;   // there K is zeros, but a probability may be no number
+              float ds = p[r] * (dp[r] - delta);
+              if (ERR) e += ds;
+              if (CAP) {
+                ds *= dt;
+                if (MEND) p[r] *= dt;
+              }
               s[r] = ds;
             }
           }
           tok_get_t(kc, Ks, b * 32);
-          tok_mul_t<DP>(dq, kc, s);
+          tok_mul_t<DP, NW == 1>(dq, kc, s);
+          if constexpr (MEND) tok_mul_t<DP, false>(pk, kc, p);
         };
         const bool edge = (BIAS && k0 < g.lead_k) || k0 + KB > nk;   // uniform
 #pragma unroll
@@ -112,10 +126,24 @@ __global__ void __launch_bounds__(NW * 64, DP <= 64 && NW == 4 ? 2 : 1) tok_dq_k
         }
       }
     }
+    if (ERR) e = tok_other_sum(e);
     if (!valid) return;
     const float f = CAP ? 4.f * g.scale : g.scale;   // scores' gradients carry a quarter of the cap's derivative
-    if (w.slot >= 0) tok_store(dq, f, g.part + ((long long)w.slot * W + wave * 32 + (lane & 31)) * g.dim, g.dim);
-    else tok_store(dq, f, (T*)g.dq + qrow * g.lddq + head * g.dim, g.dim);
+    if (w.slot >= 0) {
+      const long long at = (long long)w.slot * W + wave * 32 + (lane & 31);
+      tok_store(dq, f, g.part + at * g.dim, g.dim);
+      if constexpr (MEND) tok_store(pk, f, g.part2 + at * g.dim, g.dim);
+      if (ERR && lane < 32) g.part3[at] = e;
+      return;
+    }
+    if constexpr (MEND) {
+#pragma unroll
+      for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) dq[d][r] = fmaf(-e, pk[d][r], dq[d][r]);
+    }
+    if (ERR && lane < 32) g.delta[(long long)head * g.rows_q + qrow] = delta + e;
+    tok_store(dq, f, (T*)g.dq + qrow * g.lddq + head * g.dim, g.dim);
   });
 }
 
@@ -124,8 +152,14 @@ hipError_t run_dq(const TokAttn& g, TokCut c, hipStream_t s) {
   return tok_dispatch<T>(g, [&](auto dp, auto bias, auto cap) {
     constexpr int DP = decltype(dp)::value;
     constexpr bool BIAS = decltype(bias)::value, CAP = decltype(cap)::value;
-    if (c.waves == 4) tok_dq_k<T, DP, 4, BIAS, CAP><<<c.blocks, 256, 0, s>>>(g);
-    else tok_dq_k<T, DP, 1, BIAS, CAP><<<c.blocks, 64, 0, s>>>(g);
+    if constexpr (sizeof(T) == 2) {
+      if (c.waves == 1) tok_dq_k<T, DP, 1, BIAS, CAP, true><<<c.blocks, 64, 0, s>>>(g);
+      else if (c.mend) tok_dq_k<T, DP, 4, BIAS, CAP, true><<<c.blocks, 256, 0, s>>>(g);
+      else tok_dq_k<T, DP, 4, BIAS, CAP, false><<<c.blocks, 256, 0, s>>>(g);
+    } else {
+      if (c.waves == 4) tok_dq_k<T, DP, 4, BIAS, CAP, false><<<c.blocks, 256, 0, s>>>(g);
+      else tok_dq_k<T, DP, 1, BIAS, CAP, false><<<c.blocks, 64, 0, s>>>(g);
+    }
     return hipGetLastError();
   });
 }

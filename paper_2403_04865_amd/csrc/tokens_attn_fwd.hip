@@ -144,7 +144,7 @@ __global__ void __launch_bounds__(NW * 64, (tok_waves<T, DP, NW>())) tok_fwd_k(c
           for (int b = 0; b < NB; ++b) {
             TokCols<T, DP> vc;
             tok_get_t(vc, Vs[n * second], b * 32);
-            tok_mul_t<DP>(o[n], vc, s[n][b]);
+            tok_mul_t<DP, NW == 1>(o[n], vc, s[n][b]);
           }
         }
       }

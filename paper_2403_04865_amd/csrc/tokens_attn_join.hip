@@ -34,20 +34,38 @@ __global__ void __launch_bounds__(1024) tok_table_k(const TokSide c, const TokSi
 }
 
 // A workgroup joins COLS columns of a tile.  A column's threads are groups of `lanes` with four of its values each, group z of them takes every
-// `zs`-th piece; blockIdx.z is the head of a group; the groups' results meet in LDS.  SOFTMAX: pieces are sums under maxima of their own.
-// TWO: two results of the same columns, one after the other in blockIdx.z (keys' and values' gradients).
-template <typename T, int W, bool SOFTMAX, bool TWO>
+// `zs`-th piece; the groups' results meet in LDS, in their order.  blockIdx.z: the head of a group (forward), keys' or values' gradient.
+// Forward: pieces are sums under references of their own.  TOK_DQ, bfloat16: beside the sums those of P k and the error of delta (tokens_attn_dq.hip).
+struct Sum { f32x4 o, k; float m, l; };
+template <int PASS, bool MEND>
+__device__ __forceinline__ void add(Sum& a, const Sum& b) {
+  if (PASS == TOK_FWD) {
+    const float n = fmaxf(a.m, b.m), ns = n == -INFINITY ? 0.f : n;
+    const float wa = __builtin_amdgcn_exp2f(a.m - ns), wb = __builtin_amdgcn_exp2f(b.m - ns);
+    a.m = n;
+    a.l = fmaf(a.l, wa, b.l * wb);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) a.o[i] = fmaf(a.o[i], wa, b.o[i] * wb);
+  } else {
+    a.o += b.o;
+    if (MEND) a.k += b.k;
+    if (PASS == TOK_DQ) a.l += b.l;
+  }
+}
+struct JoinOut { void* out; int ld; };
+template <typename T, int W, int PASS, bool MEND>
 __global__ void __launch_bounds__(W == 32 ? 512 : 256) tok_join_k(const TokAttn g, const TokSide side, const TokHeads hs, int hstep, int blocks,
-                                                                  const float* __restrict__ part0, const float* __restrict__ stat, T* __restrict__ out0, int ld0, T* __restrict__ out1, int ld1) {
+                                                                  JoinOut out0, JoinOut out1) {
   constexpr int COLS = 8, NT = W == 32 ? 512 : 256;   // few columns mean many pieces
-  __shared__ f32x4 sums[NT];
-  __shared__ float2 stats[NT];
+  constexpr bool ERR = PASS == TOK_DQ && sizeof(T) == 2;
+  __shared__ f32x4 sums[NT], sums2[MEND ? NT : 1];
+  __shared__ float2 stats[PASS == TOK_DKV ? 1 : NT];
   const TokJoin j = ((const TokJoin*)g.joins)[blockIdx.x];
   if (j.pieces == 0) return;
-  const int n = TWO ? 0 : blockIdx.z, heads = TWO ? 1 : gridDim.z;
-  const float* const part = TWO && blockIdx.z ? stat : part0;
-  T* const out = TWO && blockIdx.z ? out1 : out0;
-  const int ld = TWO && blockIdx.z ? ld1 : ld0;
+  const bool second = PASS == TOK_DKV && blockIdx.z;
+  const int n = PASS == TOK_DKV ? 0 : blockIdx.z, heads = PASS == TOK_DKV ? 1 : gridDim.z;
+  const float* const part = second ? g.part2 : g.part;
+  const JoinOut out = second ? out1 : out0;
   const TokSpan c = tok_span(side, j.doc);
   const int first = j.tile * W + blockIdx.y * COLS, here = c.n - first < COLS ? c.n - first : COLS;   // columns of this workgroup
   if (here <= 0) return;
@@ -55,79 +73,72 @@ __global__ void __launch_bounds__(W == 32 ? 512 : 256) tok_join_k(const TokAttn 
   const int cols = here <= 1 ? 1 : here <= 2 ? 2 : here <= 4 ? 4 : 8, zs = NT / (lanes * cols);
   const int quad = threadIdx.x & (lanes - 1), col = (threadIdx.x / lanes) & (cols - 1), z = threadIdx.x / (lanes * cols);
   const bool on = quad < quads && col < here;
-  f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  float m = -INFINITY, l = 0.f;
+  Sum a = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}, -INFINITY, 0.f};
   if (on) {
 #pragma unroll 4
     for (int p = z; p < j.pieces; p += zs) {
       const long long slot = p == 0 ? blocks + (int)blockIdx.x : (int)blockIdx.x + p;   // the first piece is the end of its workgroup's units
       const long long at = (slot * heads + n) * W + blockIdx.y * COLS + col;
-      const f32x4 v = *reinterpret_cast<const f32x4*>(part + at * g.dim + quad * 4);
-      if (SOFTMAX) {
-        const float2 s = *reinterpret_cast<const float2*>(stat + 2 * at);
-        const float n = fmaxf(m, s.x), ns = n == -INFINITY ? 0.f : n;
-        const float wa = __builtin_amdgcn_exp2f(m - ns), wb = __builtin_amdgcn_exp2f(s.x - ns);
-        m = n;
-        l = fmaf(l, wa, s.y * wb);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) o[i] = fmaf(o[i], wa, v[i] * wb);
-      } else {
-        o += v;
+      Sum b = {};
+      b.o = *reinterpret_cast<const f32x4*>(part + at * g.dim + quad * 4);
+      if (PASS == TOK_FWD) {
+        const float2 s = *reinterpret_cast<const float2*>(g.part2 + 2 * at);
+        b.m = s.x; b.l = s.y;
       }
+      if (MEND) b.k = *reinterpret_cast<const f32x4*>(g.part2 + at * g.dim + quad * 4);
+      if (ERR) b.l = g.part3[at];
+      add<PASS, MEND>(a, b);
     }
   }
   if (zs > 1) {
-    sums[threadIdx.x] = o;
-    if (SOFTMAX) stats[threadIdx.x] = float2{m, l};
+    sums[threadIdx.x] = a.o;
+    if (MEND) sums2[threadIdx.x] = a.k;
+    if (PASS != TOK_DKV) stats[threadIdx.x] = float2{a.m, a.l};
     __syncthreads();
     if (z) return;
     const int stride = lanes * cols;
-    for (int k = 1; k < zs; ++k) {   // in the groups' order
-      const f32x4 v = sums[threadIdx.x + k * stride];
-      if (SOFTMAX) {
-        const float2 s = stats[threadIdx.x + k * stride];
-        const float n = fmaxf(m, s.x), ns = n == -INFINITY ? 0.f : n;
-        const float wa = __builtin_amdgcn_exp2f(m - ns), wb = __builtin_amdgcn_exp2f(s.x - ns);
-        m = n;
-        l = fmaf(l, wa, s.y * wb);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) o[i] = fmaf(o[i], wa, v[i] * wb);
-      } else {
-        o += v;
-      }
+    for (int k = 1; k < zs; ++k) {
+      const int at = threadIdx.x + k * stride;
+      Sum b = {};
+      b.o = sums[at];
+      if (MEND) b.k = sums2[at];
+      if (PASS != TOK_DKV) { b.m = stats[at].x; b.l = stats[at].y; }
+      add<PASS, MEND>(a, b);
     }
   }
   if (!on) return;
   const int at = first + col, qi = at / side.group, head = j.head * hstep + n * hs.step + (at - qi * side.group);
   const long long row = c.lo + qi;
-  const float f = !SOFTMAX ? 1.f : l == 0.f ? 0.f : 1.f / l;
+  const float f = PASS != TOK_FWD ? 1.f : a.l == 0.f ? 0.f : 1.f / a.l;
   typedef T T4 __attribute__((ext_vector_type(4)));
   T4 v;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) v[i] = from_f<T>(o[i] * f);
-  *reinterpret_cast<T4*>(out + row * ld + head * g.dim + quad * 4) = v;
-  if (SOFTMAX && quad == 0) g.lse[head * (long long)g.rows_q + row] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * TOK_LN2;
+  for (int i = 0; i < 4; ++i) v[i] = from_f<T>(MEND ? fmaf(-a.l, a.k[i], a.o[i]) : a.o[i] * f);
+  *reinterpret_cast<T4*>((T*)out.out + row * out.ld + head * g.dim + quad * 4) = v;
+  if (PASS == TOK_FWD && quad == 0) g.lse[head * (long long)g.rows_q + row] = a.l == 0.f ? -INFINITY : (a.m + __builtin_amdgcn_logf(a.l)) * TOK_LN2;
+  if (ERR && quad == 0) g.delta[head * (long long)g.rows_q + row] += a.l;
 }
 
 // rows of a block in LDS (the kernels' KB)
-int tok_block_rows(int pass, int dt, int dim, TokCut c) { return dt == DT_F32 || c.heads == 2 || (pass == TOK_FWD && dim > 96) ? 32 : 64; }
+int tok_block_rows(int pass, int dt, int dim, TokCut c) { return dt == DT_F32 || c.heads == 2 || (pass != TOK_DKV && dim > 96) ? 32 : 64; }
 TokSide side_of(const TokAttn& g, bool queries, int pack, int per) { return queries ? TokSide{g.q_start, g.rows_q, pack, per} : TokSide{g.k_start, g.rows_k, 1, per}; }
 
-template <typename T, bool SOFTMAX, bool TWO>
-hipError_t join(const TokAttn& g, TokCut c, void* out, int ld, void* out1, int ld1, hipStream_t s) {
-  const dim3 grid(c.blocks, c.waves * 32 / 8, TWO ? 2 : c.heads);
+template <typename T, int PASS, bool MEND>
+hipError_t join(const TokAttn& g, TokCut c, JoinOut out, JoinOut out1, hipStream_t s) {
+  constexpr bool KEYS = PASS == TOK_DKV;
+  const dim3 grid(c.blocks, c.waves * 32 / 8, KEYS ? 2 : c.heads);
   const TokHeads hs = tok_heads(g, c.heads);
-  const TokSide side = side_of(g, !TWO, hs.pack, c.waves * 32);
-  const int hstep = TWO ? 1 : g.group * (hs.kv_step + 1);   // heads from one group to the next
-  if (c.waves == 4) tok_join_k<T, 128, SOFTMAX, TWO><<<grid, 256, 0, s>>>(g, side, hs, hstep, c.blocks, g.part, g.part2, (T*)out, ld, (T*)out1, ld1);
-  else tok_join_k<T, 32, SOFTMAX, TWO><<<grid, 512, 0, s>>>(g, side, hs, hstep, c.blocks, g.part, g.part2, (T*)out, ld, (T*)out1, ld1);
+  const TokSide side = side_of(g, !KEYS, hs.pack, c.waves * 32);
+  const int hstep = KEYS ? 1 : g.group * (hs.kv_step + 1);   // heads from one group to the next
+  if (c.waves == 4) tok_join_k<T, 128, PASS, MEND><<<grid, 256, 0, s>>>(g, side, hs, hstep, c.blocks, out, out1);
+  else tok_join_k<T, 32, PASS, MEND><<<grid, 512, 0, s>>>(g, side, hs, hstep, c.blocks, out, out1);
   return hipGetLastError();
 }
 template <typename T>
 hipError_t join_pass(int pass, const TokAttn& g, TokCut c, hipStream_t s) {
-  if (pass == TOK_FWD) return join<T, true, false>(g, c, g.o, g.ldo, nullptr, 0, s);
-  if (pass == TOK_DQ) return join<T, false, false>(g, c, g.dq, g.lddq, nullptr, 0, s);
-  return join<T, false, true>(g, c, g.dk, g.lddk, g.dv, g.lddv, s);
+  if (pass == TOK_FWD) return join<T, TOK_FWD, false>(g, c, {g.o, g.ldo}, {}, s);
+  if (pass == TOK_DQ) return sizeof(T) == 2 && c.mend ? join<T, TOK_DQ, true>(g, c, {g.dq, g.lddq}, {}, s) : join<T, TOK_DQ, false>(g, c, {g.dq, g.lddq}, {}, s);
+  return join<T, TOK_DKV, false>(g, c, {g.dk, g.lddk}, {g.dv, g.lddv}, s);
 }
 
 }  // namespace
@@ -135,7 +146,7 @@ hipError_t join_pass(int pass, const TokAttn& g, TokCut c, hipStream_t s) {
 // Few columns a slide leave three of four wavefronts idle: a wavefront a workgroup then.  As many workgroups as the card holds at a time: one or
 // two of four wavefronts on each of 256 units, four or eight of one; fewer where there is less to do.  (Where there is, down to one unit each: 12 slides' tokens against 1 to 8192 keys,
 // 12 heads: 27.7 us with four units at least, 20.9 with two, 17.9 with one.)
-// Two heads at a time: a key head's, or two key heads', where the kernels are built for it.
+// dq mends the rounding of o where slides are short or there are few queries.  Two heads at a time: a key head's, or two key heads', where the kernels are built for it.
 TokCut tok_cut(int pass, const slide_tokens_attn& s, bool bias) {
   const int group = s.heads_q / s.heads_k;
   const bool queries = pass != TOK_DKV;
@@ -155,6 +166,7 @@ TokCut tok_cut(int pass, const slide_tokens_attn& s, bool bias) {
   const bool two = c.waves == 4 ? s.head_dim <= 64 || (pass == TOK_FWD && s.dtype == DT_BF16) : pass == TOK_FWD && s.head_dim <= 64;
   const long long most = (c.waves == 4 ? 256 : 1024) * (two ? 2 : 1), n = units < (double)most ? (long long)units + 1 : most;
   c.blocks = (int)((n + 7) / 8 * 8);
+  c.mend = pass == TOK_DQ && s.dtype == DT_BF16 && (c.waves == 1 || s.rows_k <= 256LL * s.docs);
   return c;
 }
 

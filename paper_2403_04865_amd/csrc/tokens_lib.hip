@@ -72,16 +72,18 @@ int attn_ok(const slide_tokens_attn* s) {
   return SLIDE_OK;
 }
 size_t up256(size_t n) { return (n + 255) / 256 * 256; }
-// Work space of a pass: the slides' table, the shared tiles, their parts and what goes with them (maxima and sums, or the values' parts).  The
+// Work space of a pass: the slides' table, the shared tiles, their parts and what goes with them (maxima and sums, sums of P k and the errors of delta, or
+// the values' parts).  The
 // backward's passes follow one another in the same place, behind the deltas.
-struct PassWork { size_t joins, part, part2, bytes; };
+struct PassWork { size_t joins, part, part2, part3, bytes; };
 PassWork pass_work(const slide_tokens_attn& s, int pass, TokCut c) {
   const size_t part = up256(tok_columns(c) * s.head_dim * 4);
   PassWork w;
   w.joins = up256(tok_table_bytes(s.docs));
   w.part = w.joins + up256(tok_joins_bytes(c));
   w.part2 = w.part + part;
-  w.bytes = w.part2 + (pass == TOK_FWD ? up256(tok_columns(c) * 8) : pass == TOK_DKV ? part : 0);
+  w.part3 = w.part2 + (pass == TOK_FWD ? up256(tok_columns(c) * 8) : part);
+  w.bytes = w.part3 + (pass == TOK_DQ ? up256(tok_columns(c) * 4) : 0);
   return w;
 }
 // for a call with a bias and for one without
@@ -97,7 +99,7 @@ size_t bwd_bytes(const slide_tokens_attn& s) {
 hipError_t run_pass(int pass, const slide_tokens_attn& s, TokAttn g, char* work, hipStream_t st) {
   const TokCut c = tok_cut(pass, s, g.slopes != nullptr);
   const PassWork w = pass_work(s, pass, c);
-  g.table = (const long long*)work; g.joins = work + w.joins; g.part = (float*)(work + w.part); g.part2 = (float*)(work + w.part2);
+  g.table = (const long long*)work; g.joins = work + w.joins; g.part = (float*)(work + w.part); g.part2 = (float*)(work + w.part2); g.part3 = (float*)(work + w.part3);
   hipError_t e = launch_tok_table(pass, s.dtype, g, c, (long long*)work, st);
   if (e != hipSuccess) return e;
   e = pass == TOK_FWD ? launch_tok_fwd(s.dtype, g, c, st) : pass == TOK_DQ ? launch_tok_dq(s.dtype, g, c, st) : launch_tok_dkv(s.dtype, g, c, st);
