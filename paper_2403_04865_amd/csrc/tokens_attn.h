@@ -204,8 +204,7 @@ __device__ __forceinline__ void tok_load_frag(TokFrag<T, DP>& f, const T* row, b
     if (valid && col < dim) f.v[i] = *reinterpret_cast<const u32x4*>(row + col);
   }
 }
-// Operands of a product out of LDS.  They are asked for all together and ahead of what comes between (left to the compiler, every product waited for
-// a read of its own).
+// Operands of a product out of LDS.
 // rows j0 .. j0 + 31 of X, contraction over the DP columns
 template <typename T, int DP> struct TokRows { u32x4 v[DP / TokType<T>::EPC / 2]; };
 template <typename T, int DP>

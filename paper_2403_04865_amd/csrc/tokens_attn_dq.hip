@@ -21,11 +21,12 @@ __device__ __forceinline__ float tok_dot(const TokFrag<T, DP>& a, const TokFrag<
   return tok_other_sum(sum);
 }
 
-// dS = P (dP - delta) with delta = dout . o = sum P dP.  Out of an o that has been rounded to bfloat16 delta is off by some e, and every dS of the row by P e.  The
-// sum of a row's dS is -e up to float32, so e is known when the row has been passed: the keys' pass gets the right delta.  MEND: this one
-// gives e times sum P k back, for another product.  Where few keys count, dP - delta is small beside both and e decides (slides of 100 rows, head of 32, strong
-// bias: gradients 3.4e-3 off, 2.4e-3 mended); in longer ones it is 2e-4 to 6e-4 beside the 2.4e-3 of the roundings to bfloat16, and the product
-// not worth its time (8193 rows, 6 heads of 64, both directions: 731 us with an unmended delta, 764 with e for the keys, 860 with the product too).  float32 results need neither.
+// dS = P (dP - delta) with delta = dout . o = sum P dP.  Out of an o that has been rounded to bfloat16 delta is some e short, and every dS of the row off by
+// P e.  The sum of a row's P (dP - delta) is that e (P sums to one), so it is known when the row has been passed: the keys' pass gets the right delta.  MEND: this
+// pass takes e times sum P k off, for another product.  Where few keys count, dP - delta is small beside both and e decides (slides of 100 rows, head of 32,
+// strong bias: gradients 3.4e-3 off, 2.4e-3 mended); in longer slides it is 2e-4 to 6e-4 beside the 2.4e-3 of the roundings to bfloat16, and the product
+// not worth its time (8193 rows, 6 heads of 64, both directions: 731 us without e, 764 with e for the keys, 860 with the product too).  float32 needs neither.
+// Bound by the vector and matrix units in turn: 51 and 31 % of the time there, two wavefronts a SIMD that do not hide all of each other's waits.
 template <typename T, int DP, int NW, bool BIAS, bool CAP, bool MEND>
 __global__ void __launch_bounds__(NW * 64, DP <= 64 && NW == 4 ? 2 : 1) tok_dq_k(const TokAttn g) {
   constexpr int KB = DP == 128 ? 32 : TokType<T>::KB, LDR = tok_ldr<T, DP>(), NB = KB / 32, W = NW * 32;
