@@ -97,6 +97,34 @@ def test_forward_and_backward(rows, hq, hk, dim, pairs, pairing, dtype, norm):
         _close(_np(got), want, 2 * size, dtype, "d" + name)
 
 
+@pytest.mark.parametrize("which", [0, 1])
+def test_one_of_the_gains(which):
+    import torch
+    from paper_2403_04865_amd import HeadRope, TokensLib
+    print(f"case rope one gain {which}", flush=True)
+    L, rope = TokensLib(), HeadRope(48, (10, 8), THETA, "neighbours", EPS)
+    qkv, pos, gains, dy = _make(301, 3, 3, 48, (10, 8), "fp32", True)
+    gains[1 - which] = None
+    x, g = qkv.cuda(), dy.cuda()
+    gq, gk = (None if v is None else v.cuda() for v in gains)
+    y, d = torch.empty_like(g), torch.empty_like(g)
+    L.slide_head_rope_fwd(rope, x[:, :3], x[:, 3:6], pos.cuda(), y[:, :3], y[:, 3:], gq=gq, gk=gk)
+    dg = [None if v is None else torch.empty(48, device="cuda") for v in gains]
+    work = torch.empty(L.slide_head_rope_workspace_bytes(rope, 301, 3, 3), dtype=torch.uint8, device="cuda")
+    L.slide_head_rope_bwd(rope, g[:, :3], g[:, 3:], x[:, :3] if which == 0 else None, x[:, 3:6] if which else None, pos.cuda(), d[:, :3], d[:, 3:], gq=gq, gk=gk,
+                          dgq=dg[0], dgk=dg[1], workspace=work)
+    c, s = to.rotation(pos.numpy(), (10, 8), 48, THETA)
+    for i in (0, 1):
+        v, w = _np(qkv[:, 3 * i:3 * i + 3]), _np(dy[:, 3 * i:3 * i + 3])
+        gain = None if gains[i] is None else _np(gains[i])
+        want, (wx, wg) = to.rope_fwd(v, gain, c, s, "neighbours", EPS), to.rope_bwd(w, v, gain, c, s, "neighbours", EPS)
+        # float32 as above, of the whole tensors' norms: 12 roundings, four times that where differences are taken, sums of 903 terms in parts
+        for got, ref, units in ((y, want, 12), (d, wx, 48)):
+            assert np.linalg.norm(_np(got[:, 3 * i:3 * i + 3]) - ref) <= units * 2.0 ** -24 * np.linalg.norm(ref)
+        if gain is not None:
+            assert np.linalg.norm(_np(dg[i]) - wg) <= 76 * 2.0 ** -24 * np.linalg.norm(np.abs(w).sum((0, 1)) + np.abs(wg))
+
+
 def test_in_place_and_bits_again():
     import torch
     from paper_2403_04865_amd import HeadRope, TokensLib

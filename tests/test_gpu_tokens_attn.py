@@ -186,13 +186,33 @@ def test_scores_that_fall_and_rise_along_the_keys():
         _check(c, out)
 
 
-def test_many_heads_share_a_key_head():
-    print("case group 128", flush=True)
-    c = Case([50, 7], [50, 7], 128, 1, 16, "bf16", bias=True, lead_q=1, lead_k=1)
+@pytest.mark.parametrize("lengths,dim", [([50, 7], 16), ([9, 30], 64)])
+def test_many_heads_share_a_key_head(lengths, dim):
+    print(f"case group 128 {lengths} {dim}", flush=True)
+    c = Case(lengths, lengths, 128, 1, dim, "bf16", bias=True, lead_q=1, lead_k=1)
     out = c.outputs()
     c.forward(out)
     c.backward(out)
     _check(c, out)
+
+
+@pytest.mark.parametrize("dtype,heads,dim", [("bf16", 2, 64), ("bf16", 3, 48), ("fp32", 2, 32)])
+def test_places_of_leading_rows_are_not_used(dtype, heads, dim):
+    print(f"case lead places {dtype} {heads} {dim}", flush=True)
+    import torch
+    lengths = [140, 1, 2, 33]
+    c = Case(lengths, lengths, heads, heads, dim, dtype, bias=True, lead_q=2, lead_k=2, front=3, behind=5)
+    want, got = c.outputs(), c.outputs()
+    c.forward(want)
+    c.backward(want)
+    _check(c, want)
+    unused = [r for a, n in zip(c.qs[:-1], lengths) for r in range(a, a + min(2, n))] + [0, 1, 2] + list(range(c.qs[-1], c.qs[-1] + 5))
+    for name, x in (("pos_q", float("nan")), ("pos_k", float("inf"))):
+        c.dev_places[name][unused] = x
+    c.forward(got)
+    c.backward(got)
+    for n in want:
+        assert torch.equal(want[n], got[n]), n
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
