@@ -117,7 +117,9 @@ def _one(out, q, k, v, do, scale, cap, dist, slope, rq, rk, h, hk, half_step, op
     u = 2.0 ** -24
     size = scale * (np.abs(q) @ np.abs(k).T)
     far = np.abs(slope) * dist if dist is not None else 0.0
-    off = u * ((dim + 8) * size + 8 * (cap + np.abs(s) + far + np.abs(lse)[:, None]) + 16)     # of a score, so relative of exp(score)
+    # tanh is right to some units of itself, but in bfloat16 up to a cap of 64, where 1 - 2 / (1 + exp 2u) is: six units of one
+    one = cap if operand and cap <= 64 else 0.0
+    off = u * ((dim + 8) * size + 8 * (one + np.abs(s) + far + np.abs(lse)[:, None]) + 16)     # of a score, so relative of exp(score)
     worst = off.max(1, keepdims=True)
     rel = 2 * worst + (m + 8) * u                                                             # of a probability
     # below 2^-126 there are no normal floats: a probability, a score's gradient, a product of either, a sum and a result may each be zero instead

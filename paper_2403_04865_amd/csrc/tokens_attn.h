@@ -327,17 +327,22 @@ __device__ __forceinline__ float tok_other_sum(float v) {
 // A score is kept as z, a probability is 2^(ex z - ex max z): without a cap z = qk - slope / scale * d, so that the scale costs nothing beside
 // the maximum; with one z = c2 tanh(c1 qk) - slope d, all in units of log2(e), and ex is 1.
 struct TokScore { float c1, c2, ex, per_slope; };
-template <bool CAP>
+// kernels without a cap, with one, and with one so large that bfloat16 takes float32's tanh too
+enum TokCapped : int { TOK_UNCAPPED = 0, TOK_CAPPED = 1, TOK_CAPPED_FAR = 2 };
+constexpr float TOK_CAP_NEAR = 64.f;
+template <int CAP>
 __device__ __forceinline__ TokScore tok_score_of(float scale, float cap) {
   return CAP ? TokScore{scale / cap, cap * TOK_LOG2E, 1.f, TOK_LOG2E} : TokScore{0.f, 0.f, scale * TOK_LOG2E, 1.f / scale};
 }
 // tanh(u) and a quarter of its derivative.  float32: e = exp(-2 |u|), (1 - e) / (1 + e) and e / (1 + e)^2, which lose nothing for large |u|; for small
 // |u| 1 - e has e's rounding, 2^-25 of one, and the series is taken (next term 2^-27 of u at 1/4).
-// bfloat16: r = 1 / (1 + exp(2 u)), 1 - 2 r and r (1 - r), four operations fewer; off by 2^-24 of one, which is 2^-19 of a score at
-// a cap of 50, where a probability is rounded to 2^-9 of itself.
-template <typename T, bool SLOPE>
+// bfloat16: r = 1 / (1 + exp(2 u)), 1 - 2 r and r (1 - r), four operations fewer.  However small u is, 1 - 2 r is off by up to six units of 2^-24 (those of
+// the exponential, the sum and the reciprocal, twice), and a score by that times the cap: 1.3e-5 at a cap of 50, 2.3e-5 at most at TOK_CAP_NEAR, where
+// a probability is rounded to 2^-8 of itself.  Beyond, that would count (a cap of 2^20: scores off by 0.1, of 2^25: all of them 0), and float32's form is
+// taken (16 slides, 8 heads of 128: 147 us in the one, 168 in the other; 7 slides, 12 heads of 64, both directions: 209 and 266).
+template <typename T, int CAP, bool SLOPE>
 __device__ __forceinline__ float tok_cap(float qk, const TokScore& c, float* slope) {
-  if constexpr (sizeof(T) == 2) {
+  if constexpr (sizeof(T) == 2 && CAP == TOK_CAPPED) {
     const float r = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(qk * (c.c1 * (2.f * TOK_LOG2E))));
     if (SLOPE) *slope = fmaf(-r, r, r);
     return fmaf(r, -2.f * c.c2, c.c2);
@@ -351,13 +356,13 @@ __device__ __forceinline__ float tok_cap(float qk, const TokScore& c, float* slo
   }
 }
 // slope: times c.per_slope
-template <typename T, bool BIAS, bool CAP, bool SLOPE>
+template <typename T, bool BIAS, int CAP, bool SLOPE>
 __device__ __forceinline__ float tok_score(float qk, float d, float slope, const TokScore& c, float* dt) {
-  const float z = CAP ? tok_cap<T, SLOPE>(qk, c, dt) : qk;
+  const float z = CAP ? tok_cap<T, CAP, SLOPE>(qk, c, dt) : qk;
   return BIAS ? fmaf(-slope, d, z) : z;
 }
 // 2^(ex z - at)
-template <bool CAP>
+template <int CAP>
 __device__ __forceinline__ float tok_exp(float z, float at, const TokScore& c) {
   return __builtin_amdgcn_exp2f(CAP ? z - at : fmaf(z, c.ex, -at));
 }
@@ -418,7 +423,12 @@ __device__ __forceinline__ void tok_dists(f32x16& d, const float* px, const floa
 // dispatch on the padded head width, bias and cap
 template <typename T, typename F>
 hipError_t tok_dispatch(const TokAttn& g, F f) {
-  auto by_cap = [&](auto dp, auto bias) { return g.cap > 0.f ? f(dp, bias, std::true_type{}) : f(dp, bias, std::false_type{}); };
+  auto by_cap = [&](auto dp, auto bias) {
+    if constexpr (sizeof(T) == 2) {
+      if (g.cap > TOK_CAP_NEAR) return f(dp, bias, std::integral_constant<int, TOK_CAPPED_FAR>{});
+    }
+    return g.cap > 0.f ? f(dp, bias, std::integral_constant<int, TOK_CAPPED>{}) : f(dp, bias, std::integral_constant<int, TOK_UNCAPPED>{});
+  };
   auto by_bias = [&](auto dp) { return g.slopes ? by_cap(dp, std::true_type{}) : by_cap(dp, std::false_type{}); };
   if (g.dim <= 32) return by_bias(std::integral_constant<int, 32>{});
   if (g.dim <= 64) return by_bias(std::integral_constant<int, 64>{});

@@ -8,7 +8,7 @@ namespace {
 
 // Four products a score beside one root and one exponential: vector and matrix units are busy 44 and 36 % of the time (8193 rows, 6 heads of 64, with a
 // bias: 320 us, 0.64 PFLOP/s), with two wavefronts a SIMD; a third has no registers.
-template <typename T, int DP, int NW, bool BIAS, bool CAP>
+template <typename T, int DP, int NW, bool BIAS, int CAP>
 __global__ void __launch_bounds__(NW * 64, DP <= 64 && NW == 4 ? 2 : 1) tok_dkv_k(const TokAttn g) {
   constexpr int KB = TokType<T>::KB, LDR = tok_ldr<T, DP>(), NB = KB / 32, W = NW * 32;
   __shared__ __attribute__((aligned(16))) T Qs[KB * LDR], Os[KB * LDR];
@@ -141,7 +141,8 @@ template <typename T>
 hipError_t run_dkv(const TokAttn& g, TokCut c, hipStream_t s) {
   return tok_dispatch<T>(g, [&](auto dp, auto bias, auto cap) {
     constexpr int DP = decltype(dp)::value;
-    constexpr bool BIAS = decltype(bias)::value, CAP = decltype(cap)::value;
+    constexpr bool BIAS = decltype(bias)::value;
+    constexpr int CAP = decltype(cap)::value;
     if (c.waves == 4) tok_dkv_k<T, DP, 4, BIAS, CAP><<<c.blocks, 256, 0, s>>>(g);
     else tok_dkv_k<T, DP, 1, BIAS, CAP><<<c.blocks, 64, 0, s>>>(g);
     return hipGetLastError();

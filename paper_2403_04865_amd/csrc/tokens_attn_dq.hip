@@ -27,7 +27,7 @@ __device__ __forceinline__ float tok_dot(const TokFrag<T, DP>& a, const TokFrag<
 // strong bias: gradients 3.4e-3 off, 2.4e-3 mended); in longer slides it is 2e-4 to 6e-4 beside the 2.4e-3 of the roundings to bfloat16, and the product
 // not worth its time (8193 rows, 6 heads of 64, both directions: 731 us without e, 764 with e for the keys, 860 with the product too).  float32 needs neither.
 // Bound by the vector and matrix units in turn: 51 and 31 % of the time there, two wavefronts a SIMD that do not hide all of each other's waits.
-template <typename T, int DP, int NW, bool BIAS, bool CAP, bool MEND>
+template <typename T, int DP, int NW, bool BIAS, int CAP, bool MEND>
 __global__ void __launch_bounds__(NW * 64, DP <= 64 && NW == 4 ? 2 : 1) tok_dq_k(const TokAttn g) {
   constexpr int KB = DP == 128 ? 32 : TokType<T>::KB, LDR = tok_ldr<T, DP>(), NB = KB / 32, W = NW * 32;
   __shared__ __attribute__((aligned(16))) T Ks[KB * LDR], Vs[KB * LDR];
@@ -152,7 +152,8 @@ template <typename T>
 hipError_t run_dq(const TokAttn& g, TokCut c, hipStream_t s) {
   return tok_dispatch<T>(g, [&](auto dp, auto bias, auto cap) {
     constexpr int DP = decltype(dp)::value;
-    constexpr bool BIAS = decltype(bias)::value, CAP = decltype(cap)::value;
+    constexpr bool BIAS = decltype(bias)::value;
+    constexpr int CAP = decltype(cap)::value;
     if constexpr (sizeof(T) == 2) {
       if (c.waves == 1) tok_dq_k<T, DP, 1, BIAS, CAP, true><<<c.blocks, 64, 0, s>>>(g);
       else if (c.mend) tok_dq_k<T, DP, 4, BIAS, CAP, true><<<c.blocks, 256, 0, s>>>(g);

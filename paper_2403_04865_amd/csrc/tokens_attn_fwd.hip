@@ -7,7 +7,7 @@ namespace {
 
 // Bound by the vector unit where there is a bias or a cap: of the 14 issue slots' time of a score with a bias its distance takes 6.4 (four operations and a
 // root), which two heads share where a wavefront has the registers (8193 rows, 12 heads of 64: 470 -> 426 us).
-template <typename T, int DP, int NW, int NH, bool BIAS, bool CAP>
+template <typename T, int DP, int NW, int NH, bool BIAS, int CAP>
 __global__ void __launch_bounds__(NW * 64, (tok_waves<T, DP, NW>())) tok_fwd_k(const TokAttn g) {
   // differences of coordinates on the matrix cores (tok_dists) for one head and four wavefronts: 16 slides, capped scores, 8 heads of 128 156 -> 152 us; with two
   // heads, which share them, 383 -> 389, and with one wavefront, which waits for its loads, 38 -> 49
@@ -171,7 +171,8 @@ template <typename T>
 hipError_t run_fwd(const TokAttn& g, TokCut c, hipStream_t s) {
   return tok_dispatch<T>(g, [&](auto dp, auto bias, auto cap) {
     constexpr int DP = decltype(dp)::value;
-    constexpr bool BIAS = decltype(bias)::value, CAP = decltype(cap)::value;
+    constexpr bool BIAS = decltype(bias)::value;
+    constexpr int CAP = decltype(cap)::value;
     if constexpr (tok_pairs<T, DP, BIAS>()) {
       if (c.heads == 2) {
         tok_fwd_k<T, DP, 4, 2, BIAS, CAP><<<c.blocks, 256, 0, s>>>(g);
