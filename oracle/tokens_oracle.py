@@ -149,3 +149,50 @@ def _one(out, q, k, v, do, scale, cap, dist, slope, rq, rk, h, hk, half_step, op
     out["dk_off"][rk, hk] += scale * ((ds_off + terms * np.abs(ds)).T @ np.abs(q)) + tiny * (n + 1)
     out["dv"][rk, hk] += p.T @ do
     out["dv_off"][rk, hk] += ((operand + rel + terms) * p + tiny).T @ np.abs(do) + tiny * (n + 1)
+
+
+# ---- the size of bfloat16's roundings ---------------------------------------------------------------
+
+def step_variance(x):
+    """Of the error of x rounded to bfloat16: even over a step of 2^-7 of the power of two below |x|, so a twelfth of its square."""
+    _, e = np.frexp(x)
+    return np.where(x == 0, 0.0, np.ldexp(1.0, 2 * (e - 8)) / 12)
+
+
+def attn_spread(q, k, v, do, q_start, k_start, scale, cap=0.0, pos_q=None, pos_k=None, slopes=None, lead_q=0, lead_k=0, operand=True):
+    """Variances of o, dq, dk and dv in bfloat16 where nothing is rounded but the results and (`operand`) the probabilities and scores' gradients that are
+    multiplied, each by itself.  Rows of no slide are 0."""
+    group = q.shape[1] // k.shape[1]
+    val = {"o": np.zeros_like(q), "dq": np.zeros_like(q), "dk": np.zeros_like(k), "dv": np.zeros_like(k)}
+    var = {n: np.zeros_like(x) for n, x in val.items()}
+    for rq, rk in slides(q_start, k_start):
+        if rq.stop == rq.start or rk.stop == rk.start:
+            continue
+        dist = _distance(pos_q[rq], pos_k[rk], lead_q, lead_k) if slopes is not None else None
+        for h in range(q.shape[1]):
+            a, b, c, g = q[rq, h], k[rk, h // group], v[rk, h // group], do[rq, h]
+            s, t = _scores(a, b, scale, cap, dist, 0.0 if slopes is None else slopes[h])
+            p = np.exp(s - s.max(1, keepdims=True))
+            p /= p.sum(1, keepdims=True)
+            o = p @ c
+            ds = p * (g @ c.T - (g * o).sum(1, keepdims=True)) * (1 - t * t if cap else 1.0)
+            vp, vd = (step_variance(p), step_variance(ds)) if operand else (0 * p, 0 * p)
+            val["o"][rq, h], var["o"][rq, h] = o, vp @ c ** 2
+            val["dq"][rq, h], var["dq"][rq, h] = scale * ds @ b, scale ** 2 * vd @ b ** 2
+            val["dk"][rk, h // group] += scale * ds.T @ a
+            var["dk"][rk, h // group] += scale ** 2 * vd.T @ a ** 2
+            val["dv"][rk, h // group] += p.T @ g
+            var["dv"][rk, h // group] += vp.T @ g ** 2
+    return {n: x + step_variance(val[n]) for n, x in var.items()}
+
+
+def spread_ratios(off, var, groups):
+    """For every group of rows: the norm of the errors `off` [rows, heads, dim] relative to what the variances say, and the limit of that ratio.  The square of an
+    error that is even over a step is its twelfth with a relative standard deviation of 0.9; counted as one rounding a row and head, their weights being
+    `var`, the group's is 0.9 / sqrt(n), n the sum's square over the sum of squares.  Five of those, and a hundredth for float32."""
+    out = []
+    for rows in groups:
+        w = var[rows].sum(-1).ravel()
+        n = w.sum() ** 2 / (w * w).sum()
+        out.append((np.sqrt((off[rows] ** 2).sum() / w.sum()), np.sqrt(1 + 5 * 0.9 / np.sqrt(n)) + 0.01))
+    return out

@@ -16,6 +16,7 @@ namespace sl {
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr float TOK_NONE = -3e38f;   // below every score
+constexpr int TOK_MEND_KEYS = 256;   // slides up to which four wavefronts mend the queries' gradients (tokens_attn_dq.hip)
 constexpr float TOK_LOG2E = 1.4426950408889634f, TOK_LN2 = 0.69314718055994531f;
 
 template <typename T> struct TokType;

@@ -22,12 +22,13 @@ __device__ __forceinline__ float tok_dot(const TokFrag<T, DP>& a, const TokFrag<
 }
 
 // dS = P (dP - delta) with delta = dout . o = sum P dP.  Out of an o that has been rounded to bfloat16 delta is some e short, and every dS of the row off by
-// P e.  The sum of a row's P (dP - delta) is that e (P sums to one), so it is known when the row has been passed: the keys' pass gets the right delta.  MEND: this
-// pass takes e times sum P k off, for another product.  Where few keys count, dP - delta is small beside both and e decides (slides of 100 rows, head of 32,
-// strong bias: gradients 3.4e-3 off, 2.4e-3 mended); in longer slides it is 2e-4 to 6e-4 beside the 2.4e-3 of the roundings to bfloat16, and the product
-// not worth its time (8193 rows, 6 heads of 64, both directions: 731 us without e, 764 with e for the keys, 860 with the product too).  float32 needs neither.
+// P e.  The sum of a row's P (dP - delta) is that e (P sums to one), so it is known when the row has been passed: the keys' pass gets the right delta.  Mending: this
+// pass takes e times sum P k off, for another product.  Where few keys count, dP - delta is small beside both and e decides (slides of 2 rows: gradients of the
+// queries 3.7e-3 off, 2.4e-3 mended; of 100 rows, head of 32, strong bias: 3.4e-3 and 2.4e-3); in slides of more than TOK_MEND_KEYS keys it is 2e-4 to 6e-4 beside the 2.4e-3
+// of the roundings to bfloat16, and the product not worth its time (8193 rows, 6 heads of 64, both directions: 731 us without e, 764 with e for the keys, 860
+// with the product too).  So it goes by the slide's keys, in a copy of the loop.  A single wavefront mends always.  float32 needs neither.
 // Bound by the vector and matrix units in turn: 51 and 31 % of the time there, two wavefronts a SIMD that do not hide all of each other's waits.
-template <typename T, int DP, int NW, bool BIAS, int CAP, bool MEND>
+template <typename T, int DP, int NW, bool BIAS, int CAP>
 __global__ void __launch_bounds__(NW * 64, DP <= 64 && NW == 4 ? 2 : 1) tok_dq_k(const TokAttn g) {
   constexpr int KB = DP == 128 ? 32 : TokType<T>::KB, LDR = tok_ldr<T, DP>(), NB = KB / 32, W = NW * 32;
   __shared__ __attribute__((aligned(16))) T Ks[KB * LDR], Vs[KB * LDR];
@@ -62,89 +63,97 @@ __global__ void __launch_bounds__(NW * 64, DP <= 64 && NW == 4 ? 2 : 1) tok_dq_k
     TokTile<T, DP, NW * 64, KB> kt(g.ldk, g.dim), vt(g.ldv, g.dim);
     TokPlace place = {0.f, 0.f};
     constexpr bool ERR = sizeof(T) == 2;
-    f32x16 dq[DP / 32], pk[MEND ? DP / 32 : 1];
-    tok_zero_all(dq);
-    tok_zero_all(pk);
-    float e = 0.f;   // sum of P (dP - delta)
-    if (nk > 0) {
-      kt.load(kp + (long long)w.a * KB * g.ldk, nk - w.a * KB, g.ldk, g.dim);
-      vt.load(vp + (long long)w.a * KB * g.ldv, nk - w.a * KB, g.ldv, g.dim);
-      if (BIAS) place = tok_place<KB>(g.pos_k, klo, w.a * KB, nk, g.lead_k);
+    auto pass = [&](auto mend) __attribute__((always_inline)) {
+      constexpr bool MEND = decltype(mend)::value;
+      f32x16 dq[DP / 32], pk[MEND ? DP / 32 : 1];
+      tok_zero_all(dq);
+      tok_zero_all(pk);
+      float e = 0.f;   // sum of P (dP - delta)
+      if (nk > 0) {
+        kt.load(kp + (long long)w.a * KB * g.ldk, nk - w.a * KB, g.ldk, g.dim);
+        vt.load(vp + (long long)w.a * KB * g.ldv, nk - w.a * KB, g.ldv, g.dim);
+        if (BIAS) place = tok_place<KB>(g.pos_k, klo, w.a * KB, nk, g.lead_k);
 #pragma unroll 1
-      for (int t = w.a; t < w.b; ++t) {
-        const int k0 = t * KB;
-        __syncthreads();
-        kt.store(Ks);
-        vt.store(Vs);
-        if (BIAS && threadIdx.x < KB) { px[threadIdx.x] = place.x; py[threadIdx.x] = place.y; }
-        __syncthreads();
-        if (t + 1 < w.b) {
-          kt.load(kp + (long long)(k0 + KB) * g.ldk, nk - k0 - KB, g.ldk, g.dim);
-          vt.load(vp + (long long)(k0 + KB) * g.ldv, nk - k0 - KB, g.ldv, g.dim);
-          if (BIAS) place = tok_place<KB>(g.pos_k, klo, k0 + KB, nk, g.lead_k);
-        }
-        if (idle) continue;   // uniform in a wavefront: none of its columns is there
-        // the first and the last blocks hold keys without a place and keys that are not there: a copy of the code of their own
-        auto block = [&](auto edge, int b) __attribute__((always_inline)) {
-          constexpr bool EDGE = decltype(edge)::value;
-          f32x16 s = tok_zero(), dp = tok_zero(), dist, p;
-          if (BIAS) tok_dists<T>(dist, px, py, b * 32, qx, qy);
-          TokRows<T, DP> kr, vr;
-          TokCols<T, DP> kc;
-          tok_get<T, DP>(kr, Ks, b * 32);
-          tok_get<T, DP>(vr, Vs, b * 32);
-          tok_mul<T, DP>(s, kr, fq);
-          tok_mul<T, DP>(dp, vr, fo);
-#pragma unroll
-          for (int q4 = 0; q4 < 4; ++q4) {
-            const int r0 = b * 32 + tok_row(q4 * 4);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const int r = q4 * 4 + i;
-              float d = BIAS ? dist[r] : 0.f, dt = 1.f;
-              if (EDGE && BIAS && k0 + r0 + i < g.lead_k) d = 0.f;
-              const float z = tok_score<T, BIAS, CAP, true>(s[r], d, slope, sc, &dt);
-              p[r] = tok_exp<CAP>(z, lse, sc);
-              if (EDGE && k0 + r0 + i >= nk) p[r] = 0.f;   // there K is zeros, but a probability may be no number
-              float ds = p[r] * (dp[r] - delta);
-              if (ERR) e += ds;
-              if (CAP) {
-                ds *= dt;
-                if (MEND) p[r] *= dt;
-              }
-              s[r] = ds;
-            }
+        for (int t = w.a; t < w.b; ++t) {
+          const int k0 = t * KB;
+          __syncthreads();
+          kt.store(Ks);
+          vt.store(Vs);
+          if (BIAS && threadIdx.x < KB) { px[threadIdx.x] = place.x; py[threadIdx.x] = place.y; }
+          __syncthreads();
+          if (t + 1 < w.b) {
+            kt.load(kp + (long long)(k0 + KB) * g.ldk, nk - k0 - KB, g.ldk, g.dim);
+            vt.load(vp + (long long)(k0 + KB) * g.ldv, nk - k0 - KB, g.ldv, g.dim);
+            if (BIAS) place = tok_place<KB>(g.pos_k, klo, k0 + KB, nk, g.lead_k);
           }
-          tok_get_t(kc, Ks, b * 32);
-          tok_mul_t<DP, NW == 1>(dq, kc, s);
-          if constexpr (MEND) tok_mul_t<DP, false>(pk, kc, p);
-        };
-        const bool edge = (BIAS && k0 < g.lead_k) || k0 + KB > nk;   // uniform
+          if (idle) continue;   // uniform in a wavefront: none of its columns is there
+          // the first and the last blocks hold keys without a place and keys that are not there: a copy of the code of their own
+          auto block = [&](auto edge, int b) __attribute__((always_inline)) {
+            constexpr bool EDGE = decltype(edge)::value;
+            f32x16 s = tok_zero(), dp = tok_zero(), dist, p;
+            if (BIAS) tok_dists<T>(dist, px, py, b * 32, qx, qy);
+            TokRows<T, DP> kr, vr;
+            TokCols<T, DP> kc;
+            tok_get<T, DP>(kr, Ks, b * 32);
+            tok_get<T, DP>(vr, Vs, b * 32);
+            tok_mul<T, DP>(s, kr, fq);
+            tok_mul<T, DP>(dp, vr, fo);
 #pragma unroll
-        for (int b = 0; b < NB; ++b) {
-          if (edge) block(std::true_type{}, b);
-          else block(std::false_type{}, b);
+            for (int q4 = 0; q4 < 4; ++q4) {
+              const int r0 = b * 32 + tok_row(q4 * 4);
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const int r = q4 * 4 + i;
+                float d = BIAS ? dist[r] : 0.f, dt = 1.f;
+                if (EDGE && BIAS && k0 + r0 + i < g.lead_k) d = 0.f;
+                const float z = tok_score<T, BIAS, CAP, true>(s[r], d, slope, sc, &dt);
+                p[r] = tok_exp<CAP>(z, lse, sc);
+                if (EDGE && k0 + r0 + i >= nk) p[r] = 0.f;   // there K is zeros, but a probability may be no number
+                float ds = p[r] * (dp[r] - delta);
+                if (ERR) e += ds;
+                if (CAP) {
+                  ds *= dt;
+                  if (MEND) p[r] *= dt;
+                }
+                s[r] = ds;
+              }
+            }
+            tok_get_t(kc, Ks, b * 32);
+            tok_mul_t<DP, NW == 1>(dq, kc, s);
+            if constexpr (MEND) tok_mul_t<DP, false>(pk, kc, p);
+          };
+          const bool edge = (BIAS && k0 < g.lead_k) || k0 + KB > nk;   // uniform
+#pragma unroll
+          for (int b = 0; b < NB; ++b) {
+            // short slides' blocks are edges mostly, and with both copies four wavefronts run out of registers (256 slides of 197 rows, both directions: 269 us, 251 without)
+            if ((MEND && NW == 4) || edge) block(std::true_type{}, b);
+            else block(std::false_type{}, b);
+          }
         }
       }
-    }
-    if (ERR) e = tok_other_sum(e);
-    if (!valid) return;
-    const float f = CAP ? 4.f * g.scale : g.scale;   // scores' gradients carry a quarter of the cap's derivative
-    if (w.slot >= 0) {
-      const long long at = (long long)w.slot * W + wave * 32 + (lane & 31);
-      tok_store(dq, f, g.part + at * g.dim, g.dim);
-      if constexpr (MEND) tok_store(pk, f, g.part2 + at * g.dim, g.dim);
-      if (ERR && lane < 32) g.part3[at] = e;
-      return;
-    }
-    if constexpr (MEND) {
+      if (ERR) e = tok_other_sum(e);
+      if (!valid) return;
+      const float f = CAP ? 4.f * g.scale : g.scale;   // scores' gradients carry a quarter of the cap's derivative
+      if (w.slot >= 0) {
+        const long long at = (long long)w.slot * W + wave * 32 + (lane & 31);
+        tok_store(dq, f, g.part + at * g.dim, g.dim);
+        if constexpr (MEND) tok_store(pk, f, g.part2 + at * g.dim, g.dim);
+        if (ERR && lane < 32) g.part3[at] = e;
+        return;
+      }
+      if constexpr (MEND) {
 #pragma unroll
-      for (int d = 0; d < DP / 32; ++d)
+        for (int d = 0; d < DP / 32; ++d)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) dq[d][r] = fmaf(-e, pk[d][r], dq[d][r]);
-    }
-    if (ERR && lane < 32) g.delta[(long long)head * g.rows_q + qrow] = delta + e;
-    tok_store(dq, f, (T*)g.dq + qrow * g.lddq + head * g.dim, g.dim);
+          for (int r = 0; r < 16; ++r) dq[d][r] = fmaf(-e, pk[d][r], dq[d][r]);
+      }
+      if (ERR && lane < 32) g.delta[(long long)head * g.rows_q + qrow] = delta + e;
+      tok_store(dq, f, (T*)g.dq + qrow * g.lddq + head * g.dim, g.dim);
+    };
+    if constexpr (!ERR) pass(std::false_type{});
+    else if constexpr (NW == 1) pass(std::true_type{});
+    else if (nk <= TOK_MEND_KEYS) pass(std::true_type{});   // uniform
+    else pass(std::false_type{});
   });
 }
 
@@ -154,14 +163,8 @@ hipError_t run_dq(const TokAttn& g, TokCut c, hipStream_t s) {
     constexpr int DP = decltype(dp)::value;
     constexpr bool BIAS = decltype(bias)::value;
     constexpr int CAP = decltype(cap)::value;
-    if constexpr (sizeof(T) == 2) {
-      if (c.waves == 1) tok_dq_k<T, DP, 1, BIAS, CAP, true><<<c.blocks, 64, 0, s>>>(g);
-      else if (c.mend) tok_dq_k<T, DP, 4, BIAS, CAP, true><<<c.blocks, 256, 0, s>>>(g);
-      else tok_dq_k<T, DP, 4, BIAS, CAP, false><<<c.blocks, 256, 0, s>>>(g);
-    } else {
-      if (c.waves == 4) tok_dq_k<T, DP, 4, BIAS, CAP, false><<<c.blocks, 256, 0, s>>>(g);
-      else tok_dq_k<T, DP, 1, BIAS, CAP, false><<<c.blocks, 64, 0, s>>>(g);
-    }
+    if (c.waves == 4) tok_dq_k<T, DP, 4, BIAS, CAP><<<c.blocks, 256, 0, s>>>(g);
+    else tok_dq_k<T, DP, 1, BIAS, CAP><<<c.blocks, 64, 0, s>>>(g);
     return hipGetLastError();
   });
 }

@@ -35,10 +35,11 @@ __global__ void __launch_bounds__(1024) tok_table_k(const TokSide c, const TokSi
 
 // A workgroup joins COLS columns of a tile.  A column's threads are groups of `lanes` with four of its values each, group z of them takes every
 // `zs`-th piece; the groups' results meet in LDS, in their order.  blockIdx.z: the head of a group (forward), keys' or values' gradient.
-// Forward: pieces are sums under references of their own.  TOK_DQ, bfloat16: beside the sums those of P k and the error of delta (tokens_attn_dq.hip).
+// Forward: pieces are sums under references of their own.  TOK_DQ, bfloat16 (ERR): beside the sums the error of delta and, where the slide's `keys` are
+// few or the wavefronts single, sums of P k to mend them with (tokens_attn_dq.hip).
 struct Sum { f32x4 o, k; float m, l; };
-template <int PASS, bool MEND>
-__device__ __forceinline__ void add(Sum& a, const Sum& b) {
+template <int PASS>
+__device__ __forceinline__ void add(Sum& a, const Sum& b, bool mend) {
   if (PASS == TOK_FWD) {
     const float n = fmaxf(a.m, b.m), ns = n == -INFINITY ? 0.f : n;
     const float wa = __builtin_amdgcn_exp2f(a.m - ns), wb = __builtin_amdgcn_exp2f(b.m - ns);
@@ -48,17 +49,17 @@ __device__ __forceinline__ void add(Sum& a, const Sum& b) {
     for (int i = 0; i < 4; ++i) a.o[i] = fmaf(a.o[i], wa, b.o[i] * wb);
   } else {
     a.o += b.o;
-    if (MEND) a.k += b.k;
+    if (mend) a.k += b.k;
     if (PASS == TOK_DQ) a.l += b.l;
   }
 }
 struct JoinOut { void* out; int ld; };
-template <typename T, int W, int PASS, bool MEND>
-__global__ void __launch_bounds__(W == 32 ? 512 : 256) tok_join_k(const TokAttn g, const TokSide side, const TokHeads hs, int hstep, int blocks,
+template <typename T, int W, int PASS>
+__global__ void __launch_bounds__(W == 32 ? 512 : 256) tok_join_k(const TokAttn g, const TokSide side, const TokSide keys, const TokHeads hs, int hstep, int blocks,
                                                                   JoinOut out0, JoinOut out1) {
   constexpr int COLS = 8, NT = W == 32 ? 512 : 256;   // few columns mean many pieces
   constexpr bool ERR = PASS == TOK_DQ && sizeof(T) == 2;
-  __shared__ f32x4 sums[NT], sums2[MEND ? NT : 1];
+  __shared__ f32x4 sums[NT], sums2[ERR ? NT : 1];
   __shared__ float2 stats[PASS == TOK_DKV ? 1 : NT];
   const TokJoin j = ((const TokJoin*)g.joins)[blockIdx.x];
   if (j.pieces == 0) return;
@@ -69,6 +70,7 @@ __global__ void __launch_bounds__(W == 32 ? 512 : 256) tok_join_k(const TokAttn 
   const TokSpan c = tok_span(side, j.doc);
   const int first = j.tile * W + blockIdx.y * COLS, here = c.n - first < COLS ? c.n - first : COLS;   // columns of this workgroup
   if (here <= 0) return;
+  const bool mend = ERR && (W == 32 || tok_span(keys, j.doc).n <= TOK_MEND_KEYS);   // uniform
   const int quads = g.dim >> 2, lanes = quads <= 4 ? 4 : quads <= 8 ? 8 : quads <= 16 ? 16 : 32;
   const int cols = here <= 1 ? 1 : here <= 2 ? 2 : here <= 4 ? 4 : 8, zs = NT / (lanes * cols);
   const int quad = threadIdx.x & (lanes - 1), col = (threadIdx.x / lanes) & (cols - 1), z = threadIdx.x / (lanes * cols);
@@ -85,14 +87,14 @@ __global__ void __launch_bounds__(W == 32 ? 512 : 256) tok_join_k(const TokAttn 
         const float2 s = *reinterpret_cast<const float2*>(g.part2 + 2 * at);
         b.m = s.x; b.l = s.y;
       }
-      if (MEND) b.k = *reinterpret_cast<const f32x4*>(g.part2 + at * g.dim + quad * 4);
+      if (mend) b.k = *reinterpret_cast<const f32x4*>(g.part2 + at * g.dim + quad * 4);
       if (ERR) b.l = g.part3[at];
-      add<PASS, MEND>(a, b);
+      add<PASS>(a, b, mend);
     }
   }
   if (zs > 1) {
     sums[threadIdx.x] = a.o;
-    if (MEND) sums2[threadIdx.x] = a.k;
+    if (mend) sums2[threadIdx.x] = a.k;
     if (PASS != TOK_DKV) stats[threadIdx.x] = float2{a.m, a.l};
     __syncthreads();
     if (z) return;
@@ -101,9 +103,9 @@ __global__ void __launch_bounds__(W == 32 ? 512 : 256) tok_join_k(const TokAttn 
       const int at = threadIdx.x + k * stride;
       Sum b = {};
       b.o = sums[at];
-      if (MEND) b.k = sums2[at];
+      if (mend) b.k = sums2[at];
       if (PASS != TOK_DKV) { b.m = stats[at].x; b.l = stats[at].y; }
-      add<PASS, MEND>(a, b);
+      add<PASS>(a, b, mend);
     }
   }
   if (!on) return;
@@ -113,7 +115,7 @@ __global__ void __launch_bounds__(W == 32 ? 512 : 256) tok_join_k(const TokAttn 
   typedef T T4 __attribute__((ext_vector_type(4)));
   T4 v;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) v[i] = from_f<T>(MEND ? fmaf(-a.l, a.k[i], a.o[i]) : a.o[i] * f);
+  for (int i = 0; i < 4; ++i) v[i] = from_f<T>(mend ? fmaf(-a.l, a.k[i], a.o[i]) : a.o[i] * f);
   *reinterpret_cast<T4*>((T*)out.out + row * out.ld + head * g.dim + quad * 4) = v;
   if (PASS == TOK_FWD && quad == 0) g.lse[head * (long long)g.rows_q + row] = a.l == 0.f ? -INFINITY : (a.m + __builtin_amdgcn_logf(a.l)) * TOK_LN2;
   if (ERR && quad == 0) g.delta[head * (long long)g.rows_q + row] += a.l;
@@ -123,22 +125,23 @@ __global__ void __launch_bounds__(W == 32 ? 512 : 256) tok_join_k(const TokAttn 
 int tok_block_rows(int pass, int dt, int dim, TokCut c) { return dt == DT_F32 || c.heads == 2 || (pass != TOK_DKV && dim > 96) ? 32 : 64; }
 TokSide side_of(const TokAttn& g, bool queries, int pack, int per) { return queries ? TokSide{g.q_start, g.rows_q, pack, per} : TokSide{g.k_start, g.rows_k, 1, per}; }
 
-template <typename T, int PASS, bool MEND>
+template <typename T, int PASS>
 hipError_t join(const TokAttn& g, TokCut c, JoinOut out, JoinOut out1, hipStream_t s) {
   constexpr bool KEYS = PASS == TOK_DKV;
   const dim3 grid(c.blocks, c.waves * 32 / 8, KEYS ? 2 : c.heads);
   const TokHeads hs = tok_heads(g, c.heads);
   const TokSide side = side_of(g, !KEYS, hs.pack, c.waves * 32);
   const int hstep = KEYS ? 1 : g.group * (hs.kv_step + 1);   // heads from one group to the next
-  if (c.waves == 4) tok_join_k<T, 128, PASS, MEND><<<grid, 256, 0, s>>>(g, side, hs, hstep, c.blocks, out, out1);
-  else tok_join_k<T, 32, PASS, MEND><<<grid, 512, 0, s>>>(g, side, hs, hstep, c.blocks, out, out1);
+  const TokSide keys = side_of(g, false, 1, 1);
+  if (c.waves == 4) tok_join_k<T, 128, PASS><<<grid, 256, 0, s>>>(g, side, keys, hs, hstep, c.blocks, out, out1);
+  else tok_join_k<T, 32, PASS><<<grid, 512, 0, s>>>(g, side, keys, hs, hstep, c.blocks, out, out1);
   return hipGetLastError();
 }
 template <typename T>
 hipError_t join_pass(int pass, const TokAttn& g, TokCut c, hipStream_t s) {
-  if (pass == TOK_FWD) return join<T, TOK_FWD, false>(g, c, {g.o, g.ldo}, {}, s);
-  if (pass == TOK_DQ) return sizeof(T) == 2 && c.mend ? join<T, TOK_DQ, true>(g, c, {g.dq, g.lddq}, {}, s) : join<T, TOK_DQ, false>(g, c, {g.dq, g.lddq}, {}, s);
-  return join<T, TOK_DKV, false>(g, c, {g.dk, g.lddk}, {g.dv, g.lddv}, s);
+  if (pass == TOK_FWD) return join<T, TOK_FWD>(g, c, {g.o, g.ldo}, {}, s);
+  if (pass == TOK_DQ) return join<T, TOK_DQ>(g, c, {g.dq, g.lddq}, {}, s);
+  return join<T, TOK_DKV>(g, c, {g.dk, g.lddk}, {g.dv, g.lddv}, s);
 }
 
 }  // namespace
@@ -146,7 +149,7 @@ hipError_t join_pass(int pass, const TokAttn& g, TokCut c, hipStream_t s) {
 // Few columns a slide leave three of four wavefronts idle: a wavefront a workgroup then.  As many workgroups as the card holds at a time: one or
 // two of four wavefronts on each of 256 units, four or eight of one; fewer where there is less to do.  (Where there is, down to one unit each: 12 slides' tokens against 1 to 8192 keys,
 // 12 heads: 27.7 us with four units at least, 20.9 with two, 17.9 with one.)
-// dq mends the rounding of o where slides are short or there are few queries.  Two heads at a time: a key head's, or two key heads', where the kernels are built for it.
+// Two heads at a time: a key head's, or two key heads', where the kernels are built for it.
 TokCut tok_cut(int pass, const slide_tokens_attn& s, bool bias) {
   const int group = s.heads_q / s.heads_k;
   const bool queries = pass != TOK_DKV;
@@ -166,7 +169,6 @@ TokCut tok_cut(int pass, const slide_tokens_attn& s, bool bias) {
   const bool two = c.waves == 4 ? s.head_dim <= 64 || (pass == TOK_FWD && s.dtype == DT_BF16) : pass == TOK_FWD && s.head_dim <= 64;
   const long long most = (c.waves == 4 ? 256 : 1024) * (two ? 2 : 1), n = units < (double)most ? (long long)units + 1 : most;
   c.blocks = (int)((n + 7) / 8 * 8);
-  c.mend = pass == TOK_DQ && s.dtype == DT_BF16 && (c.waves == 1 || s.rows_k <= 256LL * s.docs);
   return c;
 }
 

@@ -44,8 +44,8 @@ struct TokAttn {
   void* joins;              // column tiles of several workgroups
   float *part, *part2, *part3;   // their partial results: two tiles a workgroup
 };
-// How a pass is cut: `blocks` workgroups of `waves` wavefronts with 32 columns each (packed queries, or keys) and `heads` heads at a time; mend: tokens_attn_dq.hip
-struct TokCut { int waves, blocks, heads, mend; };
+// How a pass is cut: `blocks` workgroups of `waves` wavefronts with 32 columns each (packed queries, or keys) and `heads` heads at a time
+struct TokCut { int waves, blocks, heads; };
 enum { TOK_FWD = 0, TOK_DQ = 1, TOK_DKV = 2 };
 TokCut tok_cut(int pass, const slide_tokens_attn& s, bool bias);
 inline size_t tok_table_bytes(int docs) { return docs > 64 ? ((size_t)docs + 1) * 8 : 0; }
