@@ -127,7 +127,7 @@ int slide_head_rope_fwd(const slide_head_rope* s, const void* q, int64_t ldq, co
   if (rc) return rc;
   const int64_t cq = (int64_t)s->heads_q * s->head_dim, ck = (int64_t)s->heads_k * s->head_dim;
   if (!matrix_ok(q, s->dtype, ldq, cq) || !matrix_ok(yq, s->dtype, ldyq, cq) || (yq == q && ldyq != ldq) || !aligned(gq, 16)) return SLIDE_EINVAL;
-  if (s->heads_k ? !matrix_ok(k, s->dtype, ldk, ck) || !matrix_ok(yk, s->dtype, ldyk, ck) || (yk == k && ldyk != ldk) || yk == yq || !aligned(gk, 16)
+  if (s->heads_k ? !matrix_ok(k, s->dtype, ldk, ck) || !matrix_ok(yk, s->dtype, ldyk, ck) || (yk == k && ldyk != ldk) || yk == yq || yk == q || yq == k || !aligned(gk, 16)
                  : k || yk || gk)
     return SLIDE_EINVAL;
   if (s->axes ? !pos || !aligned(pos, 4) : pos != nullptr) return SLIDE_EINVAL;
@@ -150,7 +150,9 @@ int slide_head_rope_bwd(const slide_head_rope* s, const void* dyq, int64_t lddyq
   if (!matrix_ok(dyq, s->dtype, lddyq, cq) || !matrix_ok(dq, s->dtype, lddq, cq) || (dq == dyq && lddq != lddyq)) return SLIDE_EINVAL;
   if (gq ? !matrix_ok(q, s->dtype, ldq, cq) || !aligned(gq, 16) || !dgq || !aligned(dgq, 4) || dq == q : dgq != nullptr) return SLIDE_EINVAL;
   if (s->heads_k) {
-    if (!matrix_ok(dyk, s->dtype, lddyk, ck) || !matrix_ok(dk, s->dtype, lddk, ck) || (dk == dyk && lddk != lddyk) || dk == dq) return SLIDE_EINVAL;
+    if (!matrix_ok(dyk, s->dtype, lddyk, ck) || !matrix_ok(dk, s->dtype, lddk, ck) || (dk == dyk && lddk != lddyk) || dk == dq ||
+        dk == dyq || dq == dyk || (gq && dk == q) || (gk && dq == k))
+      return SLIDE_EINVAL;
     if (gk ? !matrix_ok(k, s->dtype, ldk, ck) || !aligned(gk, 16) || !dgk || !aligned(dgk, 4) || dk == k || dgk == dgq : dgk != nullptr) return SLIDE_EINVAL;
   } else if (dyk || dk || k || gk || dgk) {
     return SLIDE_EINVAL;
