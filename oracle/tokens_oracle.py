@@ -58,10 +58,11 @@ def slides(q_start, k_start):
 
 
 def _scores(q, k, scale, cap, dist, slope):
+    """Scores, and their derivative by scale q.k: 1 / cosh^2, as 1 - tanh^2 would be 0 from 19 on."""
     x = scale * (q @ k.T)
-    t = np.tanh(x / cap) if cap else None
-    s = cap * t if cap else x
-    return s - slope * dist if dist is not None else s, t
+    s = cap * np.tanh(x / cap) if cap else x
+    by = np.cosh(np.minimum(np.abs(x / cap), 300)) ** -2 if cap else 1.0
+    return s - slope * dist if dist is not None else s, by
 
 
 def _distance(pos_q, pos_k, lead_q, lead_k):
@@ -106,7 +107,7 @@ def _one(out, q, k, v, do, scale, cap, dist, slope, rq, rk, h, hk, half_step, op
         if do is not None:
             out["dq"][rq, h] = out["dq_off"][rq, h] = 0
         return
-    s, t = _scores(q, k, scale, cap, dist, slope)
+    s, slope_t = _scores(q, k, scale, cap, dist, slope)
     top = s.max(1, keepdims=True)
     e = np.exp(s - top)
     z = e.sum(1, keepdims=True)
@@ -133,7 +134,6 @@ def _one(out, q, k, v, do, scale, cap, dist, slope, rq, rk, h, hk, half_step, op
         return
     dp = do @ v.T
     delta = (do * o).sum(1, keepdims=True)
-    slope_t = 1 - t * t if cap else 1.0
     ds = p * (dp - delta) * slope_t
     delta_off = (np.abs(do) * o_off).sum(1, keepdims=True) + dim * u * (np.abs(do) * np.abs(o)).sum(1, keepdims=True)
     dp_off = (dim + 8) * u * (np.abs(do) @ np.abs(v).T)
@@ -171,11 +171,11 @@ def attn_spread(q, k, v, do, q_start, k_start, scale, cap=0.0, pos_q=None, pos_k
         dist = _distance(pos_q[rq], pos_k[rk], lead_q, lead_k) if slopes is not None else None
         for h in range(q.shape[1]):
             a, b, c, g = q[rq, h], k[rk, h // group], v[rk, h // group], do[rq, h]
-            s, t = _scores(a, b, scale, cap, dist, 0.0 if slopes is None else slopes[h])
+            s, by = _scores(a, b, scale, cap, dist, 0.0 if slopes is None else slopes[h])
             p = np.exp(s - s.max(1, keepdims=True))
             p /= p.sum(1, keepdims=True)
             o = p @ c
-            ds = p * (g @ c.T - (g * o).sum(1, keepdims=True)) * (1 - t * t if cap else 1.0)
+            ds = p * (g @ c.T - (g * o).sum(1, keepdims=True)) * by
             vp, vd = (step_variance(p), step_variance(ds)) if operand else (0 * p, 0 * p)
             val["o"][rq, h], var["o"][rq, h] = o, vp @ c ** 2
             val["dq"][rq, h], var["dq"][rq, h] = scale * ds @ b, scale ** 2 * vd @ b ** 2
