@@ -82,7 +82,8 @@ int slide_tokens_attn_fwd(const slide_tokens_attn* s, const void* q, int64_t ldq
                           const float* slopes, void* o, int64_t ldo, float* lse, void* work, size_t work_bytes, void* hip_stream);
 
 /* Gradients of the queries, keys and values from the output's, dout, with the o and lse that the forward left.  Rows of slides without queries
- * (keys) have zero gradients; rows of no slide are not written. */
+ * (keys) have zero gradients; rows of no slide are not written.  Probabilities are made again out of lse and carry its rounding: they are off by up to
+ * 2^-22 of its size, so scores belong below 2^16 or so. */
 int slide_tokens_attn_bwd(const slide_tokens_attn* s, const void* dout, int64_t lddo, const void* q, int64_t ldq, const void* k,
                           int64_t ldk, const void* v, int64_t ldv, const void* o, int64_t ldo, const float* lse,
                           const int32_t* q_start, const int32_t* k_start, const float* pos_q, const float* pos_k,

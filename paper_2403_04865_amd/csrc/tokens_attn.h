@@ -340,7 +340,7 @@ __device__ __forceinline__ TokScore tok_score_of(float scale, float cap) {
 // bfloat16: r = 1 / (1 + exp(2 u)), 1 - 2 r and r (1 - r), four operations fewer.  However small u is, 1 - 2 r is off by up to six units of 2^-24 (those of
 // the exponential, the sum and the reciprocal, twice), and a score by that times the cap: 1.3e-5 at a cap of 50, 2.3e-5 at most at TOK_CAP_NEAR, where
 // a probability is rounded to 2^-8 of itself.  Beyond, that would count (a cap of 2^20: scores off by 0.1, of 2^25: all of them 0), and float32's form is
-// taken (16 slides, 8 heads of 128: 147 us in the one, 168 in the other; 7 slides, 12 heads of 64, both directions: 209 and 266).
+// taken (16 slides, 8 heads of 128: 147 us in the one, 168 in the other; 7 slides, 12 heads of 64, both directions: 211 and 270).
 template <typename T, int CAP, bool SLOPE>
 __device__ __forceinline__ float tok_cap(float qk, const TokScore& c, float* slope) {
   if constexpr (sizeof(T) == 2 && CAP == TOK_CAPPED) {

@@ -6,8 +6,8 @@ namespace sl {
 
 namespace {
 
-// Four products a score beside one root and one exponential: vector and matrix units are busy 44 and 36 % of the time (8193 rows, 6 heads of 64, with a
-// bias: 320 us, 0.64 PFLOP/s), with two wavefronts a SIMD; a third has no registers.
+// Four products a score beside one root and one exponential: vector and matrix units are busy 43 and 36 % of the time (8193 rows, 6 heads of 64, with a
+// bias: 290 us, 0.71 PFLOP/s), with two wavefronts a SIMD; a third has no registers.
 template <typename T, int DP, int NW, bool BIAS, int CAP>
 __global__ void __launch_bounds__(NW * 64, DP <= 64 && NW == 4 ? 2 : 1) tok_dkv_k(const TokAttn g) {
   constexpr int KB = TokType<T>::KB, LDR = tok_ldr<T, DP>(), NB = KB / 32, W = NW * 32;
