@@ -59,7 +59,8 @@ int slide_head_rope_bwd(const slide_head_rope* s, const void* dyq, int64_t lddyq
 /* Attention inside each of `docs` slides (host).  head_dim: a multiple of 16 up to 128; heads_q / heads_k up to 128, times rows_q below 2^31 - 256.
  * Row i of slide b is rows q_start[b] + i of the queries and k_start[b] + i of the keys.  Score of a query and a key of the same slide:
  *     x = scale * q.k;   where cap > 0: x = cap * tanh(x / cap);   where there are slopes: x -= slopes[head] * distance(pos_q, pos_k)
- * The first lead_q queries and lead_k keys of a slide have no place (class tokens): their distances are 0 and their positions are not used. */
+ * The first lead_q queries and lead_k keys of a slide have no place (class tokens): their distances are 0 and their positions are not used.
+ * Scores are float32, right to some units of 2^-24 of their terms: a row's largest score has to be below 2^24 in size (its other ones may be as low as they like). */
 typedef struct slide_tokens_attn {
   int64_t rows_q, rows_k;                      /* 1 to 2^31 - 1 - 256 */
   int32_t docs;                                /* 1 to 2^20 */
@@ -83,7 +84,7 @@ int slide_tokens_attn_fwd(const slide_tokens_attn* s, const void* q, int64_t ldq
 
 /* Gradients of the queries, keys and values from the output's, dout, with the o and lse that the forward left.  Rows of slides without queries
  * (keys) have zero gradients; rows of no slide are not written.  Probabilities are made again out of lse and carry its rounding: they are off by up to
- * 2^-22 of its size, so scores belong below 2^16 or so. */
+ * 2^-22 of its size, so rows' largest scores belong below 2^16. */
 int slide_tokens_attn_bwd(const slide_tokens_attn* s, const void* dout, int64_t lddo, const void* q, int64_t ldq, const void* k,
                           int64_t ldk, const void* v, int64_t ldv, const void* o, int64_t ldo, const float* lse,
                           const int32_t* q_start, const int32_t* k_start, const float* pos_q, const float* pos_k,

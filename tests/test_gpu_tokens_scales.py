@@ -33,3 +33,21 @@ def test_scales_and_slopes(scale, size, cap, slopes, lq, lk, hq, hk, dim, dtype)
     c.forward(out)
     c.backward(out)
     _check(c, out)
+
+
+@pytest.mark.parametrize("heads,dim", [((2, 2), 64), ((2, 1), 48), ((2, 2), 128)])
+@pytest.mark.parametrize("rows", [[40, 3], [400, 90]])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_every_key_far(heads, dim, rows, dtype):
+    """Rows whose largest score is some -30000: the nearest of far keys share them; other keys, 2^40 away, have nothing."""
+    from test_gpu_tokens_attn import Case, _check
+    print(f"case far keys {heads} {dim} {rows} {dtype}", flush=True)
+    c = Case(rows, [300, 70], *heads, dim, dtype, bias=True)
+    c.places["pos_q"] += 30000.0
+    c.places["pos_k"][::3] -= 2.0 ** 39
+    c.places["slopes"].fill_(0.75)
+    c.dev_places = {n: x.cuda() for n, x in c.places.items()}
+    out = c.outputs()
+    c.forward(out)
+    c.backward(out)
+    _check(c, out)
