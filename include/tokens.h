@@ -84,7 +84,8 @@ int slide_tokens_attn_fwd(const slide_tokens_attn* s, const void* q, int64_t ldq
 
 /* Gradients of the queries, keys and values from the output's, dout, with the o and lse that the forward left.  Rows of slides without queries
  * (keys) have zero gradients; rows of no slide are not written.  Probabilities are made again out of lse and carry its rounding: they are off by up to
- * 2^-22 of its size, so rows' largest scores belong below 2^16. */
+ * 2^-22 of its size, so rows' largest scores belong below 2^16.  bfloat16: the rounding of o is taken off the keys' gradients, and off the queries' in slides of
+ * 256 keys or fewer. */
 int slide_tokens_attn_bwd(const slide_tokens_attn* s, const void* dout, int64_t lddo, const void* q, int64_t ldq, const void* k,
                           int64_t ldk, const void* v, int64_t ldv, const void* o, int64_t ldo, const float* lse,
                           const int32_t* q_start, const int32_t* k_start, const float* pos_q, const float* pos_k,

@@ -25,8 +25,9 @@ __device__ __forceinline__ float tok_dot(const TokFrag<T, DP>& a, const TokFrag<
 // P e.  The sum of a row's P (dP - delta) is that e (P sums to one), so it is known when the row has been passed: the keys' pass gets the right delta.  Mending: this
 // pass takes e times sum P k off, for another product.  Where few keys count, dP - delta is small beside both and e decides (slides of 2 rows: gradients of the
 // queries 3.7e-3 off, 2.4e-3 mended; of 100 rows, head of 32, strong bias: 3.4e-3 and 2.4e-3); in slides of more than TOK_MEND_KEYS keys it is 2e-4 to 6e-4 beside the 2.4e-3
-// of the roundings to bfloat16, and the product not worth its time (8193 rows, 6 heads of 64, both directions: 731 us without e, 764 with e for the keys, 860
-// with the product too).  So it goes by the slide's keys, in a copy of the loop.  A single wavefront mends always.  float32 needs neither.
+// of the roundings to bfloat16 where a row's probabilities spread (a bias of 1 a place of a grid: gradients of the queries 2.7e-3 off), and the product not worth its time (8193 rows, 6 heads
+// of 64, both directions: 731 us without e, 764 with e for the keys, 860 with the product too); a head whose bias leaves a long slide's rows one or two keys (4 a place) has
+// 8e-3.  So it goes by the slide's keys, in a copy of the loop.  A single wavefront mends always.  float32 needs neither.
 // Bound by the vector and matrix units in turn: 51 and 31 % of the time there, two wavefronts a SIMD that do not hide all of each other's waits.
 template <typename T, int DP, int NW, bool BIAS, int CAP>
 __global__ void __launch_bounds__(NW * 64, DP <= 64 && NW == 4 ? 2 : 1) tok_dq_k(const TokAttn g) {
